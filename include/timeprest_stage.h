@@ -116,8 +116,20 @@ enum tp_layer_type {
   TP_LAYER_SUBSAMPLE2 = 7, /* every second pixel of every second row (the pixels a stride-2 1x1 convolution reads), no
                              parameters: in_features = out_features = C, geom = {H, W} of the input (both even),
                              C * element size a multiple of 16 bytes */
-  TP_LAYER_AVGPOOL = 8    /* global average pooling, no parameters: a sample of [positions x C] values becomes the C
+  TP_LAYER_AVGPOOL = 8,   /* global average pooling, no parameters: a sample of [positions x C] values becomes the C
                              means over its positions; in_features = out_features = C, geom = {positions} */
+  TP_LAYER_LOCAL_ATTENTION = 9 /* causal multi-head self-attention over a window of keys: geom = {tokens, heads, kv heads, window,
+                             sinks}; out_features = heads * dh (dh: 1 .. 256), in_features = (heads + 2 * kv heads) * dh (queries | keys |
+                             values; kv heads divide heads, query head h reads key head h / (heads / kv heads)).  Query i sees key
+                             j <= i where i - j < window (0: every j <= i) or j < sinks (0 without a window).  rel = {buckets,
+                             max distance} adds a learned bias table[h][bucket(i - j)] to the scaled scores, {0, 0}: none.  2 .. 128
+                             buckets: distances 0 .. half - 1 have one each (half = buckets / 2, rounded down, < max distance <=
+                             2^20), the others lie at equal ratios: bucket half + t starts at the smallest whole distance not
+                             below half * (max distance / half)^(t / (buckets - half)), and the last has no end.  The table,
+                             [heads x buckets] and fp32 in every mode, is the layer's only parameter (where a dense layer keeps W;
+                             it has no b).  The backward pass forms the probabilities of the forward pass again, with the table
+                             that pass read (a copy is kept), under every policy.  May be the last layer of a stage.  Keys that a
+                             query does not see do not reach its results, whatever they hold */
 };
 
 #define TP_MAX_LAYERS 64
@@ -129,9 +141,10 @@ typedef struct tp_layer_desc {
   int32_t in_features;  /* dense: columns of the layer input;  conv/pool: input channels;  others: see the type */
   int32_t out_features; /* dense: columns of the layer output; conv/pool: output channels; others: see the type */
   int32_t geom[5];      /* conv: {H, W, kernel, stride, pad}; pool: {H, W, 0, 0, 0}; dense, layer norm: {tokens};
-                           attention: {tokens, heads}; residual: {tokens, mark[, tokens out]}; batch norm: {positions};
+                           attention: {tokens, heads}; windowed attention: {tokens, heads, kv heads, window, sinks}; residual: {tokens, mark[, tokens out]}; batch norm: {positions};
                            subsampling: {H, W}; average pooling: {positions}; unused entries zero */
-  int32_t reserved[7];  /* must be zero */
+  int32_t rel[2];       /* windowed attention: {buckets, max distance} of a position bias; others: zero */
+  int32_t reserved[5];  /* must be zero */
 } tp_layer_desc;
 
 typedef struct tp_stage_desc {
@@ -258,10 +271,10 @@ int stage_forward_on(tp_stage* st, uint64_t mb_id, uint32_t ub_idx, uint64_t ver
  *   - stage_backward / stage_backward_on make the stage's stream wait for the forward passes of THEIR mini-batch
  *     and for no others: forwards of later mini-batches enqueued before the call keep running beside the backward
  *     pass;
- *   - every other call that enqueues work or hands out results (stage_blend_update[_noalloc], stage_loss_softmax_ce,
+ *   - every other call that enqueues work or hands out results (stage_blend_update[_noalloc], stage_loss_softmax_ce, stage_loss_distill,
  *     stage_saved_input_ptr, stage_export_params, stage_profile_begin, stage_forward_join) first makes the stage's
  *     stream wait for all forward streams.  Read y_dev on the stage's stream only after one of them.
- * Refused (TP_EINVAL) for stages with attention layers, whose forward kernels share their scratch memory, and under
+ * Refused (TP_EINVAL) for stages with TP_LAYER_ATTENTION layers, whose forward kernels share their scratch memory, and under
  * TP_TIMEPREST.  Not used while profiling is on.  The streams must outlive the stage or be taken away first;
  * stage_destroy waits for them. */
 #define TP_MAX_FORWARD_STREAMS 3
@@ -291,6 +304,22 @@ int stage_saved_input_ptr(tp_stage* st, uint64_t mb_id, uint32_t ub_idx, int32_t
  * classes = out_features of the stage's last layer. */
 int stage_loss_softmax_ce(tp_stage* st, uint64_t mb_id, const void* logits_dev,
                           const int32_t* labels_dev, void* dlogits_dev, float* loss_dev);
+
+/* The loss of a last stage that learns from a teacher's stored top logits and from labels, and its gradient; stands in for
+ * stage_loss_softmax_ce.  rows = n*mb * token positions of the (dense) last layer.  Per row, with z the student's logits:
+ *   p = softmax(teacher logits / temperature) over the row's entries, q = softmax(z / temperature), s = softmax(z),
+ *   row = label_weight * -log s[label] + (1 - label_weight) * temperature^2 * sum over entries of p (log p - log q[id]),
+ * the loss is the mean over the rows (row values in fp32, added up in fp64), dlogits_dev its gradient.
+ * teacher_logits_dev: float[rows * k], teacher_ids_dev: int32[rows * k], the class of each entry, negative: no entry (a row may
+ * have fewer than k, or none: then, or if all its teacher logits are -inf, it has no second term).  An entry twice counts twice.
+ * labels_dev: int32[rows]; with label_weight 0 it is not read and may be NULL, with label_weight 1 the teacher has no part.
+ * A class or label that does not exist (id >= classes; label outside 0 .. classes - 1) makes the loss NaN; the gradient is that
+ * of the other terms.  logits_dev and dlogits_dev must not overlap.  TP_EINVAL: k outside 1 .. TP_MAX_TEACHER_ENTRIES, a
+ * temperature outside 1e-6 .. 1e6, a weight outside 0 .. 1. */
+#define TP_MAX_TEACHER_ENTRIES 1024
+int stage_loss_distill(tp_stage* st, uint64_t mb_id, const void* logits_dev, const float* teacher_logits_dev,
+                       const int32_t* teacher_ids_dev, int32_t k, double temperature, const int32_t* labels_dev,
+                       double label_weight, void* dlogits_dev, float* loss_dev);
 
 /* The one backward pass of mini-batch `mb_id` over all its n micro-batches (Section
  * "Methodology"), on W_b = alpha(delta) W[v_f] + beta(delta) W[latest] with

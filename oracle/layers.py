@@ -229,6 +229,118 @@ def attention_backward(dout, qkv, heads):
     return np.concatenate([back(dq), back(dk), back(dv)], axis=-1)
 
 
+def distill_loss(z, teacher, ids, temperature, labels, label_weight):
+    """Mean over the rows of label_weight * cross-entropy + (1 - label_weight) * temperature^2 * KL(p || q), p the softmax of a
+    row's stored teacher logits (entries with a negative class are none), q that of the student's, both divided by the
+    temperature; and its gradient.  Row by row."""
+    rows, classes = z.shape
+    loss, dz = 0.0, np.zeros_like(z)
+    for r in range(rows):
+        e = np.exp(z[r] - z[r].max())
+        s = e / e.sum()
+        if label_weight > 0:
+            loss -= label_weight * np.log(s[labels[r]])
+            dz[r] += label_weight * s
+            dz[r, labels[r]] -= label_weight
+        kept = np.flatnonzero((ids[r] >= 0) & (teacher[r] > -np.inf))
+        if label_weight < 1 and len(kept):
+            p = np.exp((teacher[r, kept] - teacher[r, kept].max()) / temperature)
+            p /= p.sum()
+            q = np.exp((z[r] - z[r].max()) / temperature)
+            q /= q.sum()
+            loss += (1 - label_weight) * temperature ** 2 * (p * (np.log(np.maximum(p, 1e-300)) - np.log(q[ids[r, kept]]))).sum()
+            dz[r] += (1 - label_weight) * temperature * q
+            np.add.at(dz[r], ids[r, kept], -(1 - label_weight) * temperature * p)
+    return loss / rows, dz / rows
+
+
+# ---------------------------------------------------------------------------
+# Attention over a window of keys and a few first ones, with shared key heads and a learned bias per distance bucket.
+# ---------------------------------------------------------------------------
+
+def first_distances(buckets, max_distance):
+    """First distance of each bucket, in whole numbers: half = buckets // 2 distances have one each; bucket half + t starts at
+    the smallest d with d**n >= half**(n - t) * max_distance**t, n = buckets - half."""
+    half = buckets // 2
+    n = buckets - half
+    out = list(range(half))
+    for t in range(n):
+        limit = half ** (n - t) * max_distance ** t
+        lo, hi = half, max_distance
+        while lo < hi:
+            mid = (lo + hi) // 2
+            if mid ** n >= limit:
+                hi = mid
+            else:
+                lo = mid + 1
+        out.append(lo)
+    return out
+
+
+def distance_buckets(tokens, buckets, max_distance):
+    """Bucket of each distance 0 .. tokens - 1: the last one that starts at or before it."""
+    return np.searchsorted(np.array(first_distances(buckets, max_distance)), np.arange(tokens), side="right") - 1
+
+
+def _local_parts(x, spec):
+    """Per query head: q, k, v of shape [B, heads, S, dh], and what is added to the scores [heads or 1, S, S]."""
+    B, S, _ = x.shape
+    h, kv = spec.heads, spec.kv_heads
+    dh = spec.d // h
+    x = x.reshape(B, S, h + 2 * kv, dh).transpose(0, 2, 1, 3)
+    shared = np.repeat(np.arange(kv), h // kv)
+    i, j = np.arange(S)[:, None], np.arange(S)[None, :]
+    seen = j <= i
+    if spec.window:
+        seen &= (i - j < spec.window) | (j < spec.sinks)
+    return x[:, :h], x[:, h + shared], x[:, h + kv + shared], seen
+
+
+def local_attention_probabilities(x, spec, table):
+    q, k, v, seen = _local_parts(x, spec)
+    S = x.shape[1]
+    s = q @ k.transpose(0, 1, 3, 2) / np.sqrt(spec.d // spec.heads)
+    if spec.buckets:
+        bucket = distance_buckets(S, spec.buckets, spec.max_distance)
+        distance = np.maximum(np.arange(S)[:, None] - np.arange(S)[None, :], 0)
+        s = s + np.asarray(table)[:, bucket[distance]]
+    s = np.where(seen, s, -np.inf)
+    e = np.exp(s - s.max(axis=-1, keepdims=True))
+    return e / e.sum(axis=-1, keepdims=True)
+
+
+def local_attention_forward(x, spec, table=None):
+    """x: [B, S, d + 2 * kv_heads * dh] = (queries | keys | values); returns [B, S, d]."""
+    B, S, _ = x.shape
+    v = _local_parts(x, spec)[2]
+    p = local_attention_probabilities(x, spec, table)
+    return (p @ v).transpose(0, 2, 1, 3).reshape(B, S, spec.d)
+
+
+def local_attention_backward(dout, x, spec, table=None):
+    """Gradients of local_attention_forward with respect to x and the table (None without one)."""
+    B, S, _ = x.shape
+    h, kv = spec.heads, spec.kv_heads
+    dh = spec.d // h
+    q, k, v, _ = _local_parts(x, spec)
+    p = local_attention_probabilities(x, spec, table)
+    do = dout.reshape(B, S, h, dh).transpose(0, 2, 1, 3)
+    dp = do @ v.transpose(0, 1, 3, 2)
+    ds = p * (dp - (dp * p).sum(axis=-1, keepdims=True))
+    shared = lambda t: t.reshape(B, kv, h // kv, S, dh).sum(axis=2)
+    dq = ds @ k / np.sqrt(dh)
+    dk = shared(ds.transpose(0, 1, 3, 2) @ q / np.sqrt(dh))
+    dv = shared(p.transpose(0, 1, 3, 2) @ do)
+    dx = np.concatenate([dq, dk, dv], axis=1).transpose(0, 2, 1, 3).reshape(x.shape)
+    if not spec.buckets:
+        return dx, None
+    bucket = distance_buckets(S, spec.buckets, spec.max_distance)
+    by_distance = np.stack([np.trace(ds, offset=-t, axis1=2, axis2=3).sum(axis=0) for t in range(S)], axis=1)   # [heads, S]
+    dtable = np.zeros((h, spec.buckets))
+    np.add.at(dtable, (slice(None), bucket), by_distance)
+    return dx, dtable
+
+
 # ---------------------------------------------------------------------------
 # Batch normalisation (training mode) for the bottleneck-shaped workload: statistics over all rows
 # (samples x positions) of what one forward call sees, per channel.  Standard definition.

@@ -55,7 +55,8 @@ class Stage:
         # position of each layer's weight in the flat parameter list (None: layer has no parameters)
         self.pidx, nxt = [], 0
         for spec in self.specs:
-            if getattr(spec, "kind", "dense") in ("pool", "attn", "res", "sub", "swap", "avg"):
+            kind = getattr(spec, "kind", "dense")
+            if kind in ("pool", "attn", "res", "sub", "swap", "avg") or (kind == "local" and not spec.buckets):
                 self.pidx.append(None)
             else:
                 self.pidx.append(nxt)
@@ -170,6 +171,12 @@ class Stage:
                 a = self.q(L.attention_forward(a, spec.heads))
                 outs.append(a)
                 continue
+            if kind == "local":                            # the table is read in its own precision, like a bias
+                table = None if pi is None else np.array(self.weights[v_read][pi])
+                saved.append((a, table))
+                a = self.q(L.local_attention_forward(a, spec, table))
+                outs.append(a)
+                continue
             if kind == "conv":
                 z = L.conv2d_forward(a, W[pi], W[pi + 1], spec.stride, spec.pad)
             else:
@@ -270,6 +277,13 @@ class Stage:
                     continue
                 if kind == "attn":
                     da = self.q(L.attention_backward(da, saved[li][0], spec.heads))
+                    continue
+                if kind == "local":                        # on the probabilities of the forward pass, i.e. on its table
+                    x_in, table = saved[li]
+                    da, dtable = L.local_attention_backward(da, x_in, spec, table)
+                    if table is not None:
+                        g[pi] += dtable
+                    da = self.q(da)
                     continue
                 x_in, z = saved[li]
                 dz = self.q(da * L.act_derivative(z, spec.act))

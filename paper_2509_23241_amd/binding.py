@@ -13,8 +13,10 @@ TP_ACT_NONE, TP_ACT_RELU, TP_ACT_GELU = 0, 1, 2
 TP_LAYER_DENSE, TP_LAYER_CONV2D, TP_LAYER_MAXPOOL2, TP_LAYER_LAYERNORM, TP_LAYER_ATTENTION, TP_LAYER_RESIDUAL, TP_LAYER_BATCHNORM = 0, 1, 2, 3, 4, 5, 6
 TP_LAYER_SUBSAMPLE2 = 7
 TP_LAYER_AVGPOOL = 8
+TP_LAYER_LOCAL_ATTENTION = 9
 TP_MAX_LAYERS, TP_MAX_SLOTS, TP_MAX_IN_FLIGHT = 64, 16, 16
 TP_NONE = (1 << 64) - 1
+TP_MAX_TEACHER_ENTRIES = 1024
 TP_DIAG_GRAD_SQ, TP_DIAG_WEIGHT_SQ, TP_DIAG_DRIFT_SQ, TP_DIAG_WB_SQ, TP_DIAG_COUNT = 0, 1, 2, 3, 4
 
 POLICY = {"latest": TP_LATEST, "eq1": TP_INTERMEDIATE_EQ1, "convex": TP_INTERMEDIATE_CONVEX, "stashed": TP_STASHED,
@@ -23,14 +25,14 @@ ACT = {"none": TP_ACT_NONE, "relu": TP_ACT_RELU, "gelu": TP_ACT_GELU}
 DTYPE = {"f32": TP_F32, "bf16": TP_BF16}
 
 EXPORTS = ["stage_workspace_query", "stage_init", "stage_destroy", "stage_set_forward_streams", "stage_forward_join", "stage_forward", "stage_forward_minibatch", "stage_forward_on", "stage_backward_on", "stage_input_ptr", "stage_saved_input_ptr",
-           "stage_loss_softmax_ce", "stage_backward", "stage_blend_update", "stage_blend_update_noalloc", "stash_push", "stash_evict",
+           "stage_loss_softmax_ce", "stage_loss_distill", "stage_backward", "stage_blend_update", "stage_blend_update_noalloc", "stash_push", "stash_evict",
            "stage_query", "stage_export_params", "tp_blend_coefficients", "tp_schedule_events", "tp_schedule_microbatch_events",
            "stage_profile_begin", "stage_profile_end", "tp_last_error"]
 
 
 class tp_layer_desc(C.Structure):
     _fields_ = [("type", C.c_int32), ("act", C.c_int32), ("in_features", C.c_int32), ("out_features", C.c_int32),
-                ("geom", C.c_int32 * 5), ("reserved", C.c_int32 * 7)]
+                ("geom", C.c_int32 * 5), ("rel", C.c_int32 * 2), ("reserved", C.c_int32 * 5)]
 
 
 class tp_stage_desc(C.Structure):
@@ -107,6 +109,7 @@ lib.stage_set_forward_streams.argtypes = [_vp, C.POINTER(_vp), _i32]
 lib.stage_forward_join.argtypes = [_vp]
 lib.stage_saved_input_ptr.argtypes = [_vp, _u64, _u32, _i32, C.POINTER(_vp), C.POINTER(_u64)]
 lib.stage_loss_softmax_ce.argtypes = [_vp, _u64, _vp, _vp, _vp, _vp]
+lib.stage_loss_distill.argtypes = [_vp, _u64, _vp, _vp, _vp, _i32, C.c_double, _vp, C.c_double, _vp, _vp]
 lib.stage_backward.argtypes = [_vp, _u64, _vp, _vp, C.POINTER(_u32)]
 lib.stage_blend_update.argtypes = [_vp, _u64, _u64, C.POINTER(_u64)]
 lib.stage_blend_update_noalloc.argtypes = [_vp, _u64, _u64, C.POINTER(_u64)]
@@ -141,7 +144,8 @@ def make_desc(layers, *, dtype, mb, n, stage_index, num_stages, ring_capacity, m
     (kernel-1)/2, ("pool", C, H, W) for 2x2 pooling, ("sub", C, H, W) for 2x subsampling, ("avg", C, positions) for
     global average pooling, ("ln", D, tokens), ("attn", D, heads, tokens),
     ("res", D, tokens, "begin" | "add"[, act-name]), ("swap", D_in, tokens_in, D_out, tokens_out) for the residual
-    mark that starts a projection shortcut, ("bn", C, positions, act-name)."""
+    mark that starts a projection shortcut, ("bn", C, positions, act-name), ("local", D, heads, tokens, kv_heads, window, sinks[,
+    buckets, max_distance]) for windowed attention with D = heads * head width."""
     if len(layers) > TP_MAX_LAYERS:
         raise ValueError(f"{len(layers)} layers: a stage takes at most {TP_MAX_LAYERS}")
     d = tp_stage_desc()
@@ -190,6 +194,13 @@ def make_desc(layers, *, dtype, mb, n, stage_index, num_stages, ring_capacity, m
             act = "none"
             L.type, L.in_features, L.out_features = TP_LAYER_ATTENTION, 3 * dm, dm
             L.geom[0], L.geom[1] = tokens, heads
+        elif spec[0] == "local":
+            _, dm, heads, tokens, kv_heads, window, sinks = spec[:7]
+            act = "none"
+            L.type, L.in_features, L.out_features = TP_LAYER_LOCAL_ATTENTION, _local_in_features(spec), dm
+            L.geom[0], L.geom[1], L.geom[2], L.geom[3], L.geom[4] = tokens, heads, kv_heads, window, sinks
+            if len(spec) > 7:
+                L.rel[0], L.rel[1] = spec[7], spec[8]
         elif spec[0] == "res":
             _, dm, tokens, mark = spec[:4]
             act = spec[4] if len(spec) > 4 else "none"
@@ -207,6 +218,11 @@ def make_desc(layers, *, dtype, mb, n, stage_index, num_stages, ring_capacity, m
     return d
 
 
+def _local_in_features(spec) -> int:
+    _, dm, heads, _, kv_heads = spec[:5]
+    return dm + 2 * kv_heads * (dm // heads) if heads > 0 else 0
+
+
 def layer_in_elems(spec) -> int:
     """Values per sample a layer takes in / gives out (same tuple format as make_desc)."""
     if spec[0] == "conv":
@@ -217,6 +233,8 @@ def layer_in_elems(spec) -> int:
         return spec[1] * spec[2]
     if spec[0] == "attn":
         return 3 * spec[1] * spec[3]
+    if spec[0] == "local":
+        return _local_in_features(spec) * spec[3]
     if spec[0] == "res":
         return spec[1] * spec[2]
     return spec[0] * (spec[3] if len(spec) > 3 else 1)
@@ -234,7 +252,7 @@ def layer_out_elems(spec) -> int:
         return spec[1]
     if spec[0] in ("ln", "bn"):
         return spec[1] * spec[2]
-    if spec[0] == "attn":
+    if spec[0] in ("attn", "local"):
         return spec[1] * spec[3]
     if spec[0] == "res":
         return spec[1] * spec[2]
@@ -247,6 +265,8 @@ def layer_param_shapes(spec):
         return [(spec[2], k, k, spec[1]), (spec[2],)]
     if spec[0] in ("pool", "attn", "res", "sub", "swap", "avg"):
         return []
+    if spec[0] == "local":
+        return [(spec[2], spec[7]), (0,)] if len(spec) > 7 and spec[7] else []   # the table, and no second tensor
     if spec[0] in ("ln", "bn"):
         return [(spec[1],), (spec[1],)]
     return [(spec[1], spec[0]), (spec[1],)]
@@ -324,6 +344,14 @@ def stage_saved_input_ptr(st, mb_id: int, ub_idx: int, layer: int):
 
 def stage_loss_softmax_ce(st, mb_id: int, logits_dev: int, labels_dev: int, dlogits_dev: int, loss_dev: int):
     _check(lib.stage_loss_softmax_ce(st, mb_id, _vp(logits_dev), _vp(labels_dev), _vp(dlogits_dev), _vp(loss_dev)))
+
+
+def stage_loss_distill(st, mb_id: int, logits_dev: int, teacher_logits_dev: int, teacher_ids_dev: int, k: int, temperature: float,
+                       labels_dev: int, label_weight: float, dlogits_dev: int, loss_dev: int):
+    rc = lib.stage_loss_distill(st, mb_id, logits_dev, teacher_logits_dev, teacher_ids_dev, k, temperature, labels_dev, label_weight,
+                                dlogits_dev, loss_dev)
+    if rc:
+        _check(rc)
 
 
 def stage_backward(st, mb_id: int, dy_dev: int, dx_dev: int) -> int:

@@ -16,6 +16,8 @@
 #include <vector>
 
 #include "conv.h"
+#include "distill.h"
+#include "local_attention.h"
 #include "transformer.h"
 #include "batchnorm.h"
 #include "kernels.h"
@@ -51,6 +53,8 @@ struct LayerPlan {
   uint64_t stat_off = UINT64_MAX;  // layer norm: mean and 1/std per token; attention: log-sum-exp per (head, query)
   uint64_t stat_elems = 0;         // floats per sample behind stat_off
   uint64_t stat_bytes = 0;         // batch norm: bytes behind stat_off (per micro-batch, not per sample)
+  uint64_t out_off = UINT64_MAX;   // windowed attention as last layer: its output, which the backward pass needs
+  uint64_t kept_off = UINT64_MAX;  // windowed attention with a bias: the table each micro-batch's forward pass read
   int tokens = 1;                  // positions per sample (rows of the layer's matrices per sample)
   int skip_layer = -1;             // residual add: index of the layer that remembered the skip activation
   DeferredNeed need;
@@ -83,6 +87,22 @@ struct Plan {
   size_t elt_size = 4;
   bool any_order = true;  // dense layers of whole samples alone: no normalisation follows whose results hang on an ulp of its input
 };
+
+// Windowed attention layer L on `seqs` samples, the kept table of every `per_table` of which is another.
+tp::LocalAttention local_attention(const tp_layer_desc& L, int seqs, int per_table) {
+  tp::LocalAttention a;
+  a.seqs = seqs;
+  a.S = L.geom[0];
+  a.heads = L.geom[1];
+  a.kv = L.geom[2];
+  a.dh = L.out_features / L.geom[1];
+  a.window = L.geom[3] > 0 ? std::min(L.geom[3], a.S) : a.S;
+  a.sinks = a.window < a.S ? std::min(L.geom[4], a.S) : 0;  // a window of all tokens has them anyway
+  a.buckets = L.rel[0];
+  a.max_distance = L.rel[1];
+  a.seqs_per_table = per_table;
+  return a;
+}
 
 // output pixels per image of a convolution layer (geom: H, W, kernel, stride, pad)
 inline uint64_t conv_out_px(const tp_layer_desc& L) { return (uint64_t)(L.geom[0] / L.geom[3]) * (L.geom[1] / L.geom[3]); }
@@ -165,6 +185,23 @@ int check_desc(const tp_stage_desc* d) {
       if (l == d->num_layers - 1) return fail(TP_EINVAL, "layer %d: attention must not be the last layer of a stage", l);
       in_e = (uint64_t)L.geom[0] * L.in_features;
       out_e = (uint64_t)L.geom[0] * L.out_features;
+    } else if (L.type == TP_LAYER_LOCAL_ATTENTION) {
+      const int heads = L.geom[1], kv = L.geom[2];
+      if (L.geom[0] < 1 || heads < 1 || kv < 1 || heads % kv != 0 || L.act != TP_ACT_NONE || L.out_features % heads != 0 ||
+          (int64_t)L.in_features != L.out_features + 2 * (int64_t)kv * (L.out_features / heads))
+        return fail(TP_EINVAL, "layer %d: malformed windowed attention layer", l);
+      if (L.geom[3] < 0 || L.geom[4] < 0 || (L.geom[4] > 0 && L.geom[3] == 0))
+        return fail(TP_EINVAL, "layer %d: a window is 0 (all keys) or positive, and first keys stay visible beside a window only", l);
+      if (L.rel[0] != 0 || L.rel[1] != 0) {
+        if (L.rel[0] < 2 || L.rel[0] > tp::kMaxBuckets || L.rel[1] <= L.rel[0] / 2 || L.rel[1] > tp::kMaxBucketDistance)
+          return fail(TP_EINVAL, "layer %d: a position bias has 2 .. %d buckets and reaches from more than half as many tokens to %d", l,
+                      tp::kMaxBuckets, tp::kMaxBucketDistance);
+      }
+      if (!tp::local_attention_supported(local_attention(L, d->mb * d->n, d->mb)))
+        return fail(TP_EINVAL, "layer %d: %d heads of %d on %d samples of %d tokens are outside what the windowed attention kernels take", l,
+                    heads, L.out_features / heads, d->mb * d->n, L.geom[0]);
+      in_e = (uint64_t)L.geom[0] * L.in_features;
+      out_e = (uint64_t)L.geom[0] * L.out_features;
     } else if (L.type == TP_LAYER_CONV2D) {
       if (L.geom[0] < 1 || L.geom[1] < 1) return fail(TP_EINVAL, "layer %d: empty image", l);
       if (!tp::conv_geometry_supported(L.geom[2], L.geom[3], L.geom[4]))
@@ -203,8 +240,10 @@ int check_desc(const tp_stage_desc* d) {
       return fail(TP_EINVAL, "layer %d: input of %llu values does not match previous output of %llu", l,
                   (unsigned long long)in_e, (unsigned long long)prev_out);
     prev_out = out_e;
-    for (int r = 0; r < 7; ++r)
+    for (int r = 0; r < 5; ++r)
       if (L.reserved[r] != 0) return fail(TP_EINVAL, "layer %d: reserved fields must be zero", l);
+    if (L.type != TP_LAYER_LOCAL_ATTENTION && (L.rel[0] != 0 || L.rel[1] != 0))
+      return fail(TP_EINVAL, "layer %d: only windowed attention has a position bias", l);
   }
   if (open_skip >= 0) return fail(TP_EINVAL, "layer %d: residual begin without an add", open_skip);
   return TP_OK;
@@ -246,7 +285,9 @@ DeferredNeed deferred_need(const tp_stage_desc& d, int l, const LayerPlan& lp) {
   const uint64_t rows = (uint64_t)d.mb * d.n;
   const tp_layer_desc& L = lp.d;
   uint64_t extra = 0;
-  if (L.type == TP_LAYER_LAYERNORM) {
+  if (L.type == TP_LAYER_LOCAL_ATTENTION) {
+    need.weight = round_up(tp::local_attention_table_floats(d.dtype, local_attention(L, d.mb * d.n, d.mb)), 64);
+  } else if (L.type == TP_LAYER_LAYERNORM) {
     need.norm = round_up(tp::layernorm_scratch_floats(rows * lp.tokens, L.in_features), 64);
   } else if (L.type == TP_LAYER_BATCHNORM) {
     // per micro-batch two column sums; those of dx, one row per micro-batch or as the streaming kernels leave them
@@ -317,6 +358,15 @@ int make_plan(const tp_stage_desc* d, Plan* p) {
       p->attn_scratch_bytes = std::max<uint64_t>(
           p->attn_scratch_bytes,
           tp::attention_scratch_bytes(d->dtype, (int)rows, lp.tokens, L.geom[1], L.out_features / L.geom[1]));
+    } else if (L.type == TP_LAYER_LOCAL_ATTENTION) {
+      lp.tokens = L.geom[0];
+      lp.in_elems = (uint64_t)lp.tokens * L.in_features;
+      lp.out_elems = (uint64_t)lp.tokens * L.out_features;
+      lp.w_elems = (uint64_t)L.geom[1] * L.rel[0];     // the table; no bias vector
+      lp.stat_elems = (uint64_t)lp.tokens * L.geom[1];
+      const tp::LocalAttention a = local_attention(L, (int)rows, d->mb);
+      p->attn_scratch_bytes = std::max<uint64_t>(p->attn_scratch_bytes, tp::local_attention_scratch_bytes(d->dtype, a));
+      norm_scratch = std::max<uint64_t>(norm_scratch, tp::local_attention_table_floats(d->dtype, a));
     } else if (L.type == TP_LAYER_RESIDUAL) {
       lp.tokens = L.geom[0];
       lp.in_elems = lp.out_elems = (uint64_t)lp.tokens * L.in_features;
@@ -352,7 +402,7 @@ int make_plan(const tp_stage_desc* d, Plan* p) {
     if (lp.w_elems) {
       off += round_up(lp.w_elems, 64);
       lp.b_off = off;
-      off += round_up((uint64_t)L.out_features, 64);
+      if (L.type != TP_LAYER_LOCAL_ATTENTION) off += round_up((uint64_t)L.out_features, 64);
     }
     if (alias_of >= 0) {
       lp.x_off = p->layers[alias_of].x_off;
@@ -364,6 +414,16 @@ int make_plan(const tp_stage_desc* d, Plan* p) {
     if (lp.stat_elems || lp.stat_bytes) {
       lp.stat_off = act;
       act += round_up(lp.stat_bytes ? lp.stat_bytes : rows * lp.stat_elems * 4, 256);
+    }
+    if (L.type == TP_LAYER_LOCAL_ATTENTION) {
+      if (l == d->num_layers - 1) {
+        lp.out_off = act;
+        act += round_up(rows * lp.out_elems * p->elt_size, 256);
+      }
+      if (lp.w_elems) {
+        lp.kept_off = act;
+        act += round_up((uint64_t)d->n * lp.w_elems * 4, 256);
+      }
     }
     // act'(z) is kept for the backward pass -- except for a ReLU whose output the stage keeps anyway as the next
     // layer's input: relu'(z) = (output > 0).  Not for the last layer (its output goes to the caller) and not in
@@ -399,13 +459,13 @@ int make_plan(const tp_stage_desc* d, Plan* p) {
     const LayerPlan& lp = p->layers[l];
     if (!lp.w_elems) continue;
     // bias gradients: column sums over rows (dense) or over all pixels (conv)
-    if (lp.d.type == TP_LAYER_LAYERNORM || lp.d.type == TP_LAYER_BATCHNORM) continue;
+    if (lp.d.type == TP_LAYER_LAYERNORM || lp.d.type == TP_LAYER_BATCHNORM || lp.d.type == TP_LAYER_LOCAL_ATTENTION) continue;
     const uint64_t r = lp.d.type == TP_LAYER_CONV2D ? rows * conv_out_px(lp.d) : rows * lp.tokens;
     wg = std::max<uint64_t>(wg, bias_partials(*d, l, r));
     if (lp.d.type == TP_LAYER_DENSE)
       wg = std::max<uint64_t>(wg, tp::wgrad_scratch_floats(d->dtype, (int)r, lp.d.out_features, lp.d.in_features));
   }
-  p->partial_floats = round_up(std::max<uint64_t>({wg, tp::update_scratch_floats(), rows, conv_scratch, norm_scratch}), 64);
+  p->partial_floats = round_up(std::max<uint64_t>({wg, tp::update_scratch_floats(), rows * p->layers.back().tokens, conv_scratch, norm_scratch}), 64);
   // Every sum of partials the backward pass needs (bias and split weight gradients, scale and shift gradients of the
   // normalisations) is put off to one launch at its end: each keeps partials of its own until then.  Where the line lies is
   // decided by what the sums need at least, so that column sums left by another layer's kernel, which take more rows than a
@@ -1028,6 +1088,18 @@ int forward_impl(tp_stage* st, uint64_t mb_id, uint32_t ub_idx, uint32_t ubs, co
                                        lse, st->attn_scratch(), st->plan.attn_scratch_bytes));
       continue;
     }
+    if (lp.d.type == TP_LAYER_LOCAL_ATTENTION) {
+      ProfScope ps(st, TP_K_ATTN);
+      float* lse = (float*)(aslot + lp.stat_off) + row0 * lp.stat_elems;
+      float* kept = lp.kept_off == UINT64_MAX ? nullptr : (float*)(aslot + lp.kept_off) + (uint64_t)ub_idx * lp.w_elems;
+      // as last layer the output is kept beside what the caller gets: written twice by the kernel where it can be, else copied
+      void* out = lp.out_off == UINT64_MAX ? a_out : (void*)(aslot + lp.out_off + row0 * lp.out_elems * es);
+      const bool twice = out != a_out && ((uintptr_t)a_out & 15) == 0;
+      HIP_TRY(tp::launch_local_attention_fwd(fs, d.dtype, local_attention(lp.d, mb, mb), x_saved, kept ? master + lp.w_off : nullptr, kept,
+                                             out, twice ? a_out : nullptr, lse));
+      if (out != a_out && !twice) HIP_TRY(tp::launch_copy(fs, out, a_out, (size_t)mb * lp.out_elems * es));
+      continue;
+    }
     if (lp.d.type == TP_LAYER_RESIDUAL) {
       if (lp.skip_layer < 0) continue;  // begin: the next layer reads this layer's input in place
       if (lp.d.geom[1] == 2) continue;  // swap: this layer's input stays saved for the add, the next layer reads the begin's
@@ -1127,6 +1199,47 @@ int stage_loss_softmax_ce(tp_stage* st, uint64_t mb_id, const void* logits_dev, 
   ProfScope ps(st, TP_K_LOSS);
   HIP_TRY(tp::launch_softmax_ce(st->stream, st->desc.dtype, rows, classes, logits_dev, labels_dev, dlogits_dev,
                                 st->partials(), st->counter(tp_stage::kCountLoss), loss_dev));
+  return TP_OK;
+}
+
+int stage_loss_distill(tp_stage* st, uint64_t mb_id, const void* logits_dev, const float* teacher_logits_dev,
+                       const int32_t* teacher_ids_dev, int32_t k, double temperature, const int32_t* labels_dev, double label_weight,
+                       void* dlogits_dev, float* loss_dev) {
+  if (!st) return fail(TP_EINVAL, "null stage");
+  if (k < 1 || k > TP_MAX_TEACHER_ENTRIES) return fail(TP_EINVAL, "1 .. %d stored logits per row, not %d", TP_MAX_TEACHER_ENTRIES, k);
+  if (!(temperature >= 1e-6 && temperature <= 1e6))  // its square and the scaled logits stay finite in fp32
+    return fail(TP_EINVAL, "the temperature must be 1e-6 .. 1e6");
+  if (!(label_weight >= 0.0 && label_weight <= 1.0)) return fail(TP_EINVAL, "the labels' weight must be 0 .. 1");
+  InFlight* f = st->find_mb(mb_id);
+  if (!f || f->forwards != (uint32_t)st->desc.n)
+    return fail(TP_ESTATE, "loss of mini-batch %llu needs all %d forwards", (unsigned long long)mb_id, st->desc.n);
+  if (st->plan.layers.back().d.type != TP_LAYER_DENSE) return fail(TP_EINVAL, "the loss needs a dense last layer");
+  if (st->dry) return TP_OK;
+  if (!logits_dev || !teacher_logits_dev || !teacher_ids_dev || !dlogits_dev || !loss_dev || (label_weight > 0.0 && !labels_dev))
+    return fail(TP_EINVAL, "null pointer");
+  tp::DistillArgs a;
+  const LayerPlan& last = st->plan.layers.back();
+  const int64_t rows = (int64_t)st->desc.mb * st->desc.n * last.tokens;  // one for every token position
+  if (rows > INT32_MAX) return fail(TP_EINVAL, "the loss takes at most 2^31 - 1 rows");
+  a.rows = (int)rows;
+  a.classes = last.d.out_features;
+  const size_t bytes = (size_t)a.rows * a.classes * st->plan.elt_size;
+  if ((const char*)logits_dev < (char*)dlogits_dev + bytes && (char*)dlogits_dev < (const char*)logits_dev + bytes)
+    return fail(TP_EINVAL, "the gradient must not overlap the logits");
+  if (int rc = join_forwards(st)) return rc;
+  a.k = k;
+  a.logits = logits_dev;
+  a.teacher = teacher_logits_dev;
+  a.ids = teacher_ids_dev;
+  a.labels = labels_dev;
+  a.temperature = (float)temperature;
+  a.label_weight = (float)label_weight;
+  a.dlogits = dlogits_dev;
+  a.row_loss = st->partials();
+  a.counter = st->counter(tp_stage::kCountLoss);
+  a.loss = loss_dev;
+  ProfScope ps(st, TP_K_LOSS);
+  HIP_TRY(tp::launch_distill(st->stream, st->desc.dtype, a));
   return TP_OK;
 }
 
@@ -1260,7 +1373,7 @@ int backward_impl(tp_stage* st, uint64_t mb_id, const void* dy_dev, void* dx_dev
       const bool to_caller = l == 0;
       const bool no_dx = to_caller && !d.needs_dx;
       if (no_dx && (lp.d.type == TP_LAYER_MAXPOOL2 || lp.d.type == TP_LAYER_SUBSAMPLE2 || lp.d.type == TP_LAYER_ATTENTION ||
-                    lp.d.type == TP_LAYER_AVGPOOL))
+                    lp.d.type == TP_LAYER_AVGPOOL || (lp.d.type == TP_LAYER_LOCAL_ATTENTION && !lp.w_elems)))
         break;
       // what the gradient w.r.t. this layer's input is multiplied with: the saved act'(z) of the previous layer, or
       // (dmask = 1) that layer's saved ReLU output, which is this layer's own saved input
@@ -1459,6 +1572,21 @@ int backward_impl(tp_stage* st, uint64_t mb_id, const void* dy_dev, void* dx_dev
                                            (const float*)(aslot + lp.stat_off), dst, st->attn_scratch(),
                                            st->plan.attn_scratch_bytes));
         }
+        if (int rc = through_activation(dst)) return rc;
+        dz = dst;
+        continue;
+      }
+      if (lp.d.type == TP_LAYER_LOCAL_ATTENTION) {
+        {
+          ProfScope ps(st, TP_K_ATTN);
+          SumsDeferred later(sink);
+          const void* out = aslot + (lp.out_off != UINT64_MAX ? lp.out_off : st->plan.layers[l + 1].x_off);
+          const float* kept = lp.kept_off == UINT64_MAX ? nullptr : (const float*)(aslot + lp.kept_off);
+          HIP_TRY(tp::launch_local_attention_bwd(st->stream, d.dtype, local_attention(lp.d, rows, d.mb), aslot + lp.x_off, out, dz,
+                                                 (const float*)(aslot + lp.stat_off), kept, dst, kept ? g + lp.w_off : nullptr,
+                                                 kept ? hold(need.weight) : nullptr, st->attn_scratch()));
+        }
+        if (no_dx) break;
         if (int rc = through_activation(dst)) return rc;
         dz = dst;
         continue;

@@ -33,6 +33,8 @@ def layer_tuple(spec) -> tuple:
         return ("ln", spec.d, spec.tokens)
     if kind == "attn":
         return ("attn", spec.d, spec.heads, spec.tokens)
+    if kind == "local":
+        return ("local", spec.d, spec.heads, spec.tokens, spec.kv_heads, spec.window, spec.sinks, spec.buckets, spec.max_distance)
     if kind == "res":
         return ("res", spec.d, spec.tokens, spec.mark, spec.act)
     if kind == "bn":
@@ -109,10 +111,11 @@ class GpuStage:
         def raw(nbytes):
             return torch.zeros(max(int(nbytes), 256), dtype=torch.uint8, device=dev)
 
-        self.ring = torch.zeros(self.C * self.P, dtype=torch.float32, device=dev)
-        self.momentum = torch.zeros(self.P, dtype=torch.float32, device=dev)
-        self.grad = torch.zeros(self.P, dtype=torch.float32, device=dev)
-        self.wfwd = torch.zeros(self.P if dtype == "bf16" else 64, dtype=torch.bfloat16, device=dev)
+        held = max(self.P, 64)  # a stage without parameters has buffers all the same: the library takes no null pointers
+        self.ring = torch.zeros(max(self.C * self.P, 64), dtype=torch.float32, device=dev)
+        self.momentum = torch.zeros(held, dtype=torch.float32, device=dev)
+        self.grad = torch.zeros(held, dtype=torch.float32, device=dev)
+        self.wfwd = torch.zeros(held if dtype == "bf16" else 64, dtype=torch.bfloat16, device=dev)
         self.wbwd = torch.zeros(max(self.sizes.wbwd_bytes // (2 if dtype == "bf16" else 4), 64), dtype=self.tdtype, device=dev)
         self.act = raw(self.sizes.act_bytes)
         self.scratch = raw(self.sizes.scratch_bytes)
@@ -219,6 +222,24 @@ class GpuStage:
                                 loss.data_ptr())
         return loss, dlogits
 
+    def loss_distill(self, mb_id: int, logits: torch.Tensor, teacher: torch.Tensor, ids: torch.Tensor, *, temperature: float = 1.0,
+                     labels: Optional[torch.Tensor] = None, label_weight: float = 0.0):
+        """The loss against a teacher's stored top logits: teacher (float32) and ids (int32, negative: no entry) [rows, k], one row
+        for every sample, or for every token position of a last layer that has several; labels (int32, [rows]) weighted by
+        label_weight."""
+        classes = self.layers[-1][1]
+        rows = self.mb * self.n * self.out_elems // classes
+        assert logits.numel() == rows * classes and logits.is_contiguous() and logits.dtype == self.tdtype
+        assert teacher.dim() == 2 and teacher.size(0) == rows and teacher.dtype == torch.float32 and teacher.is_contiguous()
+        assert ids.shape == teacher.shape and ids.dtype == torch.int32 and ids.is_contiguous()
+        assert labels is None or (labels.dtype == torch.int32 and labels.numel() == rows and labels.is_contiguous())
+        dlogits = torch.empty_like(logits)
+        loss = torch.empty(1, dtype=torch.float32, device=self.device)
+        B.stage_loss_distill(self.handle, mb_id, logits.data_ptr(), teacher.data_ptr(), ids.data_ptr(), teacher.size(1),
+                             temperature, labels.data_ptr() if labels is not None else 0, label_weight, dlogits.data_ptr(),
+                             loss.data_ptr())
+        return loss, dlogits
+
     def backward(self, mb_id: int, dy: torch.Tensor, dx: Optional[torch.Tensor] = None):
         rows = self.mb * self.n
         assert dy.shape[0] == rows and dy.numel() == rows * self.out_elems and dy.is_contiguous()
@@ -240,7 +261,7 @@ class GpuStage:
         return B.stage_query(self.handle)
 
     def export(self, version: int) -> torch.Tensor:
-        out = torch.empty(self.P, dtype=torch.float32, device=self.device)
+        out = torch.empty(max(self.P, 1), dtype=torch.float32, device=self.device)[: self.P]
         B.stage_export_params(self.handle, version, out.data_ptr())
         return out
 
@@ -272,7 +293,9 @@ class GpuPipeline:
         self.device = torch.device(device)
 
     def run(self, num_mb: int, get_input: Callable[[int], torch.Tensor], get_labels: Callable[[int], torch.Tensor],
-            on_event=None):
+            on_event=None, get_teacher: Optional[Callable[[int], dict]] = None):
+        """get_teacher(j): what loss_distill takes beside logits and labels (teacher, ids, temperature, label_weight); the last
+        stage then learns from it instead of from labels alone."""
         w = self.w
         events = B.tp_schedule_events(self.K, num_mb)
         # per stage: mini-batches in backward order, to name the next backward for the fused update
@@ -296,7 +319,8 @@ class GpuPipeline:
             else:
                 if s == self.K - 1:
                     logits = acts.pop((s, j))
-                    loss, dy = st.loss(j, logits, get_labels(j))
+                    loss, dy = (st.loss(j, logits, get_labels(j)) if get_teacher is None else
+                                st.loss_distill(j, logits, labels=get_labels(j), **get_teacher(j)))
                     losses[j] = loss
                     info["loss"] = loss
                 else:

@@ -109,6 +109,35 @@ class Attention:
 
 
 @dataclass(frozen=True)
+class LocalAttention:
+    """Causal attention of `heads` query heads on `kv_heads` key heads over the last `window` keys (0: all) and the first `sinks`
+    keys, on [tokens, d + 2 * kv_heads * (d / heads)] (queries | keys | values) -> [tokens, d]; parameters: with buckets a table
+    [heads, buckets] of biases by distance (and an empty second tensor, so that layers with parameters have two)."""
+    d: int
+    heads: int
+    tokens: int
+    kv_heads: int
+    window: int = 0
+    sinks: int = 0
+    buckets: int = 0
+    max_distance: int = 0
+    kind: str = "local"
+    act: str = "none"
+
+    def param_shapes(self):
+        return [(self.heads, self.buckets), (0,)] if self.buckets else []
+
+    def in_shape(self):
+        return (self.tokens, self.d + 2 * self.kv_heads * (self.d // self.heads))
+
+    def out_shape(self):
+        return (self.tokens, self.d)
+
+    def out_dim(self):
+        return self.tokens * self.d
+
+
+@dataclass(frozen=True)
 class Residual:
     """mark = "begin": remember the current activation; mark = "add": add the remembered one, then apply the
     activation (if any). No parameters."""
@@ -425,6 +454,15 @@ def transformer_block(d: int, heads: int, ffn: int, tokens: int) -> tuple:
             Dense(ffn, d, "none", tokens=tokens), Residual(d, tokens, "add"))
 
 
+def windowed_block(d: int, heads: int, ffn: int, tokens: int, kv_heads: int, window: int, sinks: int, buckets: int,
+                   max_distance: int) -> tuple:
+    """transformer_block with windowed attention on shared key heads and a learned position bias."""
+    width = d + 2 * kv_heads * (d // heads)
+    return (Residual(d, tokens, "begin"), LayerNorm(d, tokens), Dense(d, width, "none", tokens=tokens),
+            LocalAttention(d, heads, tokens, kv_heads, window, sinks, buckets, max_distance), Dense(d, d, "none", tokens=tokens),
+            Residual(d, tokens, "add")) + transformer_block(d, heads, ffn, tokens)[6:]
+
+
 def transformer_stage(d: int = 2048, heads: int = 16, ffn: int = 8192, tokens: int = 1024, layers: int = 4, mb: int = 8,
                       n: int = 4, dtype: str = "bf16") -> Workload:
     """An interior stage of a decoder-only transformer: `layers` blocks on [tokens, d] hidden states, as stage 1
@@ -458,7 +496,8 @@ def init_params(w: Workload, s: int) -> List[np.ndarray]:
             out.append(np.zeros(bshape, dtype=np.float64))
             continue
         fan_in = int(np.prod(wshape[1:]))
-        W = _normal(f"{w.name}/s{s}/l{li}/W", wshape, std=float(np.sqrt(2.0 / fan_in)), seed=w.seed)
+        std = 0.5 if layer.kind == "local" else float(np.sqrt(2.0 / fan_in))   # scores are of order one
+        W = _normal(f"{w.name}/s{s}/l{li}/W", wshape, std=std, seed=w.seed)
         out.append(round_f32(W))
         out.append(np.zeros(bshape, dtype=np.float64))
     return out
