@@ -14,7 +14,7 @@
 
 #include "device_utils.h"
 #include "kernels.h"
-#include "local_attention.h"
+#include "local_attention_device.h"
 
 namespace tp {
 
@@ -40,24 +40,6 @@ DistanceBuckets make_distance_buckets(int buckets, int max_distance) {
 namespace {
 
 constexpr int kThreads = 256;
-constexpr float kLog2e = 1.4426950408889634f, kLn2 = 0.6931471805599453f;
-
-struct Shape {
-  int S, heads, kv, dh, window, sinks;
-  __host__ __device__ __forceinline__ size_t ld() const { return (size_t)(heads + 2 * kv) * dh; }
-  __device__ __forceinline__ bool sees(int i, int j) const { return j <= i && (i - j < window || j < sinks); }
-};
-inline Shape shape_of(const LocalAttention& a) { return Shape{a.S, a.heads, a.kv, a.dh, a.window, a.sinks}; }
-
-// Bucket of a distance >= 0: a first guess from the logarithm, then to the borders (one step at most, borders that coincide aside).
-// first: the borders in LDS.
-__device__ __forceinline__ int bucket_of(const DistanceBuckets& d, const int* first, int distance) {
-  if (distance < d.half) return distance;
-  int b = min(d.count - 1, d.half + (int)(__builtin_amdgcn_logf((float)distance / (float)d.half) * d.ratio));
-  while (distance < first[b]) --b;
-  while (b + 1 < d.count && distance >= first[b + 1]) ++b;
-  return b;
-}
 
 // ---- any head width and address -------------------------------------------------------------------------------------------
 // A workgroup owns 16 rows (four per wave) and walks over the other side in tiles staged in LDS as fp32; lane = pair for the dot
@@ -449,15 +431,25 @@ bool local_attention_supported(const LocalAttention& a) {
          any_blocks(a) <= (1 << 23) && any_lds(a) <= 156 * 1024;
 }
 
-size_t local_attention_scratch_bytes(int elt, const LocalAttention& a) { return ((size_t)a.seqs * a.heads * a.S * sizeof(float) + 255) / 256 * 256; }
+size_t local_attention_scratch_bytes(int elt, const LocalAttention& a) {
+  const size_t any = (size_t)a.seqs * a.heads * a.S * sizeof(float);
+  return ((local_mfma_supported(elt, a) ? std::max(any, local_mfma_scratch_bytes(elt, a)) : any) + 255) / 256 * 256;
+}
 
 size_t local_attention_table_floats(int elt, const LocalAttention& a) {
-  return a.buckets ? (size_t)any_dkv_blocks(a) * a.heads * a.buckets : 0;
+  if (!a.buckets) return 0;
+  const int rows = local_mfma_supported(elt, a) ? std::max(any_dkv_blocks(a), local_mfma_table_rows(elt, a)) : any_dkv_blocks(a);
+  return (size_t)rows * a.heads * a.buckets;
+}
+
+static bool aligned(const void* a, const void* b, const void* c, const void* d) {
+  return (((uintptr_t)a | (uintptr_t)b | (uintptr_t)c | (uintptr_t)d) & 15) == 0;
 }
 
 hipError_t launch_local_attention_fwd(hipStream_t s, int elt, const LocalAttention& a, const void* x, const float* table, float* kept,
                                       void* out, void* out2, float* lse) {
   if (!local_attention_supported(a)) return hipErrorInvalidValue;
+  if (local_mfma_supported(elt, a) && aligned(x, out, out2, nullptr)) return local_mfma_fwd(s, elt, a, x, table, kept, out, out2, lse);
   if (elt == ELT_BF16) return any_fwd(s, a, (const uint16_t*)x, table, kept, (uint16_t*)out, (uint16_t*)out2, lse);
   return any_fwd(s, a, (const float*)x, table, kept, (float*)out, (float*)out2, lse);
 }
@@ -465,13 +457,19 @@ hipError_t launch_local_attention_fwd(hipStream_t s, int elt, const LocalAttenti
 hipError_t launch_local_attention_bwd(hipStream_t s, int elt, const LocalAttention& a, const void* x, const void* out, const void* dout,
                                       const float* lse, const float* kept, void* dx, float* dtable, float* partials, void* scratch) {
   if (!local_attention_supported(a)) return hipErrorInvalidValue;
-  float* delta = (float*)scratch;
-  const hipError_t e = elt == ELT_BF16 ? any_bwd(s, a, (const uint16_t*)x, (const uint16_t*)out, (const uint16_t*)dout, lse, kept,
-                                                 (uint16_t*)dx, partials, delta)
-                                       : any_bwd(s, a, (const float*)x, (const float*)out, (const float*)dout, lse, kept, (float*)dx,
-                                                 partials, delta);
+  hipError_t e;
+  int rows;
+  if (local_mfma_supported(elt, a) && aligned(x, out, dout, dx)) {
+    e = local_mfma_bwd(s, elt, a, x, out, dout, lse, kept, dx, partials, scratch);
+    rows = local_mfma_table_rows(elt, a);
+  } else {
+    float* delta = (float*)scratch;
+    e = elt == ELT_BF16 ? any_bwd(s, a, (const uint16_t*)x, (const uint16_t*)out, (const uint16_t*)dout, lse, kept, (uint16_t*)dx, partials, delta)
+                        : any_bwd(s, a, (const float*)x, (const float*)out, (const float*)dout, lse, kept, (float*)dx, partials, delta);
+    rows = any_dkv_blocks(a);
+  }
   if (e != hipSuccess || !a.buckets) return e;
-  return launch_sum_partials(s, (size_t)a.heads * a.buckets, any_dkv_blocks(a), partials, dtable);
+  return launch_sum_partials(s, (size_t)a.heads * a.buckets, rows, partials, dtable);
 }
 
 }  // namespace tp

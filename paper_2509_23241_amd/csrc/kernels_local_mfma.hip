@@ -1,0 +1,1075 @@
+// Windowed attention on the matrix cores, bf16 and fp32, for heads of up to 128 values in whole 16-byte units.
+//
+// A wave owns 32 rows -- queries in the forward pass and for dQ, keys for dK and dV -- with their fragments in registers, and walks over
+// blocks of the other side, which its workgroup copies global -> LDS.  It forms the transposed score tile: MFMA rows = streamed rows,
+// columns = own rows, so that a lane holds one own row (lane % 32) and 16 of a tile's 32 streamed rows, statistics of a query are scalars of
+// its lane, and eight consecutive accumulator elements are the B fragment of the second product.
+//   forward  S^T = K Q^T, online softmax, O^T += V^T P^T
+//   dQ       S^T, dP^T = V dO^T, dS, dQ^T += K^T dS^T; leaves (lse, corrected delta) of its rows for the next launch
+//   dK, dV   S = Q K^T, dP = dO V^T, dV^T += dO^T P, dK^T += Q^T dS, and the sums of dS by distance
+// Own rows: a wave takes the item (block of 32 queries, query head) of its key head, heads fastest, so that the waves of a workgroup walk
+// over nearly the same keys whether heads share them or not.
+// Streamed tiles lie in LDS once, as panels of 128-byte rows whose 16-byte chunk c is in slot c ^ f(row), f = the bits 1, 2, 3 of the row
+// number as 4, 2, 1: conflict free both for the 16-byte reads of the first products (row by row: the eight pairs of rows take all slots) and
+// for the transposing reads of the second (four rows of 64 bytes: rows that are 256 bytes apart fall into different halves).
+// Rows behind the last and columns behind the head's width are copied from zeros.
+// Pairs that are not visible count as p = dS = 0, but a product with an infinity or NaN of their row is NaN: a wave whose result is not
+// finite forms those rows again from the visible pairs alone.
+#include <hip/hip_runtime.h>
+#include <math.h>
+#include <stdint.h>
+
+#include <algorithm>
+
+#include "device_utils.h"
+#include "kernels.h"
+#include "local_attention_device.h"
+#include "mfma_common.h"
+
+namespace tp {
+
+namespace {
+
+constexpr float kLowest = -1e30f;  // running maximum of a row that has seen no key; scores below it are formed again, row by row
+constexpr int kNear = 112;         // distances with a table entry and a sum of their own: 0 .. kNear - 1, and as far as a tile reaches beyond
+constexpr int kPad = 96;           // a tile of 32 x 64 spans 95 distances
+constexpr int kNearSize = kPad + kNear + kPad;
+
+template <typename T>
+struct Type;
+template <>
+struct Type<uint16_t> {
+  static constexpr int BR = 64;  // streamed rows of a block
+  using Frag = bf16x8;
+  static __device__ __forceinline__ floatx16 mma(const Frag& a, const Frag& b, floatx16 c) {
+    return __builtin_amdgcn_mfma_f32_32x32x16_bf16(a, b, c, 0, 0, 0);
+  }
+  static __device__ __forceinline__ Frag zero() { return __builtin_bit_cast(bf16x8, make_uint4(0, 0, 0, 0)); }
+  // P and dS enter the second products rounded to bf16, like every operand there: 2^-9 of each, on average less of their sum
+  static __device__ __forceinline__ Frag pack(const float (&e)[8]) {
+    return __builtin_bit_cast(bf16x8, make_uint4(pack_bf16x2(e[0], e[1]), pack_bf16x2(e[2], e[3]), pack_bf16x2(e[4], e[5]), pack_bf16x2(e[6], e[7])));
+  }
+  // values d .. d + 7 of a row that holds `left` more of them (a multiple of 8, or none)
+  static __device__ __forceinline__ Frag load(const uint16_t* p, int left) {
+    return left > 0 ? __builtin_bit_cast(bf16x8, *reinterpret_cast<const uint4*>(p)) : zero();
+  }
+  static __device__ __forceinline__ float dot(const Frag& a, const Frag& b, float s) {
+#pragma unroll
+    for (int t = 0; t < 8; ++t) s = fmaf((float)a[t], (float)b[t], s);
+    return s;
+  }
+  static __device__ __forceinline__ void store8(uint16_t* p, const float (&v)[8], int left) {
+    if (left > 0)
+      *reinterpret_cast<uint4*>(p) = make_uint4(pack_bf16x2(v[0], v[1]), pack_bf16x2(v[2], v[3]), pack_bf16x2(v[4], v[5]), pack_bf16x2(v[6], v[7]));
+  }
+};
+typedef float floatx8 __attribute__((ext_vector_type(8)));
+template <>
+struct Type<float> {
+  static constexpr int BR = 32;
+  using Frag = floatx8;
+  static __device__ __forceinline__ floatx16 mma(const Frag& a, const Frag& b, floatx16 c) {
+#pragma unroll
+    for (int t = 0; t < 8; ++t) c = __builtin_amdgcn_mfma_f32_32x32x2f32(a[t], b[t], c, 0, 0, 0);
+    return c;
+  }
+  static __device__ __forceinline__ Frag zero() { return Frag{0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f}; }
+  static __device__ __forceinline__ Frag pack(const float (&e)[8]) {
+    Frag f;
+#pragma unroll
+    for (int t = 0; t < 8; ++t) f[t] = e[t];
+    return f;
+  }
+  static __device__ __forceinline__ Frag load(const float* p, int left) {  // left: a multiple of 4
+    Frag f = zero();
+    if (left > 0) {
+      const float4 a = *reinterpret_cast<const float4*>(p);
+      f[0] = a.x; f[1] = a.y; f[2] = a.z; f[3] = a.w;
+    }
+    if (left > 4) {
+      const float4 a = *reinterpret_cast<const float4*>(p + 4);
+      f[4] = a.x; f[5] = a.y; f[6] = a.z; f[7] = a.w;
+    }
+    return f;
+  }
+  static __device__ __forceinline__ float dot(const Frag& a, const Frag& b, float s) {
+#pragma unroll
+    for (int t = 0; t < 8; ++t) s = fmaf(a[t], b[t], s);
+    return s;
+  }
+  static __device__ __forceinline__ void store8(float* p, const float (&v)[8], int left) {
+    if (left > 0) *reinterpret_cast<float4*>(p) = make_float4(v[0], v[1], v[2], v[3]);
+    if (left > 4) *reinterpret_cast<float4*>(p + 4) = make_float4(v[4], v[5], v[6], v[7]);
+  }
+};
+
+// ---- a streamed tile in LDS -------------------------------------------------------------------------------------------------
+__device__ __forceinline__ int swizzle(int row) { return 4 * ((row >> 1) & 1) + 2 * ((row >> 2) & 1) + ((row >> 3) & 1); }
+
+template <typename T, int DHP, int NW>
+struct Tile {
+  static constexpr int BR = Type<T>::BR, E = sizeof(T);
+  static constexpr int kPanels = DHP * E / 128, kPanelBytes = BR * 128, kBytes = kPanels * kPanelBytes;
+  static constexpr int kInstr = kBytes / 1024, kPerWave = kInstr / NW;  // a wave instruction copies 8 rows of a panel
+  static_assert(kInstr % NW == 0, "copies do not divide among the waves");
+  // offsets of this lane's chunks inside a block whose rows are ld elements apart
+  struct Offsets {
+    uint32_t at[kPerWave];
+    __device__ __forceinline__ void init(size_t ld, int wave, int lane) {
+#pragma unroll
+      for (int t = 0; t < kPerWave; ++t) {
+        const int n = wave + NW * t, r = 8 * (n % (BR / 8)) + (lane >> 3);
+        at[t] = (uint32_t)(r * ld * E + (n / (BR / 8)) * 128 + (((lane & 7) ^ swizzle(r)) * 16));
+      }
+    }
+  };
+  // base: the block's first row.  whole: BR rows and DHP columns are there; else rows and `cols` of them
+  static __device__ __forceinline__ void copy(uint32_t lds, const T* base, const Offsets& o, bool whole, int rows, int cols, int wave, int lane) {
+    if (whole) {
+#pragma unroll
+      for (int t = 0; t < kPerWave; ++t) dma16(lds + (wave + NW * t) * 1024, base, o.at[t]);
+    } else {
+#pragma unroll
+      for (int t = 0; t < kPerWave; ++t) {
+        const int n = wave + NW * t, r = 8 * (n % (BR / 8)) + (lane >> 3);
+        const int byte = (n / (BR / 8)) * 128 + (((lane & 7) ^ swizzle(r)) * 16);
+        dma_addr<16>(lds + n * 1024, r < rows && byte < cols * E ? (const char*)base + o.at[t] : zero_chunk());
+      }
+    }
+  }
+  // A fragment of the first products: row rbase + lane % 32, columns 16 kk + 8 (lane / 32) .. + 7
+  static __device__ __forceinline__ typename Type<T>::Frag row_frag(const char* lds, int rbase, int kk, int lane) {
+    const int r = rbase + (lane & 31);
+    if constexpr (E == 2) {
+      const int c = 2 * (kk & 3) + (lane >> 5);
+      return __builtin_bit_cast(bf16x8, *reinterpret_cast<const uint4*>(lds + (kk >> 2) * kPanelBytes + r * 128 + ((c ^ swizzle(r)) * 16)));
+    } else {
+      const int c = 4 * (kk & 1) + 2 * (lane >> 5);
+      const char* row = lds + (kk >> 1) * kPanelBytes + r * 128;
+      const float4 a = *reinterpret_cast<const float4*>(row + ((c ^ swizzle(r)) * 16));
+      const float4 b = *reinterpret_cast<const float4*>(row + (((c + 1) ^ swizzle(r)) * 16));
+      return floatx8{a.x, a.y, a.z, a.w, b.x, b.y, b.z, b.w};
+    }
+  }
+  // A fragment of the second products: column 32 j + lane % 32 of rows 16 g + 8 (t / 4) + 4 (lane / 32) + t % 4, t = 0 .. 7, the order in
+  // which the accumulators hold them
+  static __device__ __forceinline__ typename Type<T>::Frag col_frag(const char* lds, int j, int g, int lane) {
+    if constexpr (E == 2) {
+      const int q = lane >> 4, s = lane & 15;
+      const int k = 16 * g + 4 * (q >> 1) + (s >> 2);
+      const int col = 32 * (j & 1) + 16 * (q & 1) + 4 * (s & 3);
+      typedef __attribute__((address_space(3))) shortx4* lds_ptr;
+      const char* panel = lds + (j >> 1) * kPanelBytes;
+      const shortx4 lo = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_ptr)(panel + k * 128 + (((col >> 3) ^ swizzle(k)) * 16) + (col & 7) * 2));
+      const shortx4 hi = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_ptr)(panel + (k + 8) * 128 + (((col >> 3) ^ swizzle(k + 8)) * 16) + (col & 7) * 2));
+      return __builtin_bit_cast(bf16x8, __builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7));
+    } else {
+      floatx8 f;
+      const int c = (lane & 31) >> 2;
+#pragma unroll
+      for (int t = 0; t < 8; ++t) {
+        const int k = 16 * g + 8 * (t >> 2) + 4 * (lane >> 5) + (t & 3);
+        f[t] = *reinterpret_cast<const float*>(lds + j * kPanelBytes + k * 128 + ((c ^ swizzle(k)) * 16) + (lane & 3) * 4);
+      }
+      return f;
+    }
+  }
+};
+
+// ---- the bias in LDS ----------------------------------------------------------------------------------------------------------
+// near[kPad + d], d = -kPad .. kNear + kPad - 1: the table by distance, in units of log2; beyond that by bucket.
+struct BiasLds {
+  float near[kNearSize];
+  float value[kMaxBuckets];
+  // by the `threads` threads that share it, with the borders in LDS
+  __device__ __forceinline__ void load(const DistanceBuckets& d, const int* first, const float* row, int thread, int threads) {
+    for (int b = thread; b < d.count; b += threads) value[b] = row[b] * kLog2e;
+    for (int i = thread; i < kNearSize; i += threads) near[i] = i < kPad ? 0.f : row[bucket_of(d, first, i - kPad)] * kLog2e;
+  }
+};
+__device__ __forceinline__ void load_borders(const DistanceBuckets& d, int* first) {
+  for (int b = threadIdx.x; b < d.count; b += blockDim.x) first[b] = d.first[b];
+}
+
+// What a lane's 16 elements of a tile have added to their scaled scores.  Element r has distance base + sign * (8 (r / 4) + r % 4);
+// dmin, dmax: the tile's smallest and largest, wave uniform.
+template <int SIGN>
+__device__ __forceinline__ void tile_bias(const BiasLds& bl, const DistanceBuckets& d, const int* first, int base, int dmin, int dmax,
+                                          float (&out)[16]) {
+  if (dmin < kNear) {
+    const float* at = bl.near + kPad + base;
+#pragma unroll
+    for (int r = 0; r < 16; ++r) out[r] = at[SIGN * (8 * (r >> 2) + (r & 3))];
+  } else {
+    const int b0 = __builtin_amdgcn_readfirstlane(bucket_of(d, first, dmin)), b1 = __builtin_amdgcn_readfirstlane(bucket_of(d, first, dmax));
+    const float v = bl.value[b0];
+#pragma unroll
+    for (int r = 0; r < 16; ++r) out[r] = v;
+    for (int b = b0 + 1; b <= b1; ++b) {
+      const int from = first[b];
+      const float w = bl.value[b];
+#pragma unroll
+      for (int r = 0; r < 16; ++r)
+        if (base + SIGN * (8 * (r >> 2) + (r & 3)) >= from) out[r] = w;
+    }
+  }
+}
+
+// ---- turning a wave's transposed result through LDS for whole rows ----------------------------------------------------------------
+constexpr int kTurnPitch = 64 + 4, kTurnBytes = 32 * kTurnPitch * 4;
+// write(row, column, v[8]) for the 32 rows of acc^T
+template <int TN, class Write>
+__device__ __forceinline__ void turned_rows(const floatx16 (&acc)[TN], float factor, float* lds, int lane, const Write& write) {
+#pragma unroll
+  for (int c = 0; c < TN / 2; ++c) {
+#pragma unroll
+    for (int j = 0; j < 2; ++j)
+#pragma unroll
+      for (int g = 0; g < 4; ++g) {
+        const floatx16& a = acc[2 * c + j];
+        *reinterpret_cast<float4*>(lds + (lane & 31) * kTurnPitch + 32 * j + 8 * g + 4 * (lane >> 5)) =
+            make_float4(a[4 * g] * factor, a[4 * g + 1] * factor, a[4 * g + 2] * factor, a[4 * g + 3] * factor);
+      }
+    // one wave on both sides, whose LDS operations complete in order
+    __builtin_amdgcn_fence(__ATOMIC_RELEASE, "wavefront");
+    __builtin_amdgcn_wave_barrier();
+    __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "wavefront");
+#pragma unroll
+    for (int p = 0; p < 4; ++p) {
+      const int r = 8 * p + (lane >> 3), col = 8 * (lane & 7);
+      const float4 lo = *reinterpret_cast<const float4*>(lds + r * kTurnPitch + col), hi = *reinterpret_cast<const float4*>(lds + r * kTurnPitch + col + 4);
+      const float v[8] = {lo.x, lo.y, lo.z, lo.w, hi.x, hi.y, hi.z, hi.w};
+      write(r, 64 * c + col, v);
+    }
+    __builtin_amdgcn_fence(__ATOMIC_RELEASE, "wavefront");
+    __builtin_amdgcn_wave_barrier();
+    __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "wavefront");
+  }
+}
+
+// ---- rows one by one ----------------------------------------------------------------------------------------------------------
+template <int TN>
+__device__ __forceinline__ bool finite(const floatx16 (&acc)[TN]) {
+  float s = 0.f;
+#pragma unroll
+  for (int j = 0; j < TN; ++j)
+#pragma unroll
+    for (int r = 0; r < 16; ++r) s = fmaf(acc[j][r], 0.f, s);  // 0, or NaN
+  return s == 0.f;
+}
+// bit i: row i of the wave (lanes i and i + 32) is there and not finite
+__device__ __forceinline__ uint32_t rows_to_redo(bool fine, bool there) {
+  const uint64_t m = __builtin_amdgcn_ballot_w64(!fine && there);
+  return (uint32_t)m | (uint32_t)(m >> 32);
+}
+template <typename T>
+__device__ __forceinline__ float row_dot(const T* a, const T* b, int dh) {
+  float s = 0.f;
+  for (int d = 0; d < dh; ++d) s = fmaf(to_float(a[d]), to_float(b[d]), s);
+  return s;
+}
+// acc[c] += w (of lane t) * row t's value in this lane's column, over the lanes in `which`
+template <typename T>
+__device__ __forceinline__ void add_rows(float (&acc)[2], float w, const T* rows, size_t ld, uint64_t which, int dh, int lane) {
+  for (; which; which &= which - 1) {
+    const int t = __builtin_ctzll(which);
+    const float wt = __int_as_float(__builtin_amdgcn_readlane(__float_as_int(w), t));
+#pragma unroll
+    for (int c = 0; c < 2; ++c)
+      if (lane + 64 * c < dh) acc[c] = fmaf(wt, to_float(rows[(size_t)t * ld + lane + 64 * c]), acc[c]);
+  }
+}
+// the tiles of 64 keys that query i sees something of: calls body(first key)
+template <class Body>
+__device__ __forceinline__ void visible_tiles(const Shape& a, int i, const Body& body) {
+  const int lo = max(0, i - a.window + 1);
+  for (int k0 = 0; k0 <= i; k0 += 64) {
+    if (k0 >= a.sinks && k0 + 64 <= lo) k0 = lo / 64 * 64;
+    body(k0);
+  }
+}
+
+template <typename T, bool BIAS>
+__device__ void redo_output_row(const Shape& a, const DistanceBuckets& db, const int* first, const BiasLds* bl, int i, const T* q, const T* k,
+                                const T* v, T* out, T* out2, float* lse, float scale_log2, int lane) {
+  const size_t ld = a.ld();
+  float m = -INFINITY, l = 0.f, o[2] = {};
+  visible_tiles(a, i, [&](int k0) {
+    const int j = k0 + lane;
+    const bool sees = j <= i && a.sees(i, j);
+    float sc = -INFINITY;
+    if (sees) {
+      sc = row_dot(q + (size_t)i * ld, k + (size_t)j * ld, a.dh) * scale_log2;
+      if (BIAS) sc += bl->value[bucket_of(db, first, i - j)];
+    }
+    const float mn = fmaxf(m, max_over_lanes(sc));
+    // a NaN score is NaN in p, whatever the maximum; a row whose scores are all -inf is NaN through its sum of zero
+    const float p = sc == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(sc - mn);
+    const float corr = m == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(m - mn);
+    l = l * corr + sum_over_lanes(p);
+    m = mn;
+    o[0] *= corr;
+    o[1] *= corr;
+    add_rows(o, p, v + (size_t)k0 * ld, ld, __builtin_amdgcn_ballot_w64(sees), a.dh, lane);
+  });
+  const float inv = 1.f / l;
+#pragma unroll
+  for (int c = 0; c < 2; ++c)
+    if (lane + 64 * c < a.dh) {
+      out[lane + 64 * c] = from_float<T>(o[c] * inv);
+      if (out2) out2[lane + 64 * c] = from_float<T>(o[c] * inv);
+    }
+  if (lane == 0) *lse = (m + __builtin_amdgcn_logf(l)) * kLn2;
+}
+
+template <typename T, bool BIAS>
+__device__ void redo_dq_row(const Shape& a, const DistanceBuckets& db, const int* first, const BiasLds* bl, int i, const T* q, const T* k,
+                            const T* v, const T* dout_row, float l2, float delta, T* dq, float scale, int lane) {
+  const size_t ld = a.ld();
+  float acc[2] = {};
+  visible_tiles(a, i, [&](int k0) {
+    const int j = k0 + lane;
+    const bool sees = j <= i && a.sees(i, j);
+    float ds = 0.f;
+    if (sees) {
+      float e = row_dot(q + (size_t)i * ld, k + (size_t)j * ld, a.dh) * (scale * kLog2e) - l2;
+      if (BIAS) e += bl->value[bucket_of(db, first, i - j)];
+      ds = __builtin_amdgcn_exp2f(e) * (row_dot(dout_row, v + (size_t)j * ld, a.dh) - delta);
+    }
+    add_rows(acc, ds, k + (size_t)k0 * ld, ld, __builtin_amdgcn_ballot_w64(sees), a.dh, lane);
+  });
+#pragma unroll
+  for (int c = 0; c < 2; ++c)
+    if (lane + 64 * c < a.dh) dq[lane + 64 * c] = from_float<T>(acc[c] * scale);
+}
+
+// ---- forward --------------------------------------------------------------------------------------------------------------------
+template <typename T>
+struct FwdArgs {
+  Shape a;
+  DistanceBuckets db;
+  const T* x;
+  const float* table;
+  float* kept;
+  T *out, *out2;
+  float* lse;
+  float scale_log2;
+};
+
+// LDS behind the streamed tiles where there is a bias: the borders, then a table per wave
+template <int NW>
+constexpr size_t bias_lds(bool bias) { return bias ? kMaxBuckets * 4 + NW * sizeof(BiasLds) : 0; }
+
+// Items of a workgroup: blocks of 32 queries x heads of key head kvh, and the blocks of keys they walk over
+template <int BR, int NW>
+struct QueryItems {
+  int item, items, q_lo, q_hi, blk, g;  // this wave's item; the workgroup's queries
+  int first_blk, sink_blks, count;      // streamed blocks: 0 .. sink_blks - 1, then from first_blk on
+  __device__ __forceinline__ QueryItems(const Shape& a, int group, int nblk, int wg, int wave) {
+    items = nblk * group;
+    item = wg * NW + wave;
+    blk = item / group;
+    g = item - blk * group;
+    q_lo = wg * NW / group * 32;
+    q_hi = min(a.S - 1, min(wg * NW + NW - 1, items - 1) / group * 32 + 31);
+    first_blk = max(0, q_lo - a.window + 1) / BR;
+    sink_blks = min((a.sinks + BR - 1) / BR, first_blk);
+    count = q_hi < q_lo ? 0 : sink_blks + q_hi / BR - first_blk + 1;
+  }
+  __device__ __forceinline__ int block(int t) const { return t < sink_blks ? t : first_blk + t - sink_blks; }
+};
+
+template <typename T, int DHP, int NW, bool BIAS>
+__global__ __launch_bounds__(64 * NW, 2) void local_fwd_kernel(FwdArgs<T> p) {
+  using TY = Type<T>;
+  using TL = Tile<T, DHP, NW>;
+  constexpr int BR = TY::BR, NT = BR / 32, KK = DHP / 16, TN = DHP / 32;
+  extern __shared__ __attribute__((aligned(16))) char lds[];
+  const Shape& a = p.a;
+  const int lane = threadIdx.x & 63, half = lane >> 5;
+  const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const int group = a.heads / a.kv, b = blockIdx.x / a.kv, kvh = blockIdx.x - b * a.kv;
+  const int S = a.S, dh = a.dh;
+  const size_t ld = a.ld(), D = (size_t)a.heads * dh;
+  const QueryItems<BR, NW> it(a, group, (S + 31) / 32, gridDim.y - 1 - blockIdx.y, wave);
+  const bool active = it.item < it.items;
+  const int h = kvh * group + (active ? it.g : 0), qw = (active ? it.blk : 0) * 32;
+  const T* base = p.x + (size_t)b * S * ld;
+  const T* qbase = base + (size_t)h * dh;
+  const T* kbase = base + D + (size_t)kvh * dh;
+  const T* vbase = kbase + (size_t)a.kv * dh;
+  const uint32_t lds0 = lds_addr_of(lds);
+  constexpr size_t kStages = 2 * 2 * TL::kBytes, kTiles = kStages > NW * kTurnBytes ? kStages : NW * kTurnBytes;
+  int* first = reinterpret_cast<int*>(lds + kTiles);
+  BiasLds* bl = reinterpret_cast<BiasLds*>(lds + kTiles + kMaxBuckets * 4) + wave;
+  if constexpr (BIAS) {
+    load_borders(p.db, first);
+    __syncthreads();
+    const float* row = p.table + (size_t)h * p.db.count;
+    bl->load(p.db, first, row, lane, 64);
+    if (b == 0 && active && it.blk == 0)
+      for (int t = lane; t < p.db.count; t += 64) p.kept[(size_t)h * p.db.count + t] = row[t];
+  }
+
+  const int query = min(qw + (lane & 31), S - 1);
+  typename TY::Frag qf[KK];
+#pragma unroll
+  for (int kk = 0; kk < KK; ++kk) qf[kk] = TY::load(qbase + (size_t)query * ld + 16 * kk + 8 * half, dh - 16 * kk - 8 * half);
+  wait_vmcnt<0>();  // nothing but the copies below is in flight from here on
+#pragma unroll
+  for (int kk = 0; kk < KK; ++kk) asm volatile("" : "+v"(qf[kk]));
+
+  typename TL::Offsets off;
+  off.init(ld, wave, lane);
+  auto issue = [&](int t) {
+    const int row = it.block(t) * BR;
+    const uint32_t to = lds0 + (t & 1) * 2 * TL::kBytes;
+    const bool whole = dh == DHP && row + BR <= S;
+    TL::copy(to, kbase + (size_t)row * ld, off, whole, S - row, dh, wave, lane);
+    TL::copy(to + TL::kBytes, vbase + (size_t)row * ld, off, whole, S - row, dh, wave, lane);
+  };
+  floatx16 oacc[TN];
+#pragma unroll
+  for (int j = 0; j < TN; ++j)
+#pragma unroll
+    for (int r = 0; r < 16; ++r) oacc[j][r] = 0.f;
+  float mrun = kLowest, lsum = 0.f;
+  const int q_last = min(qw + 31, S - 1);
+  if (it.count > 0) issue(0);
+  for (int t = 0; t < it.count; ++t) {
+    wait_vmcnt<0>();
+    lds_barrier();  // block t is there, and nobody reads the other stage any more
+    if (t + 1 < it.count) issue(t + 1);
+    const int kb = it.block(t) * BR;
+    // wave uniform: some pair of this wave and block is visible
+    if (!active || kb > q_last || (kb >= a.sinks && kb + BR - 1 <= qw - a.window)) continue;
+    const char* lk = lds + (t & 1) * 2 * TL::kBytes;
+    const char* lv = lk + TL::kBytes;
+    floatx16 sacc[NT];
+#pragma unroll
+    for (int u = 0; u < NT; ++u) {
+#pragma unroll
+      for (int r = 0; r < 16; ++r) sacc[u][r] = 0.f;
+#pragma unroll
+      for (int kk = 0; kk < KK; ++kk) sacc[u] = TY::mma(TL::row_frag(lk, 32 * u, kk, lane), qf[kk], sacc[u]);
+    }
+    const int dmin = qw - (kb + BR - 1), dmax = qw + 31 - kb;
+    const bool masked = !(dmin >= 0 && (dmax < a.window || kb + BR <= a.sinks));
+    const int d0 = query - kb - 4 * half;  // distance of element r of tile u: d0 - 32 u - 8 (r / 4) - r % 4
+    float mx = mrun;
+#pragma unroll
+    for (int u = 0; u < NT; ++u) {
+      float bias[16];
+      if constexpr (BIAS) tile_bias<-1>(*bl, p.db, first, d0 - 32 * u, dmin + BR - 32 * (u + 1), dmax - 32 * u, bias);
+#pragma unroll
+      for (int r = 0; r < 16; ++r) {
+        float s = BIAS ? fmaf(sacc[u][r], p.scale_log2, bias[r]) : sacc[u][r] * p.scale_log2;
+        if (masked) {
+          const int d = d0 - 32 * u - 8 * (r >> 2) - (r & 3), key = query - d;
+          s = d >= 0 && (d < a.window || key < a.sinks) ? s : -INFINITY;
+        }
+        sacc[u][r] = s;
+        mx = fmaxf(mx, s);
+      }
+    }
+    const float mnew = over_halves(mx, Max());
+    const float alpha = __builtin_amdgcn_exp2f(mrun - mnew);
+    mrun = mnew;
+    float psum = 0.f;
+    typename TY::Frag pf[2 * NT];
+#pragma unroll
+    for (int g = 0; g < 2 * NT; ++g) {
+      float e[8];
+#pragma unroll
+      for (int r = 0; r < 8; ++r) {
+        e[r] = __builtin_amdgcn_exp2f(sacc[g >> 1][8 * (g & 1) + r] - mnew);
+        psum += e[r];
+      }
+      pf[g] = TY::pack(e);
+    }
+    lsum = fmaf(lsum, alpha, psum);
+    if (__builtin_amdgcn_ballot_w64(alpha != 1.f) != 0) {  // some row's maximum moved
+#pragma unroll
+      for (int j = 0; j < TN; ++j)
+#pragma unroll
+        for (int r = 0; r < 16; ++r) oacc[j][r] *= alpha;
+    }
+#pragma unroll
+    for (int g = 0; g < 2 * NT; ++g)
+#pragma unroll
+      for (int j = 0; j < TN; ++j) oacc[j] = TY::mma(TL::col_frag(lv, j, g, lane), pf[g], oacc[j]);
+  }
+  lds_barrier();  // the stages are free
+  if (!active) return;
+  const float ltot = over_halves(lsum, Add());
+  const float inv = 1.f / ltot;
+#pragma unroll
+  for (int j = 0; j < TN; ++j)
+#pragma unroll
+    for (int r = 0; r < 16; ++r) oacc[j][r] *= inv;
+  const bool there = qw + (lane & 31) < S;
+  float* lse = p.lse + ((size_t)b * a.heads + h) * S;
+  if (half == 0 && there) lse[query] = (mrun + __builtin_amdgcn_logf(ltot)) * kLn2;
+  const size_t at = ((size_t)b * S + qw) * D + (size_t)h * dh;
+  turned_rows(oacc, 1.f, reinterpret_cast<float*>(lds) + wave * (kTurnBytes / 4), lane, [&](int r, int col, const float (&v)[8]) {
+    if (qw + r >= S) return;
+    TY::store8(p.out + at + (size_t)r * D + col, v, dh - col);
+    if (p.out2) TY::store8(p.out2 + at + (size_t)r * D + col, v, dh - col);
+  });
+  uint32_t redo = rows_to_redo(finite(oacc), there);
+  if (redo) wait_vmcnt<0>();  // what they replace is stored
+  for (; redo; redo &= redo - 1) {
+    const int r = __builtin_ctz(redo);
+    redo_output_row<T, BIAS>(a, p.db, first, bl, qw + r, qbase, kbase, vbase, p.out + at + (size_t)r * D,
+                             p.out2 ? p.out2 + at + (size_t)r * D : nullptr, lse + qw + r, p.scale_log2, lane);
+  }
+}
+
+// ---- backward -------------------------------------------------------------------------------------------------------------------
+__host__ __device__ constexpr int stat_rows(int S) { return (S + 63) / 64 * 64; }
+
+template <typename T>
+struct BwdArgs {
+  Shape a;
+  DistanceBuckets db;
+  int seqs_per_table;
+  const T *x, *out, *dout;
+  const float *lse, *kept;
+  T* dx;
+  float* stat;      // [seqs*heads][stat_rows(S)][2]: lse * log2(e) and the corrected delta, zeros behind the last token
+  float* sums;      // dK and dV of keys < sinks that lie far apart from their queries: [chunks + 1][seqs*kv][sinks][2][dh]
+  float* partials;  // of the table: [seqs * gridDim.y][heads][buckets]
+  int far_blocks, chunks, chunk_blocks;  // workgroups for those pairs: blocks of keys x ranges of chunk_blocks streamed blocks
+  float scale;
+};
+
+template <typename T, int DHP, int NW, bool BIAS>
+__global__ __launch_bounds__(64 * NW, 2) void local_dq_kernel(BwdArgs<T> p) {
+  using TY = Type<T>;
+  using TL = Tile<T, DHP, NW>;
+  constexpr int BR = TY::BR, NT = BR / 32, KK = DHP / 16, TN = DHP / 32;
+  extern __shared__ __attribute__((aligned(16))) char lds[];
+  const Shape& a = p.a;
+  const int lane = threadIdx.x & 63, half = lane >> 5;
+  const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const int group = a.heads / a.kv, b = blockIdx.x / a.kv, kvh = blockIdx.x - b * a.kv;
+  const int S = a.S, dh = a.dh, SP = stat_rows(S);
+  const size_t ld = a.ld(), D = (size_t)a.heads * dh;
+  const QueryItems<BR, NW> it(a, group, SP / 32, gridDim.y - 1 - blockIdx.y, wave);
+  const bool active = it.item < it.items;
+  const int h = kvh * group + (active ? it.g : 0), qw = (active ? it.blk : 0) * 32;
+  const T* base = p.x + (size_t)b * S * ld;
+  const T* qbase = base + (size_t)h * dh;
+  const T* kbase = base + D + (size_t)kvh * dh;
+  const T* vbase = kbase + (size_t)a.kv * dh;
+  const uint32_t lds0 = lds_addr_of(lds);
+  constexpr size_t kStages = 2 * 2 * TL::kBytes, kTiles = kStages > NW * kTurnBytes ? kStages : NW * kTurnBytes;
+  int* first = reinterpret_cast<int*>(lds + kTiles);
+  BiasLds* bl = reinterpret_cast<BiasLds*>(lds + kTiles + kMaxBuckets * 4) + wave;
+  if constexpr (BIAS) {
+    load_borders(p.db, first);
+    __syncthreads();
+    bl->load(p.db, first, p.kept + ((size_t)(b / p.seqs_per_table) * a.heads + h) * p.db.count, lane, 64);
+  }
+  const bool there = active && qw + (lane & 31) < S;
+  const int query = min(qw + (lane & 31), S - 1);
+  const T* dorow = p.dout + ((size_t)b * S + query) * D + (size_t)h * dh;
+  const T* orow = p.out + ((size_t)b * S + query) * D + (size_t)h * dh;
+  typename TY::Frag qf[KK], df[KK];
+  float delta = 0.f;
+#pragma unroll
+  for (int kk = 0; kk < KK; ++kk) {
+    const int d = 16 * kk + 8 * half;
+    qf[kk] = TY::load(qbase + (size_t)query * ld + d, dh - d);
+    df[kk] = TY::load(dorow + d, dh - d);
+    delta = TY::dot(df[kk], TY::load(orow + d, dh - d), delta);
+  }
+  delta = over_halves(delta, Add());
+  float l2 = p.lse[((size_t)b * a.heads + h) * S + query] * kLog2e;
+  wait_vmcnt<0>();
+#pragma unroll
+  for (int kk = 0; kk < KK; ++kk) asm volatile("" : "+v"(qf[kk]), "+v"(df[kk]));
+  asm volatile("" : "+v"(l2), "+v"(delta));
+
+  typename TL::Offsets off;
+  off.init(ld, wave, lane);
+  auto issue = [&](int t) {
+    const int row = it.block(t) * BR;
+    const uint32_t to = lds0 + (t & 1) * 2 * TL::kBytes;
+    const bool whole = dh == DHP && row + BR <= S;
+    TL::copy(to, kbase + (size_t)row * ld, off, whole, S - row, dh, wave, lane);
+    TL::copy(to + TL::kBytes, vbase + (size_t)row * ld, off, whole, S - row, dh, wave, lane);
+  };
+  floatx16 acc[TN];
+#pragma unroll
+  for (int j = 0; j < TN; ++j)
+#pragma unroll
+    for (int r = 0; r < 16; ++r) acc[j][r] = 0.f;
+  float total = 0.f;
+  const int q_last = min(qw + 31, S - 1);
+  const float scale_log2 = p.scale * kLog2e;
+  if (it.count > 0) issue(0);
+  for (int t = 0; t < it.count; ++t) {
+    wait_vmcnt<0>();
+    lds_barrier();
+    if (t + 1 < it.count) issue(t + 1);
+    const int kb = it.block(t) * BR;
+    if (!active || qw >= S || kb > q_last || (kb >= a.sinks && kb + BR - 1 <= qw - a.window)) continue;
+    const char* lk = lds + (t & 1) * 2 * TL::kBytes;
+    const char* lv = lk + TL::kBytes;
+    const int dmin = qw - (kb + BR - 1), dmax = qw + 31 - kb;
+    const bool masked = !(dmin >= 0 && (dmax < a.window || kb + BR <= a.sinks));
+    const int d0 = query - kb - 4 * half;
+#pragma unroll
+    for (int u = 0; u < NT; ++u) {
+      floatx16 sacc, pacc;
+#pragma unroll
+      for (int r = 0; r < 16; ++r) sacc[r] = pacc[r] = 0.f;
+#pragma unroll
+      for (int kk = 0; kk < KK; ++kk) {
+        sacc = TY::mma(TL::row_frag(lk, 32 * u, kk, lane), qf[kk], sacc);
+        pacc = TY::mma(TL::row_frag(lv, 32 * u, kk, lane), df[kk], pacc);
+      }
+      float bias[16];
+      if constexpr (BIAS) tile_bias<-1>(*bl, p.db, first, d0 - 32 * u, dmin + BR - 32 * (u + 1), dmax - 32 * u, bias);
+      typename TY::Frag dsf[2];
+#pragma unroll
+      for (int g = 0; g < 2; ++g) {
+        float e[8];
+#pragma unroll
+        for (int q = 0; q < 8; ++q) {
+          const int r = 8 * g + q;
+          const float pr = __builtin_amdgcn_exp2f((BIAS ? fmaf(sacc[r], scale_log2, bias[r]) : sacc[r] * scale_log2) - l2);
+          float ds = pr * (pacc[r] - delta);
+          if (masked) {
+            const int d = d0 - 32 * u - 8 * (r >> 2) - (r & 3), key = query - d;
+            ds = d >= 0 && (d < a.window || key < a.sinks) ? ds : 0.f;
+          }
+          e[q] = ds;
+          total += ds;
+        }
+        dsf[g] = TY::pack(e);
+      }
+#pragma unroll
+      for (int g = 0; g < 2; ++g)
+#pragma unroll
+        for (int j = 0; j < TN; ++j) acc[j] = TY::mma(TL::col_frag(lk, j, 2 * u + g, lane), dsf[g], acc[j]);
+    }
+  }
+  lds_barrier();
+  if (!active) return;
+  // what the rows of dS add up to is what delta was off by
+  const float corrected = delta + over_halves(total, Add());
+  if (half == 0)
+    *reinterpret_cast<float2*>(p.stat + (((size_t)b * a.heads + h) * SP + qw + lane) * 2) = there ? make_float2(l2, corrected) : make_float2(0.f, 0.f);
+  T* dq = p.dx + ((size_t)b * S + qw) * ld + (size_t)h * dh;
+  turned_rows(acc, p.scale, reinterpret_cast<float*>(lds) + wave * (kTurnBytes / 4), lane, [&](int r, int col, const float (&v)[8]) {
+    if (qw + r < S) TY::store8(dq + (size_t)r * ld + col, v, dh - col);
+  });
+  uint32_t redo = rows_to_redo(finite(acc), there);
+  if (redo) wait_vmcnt<0>();
+  for (; redo; redo &= redo - 1) {
+    const int r = __builtin_ctz(redo), i = qw + r;
+    auto of_row = [&](float v) { return __int_as_float(__builtin_amdgcn_readlane(__float_as_int(v), r)); };
+    redo_dq_row<T, BIAS>(a, p.db, first, bl, i, qbase, kbase, vbase, p.dout + ((size_t)b * S + i) * D + (size_t)h * dh, of_row(l2), of_row(delta),
+                         dq + (size_t)r * ld, p.scale, lane);
+  }
+}
+
+// Sums of dS by distance, per wave and half of its lanes (whose tiles' distances differ by four: together they would meet on one
+// address), kept in LDS: a wave's own additions stay in order.
+struct TableSums {
+  float near[2][kNearSize];
+  float far[kMaxBuckets];
+};
+
+template <int NW>
+constexpr size_t dkv_bias_lds(bool bias) { return bias ? kMaxBuckets * 4 + sizeof(BiasLds) + NW * sizeof(TableSums) : 0; }
+
+template <typename T, int DHP, int NW, bool BIAS>
+__global__ __launch_bounds__(64 * NW, sizeof(T) == 2 || DHP == 64 ? 2 : 1) void local_dkv_kernel(BwdArgs<T> p) {
+  using TY = Type<T>;
+  using TL = Tile<T, DHP, NW>;
+  constexpr int BR = TY::BR, NT = BR / 32, KK = DHP / 16, TN = DHP / 32, kOwn = 32 * NW;
+  constexpr int kStageBytes = 2 * TL::kBytes + 1024;  // Q, dO, statistics
+  extern __shared__ __attribute__((aligned(16))) char lds[];
+  const Shape& a = p.a;
+  const int lane = threadIdx.x & 63, half = lane >> 5;
+  const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const int group = a.heads / a.kv, b = blockIdx.x / a.kv, kvh = blockIdx.x - b * a.kv;
+  const int S = a.S, dh = a.dh, SP = stat_rows(S);
+  const size_t ld = a.ld(), D = (size_t)a.heads * dh;
+  // workgroups for the far pairs of first keys come first, then a workgroup for each block of keys, low ones (which more queries see) first
+  const int fars = p.far_blocks * p.chunks;
+  const bool far = (int)blockIdx.y < fars;
+  const int chunk = far ? blockIdx.y / p.far_blocks : 0;
+  const int k0 = (far ? blockIdx.y - chunk * p.far_blocks : blockIdx.y - fars) * kOwn;
+  const int kw = k0 + wave * 32, key = kw + (lane & 31);
+  const bool active = kw < (far ? a.sinks : S);
+  // distances that count: all in the window, or beside the far workgroups' all in it, or there all beyond it
+  const int d_from = far ? a.window : 0, d_to = far ? S : a.window;
+  const int d_end = far && key >= a.sinks ? 0 : min(d_to, S - key);  // of this lane's key; copied rows behind the last token do not count
+  int blk0 = k0 / BR, blk1 = min(S - 1, k0 + kOwn - 1 + a.window - 1) / BR + 1;  // streamed blocks of queries
+  if (far) {
+    blk0 = (k0 + a.window) / BR + chunk * p.chunk_blocks;
+    blk1 = min(blk0 + p.chunk_blocks, (S + BR - 1) / BR);
+  }
+  const int nb = max(0, blk1 - blk0), count = nb * group;
+  const T* base = p.x + (size_t)b * S * ld;
+  const T* kbase = base + D + (size_t)kvh * dh;
+  const T* vbase = kbase + (size_t)a.kv * dh;
+  const T* dobase = p.dout + (size_t)b * S * D;
+  const uint32_t lds0 = lds_addr_of(lds);
+  constexpr size_t kStages = 2 * kStageBytes, kTiles = kStages > NW * kTurnBytes ? kStages : NW * kTurnBytes;
+  int* first = reinterpret_cast<int*>(lds + kTiles);
+  BiasLds* bl = reinterpret_cast<BiasLds*>(lds + kTiles + kMaxBuckets * 4);
+  TableSums* sums = reinterpret_cast<TableSums*>(bl + 1);
+  auto table = [&](int h) { return p.kept + ((size_t)(b / p.seqs_per_table) * a.heads + h) * p.db.count; };
+  auto start_head = [&](int g) {
+    bl->load(p.db, first, table(kvh * group + g), threadIdx.x, 64 * NW);
+    for (int i = threadIdx.x; i < (int)(NW * sizeof(TableSums) / 4); i += 64 * NW) reinterpret_cast<float*>(sums)[i] = 0.f;
+  };
+  if constexpr (BIAS) {
+    load_borders(p.db, first);
+    __syncthreads();
+    start_head(0);
+  }
+  typename TY::Frag kf[KK], vf[KK];
+  {
+    const int j = min(key, S - 1);
+#pragma unroll
+    for (int kk = 0; kk < KK; ++kk) {
+      const int d = 16 * kk + 8 * half;
+      kf[kk] = TY::load(kbase + (size_t)j * ld + d, dh - d);
+      vf[kk] = TY::load(vbase + (size_t)j * ld + d, dh - d);
+    }
+  }
+  wait_vmcnt<0>();
+#pragma unroll
+  for (int kk = 0; kk < KK; ++kk) asm volatile("" : "+v"(kf[kk]), "+v"(vf[kk]));
+
+  typename TL::Offsets offq, offd;
+  offq.init(ld, wave, lane);
+  offd.init(D, wave, lane);
+  auto issue = [&](int t) {
+    const int g = t / nb, row = (blk0 + t - g * nb) * BR, h = kvh * group + g;
+    const uint32_t to = lds0 + (t & 1) * kStageBytes;
+    const bool whole = dh == DHP && row + BR <= S;
+    TL::copy(to, base + (size_t)row * ld + (size_t)h * dh, offq, whole, S - row, dh, wave, lane);
+    TL::copy(to + TL::kBytes, dobase + (size_t)row * D + (size_t)h * dh, offd, whole, S - row, dh, wave, lane);
+    // (lse, delta) of BR rows, over and over where they are fewer than the 64 lanes copy
+    dma16(to + 2 * TL::kBytes, p.stat + (((size_t)b * a.heads + h) * SP + row) * 2, (uint32_t)(lane & (BR / 2 - 1)) * 16);
+  };
+  floatx16 ak[TN], av[TN];
+#pragma unroll
+  for (int j = 0; j < TN; ++j)
+#pragma unroll
+    for (int r = 0; r < 16; ++r) ak[j][r] = av[j][r] = 0.f;
+  const float scale_log2 = p.scale * kLog2e;
+  if (count > 0) issue(0);
+  int t = 0;
+  for (int g = 0; g < group; ++g) {
+    for (int n = 0; n < nb; ++n, ++t) {
+      wait_vmcnt<0>();
+      lds_barrier();
+      if (t + 1 < count) issue(t + 1);
+      const int qb = (blk0 + n) * BR;
+      // wave uniform: distances of the wave's pairs in this block
+      const int dlo = qb - (kw + 31), dhi = qb + BR - 1 - kw;
+      if (!active || dhi < d_from || dlo >= d_to) continue;
+      const char* lq = lds + (t & 1) * kStageBytes;
+      const char* ldo = lq + TL::kBytes;
+      const float* lstat = reinterpret_cast<const float*>(ldo + TL::kBytes);
+      const bool masked = dlo < d_from || dhi >= d_to || qb + BR > S || (far && kw + 31 >= a.sinks);
+      const int d0 = qb - key + 4 * half;
+#pragma unroll
+      for (int u = 0; u < NT; ++u) {
+        floatx16 sacc, pacc;
+#pragma unroll
+        for (int r = 0; r < 16; ++r) sacc[r] = pacc[r] = 0.f;
+#pragma unroll
+        for (int kk = 0; kk < KK; ++kk) {
+          sacc = TY::mma(TL::row_frag(lq, 32 * u, kk, lane), kf[kk], sacc);
+          pacc = TY::mma(TL::row_frag(ldo, 32 * u, kk, lane), vf[kk], pacc);
+        }
+        float bias[16];
+        const int tmin = dlo + 32 * u, tmax = dlo + 32 * u + 62;
+        if constexpr (BIAS) tile_bias<1>(*bl, p.db, first, d0 + 32 * u, tmin, tmax, bias);
+        typename TY::Frag pf[2], dsf[2];
+        float ds[16];
+#pragma unroll
+        for (int v = 0; v < 2; ++v) {
+          float pe[8], de[8];
+#pragma unroll
+          for (int q = 0; q < 2; ++q) {
+            const float4* sp = reinterpret_cast<const float4*>(lstat + 2 * (32 * u + 8 * (2 * v + q) + 4 * half));
+            const float4 s0 = sp[0], s1 = sp[1];
+            const float l2v[4] = {s0.x, s0.z, s1.x, s1.z}, dlv[4] = {s0.y, s0.w, s1.y, s1.w};
+#pragma unroll
+            for (int w = 0; w < 4; ++w) {
+              const int r = 8 * v + 4 * q + w;
+              float pr = __builtin_amdgcn_exp2f((BIAS ? fmaf(sacc[r], scale_log2, bias[r]) : sacc[r] * scale_log2) - l2v[w]);
+              float dsr = pr * (pacc[r] - dlv[w]);
+              if (masked) {
+                const int d = d0 + 32 * u + 8 * (r >> 2) + (r & 3);
+                const bool counts = d >= d_from && d < d_end;
+                pr = counts ? pr : 0.f;
+                dsr = counts ? dsr : 0.f;
+              }
+              pe[4 * q + w] = pr;
+              de[4 * q + w] = dsr;
+              ds[r] = dsr;
+            }
+          }
+          pf[v] = TY::pack(pe);
+          dsf[v] = TY::pack(de);
+        }
+        if constexpr (BIAS) {
+          if (tmin < kNear) {
+            float* at = sums[wave].near[half] + kPad + d0 + 32 * u;
+#pragma unroll
+            for (int r = 0; r < 16; ++r) __hip_atomic_fetch_add(at + 8 * (r >> 2) + (r & 3), ds[r], __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_WORKGROUP);
+          } else {
+            const int b0 = __builtin_amdgcn_readfirstlane(bucket_of(p.db, first, tmin)), b1 = __builtin_amdgcn_readfirstlane(bucket_of(p.db, first, tmax));
+            for (int bk = b0; bk <= b1; ++bk) {
+              const int from = first[bk], to = bk + 1 < p.db.count ? first[bk + 1] : S;
+              float s = 0.f;
+#pragma unroll
+              for (int r = 0; r < 16; ++r) {
+                const int d = d0 + 32 * u + 8 * (r >> 2) + (r & 3);
+                if (b0 == b1 || (d >= from && d < to)) s += ds[r];
+              }
+              s = sum_over_lanes(s);
+              if (lane == 0) sums[wave].far[bk] += s;
+            }
+          }
+        }
+#pragma unroll
+        for (int v = 0; v < 2; ++v)
+#pragma unroll
+          for (int j = 0; j < TN; ++j) {
+            ak[j] = TY::mma(TL::col_frag(lq, j, 2 * u + v, lane), dsf[v], ak[j]);
+            av[j] = TY::mma(TL::col_frag(ldo, j, 2 * u + v, lane), pf[v], av[j]);
+          }
+        __builtin_amdgcn_sched_barrier(0);  // one tile's scores alive at a time
+      }
+    }
+    if constexpr (BIAS) {
+      // this head's sums: over the waves and halves by distance, then by bucket
+      __syncthreads();
+      float* by_distance = bl->near;
+      for (int i = threadIdx.x; i < kNearSize; i += 64 * NW) {
+        float s = 0.f;
+#pragma unroll
+        for (int w = 0; w < NW; ++w) s += sums[w].near[0][i] + sums[w].near[1][i];
+        by_distance[i] = s;
+      }
+      __syncthreads();
+      float* out = p.partials + (((size_t)b * gridDim.y + blockIdx.y) * a.heads + kvh * group + g) * p.db.count;
+      for (int bk = wave; bk < p.db.count; bk += NW) {
+        const int from = first[bk], to = bk + 1 < p.db.count ? min(first[bk + 1], kNear + kPad) : kNear + kPad;
+        float s = 0.f;
+        for (int d = from + lane; d < to; d += 64) s += by_distance[kPad + d];
+        s = sum_over_lanes(s);
+        if (lane == 0) {
+#pragma unroll
+          for (int w = 0; w < NW; ++w) s += sums[w].far[bk];
+          out[bk] = s;
+        }
+      }
+      __syncthreads();
+      if (g + 1 < group) {
+        start_head(g + 1);
+        __syncthreads();
+      }
+    }
+  }
+  lds_barrier();
+  if (!active) return;
+  const bool join = p.far_blocks > 0;  // dK and dV of first keys are sums of several workgroups'
+  float* part = p.sums + ((size_t)(far ? chunk + 1 : 0) * gridDim.x + blockIdx.x) * a.sinks * 2 * dh;
+  T* dk = p.dx + (size_t)b * S * ld + D + (size_t)kvh * dh;
+  T* dv = dk + (size_t)a.kv * dh;
+  const int there_end = far ? a.sinks : S;
+  float* turn = reinterpret_cast<float*>(lds) + wave * (kTurnBytes / 4);
+  auto store = [&](int which) {
+    return [=](int r, int col, const float (&v)[8]) {
+      const int j = kw + r;
+      if (j >= there_end) return;
+      if (join && j < a.sinks) Type<float>::store8(part + ((size_t)j * 2 + which) * dh + col, v, dh - col);
+      else TY::store8((which ? dv : dk) + (size_t)j * ld + col, v, dh - col);
+    };
+  };
+  turned_rows(ak, p.scale, turn, lane, store(0));
+  turned_rows(av, 1.f, turn, lane, store(1));
+  uint32_t redo = rows_to_redo(finite(ak) && finite(av), key < there_end);
+  if (redo) wait_vmcnt<0>();
+  for (; redo; redo &= redo - 1) {
+    const int j = kw + __builtin_ctz(redo);
+    float rk[2] = {}, rv[2] = {};
+    const int from = max(blk0 * BR, j + d_from), to = (int)min((long)min(S, blk1 * BR), (long)j + d_to);  // queries
+    for (int g = 0; g < group; ++g) {
+      const int h = kvh * group + g;
+      const T* q = base + (size_t)h * dh;
+      const T* dO = dobase + (size_t)h * dh;
+      for (int i0 = from; i0 < to; i0 += 64) {
+        const int i = i0 + lane;
+        float pr = 0.f, ds = 0.f;
+        if (i < to) {
+          const float2 st = *reinterpret_cast<const float2*>(p.stat + (((size_t)b * a.heads + h) * SP + i) * 2);
+          float e = row_dot(q + (size_t)i * ld, kbase + (size_t)j * ld, dh) * scale_log2 - st.x;
+          if (BIAS) e += table(h)[bucket_of(p.db, first, i - j)] * kLog2e;
+          pr = __builtin_amdgcn_exp2f(e);
+          ds = pr * (row_dot(dO + (size_t)i * D, vbase + (size_t)j * ld, dh) - st.y);
+        }
+        const uint64_t which = __builtin_amdgcn_ballot_w64(i < to);
+        add_rows(rk, ds, q + (size_t)i0 * ld, ld, which, dh, lane);
+        add_rows(rv, pr, dO + (size_t)i0 * D, D, which, dh, lane);
+      }
+    }
+#pragma unroll
+    for (int c = 0; c < 2; ++c) {
+      const int col = lane + 64 * c;
+      if (col >= dh) continue;
+      if (join && j < a.sinks) {
+        part[((size_t)j * 2) * dh + col] = rk[c] * p.scale;
+        part[((size_t)j * 2 + 1) * dh + col] = rv[c];
+      } else {
+        dk[(size_t)j * ld + col] = from_float<T>(rk[c] * p.scale);
+        dv[(size_t)j * ld + col] = from_float<T>(rv[c]);
+      }
+    }
+  }
+}
+
+// dK and dV of the first keys from the parts of several workgroups, in the order of the ranges
+template <typename T>
+__global__ __launch_bounds__(256) void local_join_kernel(Shape a, int parts, size_t count, const float* __restrict__ sums, T* __restrict__ dx) {
+  const size_t i = (size_t)blockIdx.x * 256 + threadIdx.x;
+  if (i >= count) return;
+  float s = 0.f;
+  for (int c = 0; c < parts; ++c) s += sums[(size_t)c * count + i];
+  const int d = (int)(i % a.dh), which = (int)(i / a.dh % 2), j = (int)(i / (2 * a.dh) % a.sinks);
+  const size_t z = i / ((size_t)2 * a.dh * a.sinks), b = z / a.kv, kvh = z - b * a.kv;
+  dx[((size_t)b * a.S + j) * a.ld() + (size_t)(a.heads + which * a.kv + kvh) * a.dh + d] = from_float<T>(s);
+}
+
+constexpr int kWaves = 4;
+
+// workgroups of the dK, dV launch beside those of the blocks of keys
+struct FarPlan {
+  int blocks = 0, chunks = 0, chunk_blocks = 0;
+};
+template <typename T>
+FarPlan far_plan(const LocalAttention& a) {
+  FarPlan f;
+  constexpr int BR = Type<T>::BR, kOwn = 32 * kWaves;
+  if (a.sinks == 0 || a.window >= a.S) return f;
+  f.blocks = (a.sinks + kOwn - 1) / kOwn;
+  const int total = (a.S + BR - 1) / BR - a.window / BR;  // streamed blocks that far pairs of the first keys lie in
+  // a range is about as long as what the other workgroups walk over; no more of them than give every CU four, since each leaves its sums
+  // in memory
+  const int walk = std::max(8, (a.window + kOwn) / BR);
+  const long most = std::max<long>(1, 1024 / ((long)a.seqs * a.kv * f.blocks));
+  f.chunks = (int)std::min<long>(most, (total + walk - 1) / walk);
+  f.chunk_blocks = (total + f.chunks - 1) / f.chunks;
+  return f;
+}
+template <typename T>
+unsigned dkv_rows(const LocalAttention& a) {
+  const FarPlan f = far_plan<T>(a);
+  return (unsigned)((a.S + 32 * kWaves - 1) / (32 * kWaves) + f.blocks * f.chunks);
+}
+inline size_t stat_floats(const LocalAttention& a) { return (size_t)a.seqs * a.heads * stat_rows(a.S) * 2; }
+inline unsigned query_groups(const LocalAttention& a, int rows) {
+  return (unsigned)(((long)(rows + 31) / 32 * (a.heads / a.kv) + kWaves - 1) / kWaves);
+}
+
+template <class Kernel>
+hipError_t allow_lds(Kernel kernel) {
+  return hipFuncSetAttribute(reinterpret_cast<const void*>(kernel), hipFuncAttributeMaxDynamicSharedMemorySize, 160 * 1024);
+}
+
+template <typename T, int DHP, bool BIAS>
+hipError_t run_fwd(hipStream_t s, const LocalAttention& a, const FwdArgs<T>& p) {
+  using TL = Tile<T, DHP, kWaves>;
+  constexpr size_t lds = std::max<size_t>(4 * TL::kBytes, kWaves * kTurnBytes) + bias_lds<kWaves>(BIAS);
+  auto kernel = local_fwd_kernel<T, DHP, kWaves, BIAS>;
+  static hipError_t attr = allow_lds(kernel);
+  if (attr != hipSuccess) return attr;
+  hipLaunchKernelGGL(kernel, dim3(a.seqs * a.kv, query_groups(a, a.S)), dim3(64 * kWaves), lds, s, p);
+  return hipGetLastError();
+}
+
+template <typename T, int DHP, bool BIAS>
+hipError_t run_bwd(hipStream_t s, const LocalAttention& a, const BwdArgs<T>& p) {
+  using TL = Tile<T, DHP, kWaves>;
+  constexpr size_t lds_q = std::max<size_t>(4 * TL::kBytes, kWaves * kTurnBytes) + bias_lds<kWaves>(BIAS);
+  constexpr size_t lds_kv = std::max<size_t>(2 * (2 * TL::kBytes + 1024), kWaves * kTurnBytes) + dkv_bias_lds<kWaves>(BIAS);
+  static_assert(lds_kv <= 160 * 1024, "tiles and sums do not fit the LDS of a CU");
+  auto dq = local_dq_kernel<T, DHP, kWaves, BIAS>;
+  auto dkv = local_dkv_kernel<T, DHP, kWaves, BIAS>;
+  static hipError_t attr_q = allow_lds(dq), attr_kv = allow_lds(dkv);
+  if (attr_q != hipSuccess) return attr_q;
+  if (attr_kv != hipSuccess) return attr_kv;
+  hipLaunchKernelGGL(dq, dim3(a.seqs * a.kv, query_groups(a, stat_rows(a.S))), dim3(64 * kWaves), lds_q, s, p);
+  hipError_t e = hipGetLastError();
+  if (e != hipSuccess) return e;
+  hipLaunchKernelGGL(dkv, dim3(a.seqs * a.kv, dkv_rows<T>(a)), dim3(64 * kWaves), lds_kv, s, p);
+  e = hipGetLastError();
+  if (e != hipSuccess || p.far_blocks == 0) return e;
+  const size_t count = (size_t)a.seqs * a.kv * a.sinks * 2 * a.dh;
+  hipLaunchKernelGGL(local_join_kernel<T>, dim3((unsigned)((count + 255) / 256)), dim3(256), 0, s, p.a, p.chunks + 1, count, p.sums, p.dx);
+  return hipGetLastError();
+}
+
+template <typename T>
+hipError_t fwd(hipStream_t s, const LocalAttention& a, const T* x, const float* table, float* kept, T* out, T* out2, float* lse) {
+  const FwdArgs<T> p{shape_of(a), make_distance_buckets(a.buckets, a.max_distance), x, table, kept, out, out2, lse, kLog2e / sqrtf((float)a.dh)};
+  if (a.dh <= 64) return a.buckets ? run_fwd<T, 64, true>(s, a, p) : run_fwd<T, 64, false>(s, a, p);
+  return a.buckets ? run_fwd<T, 128, true>(s, a, p) : run_fwd<T, 128, false>(s, a, p);
+}
+
+template <typename T>
+hipError_t bwd(hipStream_t s, const LocalAttention& a, const T* x, const T* out, const T* dout, const float* lse, const float* kept, T* dx,
+               float* partials, float* scratch) {
+  const FarPlan f = far_plan<T>(a);
+  const BwdArgs<T> p{shape_of(a), make_distance_buckets(a.buckets, a.max_distance), a.seqs_per_table, x, out, dout, lse, kept, dx, scratch,
+                     scratch + stat_floats(a), partials, f.blocks, f.chunks, f.chunk_blocks, 1.0f / sqrtf((float)a.dh)};
+  if (a.dh <= 64) return a.buckets ? run_bwd<T, 64, true>(s, a, p) : run_bwd<T, 64, false>(s, a, p);
+  return a.buckets ? run_bwd<T, 128, true>(s, a, p) : run_bwd<T, 128, false>(s, a, p);
+}
+
+}  // namespace
+
+bool local_mfma_supported(int elt, const LocalAttention& a) {
+  const int es = elt == ELT_BF16 ? 2 : 4;
+  const size_t ld = (size_t)(a.heads + 2 * a.kv) * a.dh;
+  return a.dh <= 128 && a.dh * es % 16 == 0 && (long)a.seqs * a.kv <= (1 << 22) && 64 * ld * es < (1ull << 31) &&
+         query_groups(a, stat_rows(a.S)) <= 65535 && dkv_rows<uint16_t>(a) <= 65535 && dkv_rows<float>(a) <= 65535;
+}
+
+size_t local_mfma_scratch_bytes(int elt, const LocalAttention& a) {
+  const FarPlan f = elt == ELT_BF16 ? far_plan<uint16_t>(a) : far_plan<float>(a);
+  const size_t sums = f.blocks ? (size_t)(f.chunks + 1) * a.seqs * a.kv * a.sinks * 2 * a.dh : 0;
+  return (stat_floats(a) + sums) * sizeof(float);
+}
+
+int local_mfma_table_rows(int elt, const LocalAttention& a) {
+  return (int)(a.seqs * (elt == ELT_BF16 ? dkv_rows<uint16_t>(a) : dkv_rows<float>(a)));
+}
+
+hipError_t local_mfma_fwd(hipStream_t s, int elt, const LocalAttention& a, const void* x, const float* table, float* kept, void* out, void* out2,
+                          float* lse) {
+  if (elt == ELT_BF16) return fwd(s, a, (const uint16_t*)x, table, kept, (uint16_t*)out, (uint16_t*)out2, lse);
+  return fwd(s, a, (const float*)x, table, kept, (float*)out, (float*)out2, lse);
+}
+
+hipError_t local_mfma_bwd(hipStream_t s, int elt, const LocalAttention& a, const void* x, const void* out, const void* dout, const float* lse,
+                          const float* kept, void* dx, float* partials, void* scratch) {
+  if (elt == ELT_BF16)
+    return bwd(s, a, (const uint16_t*)x, (const uint16_t*)out, (const uint16_t*)dout, lse, kept, (uint16_t*)dx, partials, (float*)scratch);
+  return bwd(s, a, (const float*)x, (const float*)out, (const float*)dout, lse, kept, (float*)dx, partials, (float*)scratch);
+}
+
+}  // namespace tp
