@@ -35,11 +35,16 @@ constexpr int kNear = 112;         // distances with a table entry and a sum of 
 constexpr int kPad = 96;           // a tile of 32 x 64 spans 95 distances
 constexpr int kNearSize = kPad + kNear + kPad;
 
+typedef float floatx4 __attribute__((ext_vector_type(4)));
+typedef float floatx8 __attribute__((ext_vector_type(8)));
+typedef uint32_t uintx4 __attribute__((ext_vector_type(4)));
+
 template <typename T>
 struct Type;
 template <>
 struct Type<uint16_t> {
-  static constexpr int BR = 64;  // streamed rows of a block
+  static constexpr int BR = 64;      // streamed rows of a block
+  static constexpr int kAhead = 4;   // fragments on their way from LDS
   using Frag = bf16x8;
   static __device__ __forceinline__ floatx16 mma(const Frag& a, const Frag& b, floatx16 c) {
     return __builtin_amdgcn_mfma_f32_32x32x16_bf16(a, b, c, 0, 0, 0);
@@ -49,6 +54,9 @@ struct Type<uint16_t> {
   static __device__ __forceinline__ Frag pack(const float (&e)[8]) {
     return __builtin_bit_cast(bf16x8, make_uint4(pack_bf16x2(e[0], e[1]), pack_bf16x2(e[2], e[3]), pack_bf16x2(e[4], e[5]), pack_bf16x2(e[6], e[7])));
   }
+  using Half = uint2;
+  static __device__ __forceinline__ Half half(const float (&e)[4]) { return make_uint2(pack_bf16x2(e[0], e[1]), pack_bf16x2(e[2], e[3])); }
+  static __device__ __forceinline__ Frag join(const Half& a, const Half& b) { return __builtin_bit_cast(bf16x8, make_uint4(a.x, a.y, b.x, b.y)); }
   // values d .. d + 7 of a row that holds `left` more of them (a multiple of 8, or none)
   static __device__ __forceinline__ Frag load(const uint16_t* p, int left) {
     return left > 0 ? __builtin_bit_cast(bf16x8, *reinterpret_cast<const uint4*>(p)) : zero();
@@ -63,10 +71,9 @@ struct Type<uint16_t> {
       *reinterpret_cast<uint4*>(p) = make_uint4(pack_bf16x2(v[0], v[1]), pack_bf16x2(v[2], v[3]), pack_bf16x2(v[4], v[5]), pack_bf16x2(v[6], v[7]));
   }
 };
-typedef float floatx8 __attribute__((ext_vector_type(8)));
 template <>
 struct Type<float> {
-  static constexpr int BR = 32;
+  static constexpr int BR = 32, kAhead = 2;
   using Frag = floatx8;
   static __device__ __forceinline__ floatx16 mma(const Frag& a, const Frag& b, floatx16 c) {
 #pragma unroll
@@ -80,6 +87,9 @@ struct Type<float> {
     for (int t = 0; t < 8; ++t) f[t] = e[t];
     return f;
   }
+  using Half = floatx4;
+  static __device__ __forceinline__ Half half(const float (&e)[4]) { return floatx4{e[0], e[1], e[2], e[3]}; }
+  static __device__ __forceinline__ Frag join(const Half& a, const Half& b) { return floatx8{a[0], a[1], a[2], a[3], b[0], b[1], b[2], b[3]}; }
   static __device__ __forceinline__ Frag load(const float* p, int left) {  // left: a multiple of 4
     Frag f = zero();
     if (left > 0) {
@@ -106,75 +116,112 @@ struct Type<float> {
 // ---- a streamed tile in LDS -------------------------------------------------------------------------------------------------
 __device__ __forceinline__ int swizzle(int row) { return 4 * ((row >> 1) & 1) + 2 * ((row >> 2) & 1) + ((row >> 3) & 1); }
 
+// A value whose functions are worked out where they are used, block by block, instead of once for all in registers that there are none of.
+__device__ __forceinline__ int afresh(int v) {
+  asm volatile("" : "+v"(v));
+  return v;
+}
+
 template <typename T, int DHP, int NW>
 struct Tile {
   static constexpr int BR = Type<T>::BR, E = sizeof(T);
   static constexpr int kPanels = DHP * E / 128, kPanelBytes = BR * 128, kBytes = kPanels * kPanelBytes;
-  static constexpr int kInstr = kBytes / 1024, kPerWave = kInstr / NW;  // a wave instruction copies 8 rows of a panel
-  static_assert(kInstr % NW == 0, "copies do not divide among the waves");
-  // offsets of this lane's chunks inside a block whose rows are ld elements apart
-  struct Offsets {
-    uint32_t at[kPerWave];
-    __device__ __forceinline__ void init(size_t ld, int wave, int lane) {
+  static constexpr int kPerWave = kBytes / 1024 / NW;  // a wave instruction copies 8 rows of a panel
+  // A lane's chunk of copy t lies 32 rows (whose swizzle is the same) or a panel beyond that of copy 0
+  static constexpr int kAround = BR / 8 / NW;  // copies of a panel
+  static_assert((BR / 8) % NW == 0, "a panel is copied by all waves alike");
+  static __device__ __forceinline__ size_t beyond(int t, size_t ld) { return (t % kAround) * 8 * NW * ld * E + (t / kAround) * 128; }
+  static __device__ __forceinline__ uint32_t offset(size_t ld, int wave, int lane) {
+    const int r = 8 * wave + (lane >> 3);
+    return (uint32_t)(r * ld * E + (((lane & 7) ^ swizzle(r)) * 16));
+  }
+  // base: the block's first row, ld its row stride.  whole: BR rows and DHP columns are there; else rows and `cols` of them
+  static __device__ __forceinline__ void copy(uint32_t lds, const T* base, size_t ld, uint32_t off, bool whole, int rows, int cols, int wave, int lane) {
 #pragma unroll
-      for (int t = 0; t < kPerWave; ++t) {
-        const int n = wave + NW * t, r = 8 * (n % (BR / 8)) + (lane >> 3);
-        at[t] = (uint32_t)(r * ld * E + (n / (BR / 8)) * 128 + (((lane & 7) ^ swizzle(r)) * 16));
-      }
-    }
-  };
-  // base: the block's first row.  whole: BR rows and DHP columns are there; else rows and `cols` of them
-  static __device__ __forceinline__ void copy(uint32_t lds, const T* base, const Offsets& o, bool whole, int rows, int cols, int wave, int lane) {
-    if (whole) {
-#pragma unroll
-      for (int t = 0; t < kPerWave; ++t) dma16(lds + (wave + NW * t) * 1024, base, o.at[t]);
-    } else {
-#pragma unroll
-      for (int t = 0; t < kPerWave; ++t) {
-        const int n = wave + NW * t, r = 8 * (n % (BR / 8)) + (lane >> 3);
-        const int byte = (n / (BR / 8)) * 128 + (((lane & 7) ^ swizzle(r)) * 16);
-        dma_addr<16>(lds + n * 1024, r < rows && byte < cols * E ? (const char*)base + o.at[t] : zero_chunk());
+    for (int t = 0; t < kPerWave; ++t) {
+      const uint32_t to = lds + (t / kAround) * kPanelBytes + (wave + NW * (t % kAround)) * 1024;
+      const char* from = (const char*)base + beyond(t, ld);
+      if (whole) {
+        dma16(to, from, off);
+      } else {
+        const int r = 8 * (wave + NW * (t % kAround)) + (lane >> 3), byte = (t / kAround) * 128 + (((lane & 7) ^ swizzle(r)) * 16);
+        dma_addr<16>(to, r < rows && byte < cols * E ? from + off : zero_chunk());
       }
     }
   }
-  // A fragment of the first products: row rbase + lane % 32, columns 16 kk + 8 (lane / 32) .. + 7
-  static __device__ __forceinline__ typename Type<T>::Frag row_frag(const char* lds, int rbase, int kk, int lane) {
-    const int r = rbase + (lane & 31);
+  // Where in a tile this lane's fragments lie: constants away from one address for the first products and one for the second, with bits
+  // 4 .. 6, the slot, as an exclusive or (tiles start at multiples of 128).  The two addresses stay in registers; left to the compiler, all their
+  // variants do, and the kernels with 128-wide heads spill.
+  static __device__ __forceinline__ uint32_t row_base(int lane) {
+    const int r = lane & 31, half = lane >> 5;
+    return r * 128 + (((E == 2 ? half : 2 * half) ^ swizzle(r)) * 16);
+  }
+  static __device__ __forceinline__ uint32_t col_base(int lane) {
     if constexpr (E == 2) {
-      const int c = 2 * (kk & 3) + (lane >> 5);
-      return __builtin_bit_cast(bf16x8, *reinterpret_cast<const uint4*>(lds + (kk >> 2) * kPanelBytes + r * 128 + ((c ^ swizzle(r)) * 16)));
+      const int q = lane >> 4, s = lane & 15, k = 4 * (q >> 1) + (s >> 2);
+      return k * 128 + (((2 * (q & 1) + ((s & 3) >> 1)) ^ swizzle(k)) * 16) + (s & 1) * 8;
     } else {
-      const int c = 4 * (kk & 1) + 2 * (lane >> 5);
-      const char* row = lds + (kk >> 1) * kPanelBytes + r * 128;
-      const float4 a = *reinterpret_cast<const float4*>(row + ((c ^ swizzle(r)) * 16));
-      const float4 b = *reinterpret_cast<const float4*>(row + (((c + 1) ^ swizzle(r)) * 16));
-      return floatx8{a.x, a.y, a.z, a.w, b.x, b.y, b.z, b.w};
+      const int k = 4 * (lane >> 5);
+      return k * 128 + ((((lane & 31) >> 2) ^ swizzle(k)) * 16) + (lane & 3) * 4;
+    }
+  }
+  template <class V>
+  static __device__ __forceinline__ V read(uint32_t base, uint32_t flip, uint32_t beyond) {
+    uint32_t at = base;
+    if (flip) asm volatile("v_xor_b32 %0, %1, %2" : "=v"(at) : "i"(flip), "v"(base));
+    typedef __attribute__((address_space(3))) const char* lds_ptr;
+    return *reinterpret_cast<__attribute__((address_space(3))) const V*>((lds_ptr)(uintptr_t)at + beyond);
+  }
+  // A fragment of the first products: row 32 u + lane % 32, columns 16 kk + 8 (lane / 32) .. + 7; base: the first tile of the stage plus row_base
+  static __device__ __forceinline__ typename Type<T>::Frag row_frag(uint32_t base, int u, int kk, int tile = 0) {
+    if constexpr (E == 2) {
+      return __builtin_bit_cast(bf16x8, read<uintx4>(base, 32 * (kk & 3), tile * kBytes + u * 4096 + (kk >> 2) * kPanelBytes));
+    } else {
+      const uint32_t beyond = tile * kBytes + u * 4096 + (kk >> 1) * kPanelBytes;
+      const floatx4 a = read<floatx4>(base, 64 * (kk & 1), beyond), b = read<floatx4>(base, 64 * (kk & 1) + 16, beyond);
+      return floatx8{a[0], a[1], a[2], a[3], b[0], b[1], b[2], b[3]};
     }
   }
   // A fragment of the second products: column 32 j + lane % 32 of rows 16 g + 8 (t / 4) + 4 (lane / 32) + t % 4, t = 0 .. 7, the order in
-  // which the accumulators hold them
-  static __device__ __forceinline__ typename Type<T>::Frag col_frag(const char* lds, int j, int g, int lane) {
+  // which the accumulators hold them; base: the first tile of the stage plus col_base
+  static __device__ __forceinline__ typename Type<T>::Frag col_frag(uint32_t base, int j, int g, int tile = 0) {
     if constexpr (E == 2) {
-      const int q = lane >> 4, s = lane & 15;
-      const int k = 16 * g + 4 * (q >> 1) + (s >> 2);
-      const int col = 32 * (j & 1) + 16 * (q & 1) + 4 * (s & 3);
-      typedef __attribute__((address_space(3))) shortx4* lds_ptr;
-      const char* panel = lds + (j >> 1) * kPanelBytes;
-      const shortx4 lo = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_ptr)(panel + k * 128 + (((col >> 3) ^ swizzle(k)) * 16) + (col & 7) * 2));
-      const shortx4 hi = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_ptr)(panel + (k + 8) * 128 + (((col >> 3) ^ swizzle(k + 8)) * 16) + (col & 7) * 2));
+      const uint32_t beyond = tile * kBytes + (j >> 1) * kPanelBytes + g * 2048;
+      const shortx4 lo = read_turned(base, 64 * (j & 1), beyond), hi = read_turned(base, 64 * (j & 1) + 16, beyond + 1024);
       return __builtin_bit_cast(bf16x8, __builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7));
     } else {
       floatx8 f;
-      const int c = (lane & 31) >> 2;
 #pragma unroll
-      for (int t = 0; t < 8; ++t) {
-        const int k = 16 * g + 8 * (t >> 2) + 4 * (lane >> 5) + (t & 3);
-        f[t] = *reinterpret_cast<const float*>(lds + j * kPanelBytes + k * 128 + ((c ^ swizzle(k)) * 16) + (lane & 3) * 4);
-      }
+      for (int t = 0; t < 8; ++t)
+        f[t] = read<float>(base, 64 * ((t >> 1) & 1) + 16 * (t >> 2), tile * kBytes + j * kPanelBytes + (16 * g + 8 * (t >> 2) + (t & 3)) * 128);
       return f;
     }
   }
+  static __device__ __forceinline__ shortx4 read_turned(uint32_t base, uint32_t flip, uint32_t beyond) {
+    uint32_t at = base;
+    if (flip) asm volatile("v_xor_b32 %0, %1, %2" : "=v"(at) : "i"(flip), "v"(base));
+    typedef __attribute__((address_space(3))) const char* lds_ptr;
+    typedef __attribute__((address_space(3))) shortx4* turned_ptr;
+    return __builtin_amdgcn_ds_read_tr16_b64_v4i16((turned_ptr)((lds_ptr)(uintptr_t)at + beyond));
+  }
 };
+
+// Products one behind the other whose A fragments come from LDS: load(i) is issued DEPTH products ahead.  Left to itself the compiler
+// puts every read right in front of its product, and a wave waits out the LDS's latency 24 times a tile.
+template <int N, int DEPTH, class Frag, class Load, class Use>
+__device__ __forceinline__ void pipelined(Frag (&f)[DEPTH], const Load& load, const Use& use, bool preloaded = false) {
+  if (!preloaded) {
+#pragma unroll
+    for (int i = 0; i < DEPTH && i < N; ++i) f[i] = load(i);
+  }
+  __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+  for (int i = 0; i < N; ++i) {
+    use(i, f[i % DEPTH]);
+    if (i + DEPTH < N) f[i % DEPTH] = load(i + DEPTH);
+    __builtin_amdgcn_sched_barrier(0);
+  }
+}
 
 // ---- the bias in LDS ----------------------------------------------------------------------------------------------------------
 // near[kPad + d], d = -kPad .. kNear + kPad - 1: the table by distance, in units of log2; beyond that by bucket.
@@ -191,26 +238,33 @@ __device__ __forceinline__ void load_borders(const DistanceBuckets& d, int* firs
   for (int b = threadIdx.x; b < d.count; b += blockDim.x) first[b] = d.first[b];
 }
 
-// What a lane's 16 elements of a tile have added to their scaled scores.  Element r has distance base + sign * (8 (r / 4) + r % 4);
-// dmin, dmax: the tile's smallest and largest, wave uniform.
-template <int SIGN>
-__device__ __forceinline__ void tile_bias(const BiasLds& bl, const DistanceBuckets& d, const int* first, int base, int dmin, int dmax,
-                                          float (&out)[16]) {
-  if (dmin < kNear) {
+// Buckets b0 .. b1 of a tile's distances dmin .. dmax, wave uniform; b0 = -1: near ones, by distance.
+struct TileBuckets {
+  int b0 = -1, b1 = -1;
+  __device__ __forceinline__ TileBuckets(const DistanceBuckets& d, const int* first, int dmin, int dmax) {
+    if (dmin < kNear) return;
+    b0 = __builtin_amdgcn_readfirstlane(bucket_of(d, first, dmin));
+    b1 = b0;
+    while (b1 + 1 < d.count && __builtin_amdgcn_readfirstlane(first[b1 + 1]) <= dmax) ++b1;
+  }
+};
+// What a lane's N (4 or 16) elements have added to their scaled scores.  Element r has distance base + SIGN * (8 (r / 4) + r % 4).
+template <int SIGN, int N>
+__device__ __forceinline__ void tile_bias(const BiasLds& bl, const TileBuckets& tb, const int* first, int base, float (&out)[N]) {
+  if (tb.b0 < 0) {
     const float* at = bl.near + kPad + base;
 #pragma unroll
-    for (int r = 0; r < 16; ++r) out[r] = at[SIGN * (8 * (r >> 2) + (r & 3))];
+    for (int r = 0; r < N; ++r) out[r] = at[SIGN * (8 * (r >> 2) + (r & 3))];
   } else {
-    const int b0 = __builtin_amdgcn_readfirstlane(bucket_of(d, first, dmin)), b1 = __builtin_amdgcn_readfirstlane(bucket_of(d, first, dmax));
-    const float v = bl.value[b0];
+    const float v = bl.value[tb.b0];
 #pragma unroll
-    for (int r = 0; r < 16; ++r) out[r] = v;
-    for (int b = b0 + 1; b <= b1; ++b) {
-      const int from = first[b];
+    for (int r = 0; r < N; ++r) out[r] = v;
+    for (int b = tb.b0 + 1; b <= tb.b1; ++b) {
+      const int from = first[b] - base;
       const float w = bl.value[b];
 #pragma unroll
-      for (int r = 0; r < 16; ++r)
-        if (base + SIGN * (8 * (r >> 2) + (r & 3)) >= from) out[r] = w;
+      for (int r = 0; r < N; ++r)
+        if (SIGN * (8 * (r >> 2) + (r & 3)) >= from) out[r] = w;
     }
   }
 }
@@ -419,14 +473,13 @@ __global__ __launch_bounds__(64 * NW, 2) void local_fwd_kernel(FwdArgs<T> p) {
 #pragma unroll
   for (int kk = 0; kk < KK; ++kk) asm volatile("" : "+v"(qf[kk]));
 
-  typename TL::Offsets off;
-  off.init(ld, wave, lane);
+  const uint32_t off = TL::offset(ld, wave, lane), row_at = TL::row_base(lane), col_at = TL::col_base(lane);
   auto issue = [&](int t) {
     const int row = it.block(t) * BR;
     const uint32_t to = lds0 + (t & 1) * 2 * TL::kBytes;
     const bool whole = dh == DHP && row + BR <= S;
-    TL::copy(to, kbase + (size_t)row * ld, off, whole, S - row, dh, wave, lane);
-    TL::copy(to + TL::kBytes, vbase + (size_t)row * ld, off, whole, S - row, dh, wave, lane);
+    TL::copy(to, kbase + (size_t)row * ld, ld, off, whole, S - row, dh, wave, lane);
+    TL::copy(to + TL::kBytes, vbase + (size_t)row * ld, ld, off, whole, S - row, dh, wave, lane);
   };
   floatx16 oacc[TN];
 #pragma unroll
@@ -443,34 +496,40 @@ __global__ __launch_bounds__(64 * NW, 2) void local_fwd_kernel(FwdArgs<T> p) {
     const int kb = it.block(t) * BR;
     // wave uniform: some pair of this wave and block is visible
     if (!active || kb > q_last || (kb >= a.sinks && kb + BR - 1 <= qw - a.window)) continue;
-    const char* lk = lds + (t & 1) * 2 * TL::kBytes;
-    const char* lv = lk + TL::kBytes;
+    const uint32_t stage = lds0 + (t & 1) * 2 * TL::kBytes, lk = stage + row_at, lv = stage + col_at;
     floatx16 sacc[NT];
 #pragma unroll
-    for (int u = 0; u < NT; ++u) {
+    for (int u = 0; u < NT; ++u)
 #pragma unroll
       for (int r = 0; r < 16; ++r) sacc[u][r] = 0.f;
+    typename TY::Frag ahead[TY::kAhead];
+    // the tiles in turn: no product waits for the one before it
+    pipelined<NT * KK>(ahead, [&](int i) { return TL::row_frag(lk, i % NT, i / NT); },
+                       [&](int i, const typename TY::Frag& f) { sacc[i % NT] = TY::mma(f, qf[i / NT], sacc[i % NT]); });
+    auto v_frag = [&](int i) { return TL::col_frag(lv, i % TN, i / TN, 1); };
 #pragma unroll
-      for (int kk = 0; kk < KK; ++kk) sacc[u] = TY::mma(TL::row_frag(lk, 32 * u, kk, lane), qf[kk], sacc[u]);
-    }
+    for (int i = 0; i < TY::kAhead; ++i) ahead[i] = v_frag(i);
+    __builtin_amdgcn_sched_barrier(0);
     const int dmin = qw - (kb + BR - 1), dmax = qw + 31 - kb;
     const bool masked = !(dmin >= 0 && (dmax < a.window || kb + BR <= a.sinks));
-    const int d0 = query - kb - 4 * half;  // distance of element r of tile u: d0 - 32 u - 8 (r / 4) - r % 4
+    // distance of element r of tile u: d0 - 32 u - 8 (r / 4) - r % 4
+    const int d0 = query - kb - 4 * half, sink0 = a.sinks - kb - 4 * half;
     float mx = mrun;
 #pragma unroll
     for (int u = 0; u < NT; ++u) {
       float bias[16];
-      if constexpr (BIAS) tile_bias<-1>(*bl, p.db, first, d0 - 32 * u, dmin + BR - 32 * (u + 1), dmax - 32 * u, bias);
+      if constexpr (BIAS) tile_bias<-1>(*bl, TileBuckets(p.db, first, dmin + BR - 32 * (u + 1), dmax - 32 * u), first, d0 - 32 * u, bias);
 #pragma unroll
-      for (int r = 0; r < 16; ++r) {
-        float s = BIAS ? fmaf(sacc[u][r], p.scale_log2, bias[r]) : sacc[u][r] * p.scale_log2;
-        if (masked) {
-          const int d = d0 - 32 * u - 8 * (r >> 2) - (r & 3), key = query - d;
-          s = d >= 0 && (d < a.window || key < a.sinks) ? s : -INFINITY;
+      for (int r = 0; r < 16; ++r) sacc[u][r] = BIAS ? fmaf(sacc[u][r], p.scale_log2, bias[r]) : sacc[u][r] * p.scale_log2;
+      if (masked) {
+#pragma unroll
+        for (int r = 0; r < 16; ++r) {
+          const int at = 32 * u + 8 * (r >> 2) + (r & 3);
+          sacc[u][r] = at <= d0 && (at > d0 - a.window || at < sink0) ? sacc[u][r] : -INFINITY;
         }
-        sacc[u][r] = s;
-        mx = fmaxf(mx, s);
       }
+#pragma unroll
+      for (int r = 0; r < 16; ++r) mx = fmaxf(mx, sacc[u][r]);
     }
     const float mnew = over_halves(mx, Max());
     const float alpha = __builtin_amdgcn_exp2f(mrun - mnew);
@@ -494,10 +553,7 @@ __global__ __launch_bounds__(64 * NW, 2) void local_fwd_kernel(FwdArgs<T> p) {
 #pragma unroll
         for (int r = 0; r < 16; ++r) oacc[j][r] *= alpha;
     }
-#pragma unroll
-    for (int g = 0; g < 2 * NT; ++g)
-#pragma unroll
-      for (int j = 0; j < TN; ++j) oacc[j] = TY::mma(TL::col_frag(lv, j, g, lane), pf[g], oacc[j]);
+    pipelined<2 * NT * TN>(ahead, v_frag, [&](int i, const typename TY::Frag& f) { oacc[i % TN] = TY::mma(f, pf[i / TN], oacc[i % TN]); }, true);
   }
   lds_barrier();  // the stages are free
   if (!active) return;
@@ -544,7 +600,7 @@ struct BwdArgs {
 };
 
 template <typename T, int DHP, int NW, bool BIAS>
-__global__ __launch_bounds__(64 * NW, 2) void local_dq_kernel(BwdArgs<T> p) {
+__global__ __launch_bounds__(64 * NW, sizeof(T) == 2 || DHP == 64 ? 2 : 1) void local_dq_kernel(BwdArgs<T> p) {
   using TY = Type<T>;
   using TL = Tile<T, DHP, NW>;
   constexpr int BR = TY::BR, NT = BR / 32, KK = DHP / 16, TN = DHP / 32;
@@ -580,10 +636,12 @@ __global__ __launch_bounds__(64 * NW, 2) void local_dq_kernel(BwdArgs<T> p) {
 #pragma unroll
   for (int kk = 0; kk < KK; ++kk) {
     const int d = 16 * kk + 8 * half;
-    qf[kk] = TY::load(qbase + (size_t)query * ld + d, dh - d);
     df[kk] = TY::load(dorow + d, dh - d);
     delta = TY::dot(df[kk], TY::load(orow + d, dh - d), delta);
   }
+  __builtin_amdgcn_sched_barrier(0);  // the output's registers are free again
+#pragma unroll
+  for (int kk = 0; kk < KK; ++kk) qf[kk] = TY::load(qbase + (size_t)query * ld + 16 * kk + 8 * half, dh - 16 * kk - 8 * half);
   delta = over_halves(delta, Add());
   float l2 = p.lse[((size_t)b * a.heads + h) * S + query] * kLog2e;
   wait_vmcnt<0>();
@@ -591,14 +649,13 @@ __global__ __launch_bounds__(64 * NW, 2) void local_dq_kernel(BwdArgs<T> p) {
   for (int kk = 0; kk < KK; ++kk) asm volatile("" : "+v"(qf[kk]), "+v"(df[kk]));
   asm volatile("" : "+v"(l2), "+v"(delta));
 
-  typename TL::Offsets off;
-  off.init(ld, wave, lane);
+  const uint32_t off = TL::offset(ld, wave, lane), row_at = TL::row_base(lane), col_at = TL::col_base(lane);
   auto issue = [&](int t) {
     const int row = it.block(t) * BR;
     const uint32_t to = lds0 + (t & 1) * 2 * TL::kBytes;
     const bool whole = dh == DHP && row + BR <= S;
-    TL::copy(to, kbase + (size_t)row * ld, off, whole, S - row, dh, wave, lane);
-    TL::copy(to + TL::kBytes, vbase + (size_t)row * ld, off, whole, S - row, dh, wave, lane);
+    TL::copy(to, kbase + (size_t)row * ld, ld, off, whole, S - row, dh, wave, lane);
+    TL::copy(to + TL::kBytes, vbase + (size_t)row * ld, ld, off, whole, S - row, dh, wave, lane);
   };
   floatx16 acc[TN];
 #pragma unroll
@@ -615,23 +672,36 @@ __global__ __launch_bounds__(64 * NW, 2) void local_dq_kernel(BwdArgs<T> p) {
     if (t + 1 < it.count) issue(t + 1);
     const int kb = it.block(t) * BR;
     if (!active || qw >= S || kb > q_last || (kb >= a.sinks && kb + BR - 1 <= qw - a.window)) continue;
-    const char* lk = lds + (t & 1) * 2 * TL::kBytes;
-    const char* lv = lk + TL::kBytes;
+    const uint32_t stage = lds0 + (t & 1) * 2 * TL::kBytes, lk = stage + row_at, lkc = stage + col_at;
     const int dmin = qw - (kb + BR - 1), dmax = qw + 31 - kb;
     const bool masked = !(dmin >= 0 && (dmax < a.window || kb + BR <= a.sinks));
-    const int d0 = query - kb - 4 * half;
+    const int d0 = query - kb - 4 * half, sink0 = a.sinks - kb - 4 * half;
 #pragma unroll
     for (int u = 0; u < NT; ++u) {
       floatx16 sacc, pacc;
 #pragma unroll
       for (int r = 0; r < 16; ++r) sacc[r] = pacc[r] = 0.f;
+      typename TY::Frag ahead[TY::kAhead];
+      pipelined<2 * KK>(ahead, [&](int i) { return TL::row_frag(lk, u, i >> 1, i & 1); },
+                        [&](int i, const typename TY::Frag& f) {
+                          if (i & 1) pacc = TY::mma(f, df[i >> 1], pacc);
+                          else sacc = TY::mma(f, qf[i >> 1], sacc);
+                        });
+      auto k_frag = [&](int i) { return TL::col_frag(lkc, i % TN, 2 * u + i / TN); };
 #pragma unroll
-      for (int kk = 0; kk < KK; ++kk) {
-        sacc = TY::mma(TL::row_frag(lk, 32 * u, kk, lane), qf[kk], sacc);
-        pacc = TY::mma(TL::row_frag(lv, 32 * u, kk, lane), df[kk], pacc);
+      for (int i = 0; i < TY::kAhead; ++i) ahead[i] = k_frag(i);
+      __builtin_amdgcn_sched_barrier(0);
+      if (masked) {  // p = 0, and dS = 0 whatever dP holds
+#pragma unroll
+        for (int r = 0; r < 16; ++r) {
+          const int at = 32 * u + 8 * (r >> 2) + (r & 3);
+          const bool sees = at <= d0 && (at > d0 - a.window || at < sink0);
+          sacc[r] = sees ? sacc[r] : -INFINITY;
+          pacc[r] = sees ? pacc[r] : delta;
+        }
       }
       float bias[16];
-      if constexpr (BIAS) tile_bias<-1>(*bl, p.db, first, d0 - 32 * u, dmin + BR - 32 * (u + 1), dmax - 32 * u, bias);
+      if constexpr (BIAS) tile_bias<-1>(*bl, TileBuckets(p.db, first, dmin + BR - 32 * (u + 1), dmax - 32 * u), first, d0 - 32 * u, bias);
       typename TY::Frag dsf[2];
 #pragma unroll
       for (int g = 0; g < 2; ++g) {
@@ -640,20 +710,13 @@ __global__ __launch_bounds__(64 * NW, 2) void local_dq_kernel(BwdArgs<T> p) {
         for (int q = 0; q < 8; ++q) {
           const int r = 8 * g + q;
           const float pr = __builtin_amdgcn_exp2f((BIAS ? fmaf(sacc[r], scale_log2, bias[r]) : sacc[r] * scale_log2) - l2);
-          float ds = pr * (pacc[r] - delta);
-          if (masked) {
-            const int d = d0 - 32 * u - 8 * (r >> 2) - (r & 3), key = query - d;
-            ds = d >= 0 && (d < a.window || key < a.sinks) ? ds : 0.f;
-          }
+          const float ds = pr * (pacc[r] - delta);
           e[q] = ds;
           total += ds;
         }
         dsf[g] = TY::pack(e);
       }
-#pragma unroll
-      for (int g = 0; g < 2; ++g)
-#pragma unroll
-        for (int j = 0; j < TN; ++j) acc[j] = TY::mma(TL::col_frag(lk, j, 2 * u + g, lane), dsf[g], acc[j]);
+      pipelined<2 * TN>(ahead, k_frag, [&](int i, const typename TY::Frag& f) { acc[i % TN] = TY::mma(f, dsf[i / TN], acc[i % TN]); }, true);
     }
   }
   lds_barrier();
@@ -682,6 +745,28 @@ struct TableSums {
   float near[2][kNearSize];
   float far[kMaxBuckets];
 };
+
+// ds: four elements with distances base .. base + 3
+__device__ __forceinline__ void add_to_table(TableSums& sums, const TileBuckets& tb, const int* first, int count, int base, int half, int lane,
+                                             const float (&ds)[4]) {
+  if (tb.b0 < 0) {
+    float* at = sums.near[half] + kPad + base;
+#pragma unroll
+    for (int r = 0; r < 4; ++r) __hip_atomic_fetch_add(at + r, ds[r], __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_WORKGROUP);
+  } else if (tb.b0 == tb.b1) {
+    const float s = sum_over_lanes((ds[0] + ds[1]) + (ds[2] + ds[3]));
+    if (lane == 0) sums.far[tb.b0] += s;
+  } else {
+    for (int b = tb.b0; b <= tb.b1; ++b) {
+      const int from = first[b] - base, to = b + 1 < count ? first[b + 1] - base : 4;
+      float s = 0.f;
+#pragma unroll
+      for (int r = 0; r < 4; ++r) s += r >= from && r < to ? ds[r] : 0.f;
+      s = sum_over_lanes(s);
+      if (lane == 0) sums.far[b] += s;
+    }
+  }
+}
 
 template <int NW>
 constexpr size_t dkv_bias_lds(bool bias) { return bias ? kMaxBuckets * 4 + sizeof(BiasLds) + NW * sizeof(TableSums) : 0; }
@@ -748,15 +833,14 @@ __global__ __launch_bounds__(64 * NW, sizeof(T) == 2 || DHP == 64 ? 2 : 1) void 
 #pragma unroll
   for (int kk = 0; kk < KK; ++kk) asm volatile("" : "+v"(kf[kk]), "+v"(vf[kk]));
 
-  typename TL::Offsets offq, offd;
-  offq.init(ld, wave, lane);
-  offd.init(D, wave, lane);
   auto issue = [&](int t) {
     const int g = t / nb, row = (blk0 + t - g * nb) * BR, h = kvh * group + g;
     const uint32_t to = lds0 + (t & 1) * kStageBytes;
+    const int l = afresh(lane);
+    const uint32_t offq = TL::offset(ld, wave, l), offd = TL::offset(D, wave, l);
     const bool whole = dh == DHP && row + BR <= S;
-    TL::copy(to, base + (size_t)row * ld + (size_t)h * dh, offq, whole, S - row, dh, wave, lane);
-    TL::copy(to + TL::kBytes, dobase + (size_t)row * D + (size_t)h * dh, offd, whole, S - row, dh, wave, lane);
+    TL::copy(to, base + (size_t)row * ld + (size_t)h * dh, ld, offq, whole, S - row, dh, wave, lane);
+    TL::copy(to + TL::kBytes, dobase + (size_t)row * D + (size_t)h * dh, D, offd, whole, S - row, dh, wave, lane);
     // (lse, delta) of BR rows, over and over where they are fewer than the 64 lanes copy
     dma16(to + 2 * TL::kBytes, p.stat + (((size_t)b * a.heads + h) * SP + row) * 2, (uint32_t)(lane & (BR / 2 - 1)) * 16);
   };
@@ -777,9 +861,8 @@ __global__ __launch_bounds__(64 * NW, sizeof(T) == 2 || DHP == 64 ? 2 : 1) void 
       // wave uniform: distances of the wave's pairs in this block
       const int dlo = qb - (kw + 31), dhi = qb + BR - 1 - kw;
       if (!active || dhi < d_from || dlo >= d_to) continue;
-      const char* lq = lds + (t & 1) * kStageBytes;
-      const char* ldo = lq + TL::kBytes;
-      const float* lstat = reinterpret_cast<const float*>(ldo + TL::kBytes);
+      const uint32_t stage = (t & 1) * kStageBytes, lq = lds0 + stage + TL::row_base(afresh(lane)), lqc = lds0 + stage + TL::col_base(afresh(lane));
+      const float* lstat = reinterpret_cast<const float*>(lds + stage + 2 * TL::kBytes);
       const bool masked = dlo < d_from || dhi >= d_to || qb + BR > S || (far && kw + 31 >= a.sinks);
       const int d0 = qb - key + 4 * half;
 #pragma unroll
@@ -787,71 +870,51 @@ __global__ __launch_bounds__(64 * NW, sizeof(T) == 2 || DHP == 64 ? 2 : 1) void 
         floatx16 sacc, pacc;
 #pragma unroll
         for (int r = 0; r < 16; ++r) sacc[r] = pacc[r] = 0.f;
+        typename TY::Frag ahead[2];
+        pipelined<2 * KK>(ahead, [&](int i) { return TL::row_frag(lq, u, i >> 1, i & 1); },
+                          [&](int i, const typename TY::Frag& f) {
+                            if (i & 1) pacc = TY::mma(f, vf[i >> 1], pacc);
+                            else sacc = TY::mma(f, kf[i >> 1], sacc);
+                          });
+        if (masked) {
 #pragma unroll
-        for (int kk = 0; kk < KK; ++kk) {
-          sacc = TY::mma(TL::row_frag(lq, 32 * u, kk, lane), kf[kk], sacc);
-          pacc = TY::mma(TL::row_frag(ldo, 32 * u, kk, lane), vf[kk], pacc);
+          for (int r = 0; r < 16; ++r) {
+            const int at = 32 * u + 8 * (r >> 2) + (r & 3);
+            const bool counts = at >= d_from - d0 && at < d_end - d0;
+            sacc[r] = counts ? sacc[r] : -INFINITY;
+            pacc[r] = counts ? pacc[r] : 0.f;
+          }
         }
-        float bias[16];
-        const int tmin = dlo + 32 * u, tmax = dlo + 32 * u + 62;
-        if constexpr (BIAS) tile_bias<1>(*bl, p.db, first, d0 + 32 * u, tmin, tmax, bias);
-        typename TY::Frag pf[2], dsf[2];
-        float ds[16];
+        const TileBuckets tb(p.db, first, BIAS ? dlo + 32 * u : 0, dlo + 32 * u + 62);
 #pragma unroll
-        for (int v = 0; v < 2; ++v) {
-          float pe[8], de[8];
+        for (int v = 0; v < 2; ++v) {  // elements 8 v .. 8 v + 7: streamed rows 32 u + 16 v ..
+          typename TY::Half ph[2], dsh[2];
 #pragma unroll
-          for (int q = 0; q < 2; ++q) {
-            const float4* sp = reinterpret_cast<const float4*>(lstat + 2 * (32 * u + 8 * (2 * v + q) + 4 * half));
+          for (int q = 0; q < 2; ++q) {  // four rows at a time, which keeps few of their values alive
+            const int row = 32 * u + 16 * v + 8 * q;
+            float bias[4];
+            if constexpr (BIAS) tile_bias<1>(*bl, tb, first, d0 + row, bias);
+            const float4* sp = reinterpret_cast<const float4*>(lstat + 2 * (row + 4 * half));
             const float4 s0 = sp[0], s1 = sp[1];
             const float l2v[4] = {s0.x, s0.z, s1.x, s1.z}, dlv[4] = {s0.y, s0.w, s1.y, s1.w};
+            float pe[4], de[4];
 #pragma unroll
             for (int w = 0; w < 4; ++w) {
               const int r = 8 * v + 4 * q + w;
-              float pr = __builtin_amdgcn_exp2f((BIAS ? fmaf(sacc[r], scale_log2, bias[r]) : sacc[r] * scale_log2) - l2v[w]);
-              float dsr = pr * (pacc[r] - dlv[w]);
-              if (masked) {
-                const int d = d0 + 32 * u + 8 * (r >> 2) + (r & 3);
-                const bool counts = d >= d_from && d < d_end;
-                pr = counts ? pr : 0.f;
-                dsr = counts ? dsr : 0.f;
-              }
-              pe[4 * q + w] = pr;
-              de[4 * q + w] = dsr;
-              ds[r] = dsr;
+              pe[w] = __builtin_amdgcn_exp2f((BIAS ? fmaf(sacc[r], scale_log2, bias[w]) : sacc[r] * scale_log2) - l2v[w]);
+              de[w] = pe[w] * (pacc[r] - dlv[w]);  // a pair that does not count has p = 0 and a finite dP here
             }
+            if constexpr (BIAS) add_to_table(sums[wave], tb, first, p.db.count, d0 + row, half, lane, de);
+            ph[q] = TY::half(pe);
+            dsh[q] = TY::half(de);
           }
-          pf[v] = TY::pack(pe);
-          dsf[v] = TY::pack(de);
+          const typename TY::Frag pf = TY::join(ph[0], ph[1]), dsf = TY::join(dsh[0], dsh[1]);
+          pipelined<2 * TN>(ahead, [&](int i) { return TL::col_frag(lqc, i >> 1, 2 * u + v, i & 1); },
+                            [&](int i, const typename TY::Frag& f) {
+                              if (i & 1) av[i >> 1] = TY::mma(f, pf, av[i >> 1]);
+                              else ak[i >> 1] = TY::mma(f, dsf, ak[i >> 1]);
+                            });
         }
-        if constexpr (BIAS) {
-          if (tmin < kNear) {
-            float* at = sums[wave].near[half] + kPad + d0 + 32 * u;
-#pragma unroll
-            for (int r = 0; r < 16; ++r) __hip_atomic_fetch_add(at + 8 * (r >> 2) + (r & 3), ds[r], __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_WORKGROUP);
-          } else {
-            const int b0 = __builtin_amdgcn_readfirstlane(bucket_of(p.db, first, tmin)), b1 = __builtin_amdgcn_readfirstlane(bucket_of(p.db, first, tmax));
-            for (int bk = b0; bk <= b1; ++bk) {
-              const int from = first[bk], to = bk + 1 < p.db.count ? first[bk + 1] : S;
-              float s = 0.f;
-#pragma unroll
-              for (int r = 0; r < 16; ++r) {
-                const int d = d0 + 32 * u + 8 * (r >> 2) + (r & 3);
-                if (b0 == b1 || (d >= from && d < to)) s += ds[r];
-              }
-              s = sum_over_lanes(s);
-              if (lane == 0) sums[wave].far[bk] += s;
-            }
-          }
-        }
-#pragma unroll
-        for (int v = 0; v < 2; ++v)
-#pragma unroll
-          for (int j = 0; j < TN; ++j) {
-            ak[j] = TY::mma(TL::col_frag(lq, j, 2 * u + v, lane), dsf[v], ak[j]);
-            av[j] = TY::mma(TL::col_frag(ldo, j, 2 * u + v, lane), pf[v], av[j]);
-          }
-        __builtin_amdgcn_sched_barrier(0);  // one tile's scores alive at a time
       }
     }
     if constexpr (BIAS) {
