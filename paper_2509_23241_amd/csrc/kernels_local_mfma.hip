@@ -739,23 +739,56 @@ __global__ __launch_bounds__(64 * NW, sizeof(T) == 2 || DHP == 64 ? 2 : 1) void 
   }
 }
 
-// Sums of dS by distance, per wave and half of its lanes (whose tiles' distances differ by four: together they would meet on one
-// address), kept in LDS: a wave's own additions stay in order.
+// Sums of dS by distance and, beyond the near ones, by bucket, per wave, in LDS: a wave's own additions stay in order.
 struct TableSums {
-  float near[2][kNearSize];
+  float near[kNearSize];
   float far[kMaxBuckets];
 };
 
-// ds: four elements with distances base .. base + 3
-__device__ __forceinline__ void add_to_table(TableSums& sums, const TileBuckets& tb, const int* first, int count, int base, int half, int lane,
-                                             const float (&ds)[4]) {
-  if (tb.b0 < 0) {
-    float* at = sums.near[half] + kPad + base;
+// What a lane has of the bucket that its wave's last far tiles lay in; distances ascend along a walk, so buckets change rarely.
+struct FarSum {
+  float sum = 0.f;
+  int bucket = 0;  // wave uniform
+  __device__ __forceinline__ void flush(TableSums& sums, int lane) {
+    const float s = sum_over_lanes(sum);
+    if (lane == 0) sums.far[bucket] += s;
+    sum = 0.f;
+  }
+  __device__ __forceinline__ void start_tile(TableSums& sums, const TileBuckets& tb, int lane) {
+    if (tb.b0 < 0 || tb.b0 == bucket) return;
+    flush(sums, lane);
+    bucket = tb.b0;
+  }
+};
+// Sums along the diagonals of a tile of 32 queries (rows, in order) x 32 keys (lanes): with every row the sums move a lane up, so that a
+// diagonal's stays with it, and take in the row's values; lanes 32 .. 63 add nothing and hold the diagonals that have left the tile.  After
+// the last row lane l has the sum of (row - lane) = 31 - l.  (Adding every element to its distance in LDS instead: 16 float atomics a tile, which
+// took 650 cycles each, 10 of the 13 thousand cycles of a tile.)
+struct Diagonals {
+  float sum = 0.f;
+  __device__ __forceinline__ void row(float v) {
+    sum = v + __int_as_float(__builtin_amdgcn_update_dpp(0, __float_as_int(sum), 0x138, 0xf, 0xf, true));  // wave_shr:1
+  }
+  // a lane's four rows below the others', of which lanes 0 .. 31 have the first and lanes 32 .. 63 the second four
+  __device__ __forceinline__ void rows(const float (&ds)[4]) {
+    float second[4];
 #pragma unroll
-    for (int r = 0; r < 4; ++r) __hip_atomic_fetch_add(at + r, ds[r], __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_WORKGROUP);
+    for (int r = 0; r < 4; ++r) {
+      const auto split = __builtin_amdgcn_permlane32_swap(__float_as_uint(ds[r]), 0u, false, false);
+      second[r] = __uint_as_float(split[1]);
+      row(__uint_as_float(split[0]));
+    }
+#pragma unroll
+    for (int r = 0; r < 4; ++r) row(second[r]);
+  }
+};
+// ds: four elements with distances base .. base + 3
+__device__ __forceinline__ void add_to_table(TableSums& sums, FarSum& far, Diagonals& diagonals, const TileBuckets& tb, const int* first, int count,
+                                             int base, int lane, const float (&ds)[4]) {
+  if (tb.b0 < 0) {
+    diagonals.rows(ds);
   } else if (tb.b0 == tb.b1) {
-    const float s = sum_over_lanes((ds[0] + ds[1]) + (ds[2] + ds[3]));
-    if (lane == 0) sums.far[tb.b0] += s;
+    far.sum += (ds[0] + ds[1]) + (ds[2] + ds[3]);
   } else {
     for (int b = tb.b0; b <= tb.b1; ++b) {
       const int from = first[b] - base, to = b + 1 < count ? first[b + 1] - base : 4;
@@ -851,6 +884,7 @@ __global__ __launch_bounds__(64 * NW, sizeof(T) == 2 || DHP == 64 ? 2 : 1) void 
     for (int r = 0; r < 16; ++r) ak[j][r] = av[j][r] = 0.f;
   const float scale_log2 = p.scale * kLog2e;
   if (count > 0) issue(0);
+  FarSum far_sum;
   int t = 0;
   for (int g = 0; g < group; ++g) {
     for (int n = 0; n < nb; ++n, ++t) {
@@ -870,12 +904,13 @@ __global__ __launch_bounds__(64 * NW, sizeof(T) == 2 || DHP == 64 ? 2 : 1) void 
         floatx16 sacc, pacc;
 #pragma unroll
         for (int r = 0; r < 16; ++r) sacc[r] = pacc[r] = 0.f;
-        typename TY::Frag ahead[2];
+        typename TY::Frag ahead[BIAS ? 1 : 2];
         pipelined<2 * KK>(ahead, [&](int i) { return TL::row_frag(lq, u, i >> 1, i & 1); },
                           [&](int i, const typename TY::Frag& f) {
                             if (i & 1) pacc = TY::mma(f, vf[i >> 1], pacc);
                             else sacc = TY::mma(f, kf[i >> 1], sacc);
                           });
+        __builtin_amdgcn_sched_barrier(0);
         if (masked) {
 #pragma unroll
           for (int r = 0; r < 16; ++r) {
@@ -886,6 +921,8 @@ __global__ __launch_bounds__(64 * NW, sizeof(T) == 2 || DHP == 64 ? 2 : 1) void 
           }
         }
         const TileBuckets tb(p.db, first, BIAS ? dlo + 32 * u : 0, dlo + 32 * u + 62);
+        if constexpr (BIAS) far_sum.start_tile(sums[wave], tb, lane);
+        Diagonals diagonals;
 #pragma unroll
         for (int v = 0; v < 2; ++v) {  // elements 8 v .. 8 v + 7: streamed rows 32 u + 16 v ..
           typename TY::Half ph[2], dsh[2];
@@ -904,9 +941,10 @@ __global__ __launch_bounds__(64 * NW, sizeof(T) == 2 || DHP == 64 ? 2 : 1) void 
               pe[w] = __builtin_amdgcn_exp2f((BIAS ? fmaf(sacc[r], scale_log2, bias[w]) : sacc[r] * scale_log2) - l2v[w]);
               de[w] = pe[w] * (pacc[r] - dlv[w]);  // a pair that does not count has p = 0 and a finite dP here
             }
-            if constexpr (BIAS) add_to_table(sums[wave], tb, first, p.db.count, d0 + row, half, lane, de);
+            if constexpr (BIAS) add_to_table(sums[wave], far_sum, diagonals, tb, first, p.db.count, d0 + row, lane, de);
             ph[q] = TY::half(pe);
             dsh[q] = TY::half(de);
+            if constexpr (BIAS) __builtin_amdgcn_sched_barrier(0);
           }
           const typename TY::Frag pf = TY::join(ph[0], ph[1]), dsf = TY::join(dsh[0], dsh[1]);
           pipelined<2 * TN>(ahead, [&](int i) { return TL::col_frag(lqc, i >> 1, 2 * u + v, i & 1); },
@@ -915,16 +953,20 @@ __global__ __launch_bounds__(64 * NW, sizeof(T) == 2 || DHP == 64 ? 2 : 1) void 
                               else ak[i >> 1] = TY::mma(f, dsf, ak[i >> 1]);
                             });
         }
+        if constexpr (BIAS) {
+          if (tb.b0 < 0) sums[wave].near[kPad + dlo + 32 * u + 62 - lane] += diagonals.sum;
+        }
       }
     }
     if constexpr (BIAS) {
       // this head's sums: over the waves and halves by distance, then by bucket
+      far_sum.flush(sums[wave], lane);
       __syncthreads();
       float* by_distance = bl->near;
       for (int i = threadIdx.x; i < kNearSize; i += 64 * NW) {
         float s = 0.f;
 #pragma unroll
-        for (int w = 0; w < NW; ++w) s += sums[w].near[0][i] + sums[w].near[1][i];
+        for (int w = 0; w < NW; ++w) s += sums[w].near[i];
         by_distance[i] = s;
       }
       __syncthreads();
