@@ -31,7 +31,7 @@ namespace tp {
 namespace {
 
 constexpr float kLowest = -1e30f;  // running maximum of a row that has seen no key; scores below it are formed again, row by row
-constexpr int kNear = 112;         // distances with a table entry and a sum of their own: 0 .. kNear - 1, and as far as a tile reaches beyond
+constexpr int kNear = 224;         // distances with a table entry and a sum of their own: 0 .. kNear - 1, and as far as a tile reaches beyond
 constexpr int kPad = 96;           // a tile of 32 x 64 spans 95 distances
 constexpr int kNearSize = kPad + kNear + kPad;
 
@@ -43,8 +43,7 @@ template <typename T>
 struct Type;
 template <>
 struct Type<uint16_t> {
-  static constexpr int BR = 64;      // streamed rows of a block
-  static constexpr int kAhead = 4;   // fragments on their way from LDS
+  static constexpr int kAhead = 4;  // fragments on their way from LDS
   using Frag = bf16x8;
   static __device__ __forceinline__ floatx16 mma(const Frag& a, const Frag& b, floatx16 c) {
     return __builtin_amdgcn_mfma_f32_32x32x16_bf16(a, b, c, 0, 0, 0);
@@ -73,7 +72,7 @@ struct Type<uint16_t> {
 };
 template <>
 struct Type<float> {
-  static constexpr int BR = 32, kAhead = 2;
+  static constexpr int kAhead = 2;
   using Frag = floatx8;
   static __device__ __forceinline__ floatx16 mma(const Frag& a, const Frag& b, floatx16 c) {
 #pragma unroll
@@ -122,9 +121,13 @@ __device__ __forceinline__ int afresh(int v) {
   return v;
 }
 
+// streamed rows of a block: a tile of them takes 16 KB or less
+template <typename T, int DHP>
+constexpr int kBlockRows = DHP * sizeof(T) <= 256 ? 64 : 32;
+
 template <typename T, int DHP, int NW>
 struct Tile {
-  static constexpr int BR = Type<T>::BR, E = sizeof(T);
+  static constexpr int BR = kBlockRows<T, DHP>, E = sizeof(T);
   static constexpr int kPanels = DHP * E / 128, kPanelBytes = BR * 128, kBytes = kPanels * kPanelBytes;
   static constexpr int kPerWave = kBytes / 1024 / NW;  // a wave instruction copies 8 rows of a panel
   // A lane's chunk of copy t lies 32 rows (whose swizzle is the same) or a panel beyond that of copy 0
@@ -242,7 +245,7 @@ __device__ __forceinline__ void load_borders(const DistanceBuckets& d, int* firs
 struct TileBuckets {
   int b0 = -1, b1 = -1;
   __device__ __forceinline__ TileBuckets(const DistanceBuckets& d, const int* first, int dmin, int dmax) {
-    if (dmin < kNear) return;
+    if (dmin < kNear && dmin < __builtin_amdgcn_readfirstlane(first[d.count - 1])) return;
     b0 = __builtin_amdgcn_readfirstlane(bucket_of(d, first, dmin));
     b1 = b0;
     while (b1 + 1 < d.count && __builtin_amdgcn_readfirstlane(first[b1 + 1]) <= dmax) ++b1;
@@ -437,7 +440,7 @@ template <typename T, int DHP, int NW, bool BIAS>
 __global__ __launch_bounds__(64 * NW, 2) void local_fwd_kernel(FwdArgs<T> p) {
   using TY = Type<T>;
   using TL = Tile<T, DHP, NW>;
-  constexpr int BR = TY::BR, NT = BR / 32, KK = DHP / 16, TN = DHP / 32;
+  constexpr int BR = TL::BR, NT = BR / 32, KK = DHP / 16, TN = DHP / 32;
   extern __shared__ __attribute__((aligned(16))) char lds[];
   const Shape& a = p.a;
   const int lane = threadIdx.x & 63, half = lane >> 5;
@@ -593,9 +596,11 @@ struct BwdArgs {
   const float *lse, *kept;
   T* dx;
   float* stat;      // [seqs*heads][stat_rows(S)][2]: lse * log2(e) and the corrected delta, zeros behind the last token
-  float* sums;      // dK and dV of keys < sinks that lie far apart from their queries: [chunks + 1][seqs*kv][sinks][2][dh]
+  // parts of dK and dV: [parts][seqs*kv][S, or with one part sinks][2][dh], then of far pairs of the first keys [chunks][seqs*kv][sinks][2][dh]
+  float* sums;
   float* partials;  // of the table: [seqs * gridDim.y][heads][buckets]
-  int far_blocks, chunks, chunk_blocks;  // workgroups for those pairs: blocks of keys x ranges of chunk_blocks streamed blocks
+  int parts;        // of a walk over streamed blocks, in workgroups of their own
+  int far_blocks, chunks, chunk_blocks;  // workgroups for far pairs of the first keys: blocks of keys x ranges of chunk_blocks streamed blocks
   float scale;
 };
 
@@ -603,7 +608,7 @@ template <typename T, int DHP, int NW, bool BIAS>
 __global__ __launch_bounds__(64 * NW, sizeof(T) == 2 || DHP == 64 ? 2 : 1) void local_dq_kernel(BwdArgs<T> p) {
   using TY = Type<T>;
   using TL = Tile<T, DHP, NW>;
-  constexpr int BR = TY::BR, NT = BR / 32, KK = DHP / 16, TN = DHP / 32;
+  constexpr int BR = TL::BR, NT = BR / 32, KK = DHP / 16, TN = DHP / 32;
   extern __shared__ __attribute__((aligned(16))) char lds[];
   const Shape& a = p.a;
   const int lane = threadIdx.x & 63, half = lane >> 5;
@@ -804,11 +809,14 @@ __device__ __forceinline__ void add_to_table(TableSums& sums, FarSum& far, Diago
 template <int NW>
 constexpr size_t dkv_bias_lds(bool bias) { return bias ? kMaxBuckets * 4 + sizeof(BiasLds) + NW * sizeof(TableSums) : 0; }
 
-template <typename T, int DHP, int NW, bool BIAS>
+// TEAMS: 1, a wave owns 32 keys of 128; 2, two waves own the same 32 keys of 64 and take one tile of every streamed block each, which makes
+// twice as many workgroups of half the length; their sums meet in LDS.
+template <typename T, int DHP, int NW, int TEAMS, bool BIAS>
 __global__ __launch_bounds__(64 * NW, sizeof(T) == 2 || DHP == 64 ? 2 : 1) void local_dkv_kernel(BwdArgs<T> p) {
   using TY = Type<T>;
   using TL = Tile<T, DHP, NW>;
-  constexpr int BR = TY::BR, NT = BR / 32, KK = DHP / 16, TN = DHP / 32, kOwn = 32 * NW;
+  constexpr int BR = TL::BR, NT = BR / 32, KK = DHP / 16, TN = DHP / 32, kOwn = 32 * NW / TEAMS;
+  static_assert(TEAMS == 1 || TEAMS == NT, "a team takes one tile of a block");
   constexpr int kStageBytes = 2 * TL::kBytes + 1024;  // Q, dO, statistics
   extern __shared__ __attribute__((aligned(16))) char lds[];
   const Shape& a = p.a;
@@ -821,8 +829,10 @@ __global__ __launch_bounds__(64 * NW, sizeof(T) == 2 || DHP == 64 ? 2 : 1) void 
   const int fars = p.far_blocks * p.chunks;
   const bool far = (int)blockIdx.y < fars;
   const int chunk = far ? blockIdx.y / p.far_blocks : 0;
-  const int k0 = (far ? blockIdx.y - chunk * p.far_blocks : blockIdx.y - fars) * kOwn;
-  const int kw = k0 + wave * 32, key = kw + (lane & 31);
+  const int part = far ? 0 : ((int)blockIdx.y - fars) % p.parts;
+  const int k0 = (far ? (int)blockIdx.y - chunk * p.far_blocks : ((int)blockIdx.y - fars) / p.parts) * kOwn;
+  const int team = wave / (NW / TEAMS);
+  const int kw = k0 + wave % (NW / TEAMS) * 32, key = kw + (lane & 31);
   const bool active = kw < (far ? a.sinks : S);
   // distances that count: all in the window, or beside the far workgroups' all in it, or there all beyond it
   const int d_from = far ? a.window : 0, d_to = far ? S : a.window;
@@ -832,7 +842,9 @@ __global__ __launch_bounds__(64 * NW, sizeof(T) == 2 || DHP == 64 ? 2 : 1) void 
     blk0 = (k0 + a.window) / BR + chunk * p.chunk_blocks;
     blk1 = min(blk0 + p.chunk_blocks, (S + BR - 1) / BR);
   }
-  const int nb = max(0, blk1 - blk0), count = nb * group;
+  // steps of the walk: the streamed blocks of each query head in turn; a part takes a range of them
+  const int nb = max(0, blk1 - blk0), steps = nb * group;
+  const int t_begin = far ? 0 : (int)((long)steps * part / p.parts), t_end = far ? steps : (int)((long)steps * (part + 1) / p.parts);
   const T* base = p.x + (size_t)b * S * ld;
   const T* kbase = base + D + (size_t)kvh * dh;
   const T* vbase = kbase + (size_t)a.kv * dh;
@@ -883,24 +895,25 @@ __global__ __launch_bounds__(64 * NW, sizeof(T) == 2 || DHP == 64 ? 2 : 1) void 
 #pragma unroll
     for (int r = 0; r < 16; ++r) ak[j][r] = av[j][r] = 0.f;
   const float scale_log2 = p.scale * kLog2e;
-  if (count > 0) issue(0);
+  if (t_begin < t_end) issue(t_begin);
   FarSum far_sum;
-  int t = 0;
+  int t = t_begin;
   for (int g = 0; g < group; ++g) {
-    for (int n = 0; n < nb; ++n, ++t) {
+    for (int n = t - g * nb; n < nb && t < t_end; ++n, ++t) {  // a part that begins with a later head has n >= nb here
       wait_vmcnt<0>();
       lds_barrier();
-      if (t + 1 < count) issue(t + 1);
-      const int qb = (blk0 + n) * BR;
+      if (t + 1 < t_end) issue(t + 1);
+      constexpr int kMine = BR / TEAMS;  // the wave's rows of the block
+      const int skip = TEAMS == 1 ? 0 : team * 32, qb = (blk0 + n) * BR + skip;
       // wave uniform: distances of the wave's pairs in this block
-      const int dlo = qb - (kw + 31), dhi = qb + BR - 1 - kw;
+      const int dlo = qb - (kw + 31), dhi = qb + kMine - 1 - kw;
       if (!active || dhi < d_from || dlo >= d_to) continue;
-      const uint32_t stage = (t & 1) * kStageBytes, lq = lds0 + stage + TL::row_base(afresh(lane)), lqc = lds0 + stage + TL::col_base(afresh(lane));
-      const float* lstat = reinterpret_cast<const float*>(lds + stage + 2 * TL::kBytes);
-      const bool masked = dlo < d_from || dhi >= d_to || qb + BR > S || (far && kw + 31 >= a.sinks);
+      const uint32_t stage = (t & 1) * kStageBytes, lq = lds0 + stage + skip * 128 + TL::row_base(afresh(lane)), lqc = lds0 + stage + skip * 128 + TL::col_base(afresh(lane));
+      const float* lstat = reinterpret_cast<const float*>(lds + stage + 2 * TL::kBytes) + 2 * skip;
+      const bool masked = dlo < d_from || dhi >= d_to || qb + kMine > S || (far && kw + 31 >= a.sinks);
       const int d0 = qb - key + 4 * half;
 #pragma unroll
-      for (int u = 0; u < NT; ++u) {
+      for (int u = 0; u < NT / TEAMS; ++u) {
         floatx16 sacc, pacc;
 #pragma unroll
         for (int r = 0; r < 16; ++r) sacc[r] = pacc[r] = 0.f;
@@ -990,9 +1003,39 @@ __global__ __launch_bounds__(64 * NW, sizeof(T) == 2 || DHP == 64 ? 2 : 1) void 
     }
   }
   lds_barrier();
-  if (!active) return;
-  const bool join = p.far_blocks > 0;  // dK and dV of first keys are sums of several workgroups'
-  float* part = p.sums + ((size_t)(far ? chunk + 1 : 0) * gridDim.x + blockIdx.x) * a.sinks * 2 * dh;
+  if constexpr (TEAMS == 2) {  // the second team's sums to the first
+    floatx4* mine = reinterpret_cast<floatx4*>(lds) + (size_t)(wave % (NW / TEAMS)) * 2 * TN * 4 * 64 + lane;
+    if (team == 1) {
+#pragma unroll
+      for (int j = 0; j < TN; ++j)
+#pragma unroll
+        for (int r = 0; r < 4; ++r) {
+          mine[(j * 4 + r) * 64] = floatx4{ak[j][4 * r], ak[j][4 * r + 1], ak[j][4 * r + 2], ak[j][4 * r + 3]};
+          mine[((TN + j) * 4 + r) * 64] = floatx4{av[j][4 * r], av[j][4 * r + 1], av[j][4 * r + 2], av[j][4 * r + 3]};
+        }
+    }
+    lds_barrier();
+    if (team == 0) {
+#pragma unroll
+      for (int j = 0; j < TN; ++j)
+#pragma unroll
+        for (int r = 0; r < 4; ++r) {
+          const floatx4 k = mine[(j * 4 + r) * 64], v = mine[((TN + j) * 4 + r) * 64];
+#pragma unroll
+          for (int e = 0; e < 4; ++e) {
+            ak[j][4 * r + e] += k[e];
+            av[j][4 * r + e] += v[e];
+          }
+        }
+    }
+    lds_barrier();
+  }
+  if (!active || team != 0) return;
+  // Where a row of dK and dV goes: to dx, or, if it is a sum of several workgroups', as fp32 to their parts: those of parts of the walk
+  // hold all keys, those of far pairs the first ones.
+  const int joined = far ? a.sinks : p.parts > 1 ? S : p.far_blocks > 0 ? a.sinks : 0;
+  const size_t nz = gridDim.x, part_rows = p.parts > 1 ? S : a.sinks;
+  float* to = p.sums + (far ? p.parts * nz * part_rows + (chunk * nz + blockIdx.x) * a.sinks : (part * nz + blockIdx.x) * part_rows) * 2 * dh;
   T* dk = p.dx + (size_t)b * S * ld + D + (size_t)kvh * dh;
   T* dv = dk + (size_t)a.kv * dh;
   const int there_end = far ? a.sinks : S;
@@ -1001,7 +1044,7 @@ __global__ __launch_bounds__(64 * NW, sizeof(T) == 2 || DHP == 64 ? 2 : 1) void 
     return [=](int r, int col, const float (&v)[8]) {
       const int j = kw + r;
       if (j >= there_end) return;
-      if (join && j < a.sinks) Type<float>::store8(part + ((size_t)j * 2 + which) * dh + col, v, dh - col);
+      if (j < joined) Type<float>::store8(to + ((size_t)j * 2 + which) * dh + col, v, dh - col);
       else TY::store8((which ? dv : dk) + (size_t)j * ld + col, v, dh - col);
     };
   };
@@ -1012,22 +1055,24 @@ __global__ __launch_bounds__(64 * NW, sizeof(T) == 2 || DHP == 64 ? 2 : 1) void 
   for (; redo; redo &= redo - 1) {
     const int j = kw + __builtin_ctz(redo);
     float rk[2] = {}, rv[2] = {};
-    const int from = max(blk0 * BR, j + d_from), to = (int)min((long)min(S, blk1 * BR), (long)j + d_to);  // queries
     for (int g = 0; g < group; ++g) {
       const int h = kvh * group + g;
+      // queries of this workgroup's steps that see the key
+      const int n0 = max(0, t_begin - g * nb), n1 = min(nb, t_end - g * nb);
+      const int from = max((blk0 + n0) * BR, j + d_from), to_i = (int)min((long)min(S, (blk0 + n1) * BR), (long)j + d_to);
       const T* q = base + (size_t)h * dh;
       const T* dO = dobase + (size_t)h * dh;
-      for (int i0 = from; i0 < to; i0 += 64) {
+      for (int i0 = from; i0 < to_i; i0 += 64) {
         const int i = i0 + lane;
         float pr = 0.f, ds = 0.f;
-        if (i < to) {
+        if (i < to_i) {
           const float2 st = *reinterpret_cast<const float2*>(p.stat + (((size_t)b * a.heads + h) * SP + i) * 2);
           float e = row_dot(q + (size_t)i * ld, kbase + (size_t)j * ld, dh) * scale_log2 - st.x;
           if (BIAS) e += table(h)[bucket_of(p.db, first, i - j)] * kLog2e;
           pr = __builtin_amdgcn_exp2f(e);
           ds = pr * (row_dot(dO + (size_t)i * D, vbase + (size_t)j * ld, dh) - st.y);
         }
-        const uint64_t which = __builtin_amdgcn_ballot_w64(i < to);
+        const uint64_t which = __builtin_amdgcn_ballot_w64(i < to_i);
         add_rows(rk, ds, q + (size_t)i0 * ld, ld, which, dh, lane);
         add_rows(rv, pr, dO + (size_t)i0 * D, D, which, dh, lane);
       }
@@ -1036,9 +1081,9 @@ __global__ __launch_bounds__(64 * NW, sizeof(T) == 2 || DHP == 64 ? 2 : 1) void 
     for (int c = 0; c < 2; ++c) {
       const int col = lane + 64 * c;
       if (col >= dh) continue;
-      if (join && j < a.sinks) {
-        part[((size_t)j * 2) * dh + col] = rk[c] * p.scale;
-        part[((size_t)j * 2 + 1) * dh + col] = rv[c];
+      if (j < joined) {
+        to[((size_t)j * 2) * dh + col] = rk[c] * p.scale;
+        to[((size_t)j * 2 + 1) * dh + col] = rv[c];
       } else {
         dk[(size_t)j * ld + col] = from_float<T>(rk[c] * p.scale);
         dv[(size_t)j * ld + col] = from_float<T>(rv[c]);
@@ -1047,45 +1092,70 @@ __global__ __launch_bounds__(64 * NW, sizeof(T) == 2 || DHP == 64 ? 2 : 1) void 
   }
 }
 
-// dK and dV of the first keys from the parts of several workgroups, in the order of the ranges
+// dK and dV from the parts of several workgroups, always in the same order: `parts` of [nz][rows][2][dh], then `chunks` of [nz][sinks][2][dh]
 template <typename T>
-__global__ __launch_bounds__(256) void local_join_kernel(Shape a, int parts, size_t count, const float* __restrict__ sums, T* __restrict__ dx) {
-  const size_t i = (size_t)blockIdx.x * 256 + threadIdx.x;
-  if (i >= count) return;
-  float s = 0.f;
-  for (int c = 0; c < parts; ++c) s += sums[(size_t)c * count + i];
-  const int d = (int)(i % a.dh), which = (int)(i / a.dh % 2), j = (int)(i / (2 * a.dh) % a.sinks);
-  const size_t z = i / ((size_t)2 * a.dh * a.sinks), b = z / a.kv, kvh = z - b * a.kv;
-  dx[((size_t)b * a.S + j) * a.ld() + (size_t)(a.heads + which * a.kv + kvh) * a.dh + d] = from_float<T>(s);
+__global__ __launch_bounds__(256) void local_join_kernel(Shape a, int parts, int chunks, size_t nz, int rows, const float* __restrict__ sums,
+                                                         T* __restrict__ dx) {
+  const size_t quad = (size_t)blockIdx.x * 256 + threadIdx.x, row = 2 * a.dh / 4, count = nz * rows * row;  // of four values
+  if (quad >= count) return;
+  const size_t zj = quad / row, z = zj / rows;
+  const int in = (int)(quad - zj * row) * 4, j = (int)(zj - z * rows);
+  const int which = in >= a.dh, d = in - which * a.dh;
+  float4 s = make_float4(0.f, 0.f, 0.f, 0.f);
+  auto add = [&](const float* at) {
+    const float4 v = *reinterpret_cast<const float4*>(at);
+    s.x += v.x; s.y += v.y; s.z += v.z; s.w += v.w;
+  };
+  for (int p = 0; p < parts; ++p) add(sums + ((size_t)p * count + quad) * 4);
+  if (j < a.sinks)
+    for (int c = 0; c < chunks; ++c) add(sums + (size_t)parts * count * 4 + (((size_t)c * nz + z) * a.sinks + j) * 2 * a.dh + in);
+  const size_t b = z / a.kv, kvh = z - b * a.kv;
+  T* to = dx + ((size_t)b * a.S + j) * a.ld() + (size_t)(a.heads + which * a.kv + kvh) * a.dh + d;
+  if constexpr (sizeof(T) == 2) *reinterpret_cast<uint2*>(to) = make_uint2(pack_bf16x2(s.x, s.y), pack_bf16x2(s.z, s.w));
+  else *reinterpret_cast<float4*>(to) = s;
 }
 
 constexpr int kWaves = 4;
 
-// workgroups of the dK, dV launch beside those of the blocks of keys
-struct FarPlan {
-  int blocks = 0, chunks = 0, chunk_blocks = 0;
+// How the dK, dV launch is cut up.
+struct DkvPlan {
+  int teams = 1, parts = 1;
+  int far_blocks = 0, chunks = 0, chunk_blocks = 0;  // workgroups for the far pairs of the first keys
+  int rows = 0;                                      // workgroups for a key head of a sequence
 };
-template <typename T>
-FarPlan far_plan(const LocalAttention& a) {
-  FarPlan f;
-  constexpr int BR = Type<T>::BR, kOwn = 32 * kWaves;
-  if (a.sinks == 0 || a.window >= a.S) return f;
-  f.blocks = (a.sinks + kOwn - 1) / kOwn;
-  const int total = (a.S + BR - 1) / BR - a.window / BR;  // streamed blocks that far pairs of the first keys lie in
-  // a range is about as long as what the other workgroups walk over; no more of them than give every CU four, since each leaves its sums
-  // in memory
-  const int walk = std::max(8, (a.window + kOwn) / BR);
-  const long most = std::max<long>(1, 1024 / ((long)a.seqs * a.kv * f.blocks));
-  f.chunks = (int)std::min<long>(most, (total + walk - 1) / walk);
-  f.chunk_blocks = (total + f.chunks - 1) / f.chunks;
+template <typename T, int DHP>
+DkvPlan dkv_plan(const LocalAttention& a) {
+  DkvPlan f;
+  constexpr int BR = kBlockRows<T, DHP>;
+  const long nz = (long)a.seqs * a.kv, group = a.heads / a.kv;
+  constexpr long kEnough = 512;  // workgroups that fill the chip, two on a CU
+  if (BR == 64 && nz * ((a.S + 127) / 128) < kEnough) f.teams = 2;
+  const int own = 128 / f.teams, blocks = (a.S + own - 1) / own;
+  // fewer even so: the walks in parts, of four steps at least, since a part leaves its sums in memory to be joined
+  const long steps = (std::min<long>(a.S, (long)own + a.window) + BR - 1) / BR * group;
+  f.parts = (int)std::max<long>(1, std::min({(kEnough + nz * blocks - 1) / (nz * blocks), steps / 4, 16l}));
+  if (a.sinks > 0 && a.window < a.S) {
+    f.far_blocks = (a.sinks + own - 1) / own;
+    const int total = (a.S + BR - 1) / BR - a.window / BR;  // streamed blocks that far pairs of the first keys lie in
+    // a range is about as long as what the other workgroups walk over; no more of them than give every CU four, since each leaves its sums
+    // in memory
+    const int walk = std::max<int>(4, (a.window + own) / BR / f.parts);
+    const long most = std::max<long>(1, 1024 / (nz * f.far_blocks));
+    f.chunks = (int)std::min<long>(most, (total + walk - 1) / walk);
+    f.chunk_blocks = (total + f.chunks - 1) / f.chunks;
+  }
+  f.rows = blocks * f.parts + f.far_blocks * f.chunks;
   return f;
 }
-template <typename T>
-unsigned dkv_rows(const LocalAttention& a) {
-  const FarPlan f = far_plan<T>(a);
-  return (unsigned)((a.S + 32 * kWaves - 1) / (32 * kWaves) + f.blocks * f.chunks);
+inline DkvPlan dkv_plan(int elt, const LocalAttention& a) {
+  if (elt == ELT_BF16) return a.dh <= 64 ? dkv_plan<uint16_t, 64>(a) : dkv_plan<uint16_t, 128>(a);
+  return a.dh <= 64 ? dkv_plan<float, 64>(a) : dkv_plan<float, 128>(a);
 }
 inline size_t stat_floats(const LocalAttention& a) { return (size_t)a.seqs * a.heads * stat_rows(a.S) * 2; }
+inline int join_rows(const LocalAttention& a, const DkvPlan& f) { return f.parts > 1 ? a.S : f.far_blocks ? a.sinks : 0; }
+inline size_t sum_floats(const LocalAttention& a, const DkvPlan& f) {
+  return (size_t)a.seqs * a.kv * 2 * a.dh * ((size_t)f.parts * join_rows(a, f) + (size_t)f.chunks * a.sinks);
+}
 inline unsigned query_groups(const LocalAttention& a, int rows) {
   return (unsigned)(((long)(rows + 31) / 32 * (a.heads / a.kv) + kWaves - 1) / kWaves);
 }
@@ -1113,18 +1183,22 @@ hipError_t run_bwd(hipStream_t s, const LocalAttention& a, const BwdArgs<T>& p) 
   constexpr size_t lds_kv = std::max<size_t>(2 * (2 * TL::kBytes + 1024), kWaves * kTurnBytes) + dkv_bias_lds<kWaves>(BIAS);
   static_assert(lds_kv <= 160 * 1024, "tiles and sums do not fit the LDS of a CU");
   auto dq = local_dq_kernel<T, DHP, kWaves, BIAS>;
-  auto dkv = local_dkv_kernel<T, DHP, kWaves, BIAS>;
-  static hipError_t attr_q = allow_lds(dq), attr_kv = allow_lds(dkv);
+  auto dkv = local_dkv_kernel<T, DHP, kWaves, 1, BIAS>;
+  auto dkv_teams = local_dkv_kernel<T, DHP, kWaves, TL::BR / 32, BIAS>;
+  static hipError_t attr_q = allow_lds(dq), attr_kv = allow_lds(dkv), attr_teams = allow_lds(dkv_teams);
   if (attr_q != hipSuccess) return attr_q;
   if (attr_kv != hipSuccess) return attr_kv;
+  if (attr_teams != hipSuccess) return attr_teams;
   hipLaunchKernelGGL(dq, dim3(a.seqs * a.kv, query_groups(a, stat_rows(a.S))), dim3(64 * kWaves), lds_q, s, p);
   hipError_t e = hipGetLastError();
   if (e != hipSuccess) return e;
-  hipLaunchKernelGGL(dkv, dim3(a.seqs * a.kv, dkv_rows<T>(a)), dim3(64 * kWaves), lds_kv, s, p);
+  const DkvPlan f = dkv_plan<T, DHP>(a);
+  hipLaunchKernelGGL(f.teams == 1 ? dkv : dkv_teams, dim3(a.seqs * a.kv, f.rows), dim3(64 * kWaves), lds_kv, s, p);
   e = hipGetLastError();
-  if (e != hipSuccess || p.far_blocks == 0) return e;
-  const size_t count = (size_t)a.seqs * a.kv * a.sinks * 2 * a.dh;
-  hipLaunchKernelGGL(local_join_kernel<T>, dim3((unsigned)((count + 255) / 256)), dim3(256), 0, s, p.a, p.chunks + 1, count, p.sums, p.dx);
+  const int rows = join_rows(a, f);
+  if (e != hipSuccess || rows == 0) return e;
+  const size_t nz = (size_t)a.seqs * a.kv, quads = nz * rows * 2 * a.dh / 4;
+  hipLaunchKernelGGL(local_join_kernel<T>, dim3((unsigned)((quads + 255) / 256)), dim3(256), 0, s, p.a, f.parts, f.chunks, nz, rows, p.sums, p.dx);
   return hipGetLastError();
 }
 
@@ -1138,9 +1212,9 @@ hipError_t fwd(hipStream_t s, const LocalAttention& a, const T* x, const float* 
 template <typename T>
 hipError_t bwd(hipStream_t s, const LocalAttention& a, const T* x, const T* out, const T* dout, const float* lse, const float* kept, T* dx,
                float* partials, float* scratch) {
-  const FarPlan f = far_plan<T>(a);
+  const DkvPlan f = a.dh <= 64 ? dkv_plan<T, 64>(a) : dkv_plan<T, 128>(a);
   const BwdArgs<T> p{shape_of(a), make_distance_buckets(a.buckets, a.max_distance), a.seqs_per_table, x, out, dout, lse, kept, dx, scratch,
-                     scratch + stat_floats(a), partials, f.blocks, f.chunks, f.chunk_blocks, 1.0f / sqrtf((float)a.dh)};
+                     scratch + stat_floats(a), partials, f.parts, f.far_blocks, f.chunks, f.chunk_blocks, 1.0f / sqrtf((float)a.dh)};
   if (a.dh <= 64) return a.buckets ? run_bwd<T, 64, true>(s, a, p) : run_bwd<T, 64, false>(s, a, p);
   return a.buckets ? run_bwd<T, 128, true>(s, a, p) : run_bwd<T, 128, false>(s, a, p);
 }
@@ -1151,17 +1225,15 @@ bool local_mfma_supported(int elt, const LocalAttention& a) {
   const int es = elt == ELT_BF16 ? 2 : 4;
   const size_t ld = (size_t)(a.heads + 2 * a.kv) * a.dh;
   return a.dh <= 128 && a.dh * es % 16 == 0 && (long)a.seqs * a.kv <= (1 << 22) && 64 * ld * es < (1ull << 31) &&
-         query_groups(a, stat_rows(a.S)) <= 65535 && dkv_rows<uint16_t>(a) <= 65535 && dkv_rows<float>(a) <= 65535;
+         query_groups(a, stat_rows(a.S)) <= 65535 && dkv_plan(elt, a).rows <= 65535;
 }
 
 size_t local_mfma_scratch_bytes(int elt, const LocalAttention& a) {
-  const FarPlan f = elt == ELT_BF16 ? far_plan<uint16_t>(a) : far_plan<float>(a);
-  const size_t sums = f.blocks ? (size_t)(f.chunks + 1) * a.seqs * a.kv * a.sinks * 2 * a.dh : 0;
-  return (stat_floats(a) + sums) * sizeof(float);
+  return (stat_floats(a) + sum_floats(a, dkv_plan(elt, a))) * sizeof(float);
 }
 
 int local_mfma_table_rows(int elt, const LocalAttention& a) {
-  return (int)(a.seqs * (elt == ELT_BF16 ? dkv_rows<uint16_t>(a) : dkv_rows<float>(a)));
+  return a.seqs * dkv_plan(elt, a).rows;
 }
 
 hipError_t local_mfma_fwd(hipStream_t s, int elt, const LocalAttention& a, const void* x, const float* table, float* kept, void* out, void* out2,
