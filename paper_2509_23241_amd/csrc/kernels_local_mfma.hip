@@ -30,6 +30,7 @@ namespace tp {
 
 namespace {
 
+constexpr float kSlack = 8.f;
 constexpr float kLowest = -1e30f;  // running maximum of a row that has seen no key; scores below it are formed again, row by row
 constexpr int kNear = 224;         // distances with a table entry and a sum of their own: 0 .. kNear - 1, and as far as a tile reaches beyond
 constexpr int kPad = 96;           // a tile of 32 x 64 spans 95 distances
@@ -125,9 +126,9 @@ __device__ __forceinline__ int afresh(int v) {
 template <typename T, int DHP>
 constexpr int kBlockRows = DHP * sizeof(T) <= 256 ? 64 : 32;
 
-template <typename T, int DHP, int NW>
+template <typename T, int DHP, int NW, int ROWS = kBlockRows<T, DHP>>
 struct Tile {
-  static constexpr int BR = kBlockRows<T, DHP>, E = sizeof(T);
+  static constexpr int BR = ROWS, E = sizeof(T);
   static constexpr int kPanels = DHP * E / 128, kPanelBytes = BR * 128, kBytes = kPanels * kPanelBytes;
   static constexpr int kPerWave = kBytes / 1024 / NW;  // a wave instruction copies 8 rows of a panel
   // A lane's chunk of copy t lies 32 rows (whose swizzle is the same) or a panel beyond that of copy 0
@@ -437,9 +438,9 @@ struct QueryItems {
 };
 
 template <typename T, int DHP, int NW, bool BIAS>
-__global__ __launch_bounds__(64 * NW, 2) void local_fwd_kernel(FwdArgs<T> p) {
+__global__ __launch_bounds__(64 * NW, sizeof(T) == 2 || DHP == 64 ? 3 : 2) void local_fwd_kernel(FwdArgs<T> p) {
   using TY = Type<T>;
-  using TL = Tile<T, DHP, NW>;
+  using TL = Tile<T, DHP, NW, 32>;
   constexpr int BR = TL::BR, NT = BR / 32, KK = DHP / 16, TN = DHP / 32;
   extern __shared__ __attribute__((aligned(16))) char lds[];
   const Shape& a = p.a;
@@ -517,13 +518,15 @@ __global__ __launch_bounds__(64 * NW, 2) void local_fwd_kernel(FwdArgs<T> p) {
     const bool masked = !(dmin >= 0 && (dmax < a.window || kb + BR <= a.sinks));
     // distance of element r of tile u: d0 - 32 u - 8 (r / 4) - r % 4
     const int d0 = query - kb - 4 * half, sink0 = a.sinks - kb - 4 * half;
-    float mx = mrun;
+    float mx = -INFINITY;
 #pragma unroll
     for (int u = 0; u < NT; ++u) {
-      float bias[16];
-      if constexpr (BIAS) tile_bias<-1>(*bl, TileBuckets(p.db, first, dmin + BR - 32 * (u + 1), dmax - 32 * u), first, d0 - 32 * u, bias);
+      if constexpr (BIAS) {
+        float bias[16];
+        tile_bias<-1>(*bl, TileBuckets(p.db, first, dmin + BR - 32 * (u + 1), dmax - 32 * u), first, d0 - 32 * u, bias);
 #pragma unroll
-      for (int r = 0; r < 16; ++r) sacc[u][r] = BIAS ? fmaf(sacc[u][r], p.scale_log2, bias[r]) : sacc[u][r] * p.scale_log2;
+        for (int r = 0; r < 16; ++r) sacc[u][r] = fmaf(sacc[u][r], p.scale_log2, bias[r]);
+      }
       if (masked) {
 #pragma unroll
         for (int r = 0; r < 16; ++r) {
@@ -534,27 +537,29 @@ __global__ __launch_bounds__(64 * NW, 2) void local_fwd_kernel(FwdArgs<T> p) {
 #pragma unroll
       for (int r = 0; r < 16; ++r) mx = fmaxf(mx, sacc[u][r]);
     }
-    const float mnew = over_halves(mx, Max());
-    const float alpha = __builtin_amdgcn_exp2f(mrun - mnew);
-    mrun = mnew;
-    float psum = 0.f;
+    const float factor = BIAS ? 1.f : p.scale_log2;  // what turns sacc into scores
+    const float mnew = over_halves(mx, Max()) * factor;
+    // A row's reference need not be its maximum: while no score lies above it by more than kSlack, the exponentials stay below 2^kSlack and
+    // nothing is rescaled.  (Some row's maximum of 32 moves in nearly every block.)
+    if (__builtin_amdgcn_ballot_w64(mnew > mrun + kSlack) != 0) {
+      const float m = fmaxf(mrun, mnew), alpha = __builtin_amdgcn_exp2f(mrun - m);
+      mrun = m;
+      lsum *= alpha;
+#pragma unroll
+      for (int j = 0; j < TN; ++j)
+#pragma unroll
+        for (int r = 0; r < 16; ++r) oacc[j][r] *= alpha;
+    }
     typename TY::Frag pf[2 * NT];
 #pragma unroll
     for (int g = 0; g < 2 * NT; ++g) {
       float e[8];
 #pragma unroll
       for (int r = 0; r < 8; ++r) {
-        e[r] = __builtin_amdgcn_exp2f(sacc[g >> 1][8 * (g & 1) + r] - mnew);
-        psum += e[r];
+        e[r] = __builtin_amdgcn_exp2f(fmaf(sacc[g >> 1][8 * (g & 1) + r], factor, -mrun));
+        lsum += e[r];
       }
       pf[g] = TY::pack(e);
-    }
-    lsum = fmaf(lsum, alpha, psum);
-    if (__builtin_amdgcn_ballot_w64(alpha != 1.f) != 0) {  // some row's maximum moved
-#pragma unroll
-      for (int j = 0; j < TN; ++j)
-#pragma unroll
-        for (int r = 0; r < 16; ++r) oacc[j][r] *= alpha;
     }
     pipelined<2 * NT * TN>(ahead, v_frag, [&](int i, const typename TY::Frag& f) { oacc[i % TN] = TY::mma(f, pf[i / TN], oacc[i % TN]); }, true);
   }
@@ -1167,7 +1172,7 @@ hipError_t allow_lds(Kernel kernel) {
 
 template <typename T, int DHP, bool BIAS>
 hipError_t run_fwd(hipStream_t s, const LocalAttention& a, const FwdArgs<T>& p) {
-  using TL = Tile<T, DHP, kWaves>;
+  using TL = Tile<T, DHP, kWaves, 32>;
   constexpr size_t lds = std::max<size_t>(4 * TL::kBytes, kWaves * kTurnBytes) + bias_lds<kWaves>(BIAS);
   auto kernel = local_fwd_kernel<T, DHP, kWaves, BIAS>;
   static hipError_t attr = allow_lds(kernel);
