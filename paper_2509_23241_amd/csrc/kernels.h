@@ -95,9 +95,6 @@ hipError_t launch_copy(hipStream_t s, const void* src, void* dst, size_t bytes);
 hipError_t launch_softmax_ce(hipStream_t s, int elt, int rows, int classes, const void* logits,
                              const int32_t* labels, void* dlogits, float* row_loss, uint32_t* counter, float* loss);
 
-// *out = mean of `count` values, added up in fp64.
-hipError_t launch_mean(hipStream_t s, const float* values, int count, float* out);
-
 // fp32 -> elt conversion of `count` elements (compute copy of a weight version).
 hipError_t launch_convert(hipStream_t s, int elt, size_t count, const float* src, void* dst);
 

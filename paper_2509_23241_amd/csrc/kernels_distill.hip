@@ -19,94 +19,136 @@ namespace tp {
 
 namespace {
 
-constexpr int kThreads = 256;
-constexpr float kLog2e = 1.4426950408889634f;
+constexpr float kLog2e = 1.4426950408889634f, kLn2 = 0.6931471805599453f;
 
-template <int NT, class Op>
-__device__ __forceinline__ float over_block(float v, float* sm, const Op& op) {  // sm: NT / 64 floats, free on both sides
-  v = over_lanes<32>(v, op);
-  if constexpr (NT > 64) {
-    if ((threadIdx.x & 63) == 0) sm[threadIdx.x >> 6] = v;
-    __syncthreads();
-    v = sm[0];
-#pragma unroll
-    for (int i = 1; i < NT / 64; ++i) v = op(v, sm[i]);
-    __syncthreads();
+// The threads of a row: a wave, or a whole workgroup.
+template <int NT>
+struct Team {
+  static constexpr int kRows = NT == 64 ? 4 : 1;         // rows of a workgroup
+  static constexpr int kThreads = NT == 64 ? 256 : NT;
+  static __device__ __forceinline__ int thread() { return NT == 64 ? threadIdx.x & 63 : threadIdx.x; }
+  static __device__ __forceinline__ int which() { return NT == 64 ? threadIdx.x >> 6 : 0; }
+  // what the others have written to LDS and memory is there
+  static __device__ __forceinline__ void sync() {
+    if constexpr (NT == 64) {
+      __builtin_amdgcn_fence(__ATOMIC_RELEASE, "wavefront");
+      __builtin_amdgcn_wave_barrier();
+      __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "wavefront");
+    } else {
+      __syncthreads();
+    }
   }
-  return v;
+  // sm: NT / 64 floats, free on both sides
+  template <class Op>
+  static __device__ __forceinline__ float over(float v, float* sm, const Op& op) {
+    v = over_lanes<32>(v, op);
+    if constexpr (NT > 64) {
+      if ((threadIdx.x & 63) == 0) sm[threadIdx.x >> 6] = v;
+      __syncthreads();
+      v = sm[0];
+#pragma unroll
+      for (int i = 1; i < NT / 64; ++i) v = op(v, sm[i]);
+      __syncthreads();
+    }
+    return v;
+  }
+};
+
+// Exponents: exp(x / T) = 2^(x c), with everything relative to the row's maximum, 2^(x c - top c).  top c is rounded once and enters
+// numerators, sums and logarithms alike, so that its rounding cancels.
+struct Scale {
+  float soft, hard;  // c for 1 / T and for 1
+  __device__ __forceinline__ explicit Scale(const DistillArgs& a) : soft(kLog2e / a.temperature), hard(kLog2e) {}
+};
+struct Row {
+  float top_soft, top_hard;  // the maximum times the scales
+  float soft, hard;          // what 2^(x c - top c) is multiplied with in the gradient
+};
+__device__ __forceinline__ float gradient(const Row& r, const Scale& c, float z) {
+  float g = r.soft == 0.f ? 0.f : r.soft * __builtin_amdgcn_exp2f(fmaf(z, c.soft, -r.top_soft));
+  if (r.hard != 0.f) g = fmaf(r.hard, __builtin_amdgcn_exp2f(fmaf(z, c.hard, -r.top_hard)), g);
+  return g;
 }
 
-// What a row's sums come to, and the terms of its loss and gradient that belong to single classes
-struct Row {
-  float top;           // max z
-  float hard, soft;    // what exp(z - top) and exp((z - top) / T) are multiplied with in the gradient
+// A thread's first entry and the row's label, fetched in two steps: the classes ahead of the row, their logits behind it, so that neither is
+// waited for by itself.
+struct First {
+  int id = -1, label = -1;
+  float teacher = 0.f, z = 0.f, z_label = 0.f;
+  __device__ __forceinline__ First(const DistillArgs& a, int row, int thread) {
+    if (thread < a.k) {
+      id = a.ids[(size_t)row * a.k + thread];
+      teacher = a.teacher[(size_t)row * a.k + thread];
+    }
+    if (a.label_weight > 0.f) label = a.labels[row];
+  }
+  template <typename T>
+  __device__ __forceinline__ void logits(const DistillArgs& a, const T* lg) {
+    if ((unsigned)id < (unsigned)a.classes) z = to_float(lg[id]);
+    if ((unsigned)label < (unsigned)a.classes) z_label = to_float(lg[label]);
+  }
 };
 
 // The stored entries and the label, behind the row's maximum and sums.  share[e] (LDS): what entry e takes off the gradient of its
-// class, e = k for the label; id[e]: its class, -1 none.  Returns the row's loss in every thread of the block.
+// class, e = k for the label; id[e]: its class, -1 none.  Completes r and returns the row's loss in every thread.
 template <int NT, typename T>
-__device__ __forceinline__ float entries(const DistillArgs& a, int row, const T* lg, float top, float sum_hard, float sum_soft, float* sm,
-                                         float* share, int* id, Row* r) {
-  const float inv_t = 1.f / a.temperature, inv_rows = 1.f / (float)a.rows;
+__device__ __forceinline__ float entries(const DistillArgs& a, const Scale& c, int row, const T* lg, const First& f, float sum_hard, float sum_soft,
+                                         float* sm, float* share, int* id, Row* r) {
+  using TM = Team<NT>;
+  const int thread = TM::thread();
+  const float inv_rows = 1.f / (float)a.rows;
   const float* t = a.teacher + (size_t)row * a.k;
   const int32_t* ids = a.ids + (size_t)row * a.k;
   float tm = -INFINITY;
-  for (int e = threadIdx.x; e < a.k; e += NT) {
-    id[e] = ids[e] < 0 ? -1 : ids[e];
-    share[e] = ids[e] < 0 ? -INFINITY : t[e];
+  for (int e = thread; e < a.k; e += NT) {
+    const int mine = e == thread ? f.id : ids[e];
+    id[e] = mine < 0 ? -1 : mine;
+    share[e] = mine < 0 ? -INFINITY : e == thread ? f.teacher : t[e];
     tm = fmaxf(tm, share[e] == share[e] ? share[e] : INFINITY);  // a NaN is an entry, too, and makes the sum NaN
   }
-  tm = over_block<NT>(tm, sm, Max());
+  tm = TM::over(tm, sm, Max());
   const bool has = tm != -INFINITY && a.label_weight < 1.f;
   float total = 0.f;
-  for (int e = threadIdx.x; e < a.k; e += NT) total += has ? expf((share[e] - tm) * inv_t) : 0.f;
-  total = over_block<NT>(total, sm, Add());
-  const float log_total = logf(total), log_soft = logf(sum_soft);
-  const float c = (1.f - a.label_weight) * a.temperature * inv_rows;
+  for (int e = thread; e < a.k; e += NT) total += has ? __builtin_amdgcn_exp2f((share[e] - tm) * c.soft) : 0.f;
+  total = TM::over(total, sm, Add());
+  const float log_total = __builtin_amdgcn_logf(total), log_soft = __builtin_amdgcn_logf(sum_soft);  // base 2
+  const float weight = (1.f - a.label_weight) * a.temperature * inv_rows;
   float kl = 0.f;
-  for (int e = threadIdx.x; e < a.k; e += NT) {
-    const float log_p = has ? (share[e] - tm) * inv_t - log_total : -INFINITY;
-    const float p = has ? expf(log_p) : 0.f;
-    share[e] = c * p;
+  for (int e = thread; e < a.k; e += NT) {
+    const float log_p = has ? (share[e] - tm) * c.soft - log_total : -INFINITY;
+    const float p = has ? __builtin_amdgcn_exp2f(log_p) : 0.f;
+    share[e] = weight * p;
     if (id[e] >= a.classes) {
       kl = __builtin_nanf("");  // a class that does not exist: the loss says so
       id[e] = -1;
     } else if (id[e] >= 0 && p != 0.f) {
-      kl += p * (log_p - ((to_float(lg[id[e]]) - top) * inv_t - log_soft));
+      const float z = e == thread ? f.z : to_float(lg[id[e]]);
+      kl += p * (log_p - (fmaf(z, c.soft, -r->top_soft) - log_soft));
     }
   }
-  kl = over_block<NT>(kl, sm, Add());
+  kl = TM::over(kl, sm, Add()) * kLn2;
   float loss = a.label_weight < 1.f ? (1.f - a.label_weight) * a.temperature * a.temperature * kl : 0.f;
   if (a.label_weight > 0.f) {
-    const int label = a.labels[row];
-    const bool known = (unsigned)label < (unsigned)a.classes;
-    loss += a.label_weight * (known ? logf(sum_hard) - (to_float(lg[label]) - top) : __builtin_nanf(""));
-    if (threadIdx.x == 0) {
-      id[a.k] = known ? label : -1;
+    const bool known = (unsigned)f.label < (unsigned)a.classes;
+    const float ce = known ? __builtin_amdgcn_logf(sum_hard) - fmaf(f.z_label, c.hard, -r->top_hard) : __builtin_nanf("");
+    loss += a.label_weight * kLn2 * ce;
+    if (thread == 0) {
+      id[a.k] = known ? f.label : -1;
       share[a.k] = a.label_weight * inv_rows;
     }
-  } else if (threadIdx.x == 0) {
+  } else if (thread == 0) {
     id[a.k] = -1;
   }
-  r->top = top;
   r->hard = a.label_weight > 0.f ? a.label_weight * inv_rows / sum_hard : 0.f;
-  r->soft = has ? c / sum_soft : 0.f;
+  r->soft = has ? weight / sum_soft : 0.f;
   return loss;
-}
-
-__device__ __forceinline__ float gradient(const Row& r, float z, float inv_t_log2, bool labels) {
-  const float x = z - r.top;
-  float g = r.soft * __builtin_amdgcn_exp2f(x * inv_t_log2);
-  if (labels) g = fmaf(r.hard, __builtin_amdgcn_exp2f(x * kLog2e), g);
-  return g;
 }
 
 // The gradient of the entries' classes, behind the stores of the others: the first entry of a class takes off what all of it do.
 template <int NT, typename T>
-__device__ __forceinline__ void finish_entries(const DistillArgs& a, const T* lg, T* dl, const Row& r, float inv_t_log2, const float* share,
+__device__ __forceinline__ void finish_entries(const DistillArgs& a, const Scale& c, const T* lg, T* dl, const Row& r, const float* share,
                                                const int* id) {
-  const bool labels = a.label_weight > 0.f;
-  for (int e = threadIdx.x; e <= a.k; e += NT) {
+  for (int e = Team<NT>::thread(); e <= a.k; e += NT) {
     const int mine = id[e];
     if (mine < 0) continue;
     float off = 0.f;
@@ -116,54 +158,268 @@ __device__ __forceinline__ void finish_entries(const DistillArgs& a, const T* lg
         first = first && f >= e;
         off += share[f];
       }
-    if (first) dl[mine] = from_float<T>(gradient(r, to_float(lg[mine]), inv_t_log2, labels) - off);
+    if (first) dl[mine] = from_float<T>(gradient(r, c, to_float(lg[mine])) - off);
   }
 }
 
-// A workgroup per row, which is read three times.
+// The mean of the row losses by the workgroup that arrives last, where a counter is given.
+__device__ __forceinline__ void finish_mean(const DistillArgs& a) {
+  __shared__ double sums[256];
+  __shared__ int finishes;
+  if (!a.counter) return;
+  asm volatile("s_waitcnt vmcnt(0)" ::: "memory");  // this wave's row losses have arrived
+  __syncthreads();
+  if (threadIdx.x == 0) finishes = last_to_arrive(a.counter, gridDim.x);
+  __syncthreads();
+  if (!finishes) return;
+  if (threadIdx.x < 256) {
+    double s = 0.0;
+    for (int i = threadIdx.x; i < a.rows; i += 256) s += (double)published(a.row_loss + i);
+    sums[threadIdx.x] = s;
+  }
+  __syncthreads();
+  for (int w = 128; w > 0; w >>= 1) {
+    if ((int)threadIdx.x < w) sums[threadIdx.x] += sums[threadIdx.x + w];
+    __syncthreads();
+  }
+  if (threadIdx.x == 0) *a.loss = (float)(sums[0] / (double)a.rows);
+}
+
+template <typename T>
+constexpr int kVec = 16 / sizeof(T);  // values of a 16-byte unit
+template <typename T>
+__device__ __forceinline__ void unpack(const uint4& u, float (&v)[kVec<T>]) {
+  const uint32_t w[4] = {u.x, u.y, u.z, u.w};
+#pragma unroll
+  for (int i = 0; i < 4; ++i) {
+    if constexpr (sizeof(T) == 2) {
+      v[2 * i] = __uint_as_float(w[i] << 16);
+      v[2 * i + 1] = __uint_as_float(w[i] & 0xffff0000u);
+    } else {
+      v[i] = __uint_as_float(w[i]);
+    }
+  }
+}
+template <typename T>
+__device__ __forceinline__ uint4 pack(const float (&v)[kVec<T>]) {
+  if constexpr (sizeof(T) == 2)
+    return make_uint4(pack_bf16x2(v[0], v[1]), pack_bf16x2(v[2], v[3]), pack_bf16x2(v[4], v[5]), pack_bf16x2(v[6], v[7]));
+  else
+    return make_uint4(__float_as_uint(v[0]), __float_as_uint(v[1]), __float_as_uint(v[2]), __float_as_uint(v[3]));
+}
+
+// Which exponentials a row needs.  kOne: of one scale (the teacher or the labels alone, or a temperature of 1); kSquare: the temperature
+// is 2, so that exp(x) is the square of exp(x / 2); kTwo: both.  An exponential costs a wave 16 cycles, any other instruction here 4.
+enum Exponentials : int { kOne = 0, kSquare = 1, kTwo = 2 };
+
+// A row is read once and held in registers, from the second step on as its exponentials: HELD units of 16 bytes for each of its NT threads.
+// Rows may start at any element: units lie at 16-byte addresses, and the first and last, which other rows share, are read and written one
+// by one.  Reading and writing at the rate of a copy is the floor; what comes near it is instructions, 12 for a logit with kSquare (29
+// with both exponentials formed twice, before they were held).
+template <typename T, int NT, int HELD, int EXPS>
+__global__ __launch_bounds__(Team<NT>::kThreads, HELD * kVec<T> == 64 && EXPS != kTwo ? 4 : 1) void distill_held_kernel(DistillArgs a) {
+  using TM = Team<NT>;
+  constexpr int V = kVec<T>;
+  __shared__ float sm_all[TM::kThreads / 64];
+  extern __shared__ float entry_lds[];  // for each row [k + 1] shares, [k + 1] classes
+  const int thread = TM::thread(), row = blockIdx.x * TM::kRows + TM::which();
+  float* sm = sm_all;
+  float* share = entry_lds + TM::which() * 2 * (a.k + 1);
+  int* id = reinterpret_cast<int*>(share + a.k + 1);
+  const Scale c(a);
+  if (row < a.rows) {
+    const T* lg = (const T*)a.logits + (size_t)row * a.classes;
+    T* dl = (T*)a.dlogits + (size_t)row * a.classes;
+    const int lead = (int)((uintptr_t)lg % 16 / sizeof(T));  // values of the first unit that are another row's
+    const int whole_from = lead > 0, whole_to = (lead + a.classes) / V;  // units that are this row's alone
+    const int units = (lead + a.classes + V - 1) / V;
+    const T* unit0 = lg - lead;
+    First entry(a, row, thread);
+    uint4 raw[HELD];
+#pragma unroll
+    for (int i = 0; i < HELD; ++i) {
+      const int u = min(max(thread + NT * i, whole_from), whole_to - 1);
+      raw[i] = *reinterpret_cast<const uint4*>(unit0 + (size_t)u * V);
+    }
+    entry.logits(a, lg);
+    float x[HELD][V];
+#pragma unroll
+    for (int i = 0; i < HELD; ++i) {
+      const int u = thread + NT * i;
+      unpack<T>(raw[i], x[i]);
+      if (u < whole_from || u >= whole_to) {
+#pragma unroll
+        for (int e = 0; e < V; ++e) {
+          const int j = u * V + e - lead;
+          x[i][e] = u < units && j >= 0 && j < a.classes ? to_float(lg[j]) : -INFINITY;
+        }
+      }
+    }
+    float top = -INFINITY;
+#pragma unroll
+    for (int i = 0; i < HELD; ++i)
+#pragma unroll
+      for (int e = 0; e < V; ++e) top = fmaxf(top, x[i][e]);
+    top = TM::over(top, sm, Max());
+    Row r;
+    r.top_soft = top * c.soft;
+    r.top_hard = EXPS == kSquare ? 2.f * r.top_soft : top * c.hard;
+    // with one exponential it is that of the only scale
+    const bool only_hard = EXPS == kOne && a.label_weight >= 1.f;
+    const float scale = only_hard ? c.hard : c.soft, shift = only_hard ? r.top_hard : r.top_soft;
+    float other[EXPS == kTwo ? HELD : 1][V];
+    float soft = 0.f, hard = 0.f;
+#pragma unroll
+    for (int i = 0; i < HELD; ++i)
+#pragma unroll
+      for (int e = 0; e < V; ++e) {
+        if constexpr (EXPS == kTwo) {
+          other[i][e] = __builtin_amdgcn_exp2f(fmaf(x[i][e], c.hard, -r.top_hard));
+          hard += other[i][e];
+        }
+        x[i][e] = __builtin_amdgcn_exp2f(fmaf(x[i][e], scale, -shift));
+        soft += x[i][e];
+        if constexpr (EXPS == kSquare) hard = fmaf(x[i][e], x[i][e], hard);
+      }
+    soft = TM::over(soft, sm, Add());
+    hard = EXPS == kOne ? soft : TM::over(hard, sm, Add());
+    const float loss = entries<NT>(a, c, row, lg, entry, hard, soft, sm, share, id, &r);
+    if (thread == 0) publish(a.row_loss + row, loss);
+    const float one = r.soft + r.hard;  // kOne: both are of the same exponential
+#pragma unroll
+    for (int i = 0; i < HELD; ++i) {
+      const int u = thread + NT * i;
+#pragma unroll
+      for (int e = 0; e < V; ++e) {
+        if constexpr (EXPS == kOne) x[i][e] *= one;
+        else if constexpr (EXPS == kSquare) x[i][e] *= fmaf(r.hard, x[i][e], r.soft);
+        else x[i][e] = fmaf(r.hard, other[i][e], r.soft * x[i][e]);
+      }
+      if (u >= whole_from && u < whole_to) {
+        *reinterpret_cast<uint4*>(dl - lead + (size_t)u * V) = pack<T>(x[i]);
+      } else if (u < units) {
+#pragma unroll
+        for (int e = 0; e < V; ++e) {
+          const int j = u * V + e - lead;
+          if (j >= 0 && j < a.classes) dl[j] = from_float<T>(x[i][e]);
+        }
+      }
+    }
+    asm volatile("s_waitcnt vmcnt(0)" ::: "memory");  // the row is stored before single values of it are replaced
+    TM::sync();
+    finish_entries<NT>(a, c, lg, dl, r, share, id);
+  }
+  finish_mean(a);
+}
+
+// Any row, read three times by a workgroup of its own.
+constexpr int kThreads = 256;
 template <typename T>
 __global__ __launch_bounds__(kThreads) void distill_rows_kernel(DistillArgs a) {
   __shared__ float sm[kThreads / 64];
-  extern __shared__ float entry_lds[];  // [k + 1] shares, [k + 1] classes
+  extern __shared__ float entry_lds[];
   float* share = entry_lds;
   int* id = reinterpret_cast<int*>(share + a.k + 1);
-  const float inv_t_log2 = kLog2e / a.temperature;
+  const Scale c(a);
   const bool labels = a.label_weight > 0.f;
   for (int row = blockIdx.x; row < a.rows; row += gridDim.x) {
     const T* lg = (const T*)a.logits + (size_t)row * a.classes;
     T* dl = (T*)a.dlogits + (size_t)row * a.classes;
+    First entry(a, row, threadIdx.x);
+    entry.logits(a, lg);
     float top = -INFINITY;
     for (int j = threadIdx.x; j < a.classes; j += kThreads) top = fmaxf(top, to_float(lg[j]));
-    top = over_block<kThreads>(top, sm, Max());
+    top = Team<kThreads>::over(top, sm, Max());
+    Row r;
+    r.top_soft = top * c.soft;
+    r.top_hard = top * c.hard;
     float hard = 0.f, soft = 0.f;
     for (int j = threadIdx.x; j < a.classes; j += kThreads) {
-      const float x = to_float(lg[j]) - top;
-      soft += __builtin_amdgcn_exp2f(x * inv_t_log2);
-      if (labels) hard += __builtin_amdgcn_exp2f(x * kLog2e);
+      const float z = to_float(lg[j]);
+      soft += __builtin_amdgcn_exp2f(fmaf(z, c.soft, -r.top_soft));
+      if (labels) hard += __builtin_amdgcn_exp2f(fmaf(z, c.hard, -r.top_hard));
     }
-    soft = over_block<kThreads>(soft, sm, Add());
-    if (labels) hard = over_block<kThreads>(hard, sm, Add());
-    Row r;
-    const float loss = entries<kThreads>(a, row, lg, top, hard, soft, sm, share, id, &r);
+    soft = Team<kThreads>::over(soft, sm, Add());
+    if (labels) hard = Team<kThreads>::over(hard, sm, Add());
+    const float loss = entries<kThreads>(a, c, row, lg, entry, hard, soft, sm, share, id, &r);
     if (threadIdx.x == 0) publish(a.row_loss + row, loss);
-    for (int j = threadIdx.x; j < a.classes; j += kThreads) dl[j] = from_float<T>(gradient(r, to_float(lg[j]), inv_t_log2, labels));
+    for (int j = threadIdx.x; j < a.classes; j += kThreads) dl[j] = from_float<T>(gradient(r, c, to_float(lg[j])));
     asm volatile("s_waitcnt vmcnt(0)" ::: "memory");  // the row is stored before single values of it are replaced
     __syncthreads();
-    finish_entries<kThreads>(a, lg, dl, r, inv_t_log2, share, id);
+    finish_entries<kThreads>(a, c, lg, dl, r, share, id);
     __syncthreads();  // the entries' LDS is free
   }
+  finish_mean(a);
+}
+
+constexpr int kCounted = 128;  // workgroups up to which the last of them forms the mean; more take a launch of its own
+constexpr int kMeanThreads = 1024;
+__global__ __launch_bounds__(kMeanThreads) void distill_mean_kernel(const float* __restrict__ row_loss, int rows, float* __restrict__ loss) {
+  __shared__ double sums[kMeanThreads / 64];
+  double s = 0.0;
+  int i = threadIdx.x;
+  for (; i + 7 * kMeanThreads < rows; i += 8 * kMeanThreads) {  // eight loads on their way
+    float v[8];
+#pragma unroll
+    for (int u = 0; u < 8; ++u) v[u] = row_loss[i + u * kMeanThreads];
+#pragma unroll
+    for (int u = 0; u < 8; ++u) s += (double)v[u];
+  }
+  for (; i < rows; i += kMeanThreads) s += (double)row_loss[i];
+#pragma unroll
+  for (int off = 32; off > 0; off >>= 1) s += __shfl_xor(s, off, 64);
+  if ((threadIdx.x & 63) == 0) sums[threadIdx.x >> 6] = s;
+  __syncthreads();
+  if (threadIdx.x == 0) {
+    s = 0.0;
+    for (int w = 0; w < kMeanThreads / 64; ++w) s += sums[w];
+    *loss = (float)(s / (double)rows);
+  }
+}
+hipError_t finish(hipStream_t s, const DistillArgs& a) {
+  const hipError_t e = hipGetLastError();
+  if (e != hipSuccess || a.counter) return e;
+  hipLaunchKernelGGL(distill_mean_kernel, dim3(1), dim3(kMeanThreads), 0, s, a.row_loss, a.rows, a.loss);
+  return hipGetLastError();
+}
+
+template <typename T, int NT, int HELD>
+hipError_t launch_held(hipStream_t s, DistillArgs a) {
+  using TM = Team<NT>;
+  const unsigned blocks = (unsigned)((a.rows + TM::kRows - 1) / TM::kRows);
+  if (blocks > kCounted) a.counter = nullptr;
+  const size_t lds = (size_t)TM::kRows * 2 * (a.k + 1) * sizeof(float);
+  const bool one = a.label_weight <= 0.f || a.label_weight >= 1.f || a.temperature == 1.f;
+  auto kernel = one ? distill_held_kernel<T, NT, HELD, kOne>
+                    : a.temperature == 2.f ? distill_held_kernel<T, NT, HELD, kSquare> : distill_held_kernel<T, NT, HELD, kTwo>;
+  hipLaunchKernelGGL(kernel, dim3(blocks), dim3(TM::kThreads), lds, s, a);
+  return finish(s, a);
+}
+
+template <typename T>
+hipError_t launch(hipStream_t s, DistillArgs a) {
+  constexpr int V = kVec<T>;
+  const long units = a.classes / V + 2;  // with a first and a last one that are shared
+  // whole units to hold, and rows that start at the same place in a unit on both sides
+  if (a.classes >= 2 * V && ((uintptr_t)a.logits - (uintptr_t)a.dlogits) % 16 == 0) {
+    constexpr int W = 64 / V;  // units of 64 values
+    if (units <= 64) return launch_held<T, 64, 1>(s, a);
+    if (units <= 64 * 2) return launch_held<T, 64, 2>(s, a);
+    if (units <= 256) return launch_held<T, 256, 1>(s, a);
+    if (units <= 256 * W / 4) return launch_held<T, 256, W / 4>(s, a);
+    if (units <= 256 * W / 2) return launch_held<T, 256, W / 2>(s, a);
+    if (units <= 256 * W) return launch_held<T, 256, W>(s, a);
+    if (units <= 512 * W) return launch_held<T, 512, W>(s, a);
+    if (units <= 1024 * W) return launch_held<T, 1024, W>(s, a);
+  }
+  const int blocks = std::min(a.rows, 1 << 20);
+  if (blocks > kCounted) a.counter = nullptr;
+  hipLaunchKernelGGL(distill_rows_kernel<T>, dim3(blocks), dim3(kThreads), (size_t)2 * (a.k + 1) * sizeof(float), s, a);
+  return finish(s, a);
 }
 
 }  // namespace
 
-hipError_t launch_distill(hipStream_t s, int elt, const DistillArgs& a) {
-  const size_t lds = (size_t)2 * (a.k + 1) * sizeof(float);
-  const int blocks = std::min(a.rows, 1 << 20);
-  if (elt == ELT_BF16) hipLaunchKernelGGL(distill_rows_kernel<uint16_t>, dim3(blocks), dim3(kThreads), lds, s, a);
-  else hipLaunchKernelGGL(distill_rows_kernel<float>, dim3(blocks), dim3(kThreads), lds, s, a);
-  const hipError_t e = hipGetLastError();
-  if (e != hipSuccess) return e;
-  return launch_mean(s, a.row_loss, a.rows, a.loss);
-}
+hipError_t launch_distill(hipStream_t s, int elt, const DistillArgs& a) { return elt == ELT_BF16 ? launch<uint16_t>(s, a) : launch<float>(s, a); }
 
 }  // namespace tp

@@ -502,11 +502,7 @@ hipError_t launch_softmax_ce(hipStream_t s, int elt, int rows, int classes, cons
   else typed((float*)dlogits);
   const hipError_t e = hipGetLastError();
   if (e != hipSuccess || counter) return e;
-  return launch_mean(s, row_loss, rows, loss);
-}
-
-hipError_t launch_mean(hipStream_t s, const float* values, int count, float* out) {
-  hipLaunchKernelGGL(mean_kernel, dim3(1), dim3(kThreads), 0, s, values, count, out);
+  hipLaunchKernelGGL(mean_kernel, dim3(1), dim3(kThreads), 0, s, row_loss, rows, loss);
   return hipGetLastError();
 }
 
