@@ -1130,27 +1130,44 @@ struct DkvPlan {
 };
 template <typename T, int DHP>
 DkvPlan dkv_plan(const LocalAttention& a) {
-  DkvPlan f;
   constexpr int BR = kBlockRows<T, DHP>;
+  constexpr double kSlots = 512;  // workgroups the chip runs at a time, two on a CU
   const long nz = (long)a.seqs * a.kv, group = a.heads / a.kv;
-  constexpr long kEnough = 512;  // workgroups that fill the chip, two on a CU
-  if (BR == 64 && nz * ((a.S + 127) / 128) < kEnough) f.teams = 2;
-  const int own = 128 / f.teams, blocks = (a.S + own - 1) / own;
-  // fewer even so: the walks in parts, of four steps at least, since a part leaves its sums in memory to be joined
-  const long steps = (std::min<long>(a.S, (long)own + a.window) + BR - 1) / BR * group;
-  f.parts = (int)std::max<long>(1, std::min({(kEnough + nz * blocks - 1) / (nz * blocks), steps / 4, 16l}));
-  if (a.sinks > 0 && a.window < a.S) {
-    f.far_blocks = (a.sinks + own - 1) / own;
-    const int total = (a.S + BR - 1) / BR - a.window / BR;  // streamed blocks that far pairs of the first keys lie in
-    // a range is about as long as what the other workgroups walk over; no more of them than give every CU four, since each leaves its sums
-    // in memory
-    const int walk = std::max<int>(4, (a.window + own) / BR / f.parts);
-    const long most = std::max<long>(1, 1024 / (nz * f.far_blocks));
-    f.chunks = (int)std::min<long>(most, (total + walk - 1) / walk);
-    f.chunk_blocks = (total + f.chunks - 1) / f.chunks;
+  const bool causal = a.window >= a.S;
+  DkvPlan best;
+  double best_time = 0;
+  for (int teams = 1; teams <= BR / 32; ++teams) {
+    const int own = 128 / teams, blocks = (a.S + own - 1) / own;
+    // Times in steps of a workgroup whose waves each take whole blocks (about 2.6 us for 128-wide heads); starting and ending one cost
+    // three, and a step of two teams 0.6.
+    const double walk = (double)((std::min<long>(a.S, (long)own + a.window) + BR - 1) / BR * group), step = teams == 1 ? 1.0 : 0.6;
+    for (int parts = 1; parts <= 16 && (parts == 1 || walk >= 4 * parts); ++parts) {
+      DkvPlan f;
+      f.teams = teams;
+      f.parts = parts;
+      if (a.sinks > 0 && !causal) {
+        f.far_blocks = (a.sinks + own - 1) / own;
+        const int total = (a.S + BR - 1) / BR - a.window / BR;  // streamed blocks that far pairs of the first keys lie in
+        // a range is about as long as what the other workgroups walk over; no more of them than give every CU four, since each leaves
+        // its sums in memory
+        const int length = std::max(4, (a.window + own) / BR / parts);
+        const long most = std::max<long>(1, 1024 / (nz * f.far_blocks));
+        f.chunks = (int)std::min<long>(most, (total + length - 1) / length);
+        f.chunk_blocks = (total + f.chunks - 1) / f.chunks;
+      }
+      f.rows = blocks * parts + f.far_blocks * f.chunks;
+      const double one = 3 + step * std::max(walk / parts, (double)f.chunk_blocks * group), all = (double)nz * f.rows;
+      // equal walks run in rounds; those of a causal triangle, the longest first, fill one another's gaps
+      double time = causal ? std::max(one, all * (3 + step * walk / parts / 2) / kSlots) : std::ceil(all / kSlots) * one;
+      // parts meet in memory: written and read at some 4 TB/s, and a launch
+      if (parts > 1) time += 1 + (double)parts * nz * a.S * 2 * a.dh * 8 / 4e12 / (2.6e-6 * DHP / 128);
+      if (best.rows == 0 || time < best_time) {
+        best = f;
+        best_time = time;
+      }
+    }
   }
-  f.rows = blocks * f.parts + f.far_blocks * f.chunks;
-  return f;
+  return best;
 }
 inline DkvPlan dkv_plan(int elt, const LocalAttention& a) {
   if (elt == ELT_BF16) return a.dh <= 64 ? dkv_plan<uint16_t, 64>(a) : dkv_plan<uint16_t, 128>(a);
