@@ -531,7 +531,7 @@ __global__ __launch_bounds__(64 * NW, sizeof(T) == 2 || DHP == 64 ? 3 : 2) void 
 #pragma unroll
         for (int r = 0; r < 16; ++r) {
           const int at = 32 * u + 8 * (r >> 2) + (r & 3);
-          sacc[u][r] = at <= d0 && (at > d0 - a.window || at < sink0) ? sacc[u][r] : -INFINITY;
+          sacc[u][r] = (at <= d0) & ((at > d0 - a.window) | (at < sink0)) ? sacc[u][r] : -INFINITY;
         }
       }
 #pragma unroll
@@ -683,11 +683,13 @@ __global__ __launch_bounds__(64 * NW, sizeof(T) == 2 || DHP == 64 ? 2 : 1) void 
     const int kb = it.block(t) * BR;
     if (!active || qw >= S || kb > q_last || (kb >= a.sinks && kb + BR - 1 <= qw - a.window)) continue;
     const uint32_t stage = lds0 + (t & 1) * 2 * TL::kBytes, lk = stage + row_at, lkc = stage + col_at;
-    const int dmin = qw - (kb + BR - 1), dmax = qw + 31 - kb;
-    const bool masked = !(dmin >= 0 && (dmax < a.window || kb + BR <= a.sinks));
     const int d0 = query - kb - 4 * half, sink0 = a.sinks - kb - 4 * half;
 #pragma unroll
     for (int u = 0; u < NT; ++u) {
+      // the tile's smallest and largest distance; wave uniform
+      const int k0 = kb + 32 * u, dmin = qw - (k0 + 31), dmax = qw + 31 - k0;
+      if (dmax < 0 || (dmin >= a.window && k0 >= a.sinks)) continue;
+      const bool masked = !(dmin >= 0 && (dmax < a.window || k0 + 32 <= a.sinks));
       floatx16 sacc, pacc;
 #pragma unroll
       for (int r = 0; r < 16; ++r) sacc[r] = pacc[r] = 0.f;
@@ -705,13 +707,13 @@ __global__ __launch_bounds__(64 * NW, sizeof(T) == 2 || DHP == 64 ? 2 : 1) void 
 #pragma unroll
         for (int r = 0; r < 16; ++r) {
           const int at = 32 * u + 8 * (r >> 2) + (r & 3);
-          const bool sees = at <= d0 && (at > d0 - a.window || at < sink0);
+          const bool sees = (at <= d0) & ((at > d0 - a.window) | (at < sink0));  // without branches
           sacc[r] = sees ? sacc[r] : -INFINITY;
           pacc[r] = sees ? pacc[r] : delta;
         }
       }
       float bias[16];
-      if constexpr (BIAS) tile_bias<-1>(*bl, TileBuckets(p.db, first, dmin + BR - 32 * (u + 1), dmax - 32 * u), first, d0 - 32 * u, bias);
+      if constexpr (BIAS) tile_bias<-1>(*bl, TileBuckets(p.db, first, dmin, dmax), first, d0 - 32 * u, bias);
       typename TY::Frag dsf[2];
 #pragma unroll
       for (int g = 0; g < 2; ++g) {
@@ -915,10 +917,12 @@ __global__ __launch_bounds__(64 * NW, sizeof(T) == 2 || DHP == 64 ? 2 : 1) void 
       if (!active || dhi < d_from || dlo >= d_to) continue;
       const uint32_t stage = (t & 1) * kStageBytes, lq = lds0 + stage + skip * 128 + TL::row_base(afresh(lane)), lqc = lds0 + stage + skip * 128 + TL::col_base(afresh(lane));
       const float* lstat = reinterpret_cast<const float*>(lds + stage + 2 * TL::kBytes) + 2 * skip;
-      const bool masked = dlo < d_from || dhi >= d_to || qb + kMine > S || (far && kw + 31 >= a.sinks);
       const int d0 = qb - key + 4 * half;
 #pragma unroll
       for (int u = 0; u < NT / TEAMS; ++u) {
+        const int tlo = dlo + 32 * u, thi = tlo + 62;  // the tile's smallest and largest distance
+        if (thi < d_from || tlo >= d_to) continue;
+        const bool masked = tlo < d_from || thi >= d_to || qb + 32 * u + 32 > S || (far && kw + 31 >= a.sinks);
         floatx16 sacc, pacc;
 #pragma unroll
         for (int r = 0; r < 16; ++r) sacc[r] = pacc[r] = 0.f;
@@ -933,12 +937,12 @@ __global__ __launch_bounds__(64 * NW, sizeof(T) == 2 || DHP == 64 ? 2 : 1) void 
 #pragma unroll
           for (int r = 0; r < 16; ++r) {
             const int at = 32 * u + 8 * (r >> 2) + (r & 3);
-            const bool counts = at >= d_from - d0 && at < d_end - d0;
+            const bool counts = (at >= d_from - d0) & (at < d_end - d0);
             sacc[r] = counts ? sacc[r] : -INFINITY;
             pacc[r] = counts ? pacc[r] : 0.f;
           }
         }
-        const TileBuckets tb(p.db, first, BIAS ? dlo + 32 * u : 0, dlo + 32 * u + 62);
+        const TileBuckets tb(p.db, first, BIAS ? tlo : 0, thi);
         if constexpr (BIAS) far_sum.start_tile(sums[wave], tb, lane);
         Diagonals diagonals;
 #pragma unroll
@@ -972,7 +976,7 @@ __global__ __launch_bounds__(64 * NW, sizeof(T) == 2 || DHP == 64 ? 2 : 1) void 
                             });
         }
         if constexpr (BIAS) {
-          if (tb.b0 < 0) sums[wave].near[kPad + dlo + 32 * u + 62 - lane] += diagonals.sum;
+          if (tb.b0 < 0) sums[wave].near[kPad + thi - lane] += diagonals.sum;
         }
       }
     }
