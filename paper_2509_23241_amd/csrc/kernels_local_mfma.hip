@@ -469,14 +469,6 @@ __global__ __launch_bounds__(64 * NW, sizeof(T) == 2 || DHP == 64 ? 3 : 2) void 
       for (int t = lane; t < p.db.count; t += 64) p.kept[(size_t)h * p.db.count + t] = row[t];
   }
 
-  const int query = min(qw + (lane & 31), S - 1);
-  typename TY::Frag qf[KK];
-#pragma unroll
-  for (int kk = 0; kk < KK; ++kk) qf[kk] = TY::load(qbase + (size_t)query * ld + 16 * kk + 8 * half, dh - 16 * kk - 8 * half);
-  wait_vmcnt<0>();  // nothing but the copies below is in flight from here on
-#pragma unroll
-  for (int kk = 0; kk < KK; ++kk) asm volatile("" : "+v"(qf[kk]));
-
   const uint32_t off = TL::offset(ld, wave, lane), row_at = TL::row_base(lane), col_at = TL::col_base(lane);
   auto issue = [&](int t) {
     const int row = it.block(t) * BR;
@@ -485,6 +477,15 @@ __global__ __launch_bounds__(64 * NW, sizeof(T) == 2 || DHP == 64 ? 3 : 2) void 
     TL::copy(to, kbase + (size_t)row * ld, ld, off, whole, S - row, dh, wave, lane);
     TL::copy(to + TL::kBytes, vbase + (size_t)row * ld, ld, off, whole, S - row, dh, wave, lane);
   };
+  if (it.count > 0) issue(0);  // on its way while the wave's own rows are fetched
+  const int query = min(qw + (lane & 31), S - 1);
+  typename TY::Frag qf[KK];
+#pragma unroll
+  for (int kk = 0; kk < KK; ++kk) qf[kk] = TY::load(qbase + (size_t)query * ld + 16 * kk + 8 * half, dh - 16 * kk - 8 * half);
+  wait_vmcnt<0>();  // nothing but copies is in flight from here on
+#pragma unroll
+  for (int kk = 0; kk < KK; ++kk) asm volatile("" : "+v"(qf[kk]));
+
   floatx16 oacc[TN];
 #pragma unroll
   for (int j = 0; j < TN; ++j)
@@ -492,7 +493,6 @@ __global__ __launch_bounds__(64 * NW, sizeof(T) == 2 || DHP == 64 ? 3 : 2) void 
     for (int r = 0; r < 16; ++r) oacc[j][r] = 0.f;
   float mrun = kLowest, lsum = 0.f;
   const int q_last = min(qw + 31, S - 1);
-  if (it.count > 0) issue(0);
   for (int t = 0; t < it.count; ++t) {
     wait_vmcnt<0>();
     lds_barrier();  // block t is there, and nobody reads the other stage any more
@@ -637,6 +637,15 @@ __global__ __launch_bounds__(64 * NW, sizeof(T) == 2 || DHP == 64 ? 2 : 1) void 
     __syncthreads();
     bl->load(p.db, first, p.kept + ((size_t)(b / p.seqs_per_table) * a.heads + h) * p.db.count, lane, 64);
   }
+  const uint32_t off = TL::offset(ld, wave, lane), row_at = TL::row_base(lane), col_at = TL::col_base(lane);
+  auto issue = [&](int t) {
+    const int row = it.block(t) * BR;
+    const uint32_t to = lds0 + (t & 1) * 2 * TL::kBytes;
+    const bool whole = dh == DHP && row + BR <= S;
+    TL::copy(to, kbase + (size_t)row * ld, ld, off, whole, S - row, dh, wave, lane);
+    TL::copy(to + TL::kBytes, vbase + (size_t)row * ld, ld, off, whole, S - row, dh, wave, lane);
+  };
+  if (it.count > 0) issue(0);  // on its way while the wave's own rows are fetched
   const bool there = active && qw + (lane & 31) < S;
   const int query = min(qw + (lane & 31), S - 1);
   const T* dorow = p.dout + ((size_t)b * S + query) * D + (size_t)h * dh;
@@ -659,14 +668,6 @@ __global__ __launch_bounds__(64 * NW, sizeof(T) == 2 || DHP == 64 ? 2 : 1) void 
   for (int kk = 0; kk < KK; ++kk) asm volatile("" : "+v"(qf[kk]), "+v"(df[kk]));
   asm volatile("" : "+v"(l2), "+v"(delta));
 
-  const uint32_t off = TL::offset(ld, wave, lane), row_at = TL::row_base(lane), col_at = TL::col_base(lane);
-  auto issue = [&](int t) {
-    const int row = it.block(t) * BR;
-    const uint32_t to = lds0 + (t & 1) * 2 * TL::kBytes;
-    const bool whole = dh == DHP && row + BR <= S;
-    TL::copy(to, kbase + (size_t)row * ld, ld, off, whole, S - row, dh, wave, lane);
-    TL::copy(to + TL::kBytes, vbase + (size_t)row * ld, ld, off, whole, S - row, dh, wave, lane);
-  };
   floatx16 acc[TN];
 #pragma unroll
   for (int j = 0; j < TN; ++j)
@@ -675,7 +676,6 @@ __global__ __launch_bounds__(64 * NW, sizeof(T) == 2 || DHP == 64 ? 2 : 1) void 
   float total = 0.f;
   const int q_last = min(qw + 31, S - 1);
   const float scale_log2 = p.scale * kLog2e;
-  if (it.count > 0) issue(0);
   for (int t = 0; t < it.count; ++t) {
     wait_vmcnt<0>();
     lds_barrier();
@@ -871,6 +871,18 @@ __global__ __launch_bounds__(64 * NW, sizeof(T) == 2 || DHP == 64 ? 2 : 1) void 
     __syncthreads();
     start_head(0);
   }
+  auto issue = [&](int t) {
+    const int g = t / nb, row = (blk0 + t - g * nb) * BR, h = kvh * group + g;
+    const uint32_t to = lds0 + (t & 1) * kStageBytes;
+    const int l = afresh(lane);
+    const uint32_t offq = TL::offset(ld, wave, l), offd = TL::offset(D, wave, l);
+    const bool whole = dh == DHP && row + BR <= S;
+    TL::copy(to, base + (size_t)row * ld + (size_t)h * dh, ld, offq, whole, S - row, dh, wave, lane);
+    TL::copy(to + TL::kBytes, dobase + (size_t)row * D + (size_t)h * dh, D, offd, whole, S - row, dh, wave, lane);
+    // (lse, delta) of BR rows, over and over where they are fewer than the 64 lanes copy
+    dma16(to + 2 * TL::kBytes, p.stat + (((size_t)b * a.heads + h) * SP + row) * 2, (uint32_t)(lane & (BR / 2 - 1)) * 16);
+  };
+  if (t_begin < t_end) issue(t_begin);  // on its way while the wave's own rows are fetched
   typename TY::Frag kf[KK], vf[KK];
   {
     const int j = min(key, S - 1);
@@ -885,24 +897,12 @@ __global__ __launch_bounds__(64 * NW, sizeof(T) == 2 || DHP == 64 ? 2 : 1) void 
 #pragma unroll
   for (int kk = 0; kk < KK; ++kk) asm volatile("" : "+v"(kf[kk]), "+v"(vf[kk]));
 
-  auto issue = [&](int t) {
-    const int g = t / nb, row = (blk0 + t - g * nb) * BR, h = kvh * group + g;
-    const uint32_t to = lds0 + (t & 1) * kStageBytes;
-    const int l = afresh(lane);
-    const uint32_t offq = TL::offset(ld, wave, l), offd = TL::offset(D, wave, l);
-    const bool whole = dh == DHP && row + BR <= S;
-    TL::copy(to, base + (size_t)row * ld + (size_t)h * dh, ld, offq, whole, S - row, dh, wave, lane);
-    TL::copy(to + TL::kBytes, dobase + (size_t)row * D + (size_t)h * dh, D, offd, whole, S - row, dh, wave, lane);
-    // (lse, delta) of BR rows, over and over where they are fewer than the 64 lanes copy
-    dma16(to + 2 * TL::kBytes, p.stat + (((size_t)b * a.heads + h) * SP + row) * 2, (uint32_t)(lane & (BR / 2 - 1)) * 16);
-  };
   floatx16 ak[TN], av[TN];
 #pragma unroll
   for (int j = 0; j < TN; ++j)
 #pragma unroll
     for (int r = 0; r < 16; ++r) ak[j][r] = av[j][r] = 0.f;
   const float scale_log2 = p.scale * kLog2e;
-  if (t_begin < t_end) issue(t_begin);
   FarSum far_sum;
   int t = t_begin;
   for (int g = 0; g < group; ++g) {
