@@ -228,25 +228,55 @@ __device__ __forceinline__ void pipelined(Frag (&f)[DEPTH], const Load& load, co
 }
 
 // ---- the bias in LDS ----------------------------------------------------------------------------------------------------------
+// The buckets of distances 0 .. kNear + kPad - 1, four to a word.  A lane fetches a word, its borders and its values at the same time; a search by
+// distance, or a walk over the buckets' runs, waited for memory again and again: 8 to 9 of the 12 thousand cycles before the first tile.
+struct NearBuckets {
+  uint32_t of[(kNear + kPad) / 4];
+};
+inline NearBuckets near_buckets(const DistanceBuckets& d) {
+  NearBuckets n{};
+  if (d.count == 0) return n;
+  for (int i = 0, b = 0; i < kNear + kPad; ++i) {
+    while (b + 1 < d.count && i >= d.first[b + 1]) ++b;
+    n.of[i / 4] |= (uint32_t)b << 8 * (i % 4);
+  }
+  return n;
+}
 // near[kPad + d], d = -kPad .. kNear + kPad - 1: the table by distance, in units of log2; beyond that by bucket.
 struct BiasLds {
   float near[kNearSize];
   float value[kMaxBuckets];
-  // by the `threads` threads that share it, with the borders in LDS
-  __device__ __forceinline__ void load(const DistanceBuckets& d, const int* first, const float* row, int thread, int threads) {
-    for (int b = thread; b < d.count; b += threads) value[b] = row[b] * kLog2e;
-    for (int i = thread; i < kNearSize; i += threads) near[i] = i < kPad ? 0.f : row[bucket_of(d, first, i - kPad)] * kLog2e;
+  // by the WAVES waves that share it
+  template <int WAVES>
+  __device__ __forceinline__ void load(const DistanceBuckets& d, const NearBuckets& n, const float* row, int lane, int thread) {
+    constexpr int kWords = (kNear + kPad) / 4, kEach = (kWords + 64 * WAVES - 1) / (64 * WAVES);
+    uint32_t word[kEach];
+#pragma unroll
+    for (int c = 0; c < kEach; ++c) word[c] = n.of[min(thread + 64 * WAVES * c, kWords - 1)];
+    // all values by every wave, which then reads its own
+#pragma unroll
+    for (int c = 0; c < kMaxBuckets / 64; ++c) value[lane + 64 * c] = row[min(lane + 64 * c, d.count - 1)] * kLog2e;
+    for (int i = thread; i < kPad; i += 64 * WAVES) near[i] = 0.f;
+#pragma unroll
+    for (int c = 0; c < kEach; ++c) {
+      const int at = min(thread + 64 * WAVES * c, kWords - 1);
+      const uint32_t w = word[c];
+      *reinterpret_cast<float4*>(near + kPad + 4 * at) = make_float4(value[w & 255], value[w >> 8 & 255], value[w >> 16 & 255], value[w >> 24]);
+    }
   }
 };
 __device__ __forceinline__ void load_borders(const DistanceBuckets& d, int* first) {
-  for (int b = threadIdx.x; b < d.count; b += blockDim.x) first[b] = d.first[b];
+  if ((int)threadIdx.x < d.count) first[threadIdx.x] = d.first[threadIdx.x];
 }
 
 // Buckets b0 .. b1 of a tile's distances dmin .. dmax, wave uniform; b0 = -1: near ones, by distance.
 struct TileBuckets {
   int b0 = -1, b1 = -1;
   __device__ __forceinline__ TileBuckets(const DistanceBuckets& d, const int* first, int dmin, int dmax) {
-    if (dmin < kNear && dmin < __builtin_amdgcn_readfirstlane(first[d.count - 1])) return;
+    const int last = d.first[d.count - 1];
+    if (dmin < kNear && dmin < last) return;
+    b0 = b1 = d.count - 1;
+    if (dmin >= last) return;
     b0 = __builtin_amdgcn_readfirstlane(bucket_of(d, first, dmin));
     b1 = b0;
     while (b1 + 1 < d.count && __builtin_amdgcn_readfirstlane(first[b1 + 1]) <= dmax) ++b1;
@@ -406,6 +436,7 @@ template <typename T>
 struct FwdArgs {
   Shape a;
   DistanceBuckets db;
+  NearBuckets near;
   const T* x;
   const float* table;
   float* kept;
@@ -460,15 +491,6 @@ __global__ __launch_bounds__(64 * NW, sizeof(T) == 2 || DHP == 64 ? 3 : 2) void 
   constexpr size_t kStages = 2 * 2 * TL::kBytes, kTiles = kStages > NW * kTurnBytes ? kStages : NW * kTurnBytes;
   int* first = reinterpret_cast<int*>(lds + kTiles);
   BiasLds* bl = reinterpret_cast<BiasLds*>(lds + kTiles + kMaxBuckets * 4) + wave;
-  if constexpr (BIAS) {
-    load_borders(p.db, first);
-    __syncthreads();
-    const float* row = p.table + (size_t)h * p.db.count;
-    bl->load(p.db, first, row, lane, 64);
-    if (b == 0 && active && it.blk == 0)
-      for (int t = lane; t < p.db.count; t += 64) p.kept[(size_t)h * p.db.count + t] = row[t];
-  }
-
   const uint32_t off = TL::offset(ld, wave, lane), row_at = TL::row_base(lane), col_at = TL::col_base(lane);
   auto issue = [&](int t) {
     const int row = it.block(t) * BR;
@@ -482,6 +504,13 @@ __global__ __launch_bounds__(64 * NW, sizeof(T) == 2 || DHP == 64 ? 3 : 2) void 
   typename TY::Frag qf[KK];
 #pragma unroll
   for (int kk = 0; kk < KK; ++kk) qf[kk] = TY::load(qbase + (size_t)query * ld + 16 * kk + 8 * half, dh - 16 * kk - 8 * half);
+  if constexpr (BIAS) {
+    load_borders(p.db, first);
+    const float* row = p.table + (size_t)h * p.db.count;
+    bl->load<1>(p.db, p.near, row, lane, lane);
+    if (b == 0 && active && it.blk == 0)
+      for (int t = lane; t < p.db.count; t += 64) p.kept[(size_t)h * p.db.count + t] = row[t];
+  }
   wait_vmcnt<0>();  // nothing but copies is in flight from here on
 #pragma unroll
   for (int kk = 0; kk < KK; ++kk) asm volatile("" : "+v"(qf[kk]));
@@ -596,6 +625,7 @@ template <typename T>
 struct BwdArgs {
   Shape a;
   DistanceBuckets db;
+  NearBuckets near;
   int seqs_per_table;
   const T *x, *out, *dout;
   const float *lse, *kept;
@@ -605,7 +635,7 @@ struct BwdArgs {
   float* sums;
   float* partials;  // of the table: [seqs * gridDim.y][heads][buckets]
   int parts;        // of a walk over streamed blocks, in workgroups of their own
-  int far_blocks, chunks, chunk_blocks;  // workgroups for far pairs of the first keys: blocks of keys x ranges of chunk_blocks streamed blocks
+  int far_blocks, chunks;  // workgroups for far pairs of the first keys: blocks of keys x ranges of the walk; none: the others take these pairs
   float scale;
 };
 
@@ -632,11 +662,6 @@ __global__ __launch_bounds__(64 * NW, sizeof(T) == 2 || DHP == 64 ? 2 : 1) void 
   constexpr size_t kStages = 2 * 2 * TL::kBytes, kTiles = kStages > NW * kTurnBytes ? kStages : NW * kTurnBytes;
   int* first = reinterpret_cast<int*>(lds + kTiles);
   BiasLds* bl = reinterpret_cast<BiasLds*>(lds + kTiles + kMaxBuckets * 4) + wave;
-  if constexpr (BIAS) {
-    load_borders(p.db, first);
-    __syncthreads();
-    bl->load(p.db, first, p.kept + ((size_t)(b / p.seqs_per_table) * a.heads + h) * p.db.count, lane, 64);
-  }
   const uint32_t off = TL::offset(ld, wave, lane), row_at = TL::row_base(lane), col_at = TL::col_base(lane);
   auto issue = [&](int t) {
     const int row = it.block(t) * BR;
@@ -663,6 +688,10 @@ __global__ __launch_bounds__(64 * NW, sizeof(T) == 2 || DHP == 64 ? 2 : 1) void 
   for (int kk = 0; kk < KK; ++kk) qf[kk] = TY::load(qbase + (size_t)query * ld + 16 * kk + 8 * half, dh - 16 * kk - 8 * half);
   delta = over_halves(delta, Add());
   float l2 = p.lse[((size_t)b * a.heads + h) * S + query] * kLog2e;
+  if constexpr (BIAS) {
+    load_borders(p.db, first);
+    bl->load<1>(p.db, p.near, p.kept + ((size_t)(b / p.seqs_per_table) * a.heads + h) * p.db.count, lane, lane);
+  }
   wait_vmcnt<0>();
 #pragma unroll
   for (int kk = 0; kk < KK; ++kk) asm volatile("" : "+v"(qf[kk]), "+v"(df[kk]));
@@ -841,17 +870,17 @@ __global__ __launch_bounds__(64 * NW, sizeof(T) == 2 || DHP == 64 ? 2 : 1) void 
   const int team = wave / (NW / TEAMS);
   const int kw = k0 + wave % (NW / TEAMS) * 32, key = kw + (lane & 31);
   const bool active = kw < (far ? a.sinks : S);
-  // distances that count: all in the window, or beside the far workgroups' all in it, or there all beyond it
-  const int d_from = far ? a.window : 0, d_to = far ? S : a.window;
-  const int d_end = far && key >= a.sinks ? 0 : min(d_to, S - key);  // of this lane's key; copied rows behind the last token do not count
-  int blk0 = k0 / BR, blk1 = min(S - 1, k0 + kOwn - 1 + a.window - 1) / BR + 1;  // streamed blocks of queries
-  if (far) {
-    blk0 = (k0 + a.window) / BR + chunk * p.chunk_blocks;
-    blk1 = min(blk0 + p.chunk_blocks, (S + BR - 1) / BR);
-  }
-  // steps of the walk: the streamed blocks of each query head in turn; a part takes a range of them
-  const int nb = max(0, blk1 - blk0), steps = nb * group;
-  const int t_begin = far ? 0 : (int)((long)steps * part / p.parts), t_end = far ? steps : (int)((long)steps * (part + 1) / p.parts);
+  // Distances that count, from d_from up to an end: those in the window, of first keys without far workgroups all, and of far workgroups
+  // those beyond the window.
+  const bool to_last = far || p.far_blocks == 0;
+  auto end_of = [&](int j) { return j >= a.sinks ? (far ? 0 : a.window) : to_last ? S : a.window; };
+  const int d_from = far ? a.window : 0, d_to = end_of(kw);
+  const int d_end = min(end_of(key), S - key);  // of this lane's key; copied rows behind the last token do not count
+  // streamed blocks of queries
+  const int blk0 = (k0 + d_from) / BR, blk1 = (int)min((long)S - 1, (long)k0 + kOwn - 2 + end_of(k0)) / BR + 1;
+  // steps of the walk: the streamed blocks of each query head in turn; a part or a chunk takes a range of them
+  const int nb = max(0, blk1 - blk0), pieces = far ? p.chunks : p.parts, piece = far ? chunk : part;
+  const int t_begin = (int)((long)nb * group * piece / pieces), t_end = (int)((long)nb * group * (piece + 1) / pieces);
   const T* base = p.x + (size_t)b * S * ld;
   const T* kbase = base + D + (size_t)kvh * dh;
   const T* vbase = kbase + (size_t)a.kv * dh;
@@ -863,14 +892,9 @@ __global__ __launch_bounds__(64 * NW, sizeof(T) == 2 || DHP == 64 ? 2 : 1) void 
   TableSums* sums = reinterpret_cast<TableSums*>(bl + 1);
   auto table = [&](int h) { return p.kept + ((size_t)(b / p.seqs_per_table) * a.heads + h) * p.db.count; };
   auto start_head = [&](int g) {
-    bl->load(p.db, first, table(kvh * group + g), threadIdx.x, 64 * NW);
+    bl->load<NW>(p.db, p.near, table(kvh * group + g), lane, threadIdx.x);
     for (int i = threadIdx.x; i < (int)(NW * sizeof(TableSums) / 4); i += 64 * NW) reinterpret_cast<float*>(sums)[i] = 0.f;
   };
-  if constexpr (BIAS) {
-    load_borders(p.db, first);
-    __syncthreads();
-    start_head(0);
-  }
   auto issue = [&](int t) {
     const int g = t / nb, row = (blk0 + t - g * nb) * BR, h = kvh * group + g;
     const uint32_t to = lds0 + (t & 1) * kStageBytes;
@@ -893,6 +917,10 @@ __global__ __launch_bounds__(64 * NW, sizeof(T) == 2 || DHP == 64 ? 2 : 1) void 
       vf[kk] = TY::load(vbase + (size_t)j * ld + d, dh - d);
     }
   }
+  if constexpr (BIAS) {
+    load_borders(p.db, first);
+    if (t_begin < t_end) start_head(t_begin / nb);
+  }
   wait_vmcnt<0>();
 #pragma unroll
   for (int kk = 0; kk < KK; ++kk) asm volatile("" : "+v"(kf[kk]), "+v"(vf[kk]));
@@ -904,9 +932,18 @@ __global__ __launch_bounds__(64 * NW, sizeof(T) == 2 || DHP == 64 ? 2 : 1) void 
     for (int r = 0; r < 16; ++r) ak[j][r] = av[j][r] = 0.f;
   const float scale_log2 = p.scale * kLog2e;
   FarSum far_sum;
-  int t = t_begin;
   for (int g = 0; g < group; ++g) {
-    for (int n = t - g * nb; n < nb && t < t_end; ++n, ++t) {  // a part that begins with a later head has n >= nb here
+    const int n_begin = max(0, t_begin - g * nb), n_end = min(nb, t_end - g * nb);
+    float* table_sums = BIAS ? p.partials + (((size_t)b * gridDim.y + blockIdx.y) * a.heads + kvh * group + g) * p.db.count : nullptr;
+    if (n_begin >= n_end) {  // a head of other parts
+      if (BIAS && (int)threadIdx.x < p.db.count) table_sums[threadIdx.x] = 0.f;
+      continue;
+    }
+    if constexpr (BIAS) {
+      if (g * nb > t_begin) start_head(g);
+    }
+    for (int n = n_begin; n < n_end; ++n) {
+      const int t = g * nb + n;
       wait_vmcnt<0>();
       lds_barrier();
       if (t + 1 < t_end) issue(t + 1);
@@ -922,7 +959,7 @@ __global__ __launch_bounds__(64 * NW, sizeof(T) == 2 || DHP == 64 ? 2 : 1) void 
       for (int u = 0; u < NT / TEAMS; ++u) {
         const int tlo = dlo + 32 * u, thi = tlo + 62;  // the tile's smallest and largest distance
         if (thi < d_from || tlo >= d_to) continue;
-        const bool masked = tlo < d_from || thi >= d_to || qb + 32 * u + 32 > S || (far && kw + 31 >= a.sinks);
+        const bool masked = tlo < d_from || thi >= end_of(kw + 31) || qb + 32 * u + 32 > S;
         floatx16 sacc, pacc;
 #pragma unroll
         for (int r = 0; r < 16; ++r) sacc[r] = pacc[r] = 0.f;
@@ -992,23 +1029,16 @@ __global__ __launch_bounds__(64 * NW, sizeof(T) == 2 || DHP == 64 ? 2 : 1) void 
         by_distance[i] = s;
       }
       __syncthreads();
-      float* out = p.partials + (((size_t)b * gridDim.y + blockIdx.y) * a.heads + kvh * group + g) * p.db.count;
-      for (int bk = wave; bk < p.db.count; bk += NW) {
-        const int from = first[bk], to = bk + 1 < p.db.count ? min(first[bk + 1], kNear + kPad) : kNear + kPad;
-        float s = 0.f;
-        for (int d = from + lane; d < to; d += 64) s += by_distance[kPad + d];
-        s = sum_over_lanes(s);
-        if (lane == 0) {
-#pragma unroll
-          for (int w = 0; w < NW; ++w) s += sums[w].far[bk];
-          out[bk] = s;
-        }
+      // a bucket by 16 lanes; one after the other by whole waves, 8 of 32 each, took 5 to 10 thousand cycles
+      for (int bk = threadIdx.x / 16; bk < p.db.count; bk += 4 * NW) {
+        const int to = bk + 1 < p.db.count ? min(first[bk + 1], kNear + kPad) : kNear + kPad;
+        float s = (lane & 15) < NW ? sums[lane & 15].far[bk] : 0.f;
+#pragma unroll 4
+        for (int d = first[bk] + (lane & 15); d < to; d += 16) s += by_distance[kPad + d];
+        s = sum_over_lanes<8>(s);
+        if ((lane & 15) == 0) table_sums[bk] = s;
       }
       __syncthreads();
-      if (g + 1 < group) {
-        start_head(g + 1);
-        __syncthreads();
-      }
     }
   }
   lds_barrier();
@@ -1068,7 +1098,7 @@ __global__ __launch_bounds__(64 * NW, sizeof(T) == 2 || DHP == 64 ? 2 : 1) void 
       const int h = kvh * group + g;
       // queries of this workgroup's steps that see the key
       const int n0 = max(0, t_begin - g * nb), n1 = min(nb, t_end - g * nb);
-      const int from = max((blk0 + n0) * BR, j + d_from), to_i = (int)min((long)min(S, (blk0 + n1) * BR), (long)j + d_to);
+      const int from = max((blk0 + n0) * BR, j + d_from), to_i = (int)min((long)min(S, (blk0 + n1) * BR), (long)j + end_of(j));
       const T* q = base + (size_t)h * dh;
       const T* dO = dobase + (size_t)h * dh;
       for (int i0 = from; i0 < to_i; i0 += 64) {
@@ -1129,7 +1159,7 @@ constexpr int kWaves = 4;
 // How the dK, dV launch is cut up.
 struct DkvPlan {
   int teams = 1, parts = 1;
-  int far_blocks = 0, chunks = 0, chunk_blocks = 0;  // workgroups for the far pairs of the first keys
+  int far_blocks = 0, chunks = 0;  // workgroups for the far pairs of the first keys; none: those keys' own workgroups take them
   int rows = 0;                                      // workgroups for a key head of a sequence
 };
 template <typename T, int DHP>
@@ -1144,30 +1174,33 @@ DkvPlan dkv_plan(const LocalAttention& a) {
     const int own = 128 / teams, blocks = (a.S + own - 1) / own;
     // Times in steps of a workgroup whose waves each take whole blocks (about 2.6 us for 128-wide heads); starting and ending one cost
     // three, and a step of two teams 0.6.
-    const double walk = (double)((std::min<long>(a.S, (long)own + a.window) + BR - 1) / BR * group), step = teams == 1 ? 1.0 : 0.6;
+    auto steps = [&](long queries) { return (double)((std::min<long>(a.S, queries) + BR - 1) / BR * group); };
+    const double step = teams == 1 ? 1.0 : 0.6, walk = steps((long)own + a.window), far_walk = steps(a.S - a.window);
     for (int parts = 1; parts <= 16 && (parts == 1 || walk >= 4 * parts); ++parts) {
-      DkvPlan f;
-      f.teams = teams;
-      f.parts = parts;
-      if (a.sinks > 0 && !causal) {
-        f.far_blocks = (a.sinks + own - 1) / own;
-        const int total = (a.S + BR - 1) / BR - a.window / BR;  // streamed blocks that far pairs of the first keys lie in
-        // a range is about as long as what the other workgroups walk over; no more of them than give every CU four, since each leaves
-        // its sums in memory
-        const int length = std::max(4, (a.window + own) / BR / parts);
-        const long most = std::max<long>(1, 1024 / (nz * f.far_blocks));
-        f.chunks = (int)std::min<long>(most, (total + length - 1) / length);
-        f.chunk_blocks = (total + f.chunks - 1) / f.chunks;
-      }
-      f.rows = blocks * parts + f.far_blocks * f.chunks;
-      const double one = 3 + step * std::max(walk / parts, (double)f.chunk_blocks * group), all = (double)nz * f.rows;
-      // equal walks run in rounds; those of a causal triangle, the longest first, fill one another's gaps
-      double time = causal ? std::max(one, all * (3 + step * walk / parts / 2) / kSlots) : std::ceil(all / kSlots) * one;
-      // parts meet in memory: written and read at some 4 TB/s, and a launch
-      if (parts > 1) time += 1 + (double)parts * nz * a.S * 2 * a.dh * 8 / 4e12 / (2.6e-6 * DHP / 128);
-      if (best.rows == 0 || time < best_time) {
-        best = f;
-        best_time = time;
+      for (int apart = 0; apart <= (a.sinks > 0 && !causal); ++apart) {  // far pairs in workgroups of their own
+        DkvPlan f;
+        f.teams = teams;
+        f.parts = parts;
+        if (apart) {
+          // chunks as long as a part; no more of them than give every CU four, since each leaves its sums in memory
+          f.far_blocks = (a.sinks + own - 1) / own;
+          const long most = std::max<long>(1, 1024 / (nz * f.far_blocks));
+          f.chunks = (int)std::min<long>(most, (long)std::ceil(far_walk / std::max(4.0, walk / parts)));
+        }
+        f.rows = blocks * parts + f.far_blocks * f.chunks;
+        const bool longer = a.sinks > 0 && !apart;  // the first keys' workgroups
+        const double one = 3 + step * std::max(walk / parts, apart ? far_walk / f.chunks : 0.0);
+        const double first = longer ? 3 + step * steps(a.S) / parts : one, firsts = longer ? (double)nz * parts * ((a.sinks + own - 1) / own) : 0;
+        const double all = (double)nz * f.rows;
+        // equal walks run in rounds; those of a causal triangle, the longest first, fill one another's gaps
+        double time = causal ? std::max(one, all * (3 + step * walk / parts / 2) / kSlots)
+                             : std::max(first, std::ceil((firsts * first / one + all - firsts) / kSlots) * one);
+        // parts meet in memory: written and read at some 4 TB/s, and a launch
+        if (parts > 1 || apart) time += 1 + (parts > 1 ? (double)parts * nz * a.S * 2 * a.dh * 8 / 4e12 / (2.6e-6 * DHP / 128) : 0.0);
+        if (best.rows == 0 || time < best_time) {
+          best = f;
+          best_time = time;
+        }
       }
     }
   }
@@ -1230,7 +1263,8 @@ hipError_t run_bwd(hipStream_t s, const LocalAttention& a, const BwdArgs<T>& p) 
 
 template <typename T>
 hipError_t fwd(hipStream_t s, const LocalAttention& a, const T* x, const float* table, float* kept, T* out, T* out2, float* lse) {
-  const FwdArgs<T> p{shape_of(a), make_distance_buckets(a.buckets, a.max_distance), x, table, kept, out, out2, lse, kLog2e / sqrtf((float)a.dh)};
+  const DistanceBuckets db = make_distance_buckets(a.buckets, a.max_distance);
+  const FwdArgs<T> p{shape_of(a), db, near_buckets(db), x, table, kept, out, out2, lse, kLog2e / sqrtf((float)a.dh)};
   if (a.dh <= 64) return a.buckets ? run_fwd<T, 64, true>(s, a, p) : run_fwd<T, 64, false>(s, a, p);
   return a.buckets ? run_fwd<T, 128, true>(s, a, p) : run_fwd<T, 128, false>(s, a, p);
 }
@@ -1239,8 +1273,9 @@ template <typename T>
 hipError_t bwd(hipStream_t s, const LocalAttention& a, const T* x, const T* out, const T* dout, const float* lse, const float* kept, T* dx,
                float* partials, float* scratch) {
   const DkvPlan f = a.dh <= 64 ? dkv_plan<T, 64>(a) : dkv_plan<T, 128>(a);
-  const BwdArgs<T> p{shape_of(a), make_distance_buckets(a.buckets, a.max_distance), a.seqs_per_table, x, out, dout, lse, kept, dx, scratch,
-                     scratch + stat_floats(a), partials, f.parts, f.far_blocks, f.chunks, f.chunk_blocks, 1.0f / sqrtf((float)a.dh)};
+  const DistanceBuckets db = make_distance_buckets(a.buckets, a.max_distance);
+  const BwdArgs<T> p{shape_of(a), db, near_buckets(db), a.seqs_per_table, x, out, dout, lse, kept, dx, scratch,
+                     scratch + stat_floats(a), partials, f.parts, f.far_blocks, f.chunks, 1.0f / sqrtf((float)a.dh)};
   if (a.dh <= 64) return a.buckets ? run_bwd<T, 64, true>(s, a, p) : run_bwd<T, 64, false>(s, a, p);
   return a.buckets ? run_bwd<T, 128, true>(s, a, p) : run_bwd<T, 128, false>(s, a, p);
 }
