@@ -49,6 +49,7 @@ struct Type<uint16_t> {
   static __device__ __forceinline__ floatx16 mma(const Frag& a, const Frag& b, floatx16 c) {
     return __builtin_amdgcn_mfma_f32_32x32x16_bf16(a, b, c, 0, 0, 0);
   }
+  static __device__ __forceinline__ bool skips(int, int) { return false; }  // one instruction: less than it takes to decide
   static __device__ __forceinline__ Frag zero() { return __builtin_bit_cast(bf16x8, make_uint4(0, 0, 0, 0)); }
   // P and dS enter the second products rounded to bf16, like every operand there: 2^-9 of each, on average less of their sum
   static __device__ __forceinline__ Frag pack(const float (&e)[8]) {
@@ -80,6 +81,9 @@ struct Type<float> {
     for (int t = 0; t < 8; ++t) c = __builtin_amdgcn_mfma_f32_32x32x2f32(a[t], b[t], c, 0, 0, 0);
     return c;
   }
+  // A product of columns from `col` on, which are all padding: not worth its eight instructions of 64 cycles.  Heads of 32 or 80 take 15 to
+  // 20 % less time for it, those of 64 or 128 2 % more for asking.
+  static __device__ __forceinline__ bool skips(int col, int dh) { return col >= dh; }
   static __device__ __forceinline__ Frag zero() { return Frag{0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f}; }
   static __device__ __forceinline__ Frag pack(const float (&e)[8]) {
     Frag f;
@@ -538,7 +542,7 @@ __global__ __launch_bounds__(64 * NW, sizeof(T) == 2 || DHP == 64 ? 3 : 2) void 
     typename TY::Frag ahead[TY::kAhead];
     // the tiles in turn: no product waits for the one before it
     pipelined<NT * KK>(ahead, [&](int i) { return TL::row_frag(lk, i % NT, i / NT); },
-                       [&](int i, const typename TY::Frag& f) { sacc[i % NT] = TY::mma(f, qf[i / NT], sacc[i % NT]); });
+                       [&](int i, const typename TY::Frag& f) { if (!TY::skips(16 * (i / NT), dh)) sacc[i % NT] = TY::mma(f, qf[i / NT], sacc[i % NT]); });
     auto v_frag = [&](int i) { return TL::col_frag(lv, i % TN, i / TN, 1); };
 #pragma unroll
     for (int i = 0; i < TY::kAhead; ++i) ahead[i] = v_frag(i);
@@ -590,7 +594,7 @@ __global__ __launch_bounds__(64 * NW, sizeof(T) == 2 || DHP == 64 ? 3 : 2) void 
       }
       pf[g] = TY::pack(e);
     }
-    pipelined<2 * NT * TN>(ahead, v_frag, [&](int i, const typename TY::Frag& f) { oacc[i % TN] = TY::mma(f, pf[i / TN], oacc[i % TN]); }, true);
+    pipelined<2 * NT * TN>(ahead, v_frag, [&](int i, const typename TY::Frag& f) { if (!TY::skips(32 * (i % TN), dh)) oacc[i % TN] = TY::mma(f, pf[i / TN], oacc[i % TN]); }, true);
   }
   lds_barrier();  // the stages are free
   if (!active) return;
@@ -725,6 +729,7 @@ __global__ __launch_bounds__(64 * NW, sizeof(T) == 2 || DHP == 64 ? 2 : 1) void 
       typename TY::Frag ahead[TY::kAhead];
       pipelined<2 * KK>(ahead, [&](int i) { return TL::row_frag(lk, u, i >> 1, i & 1); },
                         [&](int i, const typename TY::Frag& f) {
+                          if (TY::skips(16 * (i >> 1), dh)) return;
                           if (i & 1) pacc = TY::mma(f, df[i >> 1], pacc);
                           else sacc = TY::mma(f, qf[i >> 1], sacc);
                         });
@@ -757,7 +762,7 @@ __global__ __launch_bounds__(64 * NW, sizeof(T) == 2 || DHP == 64 ? 2 : 1) void 
         }
         dsf[g] = TY::pack(e);
       }
-      pipelined<2 * TN>(ahead, k_frag, [&](int i, const typename TY::Frag& f) { acc[i % TN] = TY::mma(f, dsf[i / TN], acc[i % TN]); }, true);
+      pipelined<2 * TN>(ahead, k_frag, [&](int i, const typename TY::Frag& f) { if (!TY::skips(32 * (i % TN), dh)) acc[i % TN] = TY::mma(f, dsf[i / TN], acc[i % TN]); }, true);
     }
   }
   lds_barrier();
@@ -966,6 +971,7 @@ __global__ __launch_bounds__(64 * NW, sizeof(T) == 2 || DHP == 64 ? 2 : 1) void 
         typename TY::Frag ahead[BIAS ? 1 : 2];
         pipelined<2 * KK>(ahead, [&](int i) { return TL::row_frag(lq, u, i >> 1, i & 1); },
                           [&](int i, const typename TY::Frag& f) {
+                            if (TY::skips(16 * (i >> 1), dh)) return;
                             if (i & 1) pacc = TY::mma(f, vf[i >> 1], pacc);
                             else sacc = TY::mma(f, kf[i >> 1], sacc);
                           });
@@ -1008,6 +1014,7 @@ __global__ __launch_bounds__(64 * NW, sizeof(T) == 2 || DHP == 64 ? 2 : 1) void 
           const typename TY::Frag pf = TY::join(ph[0], ph[1]), dsf = TY::join(dsh[0], dsh[1]);
           pipelined<2 * TN>(ahead, [&](int i) { return TL::col_frag(lqc, i >> 1, 2 * u + v, i & 1); },
                             [&](int i, const typename TY::Frag& f) {
+                              if (TY::skips(32 * (i >> 1), dh)) return;
                               if (i & 1) av[i >> 1] = TY::mma(f, pf, av[i >> 1]);
                               else ak[i >> 1] = TY::mma(f, dsf, ak[i >> 1]);
                             });
