@@ -164,6 +164,51 @@ def test_against_fp64(case, dtype):
     _check(_run(c, x, dy, table), _reference(c, x, dy, table))
 
 
+LAUNCHES = [
+    # as many sequences as fill the chip: a workgroup takes all of a key head, first keys among them
+    _case(70, heads=8, kv=8, dh=16, seqs=64), _case(90, heads=8, kv=8, dh=80, window=20, sinks=2, buckets=8, reach=30, seqs=64),
+    _case(70, heads=8, kv=8, dh=32, window=30, sinks=3, buckets=32, reach=64, seqs=64),
+    # more workgroups than the chip runs at a time, the first of them with longer walks
+    _case(300, heads=16, kv=16, dh=64, window=40, sinks=1, buckets=16, reach=100, seqs=20), _case(1100, heads=8, kv=8, dh=16, window=100, sinks=3, seqs=8),
+    # one long sequence: walks in parts, pairs of first keys in many chunks, first keys over several workgroups; parts that begin within a
+    # query head or leave some out
+    _case(1500, heads=4, kv=1, dh=16, window=64, sinks=5, buckets=12, reach=300, seqs=1),
+    _case(1500, heads=4, kv=2, dh=80, window=700, sinks=70, buckets=20, reach=1000, seqs=1),
+    _case(1501, heads=2, kv=1, dh=128, window=64, sinks=140, seqs=1), _case(2100, heads=6, kv=1, dh=24, window=500, buckets=9, reach=50, seqs=1),
+]
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("case", LAUNCHES, ids=lambda c: "-".join(str(v) for v in list(c.values())[:-1]))
+def test_launches_cut_up_in_every_way(case, dtype):
+    c = dict(case, dtype=dtype)
+    x, dy, table = _inputs(c)
+    _check(_run(c, x, dy, table), _reference(c, x, dy, table))
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("tokens,window,sinks,seqs", [(1500, 64, 5, 1), (70, 30, 3, 64)])
+def test_a_query_that_is_not_finite_reaches_its_own_keys_only(tokens, window, sinks, seqs, dtype):
+    """An infinite gradient of the last token: the first keys take it over whatever workgroup adds their distant pairs up, all others not."""
+    import torch
+    c = _case(tokens, heads=8, kv=8 if seqs > 1 else 2, dh=32, window=window, sinks=sinks, buckets=8, reach=40, seqs=seqs, dtype=dtype)
+    x, dy, table = _inputs(c)
+    clean = _run(c, x, dy, table)
+    bad = dy.clone()
+    bad[0, -1, ::3] = float("inf")
+    got = _run(c, x, bad, table)
+    at = torch.arange(tokens, device="cuda")
+    key_of = (tokens - 1 - at < window) | (at < sinks)
+    for k, rows in (("y", at >= 0), ("dq", at < tokens - 1), ("dk", ~key_of), ("dv", ~key_of)):
+        new, old = got[k][0, rows].double(), clean[k][0, rows].double()
+        assert bool(torch.isfinite(new).all()), k
+        # another order of the sums: fp32 sums of at most 4 x `tokens` terms, stored with one rounding
+        assert float((new - old).norm()) <= (2.0 ** -8 if dtype == "bf16" else tokens * 2.0 ** -20) * float(old.norm()), k
+    assert not bool(torch.isfinite(got["dv"][0, key_of].float()).all(1).any())
+    for k in ("y", "dq", "dk", "dv"):
+        assert torch.equal(got[k][1:], clean[k][1:]), k
+
+
 @pytest.mark.parametrize("dtype", ["f32", "bf16"])
 def test_micro_batches_and_repeated_calls_give_the_same_bits(dtype):
     import torch
