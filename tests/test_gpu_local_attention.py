@@ -357,6 +357,17 @@ def test_last_layer_of_a_stage():
         print(dtype, run_stage(specs, f"local_last_{dtype}", dtype, mb=2, n=2))
 
 
+def test_layers_beside_it():
+    """First in a stage, one behind another, behind a ReLU, in front of a residual begin and of the addition itself."""
+    from stage_parity import run_stage
+    from synth_inputs import workloads as W
+    for dtype in ("f32", "bf16"):
+        specs = (W.LocalAttention(96, 6, 45, 2, 20, 1, 4, 9), W.LocalAttention(64, 4, 45, 1), W.Residual(64, 45, "begin"),
+                 W.Dense(64, 96, "relu", tokens=45), W.LocalAttention(64, 4, 45, 1, 9, 0, 8, 30), W.Residual(64, 45, "add"),
+                 W.Dense(64, 40, "gelu", tokens=45))
+        print(dtype, run_stage(specs, f"local_beside_{dtype}", dtype, mb=2, n=2, policy="convex"))
+
+
 def test_forward_streams():
     """Micro-batches on streams of their own share no scratch memory: the same bits."""
     import torch
