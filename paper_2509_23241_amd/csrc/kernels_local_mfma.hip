@@ -339,6 +339,26 @@ __device__ __forceinline__ void turned_rows(const floatx16 (&acc)[TN], float fac
   }
 }
 
+// Sums of two waves over the same rows: one leaves its own in LDS, a lane's values 64 x 16 bytes apart, the other adds them to its own.
+template <int TN>
+__device__ __forceinline__ void hand_over(const floatx16 (&acc)[TN], floatx4* to) {
+#pragma unroll
+  for (int j = 0; j < TN; ++j)
+#pragma unroll
+    for (int r = 0; r < 4; ++r) to[(j * 4 + r) * 64] = floatx4{acc[j][4 * r], acc[j][4 * r + 1], acc[j][4 * r + 2], acc[j][4 * r + 3]};
+}
+template <int TN>
+__device__ __forceinline__ void take_over(floatx16 (&acc)[TN], const floatx4* from) {
+#pragma unroll
+  for (int j = 0; j < TN; ++j)
+#pragma unroll
+    for (int r = 0; r < 4; ++r) {
+      const floatx4 v = from[(j * 4 + r) * 64];
+#pragma unroll
+      for (int e = 0; e < 4; ++e) acc[j][4 * r + e] += v[e];
+    }
+}
+
 // ---- rows one by one ----------------------------------------------------------------------------------------------------------
 template <int TN>
 __device__ __forceinline__ bool finite(const floatx16 (&acc)[TN]) {
@@ -649,11 +669,14 @@ struct BwdArgs {
 
 // Three products a tile at two waves a SIMD: 140 registers are q, dy and the sums.  8 x 1024 tokens, 16 heads of 128, window 256: 63 us;
 // 1 x 16384, 8 heads, window 1024: 142 us, 0.71 PFLOP/s; 8 x 1024, 16 heads, all keys: 82 us, with a bias 97.
-template <typename T, int DHP, int NW, bool BIAS>
+// TEAMS: 1, a wave has 32 queries of a head to itself; 2, two waves take one tile of every streamed block each, and their sums meet in LDS:
+// for launches that leave SIMDs without a wave.
+template <typename T, int DHP, int NW, int TEAMS, bool BIAS>
 __global__ __launch_bounds__(64 * NW, sizeof(T) == 2 || DHP == 64 ? 2 : 1) void local_dq_kernel(BwdArgs<T> p) {
   using TY = Type<T>;
   using TL = Tile<T, DHP, NW>;
   constexpr int BR = TL::BR, NT = BR / 32, KK = DHP / 16, TN = DHP / 32;
+  static_assert(TEAMS == 1 || TEAMS == NT, "a team takes one tile of a block");
   extern __shared__ __attribute__((aligned(16))) char lds[];
   const Shape& a = p.a;
   const int lane = threadIdx.x & 63, half = lane >> 5;
@@ -661,7 +684,8 @@ __global__ __launch_bounds__(64 * NW, sizeof(T) == 2 || DHP == 64 ? 2 : 1) void 
   const int group = a.heads / a.kv, b = blockIdx.x / a.kv, kvh = blockIdx.x - b * a.kv;
   const int S = a.S, dh = a.dh, SP = stat_rows(S);
   const size_t ld = a.ld(), D = (size_t)a.heads * dh;
-  const QueryItems<BR, NW> it(a, group, SP / 32, gridDim.y - 1 - blockIdx.y, wave);
+  const int team = wave / (NW / TEAMS);
+  const QueryItems<BR, NW / TEAMS> it(a, group, SP / 32, gridDim.y - 1 - blockIdx.y, wave % (NW / TEAMS));
   const bool active = it.item < it.items;
   const int h = kvh * group + (active ? it.g : 0), qw = (active ? it.blk : 0) * 32;
   const T* base = p.x + (size_t)b * S * ld;
@@ -719,12 +743,13 @@ __global__ __launch_bounds__(64 * NW, sizeof(T) == 2 || DHP == 64 ? 2 : 1) void 
     wait_vmcnt<0>();
     lds_barrier();
     if (t + 1 < it.count) issue(t + 1);
-    const int kb = it.block(t) * BR;
-    if (!active || qw >= S || kb > q_last || (kb >= a.sinks && kb + BR - 1 <= qw - a.window)) continue;
-    const uint32_t stage = lds0 + (t & 1) * 2 * TL::kBytes, lk = stage + row_at, lkc = stage + col_at;
+    constexpr int kMine = BR / TEAMS;  // the wave's rows of the block
+    const int skip = TEAMS == 1 ? 0 : team * 32, kb = it.block(t) * BR + skip;
+    if (!active || qw >= S || kb > q_last || (kb >= a.sinks && kb + kMine - 1 <= qw - a.window)) continue;
+    const uint32_t stage = lds0 + (t & 1) * 2 * TL::kBytes + skip * 128, lk = stage + row_at, lkc = stage + col_at;
     const int d0 = query - kb - 4 * half, sink0 = a.sinks - kb - 4 * half;
 #pragma unroll
-    for (int u = 0; u < NT; ++u) {
+    for (int u = 0; u < NT / TEAMS; ++u) {
       // the tile's smallest and largest distance; wave uniform
       const int k0 = kb + 32 * u, dmin = qw - (k0 + 31), dmax = qw + 31 - k0;
       if (dmax < 0 || (dmin >= a.window && k0 >= a.sinks)) continue;
@@ -772,7 +797,21 @@ __global__ __launch_bounds__(64 * NW, sizeof(T) == 2 || DHP == 64 ? 2 : 1) void 
     }
   }
   lds_barrier();
-  if (!active) return;
+  if constexpr (TEAMS == 2) {  // the second team's sums to the first
+    floatx4* mine = reinterpret_cast<floatx4*>(lds) + (size_t)(wave % (NW / TEAMS)) * TN * 4 * 64 + lane;
+    float* totals = reinterpret_cast<float*>(lds + (size_t)NW / TEAMS * TN * 4 * 64 * 16) + wave % (NW / TEAMS) * 64 + lane;
+    if (team == 1) {
+      hand_over(acc, mine);
+      *totals = total;
+    }
+    lds_barrier();
+    if (team == 0) {
+      take_over(acc, mine);
+      total += *totals;
+    }
+    lds_barrier();
+  }
+  if (!active || team != 0) return;
   // what the rows of dS add up to is what delta was off by
   const float corrected = delta + over_halves(total, Add());
   if (half == 0)
@@ -1060,27 +1099,13 @@ __global__ __launch_bounds__(64 * NW, sizeof(T) == 2 || DHP == 64 ? 2 : 1) void 
   if constexpr (TEAMS == 2) {  // the second team's sums to the first
     floatx4* mine = reinterpret_cast<floatx4*>(lds) + (size_t)(wave % (NW / TEAMS)) * 2 * TN * 4 * 64 + lane;
     if (team == 1) {
-#pragma unroll
-      for (int j = 0; j < TN; ++j)
-#pragma unroll
-        for (int r = 0; r < 4; ++r) {
-          mine[(j * 4 + r) * 64] = floatx4{ak[j][4 * r], ak[j][4 * r + 1], ak[j][4 * r + 2], ak[j][4 * r + 3]};
-          mine[((TN + j) * 4 + r) * 64] = floatx4{av[j][4 * r], av[j][4 * r + 1], av[j][4 * r + 2], av[j][4 * r + 3]};
-        }
+      hand_over(ak, mine);
+      hand_over(av, mine + TN * 4 * 64);
     }
     lds_barrier();
     if (team == 0) {
-#pragma unroll
-      for (int j = 0; j < TN; ++j)
-#pragma unroll
-        for (int r = 0; r < 4; ++r) {
-          const floatx4 k = mine[(j * 4 + r) * 64], v = mine[((TN + j) * 4 + r) * 64];
-#pragma unroll
-          for (int e = 0; e < 4; ++e) {
-            ak[j][4 * r + e] += k[e];
-            av[j][4 * r + e] += v[e];
-          }
-        }
+      take_over(ak, mine);
+      take_over(av, mine + TN * 4 * 64);
     }
     lds_barrier();
   }
@@ -1234,9 +1259,11 @@ inline int join_rows(const LocalAttention& a, const DkvPlan& f) { return f.parts
 inline size_t sum_floats(const LocalAttention& a, const DkvPlan& f) {
   return (size_t)a.seqs * a.kv * 2 * a.dh * ((size_t)f.parts * join_rows(a, f) + (size_t)f.chunks * a.sinks);
 }
-inline unsigned query_groups(const LocalAttention& a, int rows) {
-  return (unsigned)(((long)(rows + 31) / 32 * (a.heads / a.kv) + kWaves - 1) / kWaves);
+inline unsigned query_groups(const LocalAttention& a, int rows, int items = kWaves) {
+  return (unsigned)(((long)(rows + 31) / 32 * (a.heads / a.kv) + items - 1) / items);
 }
+// Two waves for 32 queries where one each would leave more SIMDs idle than not.  TWO_TEAMS_FIGURES
+inline bool dq_in_teams(const LocalAttention& a) { return (long)a.seqs * a.kv * ((stat_rows(a.S) / 32) * (a.heads / a.kv)) <= 1024; }
 
 template <class Kernel>
 hipError_t allow_lds(Kernel kernel) {
@@ -1260,14 +1287,19 @@ hipError_t run_bwd(hipStream_t s, const LocalAttention& a, const BwdArgs<T>& p) 
   constexpr size_t lds_q = std::max<size_t>(4 * TL::kBytes, kWaves * kTurnBytes) + bias_lds<kWaves>(BIAS);
   constexpr size_t lds_kv = std::max<size_t>(2 * (2 * TL::kBytes + 1024), kWaves * kTurnBytes) + dkv_bias_lds<kWaves>(BIAS);
   static_assert(lds_kv <= 160 * 1024, "tiles and sums do not fit the LDS of a CU");
-  auto dq = local_dq_kernel<T, DHP, kWaves, BIAS>;
+  constexpr int kTeams = TL::BR / 32;
+  auto dq = local_dq_kernel<T, DHP, kWaves, 1, BIAS>;
+  auto dq_teams = local_dq_kernel<T, DHP, kWaves, kTeams, BIAS>;
   auto dkv = local_dkv_kernel<T, DHP, kWaves, 1, BIAS>;
-  auto dkv_teams = local_dkv_kernel<T, DHP, kWaves, TL::BR / 32, BIAS>;
-  static hipError_t attr_q = allow_lds(dq), attr_kv = allow_lds(dkv), attr_teams = allow_lds(dkv_teams);
+  auto dkv_teams = local_dkv_kernel<T, DHP, kWaves, kTeams, BIAS>;
+  static hipError_t attr_q = allow_lds(dq), attr_q_teams = allow_lds(dq_teams), attr_kv = allow_lds(dkv), attr_teams = allow_lds(dkv_teams);
   if (attr_q != hipSuccess) return attr_q;
+  if (attr_q_teams != hipSuccess) return attr_q_teams;
   if (attr_kv != hipSuccess) return attr_kv;
   if (attr_teams != hipSuccess) return attr_teams;
-  hipLaunchKernelGGL(dq, dim3(a.seqs * a.kv, query_groups(a, stat_rows(a.S))), dim3(64 * kWaves), lds_q, s, p);
+  const bool teams = kTeams > 1 && dq_in_teams(a);
+  hipLaunchKernelGGL(teams ? dq_teams : dq, dim3(a.seqs * a.kv, query_groups(a, stat_rows(a.S), teams ? kWaves / kTeams : kWaves)), dim3(64 * kWaves),
+                     lds_q, s, p);
   hipError_t e = hipGetLastError();
   if (e != hipSuccess) return e;
   const DkvPlan f = dkv_plan<T, DHP>(a);
