@@ -339,7 +339,8 @@ __device__ __forceinline__ void turned_rows(const floatx16 (&acc)[TN], float fac
   }
 }
 
-// Sums of two waves over the same rows: one leaves its own in LDS, a lane's values 64 x 16 bytes apart, the other adds them to its own.
+// Sums of two waves over the same rows: one leaves its own in LDS, a lane's values 64 x 16 bytes apart, the other adds them to its own,
+// each with a factor.
 template <int TN>
 __device__ __forceinline__ void hand_over(const floatx16 (&acc)[TN], floatx4* to) {
 #pragma unroll
@@ -348,14 +349,14 @@ __device__ __forceinline__ void hand_over(const floatx16 (&acc)[TN], floatx4* to
     for (int r = 0; r < 4; ++r) to[(j * 4 + r) * 64] = floatx4{acc[j][4 * r], acc[j][4 * r + 1], acc[j][4 * r + 2], acc[j][4 * r + 3]};
 }
 template <int TN>
-__device__ __forceinline__ void take_over(floatx16 (&acc)[TN], const floatx4* from) {
+__device__ __forceinline__ void take_over(floatx16 (&acc)[TN], const floatx4* from, float mine = 1.f, float its = 1.f) {
 #pragma unroll
   for (int j = 0; j < TN; ++j)
 #pragma unroll
     for (int r = 0; r < 4; ++r) {
       const floatx4 v = from[(j * 4 + r) * 64];
 #pragma unroll
-      for (int e = 0; e < 4; ++e) acc[j][4 * r + e] += v[e];
+      for (int e = 0; e < 4; ++e) acc[j][4 * r + e] = fmaf(acc[j][4 * r + e], mine, v[e] * its);
     }
 }
 
@@ -496,11 +497,13 @@ struct QueryItems {
 // every new maximum: 55, 114 and, with a bias, 86 us of the following.)
 // 8 x 1024 tokens, 16 heads of 128, window 256: 46 us; 1 x 16384, 8 heads on 2, window 1024: 104 us, 0.65 PFLOP/s; 8 x 1024, 16 heads, all
 // keys: 55 us, with a bias 65.
-template <typename T, int DHP, int NW, bool BIAS>
-__global__ __launch_bounds__(64 * NW, sizeof(T) == 2 || DHP == 64 ? 3 : 2) void local_fwd_kernel(FwdArgs<T> p) {
+// TEAMS: 1, a wave has 32 queries of a head to itself; 2, blocks have 64 keys and two waves take 32 each, for launches that leave SIMDs without
+// a wave: their maxima, sums and outputs meet in LDS.
+template <typename T, int DHP, int NW, int TEAMS, bool BIAS>
+__global__ __launch_bounds__(64 * NW, TEAMS == 1 && (sizeof(T) == 2 || DHP == 64) ? 3 : 2) void local_fwd_kernel(FwdArgs<T> p) {
   using TY = Type<T>;
-  using TL = Tile<T, DHP, NW, 32>;
-  constexpr int BR = TL::BR, NT = BR / 32, KK = DHP / 16, TN = DHP / 32;
+  using TL = Tile<T, DHP, NW, 32 * TEAMS>;
+  constexpr int BR = TL::BR, kMine = BR / TEAMS, NT = kMine / 32, KK = DHP / 16, TN = DHP / 32;
   extern __shared__ __attribute__((aligned(16))) char lds[];
   const Shape& a = p.a;
   const int lane = threadIdx.x & 63, half = lane >> 5;
@@ -508,7 +511,8 @@ __global__ __launch_bounds__(64 * NW, sizeof(T) == 2 || DHP == 64 ? 3 : 2) void 
   const int group = a.heads / a.kv, b = blockIdx.x / a.kv, kvh = blockIdx.x - b * a.kv;
   const int S = a.S, dh = a.dh;
   const size_t ld = a.ld(), D = (size_t)a.heads * dh;
-  const QueryItems<BR, NW> it(a, group, (S + 31) / 32, gridDim.y - 1 - blockIdx.y, wave);
+  const int team = wave / (NW / TEAMS);
+  const QueryItems<BR, NW / TEAMS> it(a, group, (S + 31) / 32, gridDim.y - 1 - blockIdx.y, wave % (NW / TEAMS));
   const bool active = it.item < it.items;
   const int h = kvh * group + (active ? it.g : 0), qw = (active ? it.blk : 0) * 32;
   const T* base = p.x + (size_t)b * S * ld;
@@ -554,10 +558,10 @@ __global__ __launch_bounds__(64 * NW, sizeof(T) == 2 || DHP == 64 ? 3 : 2) void 
     wait_vmcnt<0>();
     lds_barrier();  // block t is there, and nobody reads the other stage any more
     if (t + 1 < it.count) issue(t + 1);
-    const int kb = it.block(t) * BR;
+    const int skip = TEAMS == 1 ? 0 : team * kMine, kb = it.block(t) * BR + skip;
     // wave uniform: some pair of this wave and block is visible
-    if (!active || kb > q_last || (kb >= a.sinks && kb + BR - 1 <= qw - a.window)) continue;
-    const uint32_t stage = lds0 + (t & 1) * 2 * TL::kBytes, lk = stage + row_at, lv = stage + col_at;
+    if (!active || kb > q_last || (kb >= a.sinks && kb + kMine - 1 <= qw - a.window)) continue;
+    const uint32_t stage = lds0 + (t & 1) * 2 * TL::kBytes + skip * 128, lk = stage + row_at, lv = stage + col_at;
     floatx16 sacc[NT];
 #pragma unroll
     for (int u = 0; u < NT; ++u)
@@ -571,8 +575,8 @@ __global__ __launch_bounds__(64 * NW, sizeof(T) == 2 || DHP == 64 ? 3 : 2) void 
 #pragma unroll
     for (int i = 0; i < TY::kAhead; ++i) ahead[i] = v_frag(i);
     __builtin_amdgcn_sched_barrier(0);
-    const int dmin = qw - (kb + BR - 1), dmax = qw + 31 - kb;
-    const bool masked = !(dmin >= 0 && (dmax < a.window || kb + BR <= a.sinks));
+    const int dmin = qw - (kb + kMine - 1), dmax = qw + 31 - kb;
+    const bool masked = !(dmin >= 0 && (dmax < a.window || kb + kMine <= a.sinks));
     // distance of element r of tile u: d0 - 32 u - 8 (r / 4) - r % 4
     const int d0 = query - kb - 4 * half, sink0 = a.sinks - kb - 4 * half;
     float mx = -INFINITY;
@@ -580,7 +584,7 @@ __global__ __launch_bounds__(64 * NW, sizeof(T) == 2 || DHP == 64 ? 3 : 2) void 
     for (int u = 0; u < NT; ++u) {
       if constexpr (BIAS) {
         float bias[16];
-        tile_bias<-1>(*bl, TileBuckets(p.db, first, dmin + BR - 32 * (u + 1), dmax - 32 * u), first, d0 - 32 * u, bias);
+        tile_bias<-1>(*bl, TileBuckets(p.db, first, dmin + kMine - 32 * (u + 1), dmax - 32 * u), first, d0 - 32 * u, bias);
 #pragma unroll
         for (int r = 0; r < 16; ++r) sacc[u][r] = fmaf(sacc[u][r], p.scale_log2, bias[r]);
       }
@@ -621,7 +625,24 @@ __global__ __launch_bounds__(64 * NW, sizeof(T) == 2 || DHP == 64 ? 3 : 2) void 
     pipelined<2 * NT * TN>(ahead, v_frag, [&](int i, const typename TY::Frag& f) { if (!TY::skips(32 * (i % TN), dh)) oacc[i % TN] = TY::mma(f, pf[i / TN], oacc[i % TN]); }, true);
   }
   lds_barrier();  // the stages are free
-  if (!active) return;
+  if constexpr (TEAMS == 2) {
+    floatx4* theirs = reinterpret_cast<floatx4*>(lds) + (size_t)(wave % (NW / TEAMS)) * TN * 4 * 64 + lane;
+    float2* stats = reinterpret_cast<float2*>(lds + (size_t)NW / TEAMS * TN * 4 * 64 * 16) + wave % (NW / TEAMS) * 64 + lane;
+    if (team == 1) {
+      hand_over(oacc, theirs);
+      *stats = make_float2(mrun, lsum);
+    }
+    lds_barrier();
+    if (team == 0) {
+      const float2 other = *stats;
+      const float m = fmaxf(mrun, other.x), mine = __builtin_amdgcn_exp2f(mrun - m), its = __builtin_amdgcn_exp2f(other.x - m);
+      mrun = m;
+      lsum = fmaf(lsum, mine, other.y * its);
+      take_over(oacc, theirs, mine, its);
+    }
+    lds_barrier();
+  }
+  if (!active || team != 0) return;
   const float ltot = over_halves(lsum, Add());
   const float inv = 1.f / ltot;
 #pragma unroll
@@ -1262,8 +1283,12 @@ inline size_t sum_floats(const LocalAttention& a, const DkvPlan& f) {
 inline unsigned query_groups(const LocalAttention& a, int rows, int items = kWaves) {
   return (unsigned)(((long)(rows + 31) / 32 * (a.heads / a.kv) + items - 1) / items);
 }
-// Two waves for 32 queries where one each would leave more SIMDs idle than not.  TWO_TEAMS_FIGURES
-inline bool dq_in_teams(const LocalAttention& a) { return (long)a.seqs * a.kv * ((stat_rows(a.S) / 32) * (a.heads / a.kv)) <= 1024; }
+// Forward and dQ: two waves for 32 queries where one each would not give every SIMD of the 256 CUs a wave, and there is more than one tile to
+// share.  fp32, 4 x 512 tokens, 8 heads of 64 (512 waves): forward 32 -> 18 us, dQ 40 -> 24; bf16, 4 x 777, 6 heads of 80 on 2 (624): 25 -> 19 and
+// 27 -> 21; 32 x 200, 8 heads (2048): 16.6 -> 17.8 and 15.5 -> 19.1; 16 tokens: 4.4 -> 5.0 and the same.
+inline bool in_teams(const LocalAttention& a) {
+  return a.S > 32 && (long)a.seqs * a.kv * ((stat_rows(a.S) / 32) * (a.heads / a.kv)) <= 1024;
+}
 
 template <class Kernel>
 hipError_t allow_lds(Kernel kernel) {
@@ -1272,13 +1297,17 @@ hipError_t allow_lds(Kernel kernel) {
 
 template <typename T, int DHP, bool BIAS>
 hipError_t run_fwd(hipStream_t s, const LocalAttention& a, const FwdArgs<T>& p) {
-  using TL = Tile<T, DHP, kWaves, 32>;
-  constexpr size_t lds = std::max<size_t>(4 * TL::kBytes, kWaves * kTurnBytes) + bias_lds<kWaves>(BIAS);
-  auto kernel = local_fwd_kernel<T, DHP, kWaves, BIAS>;
-  static hipError_t attr = allow_lds(kernel);
-  if (attr != hipSuccess) return attr;
-  hipLaunchKernelGGL(kernel, dim3(a.seqs * a.kv, query_groups(a, a.S)), dim3(64 * kWaves), lds, s, p);
-  return hipGetLastError();
+  auto launch = [&](auto kernel, auto teams) {
+    constexpr int kTeams = decltype(teams)::value;
+    constexpr size_t lds = std::max<size_t>(4 * Tile<T, DHP, kWaves, 32 * kTeams>::kBytes, kWaves * kTurnBytes) + bias_lds<kWaves>(BIAS);
+    static_assert(lds <= 160 * 1024, "stages and tables do not fit the LDS of a CU");
+    static hipError_t attr = allow_lds(kernel);
+    if (attr != hipSuccess) return attr;
+    hipLaunchKernelGGL(kernel, dim3(a.seqs * a.kv, query_groups(a, a.S, kWaves / kTeams)), dim3(64 * kWaves), lds, s, p);
+    return hipGetLastError();
+  };
+  if (in_teams(a)) return launch(local_fwd_kernel<T, DHP, kWaves, 2, BIAS>, std::integral_constant<int, 2>());
+  return launch(local_fwd_kernel<T, DHP, kWaves, 1, BIAS>, std::integral_constant<int, 1>());
 }
 
 template <typename T, int DHP, bool BIAS>
@@ -1297,7 +1326,7 @@ hipError_t run_bwd(hipStream_t s, const LocalAttention& a, const BwdArgs<T>& p) 
   if (attr_q_teams != hipSuccess) return attr_q_teams;
   if (attr_kv != hipSuccess) return attr_kv;
   if (attr_teams != hipSuccess) return attr_teams;
-  const bool teams = kTeams > 1 && dq_in_teams(a);
+  const bool teams = kTeams > 1 && in_teams(a);
   hipLaunchKernelGGL(teams ? dq_teams : dq, dim3(a.seqs * a.kv, query_groups(a, stat_rows(a.S), teams ? kWaves / kTeams : kWaves)), dim3(64 * kWaves),
                      lds_q, s, p);
   hipError_t e = hipGetLastError();

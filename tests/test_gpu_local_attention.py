@@ -168,6 +168,7 @@ LAUNCHES = [
     # as many sequences as fill the chip: a workgroup takes all of a key head, first keys among them
     _case(70, heads=8, kv=8, dh=16, seqs=64), _case(90, heads=8, kv=8, dh=80, window=20, sinks=2, buckets=8, reach=30, seqs=64),
     _case(70, heads=8, kv=8, dh=32, window=30, sinks=3, buckets=32, reach=64, seqs=64),
+    _case(100, heads=8, kv=8, dh=128, window=40, sinks=1, seqs=40), _case(130, heads=16, kv=4, dh=64, buckets=16, reach=100, seqs=20),
     # more workgroups than the chip runs at a time, the first of them with longer walks
     _case(300, heads=16, kv=16, dh=64, window=40, sinks=1, buckets=16, reach=100, seqs=20), _case(1100, heads=8, kv=8, dh=16, window=100, sinks=3, seqs=8),
     # one long sequence: walks in parts, pairs of first keys in many chunks, first keys over several workgroups; parts that begin within a
