@@ -208,16 +208,23 @@ __device__ __forceinline__ uint4 pack(const float (&v)[kVec<T>]) {
     return make_uint4(__float_as_uint(v[0]), __float_as_uint(v[1]), __float_as_uint(v[2]), __float_as_uint(v[3]));
 }
 
-// Which exponentials a row needs.  kOne: of one scale (the teacher or the labels alone, or a temperature of 1); kSquare: the temperature
-// is 2, so that exp(x) is the square of exp(x / 2); kTwo: both.  An exponential costs a wave 16 cycles, any other instruction here 4.
-enum Exponentials : int { kOne = 0, kSquare = 1, kTwo = 2 };
+// A value of which the compiler forgets what has been worked out from it before, and holds none of that.
+__device__ __forceinline__ float afresh(float v) {
+  asm volatile("" : "+v"(v));
+  return v;
+}
 
-// A row is read once and held in registers, from the second step on as its exponentials: HELD units of 16 bytes for each of its NT threads.
+// Which exponentials a row needs.  kOne: of one scale (the teacher or the labels alone, or a temperature of 1), held in the logits' place from the
+// second step on; kTwo: both, whose power is held and whose exponentials are formed for the sums and again for the gradient.  8192 x 32000 in
+// bf16: 217 us with one, 278 with two (holding both, which leaves a SIMD one wave, 407).
+enum Exponentials : int { kOne = 0, kTwo = 1 };
+
+// A row is read once and held in registers, HELD units of 16 bytes for each of its NT threads, and written once.
 // Rows may start at any element: units lie at 16-byte addresses, and the first and last, which other rows share, are read and written one
-// by one.  Reading and writing at the rate of a copy is the floor; what comes near it is instructions, 12 for a logit with kSquare (29
-// with both exponentials formed twice, before they were held).
+// by one.  Reading and writing at the rate of a copy is the floor (218 us at 8192 x 32000); what comes near it is instructions, an exponential
+// taking a wave 16 cycles and any other 4.
 template <typename T, int NT, int HELD, int EXPS>
-__global__ __launch_bounds__(Team<NT>::kThreads, HELD * kVec<T> == 64 && EXPS != kTwo ? 4 : 1) void distill_held_kernel(DistillArgs a) {
+__global__ __launch_bounds__(Team<NT>::kThreads, HELD * kVec<T> == 64 ? 4 : 1) void distill_held_kernel(DistillArgs a) {
   using TM = Team<NT>;
   constexpr int V = kVec<T>;
   __shared__ float sm_all[TM::kThreads / 64];
@@ -263,23 +270,23 @@ __global__ __launch_bounds__(Team<NT>::kThreads, HELD * kVec<T> == 64 && EXPS !=
     top = TM::over(top, sm, Max());
     Row r;
     r.top_soft = top * c.soft;
-    r.top_hard = EXPS == kSquare ? 2.f * r.top_soft : top * c.hard;
-    // with one exponential it is that of the only scale
+    r.top_hard = top * c.hard;
+    // with one exponential it is that of the only scale; with two, one's power is the other's times the temperature
     const bool only_hard = EXPS == kOne && a.label_weight >= 1.f;
     const float scale = only_hard ? c.hard : c.soft, shift = only_hard ? r.top_hard : r.top_soft;
-    float other[EXPS == kTwo ? HELD : 1][V];
     float soft = 0.f, hard = 0.f;
 #pragma unroll
     for (int i = 0; i < HELD; ++i)
 #pragma unroll
       for (int e = 0; e < V; ++e) {
+        const float power = fmaf(x[i][e], scale, -shift), of_soft = __builtin_amdgcn_exp2f(power);
+        soft += of_soft;
         if constexpr (EXPS == kTwo) {
-          other[i][e] = __builtin_amdgcn_exp2f(fmaf(x[i][e], c.hard, -r.top_hard));
-          hard += other[i][e];
+          hard += __builtin_amdgcn_exp2f(power * a.temperature);  // as far off as the other's power is, relative to its size
+          x[i][e] = power;
+        } else {
+          x[i][e] = of_soft;
         }
-        x[i][e] = __builtin_amdgcn_exp2f(fmaf(x[i][e], scale, -shift));
-        soft += x[i][e];
-        if constexpr (EXPS == kSquare) hard = fmaf(x[i][e], x[i][e], hard);
       }
     soft = TM::over(soft, sm, Add());
     hard = EXPS == kOne ? soft : TM::over(hard, sm, Add());
@@ -291,9 +298,12 @@ __global__ __launch_bounds__(Team<NT>::kThreads, HELD * kVec<T> == 64 && EXPS !=
       const int u = thread + NT * i;
 #pragma unroll
       for (int e = 0; e < V; ++e) {
-        if constexpr (EXPS == kOne) x[i][e] *= one;
-        else if constexpr (EXPS == kSquare) x[i][e] *= fmaf(r.hard, x[i][e], r.soft);
-        else x[i][e] = fmaf(r.hard, other[i][e], r.soft * x[i][e]);
+        if constexpr (EXPS == kOne) {
+          x[i][e] *= one;
+        } else {
+          const float power = afresh(x[i][e]);
+          x[i][e] = fmaf(r.hard, __builtin_amdgcn_exp2f(power * a.temperature), r.soft * __builtin_amdgcn_exp2f(power));
+        }
       }
       if (u >= whole_from && u < whole_to) {
         *reinterpret_cast<uint4*>(dl - lead + (size_t)u * V) = pack<T>(x[i]);
@@ -390,8 +400,7 @@ hipError_t launch_held(hipStream_t s, DistillArgs a) {
   if (blocks > kCounted) a.counter = nullptr;
   const size_t lds = (size_t)TM::kRows * 2 * (a.k + 1) * sizeof(float);
   const bool one = a.label_weight <= 0.f || a.label_weight >= 1.f || a.temperature == 1.f;
-  auto kernel = one ? distill_held_kernel<T, NT, HELD, kOne>
-                    : a.temperature == 2.f ? distill_held_kernel<T, NT, HELD, kSquare> : distill_held_kernel<T, NT, HELD, kTwo>;
+  auto kernel = one ? distill_held_kernel<T, NT, HELD, kOne> : distill_held_kernel<T, NT, HELD, kTwo>;
   hipLaunchKernelGGL(kernel, dim3(blocks), dim3(TM::kThreads), lds, s, a);
   return finish(s, a);
 }
