@@ -54,21 +54,28 @@ struct Team {
   }
 };
 
-// Exponents: exp(x / T) = 2^(x c), with everything relative to the row's maximum, 2^(x c - top c).  top c is rounded once and enters
-// numerators, sums and logarithms alike, so that its rounding cancels.
-struct Scale {
-  float soft, hard;  // c for 1 / T and for 1
-  __device__ __forceinline__ explicit Scale(const DistillArgs& a) : soft(kLog2e / a.temperature), hard(kLog2e) {}
-};
+// Exponents: exp(z / T) = 2^(power), power = z c - top c with c = log2(e) / T and the row's maximum `top`; exp(z) = 2^(T power).  top c is
+// rounded once and its rounding, that of `max / T`, is large where all of a row's logits are: it cancels because every numerator, sum and
+// logarithm of both exponentials is formed from this one power.  (With labels alone c = log2(e) and the power is that of exp(z) itself.)
+// T = 3, logits around 1000 or 10000, the label's logarithm from z log2(e) - top log2(e) instead: cross entropy 4e-5 or 2e-4 off.
 struct Row {
-  float top_soft, top_hard;  // the maximum times the scales
-  float soft, hard;          // what 2^(x c - top c) is multiplied with in the gradient
+  float scale, shift;  // c and top c
+  float to_hard;       // what turns the power into that of exp(z)
+  float soft, hard;    // what the exponentials are multiplied with in the gradient
+  __device__ __forceinline__ Row(const DistillArgs& a, float soft_scale, float top) {
+    const bool only_hard = a.label_weight >= 1.f;
+    scale = only_hard ? kLog2e : soft_scale;
+    to_hard = only_hard ? 1.f : a.temperature;
+    shift = top * scale;
+  }
+  __device__ __forceinline__ float power(float z) const { return fmaf(z, scale, -shift); }
+  __device__ __forceinline__ float gradient(float z) const {
+    const float p = power(z);
+    float g = soft == 0.f ? 0.f : soft * __builtin_amdgcn_exp2f(p);
+    if (hard != 0.f) g = fmaf(hard, __builtin_amdgcn_exp2f(p * to_hard), g);
+    return g;
+  }
 };
-__device__ __forceinline__ float gradient(const Row& r, const Scale& c, float z) {
-  float g = r.soft == 0.f ? 0.f : r.soft * __builtin_amdgcn_exp2f(fmaf(z, c.soft, -r.top_soft));
-  if (r.hard != 0.f) g = fmaf(r.hard, __builtin_amdgcn_exp2f(fmaf(z, c.hard, -r.top_hard)), g);
-  return g;
-}
 
 // A thread's first entry and the row's label, fetched in two steps: the classes ahead of the row, their logits behind it, so that neither is
 // waited for by itself.
@@ -92,8 +99,8 @@ struct First {
 // The stored entries and the label, behind the row's maximum and sums.  share[e] (LDS): what entry e takes off the gradient of its
 // class, e = k for the label; id[e]: its class, -1 none.  Completes r and returns the row's loss in every thread.
 template <int NT, typename T>
-__device__ __forceinline__ float entries(const DistillArgs& a, const Scale& c, int row, const T* lg, const First& f, float sum_hard, float sum_soft,
-                                         float* sm, float* share, int* id, Row* r) {
+__device__ __forceinline__ float entries(const DistillArgs& a, float soft_scale, int row, const T* lg, const First& f, float sum_hard,
+                                         float sum_soft, float* sm, float* share, int* id, Row* r) {
   using TM = Team<NT>;
   const int thread = TM::thread();
   const float inv_rows = 1.f / (float)a.rows;
@@ -109,13 +116,13 @@ __device__ __forceinline__ float entries(const DistillArgs& a, const Scale& c, i
   tm = TM::over(tm, sm, Max());
   const bool has = tm != -INFINITY && a.label_weight < 1.f;
   float total = 0.f;
-  for (int e = thread; e < a.k; e += NT) total += has ? __builtin_amdgcn_exp2f((share[e] - tm) * c.soft) : 0.f;
+  for (int e = thread; e < a.k; e += NT) total += has ? __builtin_amdgcn_exp2f((share[e] - tm) * soft_scale) : 0.f;
   total = TM::over(total, sm, Add());
   const float log_total = __builtin_amdgcn_logf(total), log_soft = __builtin_amdgcn_logf(sum_soft);  // base 2
   const float weight = (1.f - a.label_weight) * a.temperature * inv_rows;
   float kl = 0.f;
   for (int e = thread; e < a.k; e += NT) {
-    const float log_p = has ? (share[e] - tm) * c.soft - log_total : -INFINITY;
+    const float log_p = has ? (share[e] - tm) * soft_scale - log_total : -INFINITY;
     const float p = has ? __builtin_amdgcn_exp2f(log_p) : 0.f;
     share[e] = weight * p;
     if (id[e] >= a.classes) {
@@ -123,14 +130,14 @@ __device__ __forceinline__ float entries(const DistillArgs& a, const Scale& c, i
       id[e] = -1;
     } else if (id[e] >= 0 && p != 0.f) {
       const float z = e == thread ? f.z : to_float(lg[id[e]]);
-      kl += p * (log_p - (fmaf(z, c.soft, -r->top_soft) - log_soft));
+      kl += p * (log_p - (r->power(z) - log_soft));
     }
   }
   kl = TM::over(kl, sm, Add()) * kLn2;
   float loss = a.label_weight < 1.f ? (1.f - a.label_weight) * a.temperature * a.temperature * kl : 0.f;
   if (a.label_weight > 0.f) {
     const bool known = (unsigned)f.label < (unsigned)a.classes;
-    const float ce = known ? __builtin_amdgcn_logf(sum_hard) - fmaf(f.z_label, c.hard, -r->top_hard) : __builtin_nanf("");
+    const float ce = known ? __builtin_amdgcn_logf(sum_hard) - r->power(f.z_label) * r->to_hard : __builtin_nanf("");
     loss += a.label_weight * kLn2 * ce;
     if (thread == 0) {
       id[a.k] = known ? f.label : -1;
@@ -146,8 +153,7 @@ __device__ __forceinline__ float entries(const DistillArgs& a, const Scale& c, i
 
 // The gradient of the entries' classes, behind the stores of the others: the first entry of a class takes off what all of it do.
 template <int NT, typename T>
-__device__ __forceinline__ void finish_entries(const DistillArgs& a, const Scale& c, const T* lg, T* dl, const Row& r, const float* share,
-                                               const int* id) {
+__device__ __forceinline__ void finish_entries(const DistillArgs& a, const T* lg, T* dl, const Row& r, const float* share, const int* id) {
   for (int e = Team<NT>::thread(); e <= a.k; e += NT) {
     const int mine = id[e];
     if (mine < 0) continue;
@@ -158,7 +164,7 @@ __device__ __forceinline__ void finish_entries(const DistillArgs& a, const Scale
         first = first && f >= e;
         off += share[f];
       }
-    if (first) dl[mine] = from_float<T>(gradient(r, c, to_float(lg[mine])) - off);
+    if (first) dl[mine] = from_float<T>(r.gradient(to_float(lg[mine])) - off);
   }
 }
 
@@ -233,7 +239,7 @@ __global__ __launch_bounds__(Team<NT>::kThreads, HELD * kVec<T> == 64 ? 4 : 1) v
   float* sm = sm_all;
   float* share = entry_lds + TM::which() * 2 * (a.k + 1);
   int* id = reinterpret_cast<int*>(share + a.k + 1);
-  const Scale c(a);
+  const float soft_scale = kLog2e / a.temperature;
   if (row < a.rows) {
     const T* lg = (const T*)a.logits + (size_t)row * a.classes;
     T* dl = (T*)a.dlogits + (size_t)row * a.classes;
@@ -268,29 +274,24 @@ __global__ __launch_bounds__(Team<NT>::kThreads, HELD * kVec<T> == 64 ? 4 : 1) v
 #pragma unroll
       for (int e = 0; e < V; ++e) top = fmaxf(top, x[i][e]);
     top = TM::over(top, sm, Max());
-    Row r;
-    r.top_soft = top * c.soft;
-    r.top_hard = top * c.hard;
-    // with one exponential it is that of the only scale; with two, one's power is the other's times the temperature
-    const bool only_hard = EXPS == kOne && a.label_weight >= 1.f;
-    const float scale = only_hard ? c.hard : c.soft, shift = only_hard ? r.top_hard : r.top_soft;
+    Row r(a, soft_scale, top);
     float soft = 0.f, hard = 0.f;
 #pragma unroll
     for (int i = 0; i < HELD; ++i)
 #pragma unroll
       for (int e = 0; e < V; ++e) {
-        const float power = fmaf(x[i][e], scale, -shift), of_soft = __builtin_amdgcn_exp2f(power);
-        soft += of_soft;
+        const float power = r.power(x[i][e]), one = __builtin_amdgcn_exp2f(power);
+        soft += one;
         if constexpr (EXPS == kTwo) {
-          hard += __builtin_amdgcn_exp2f(power * a.temperature);  // as far off as the other's power is, relative to its size
+          hard += __builtin_amdgcn_exp2f(power * r.to_hard);
           x[i][e] = power;
         } else {
-          x[i][e] = of_soft;
+          x[i][e] = one;
         }
       }
     soft = TM::over(soft, sm, Add());
     hard = EXPS == kOne ? soft : TM::over(hard, sm, Add());
-    const float loss = entries<NT>(a, c, row, lg, entry, hard, soft, sm, share, id, &r);
+    const float loss = entries<NT>(a, soft_scale, row, lg, entry, hard, soft, sm, share, id, &r);
     if (thread == 0) publish(a.row_loss + row, loss);
     const float one = r.soft + r.hard;  // kOne: both are of the same exponential
 #pragma unroll
@@ -302,7 +303,7 @@ __global__ __launch_bounds__(Team<NT>::kThreads, HELD * kVec<T> == 64 ? 4 : 1) v
           x[i][e] *= one;
         } else {
           const float power = afresh(x[i][e]);
-          x[i][e] = fmaf(r.hard, __builtin_amdgcn_exp2f(power * a.temperature), r.soft * __builtin_amdgcn_exp2f(power));
+          x[i][e] = fmaf(r.hard, __builtin_amdgcn_exp2f(power * r.to_hard), r.soft * __builtin_amdgcn_exp2f(power));
         }
       }
       if (u >= whole_from && u < whole_to) {
@@ -317,7 +318,7 @@ __global__ __launch_bounds__(Team<NT>::kThreads, HELD * kVec<T> == 64 ? 4 : 1) v
     }
     asm volatile("s_waitcnt vmcnt(0)" ::: "memory");  // the row is stored before single values of it are replaced
     TM::sync();
-    finish_entries<NT>(a, c, lg, dl, r, share, id);
+    finish_entries<NT>(a, lg, dl, r, share, id);
   }
   finish_mean(a);
 }
@@ -330,7 +331,7 @@ __global__ __launch_bounds__(kThreads) void distill_rows_kernel(DistillArgs a) {
   extern __shared__ float entry_lds[];
   float* share = entry_lds;
   int* id = reinterpret_cast<int*>(share + a.k + 1);
-  const Scale c(a);
+  const float soft_scale = kLog2e / a.temperature;
   const bool labels = a.label_weight > 0.f;
   for (int row = blockIdx.x; row < a.rows; row += gridDim.x) {
     const T* lg = (const T*)a.logits + (size_t)row * a.classes;
@@ -340,23 +341,21 @@ __global__ __launch_bounds__(kThreads) void distill_rows_kernel(DistillArgs a) {
     float top = -INFINITY;
     for (int j = threadIdx.x; j < a.classes; j += kThreads) top = fmaxf(top, to_float(lg[j]));
     top = Team<kThreads>::over(top, sm, Max());
-    Row r;
-    r.top_soft = top * c.soft;
-    r.top_hard = top * c.hard;
+    Row r(a, soft_scale, top);
     float hard = 0.f, soft = 0.f;
     for (int j = threadIdx.x; j < a.classes; j += kThreads) {
-      const float z = to_float(lg[j]);
-      soft += __builtin_amdgcn_exp2f(fmaf(z, c.soft, -r.top_soft));
-      if (labels) hard += __builtin_amdgcn_exp2f(fmaf(z, c.hard, -r.top_hard));
+      const float power = r.power(to_float(lg[j]));
+      soft += __builtin_amdgcn_exp2f(power);
+      if (labels) hard += __builtin_amdgcn_exp2f(power * r.to_hard);
     }
     soft = Team<kThreads>::over(soft, sm, Add());
     if (labels) hard = Team<kThreads>::over(hard, sm, Add());
-    const float loss = entries<kThreads>(a, c, row, lg, entry, hard, soft, sm, share, id, &r);
+    const float loss = entries<kThreads>(a, soft_scale, row, lg, entry, hard, soft, sm, share, id, &r);
     if (threadIdx.x == 0) publish(a.row_loss + row, loss);
-    for (int j = threadIdx.x; j < a.classes; j += kThreads) dl[j] = from_float<T>(gradient(r, c, to_float(lg[j])));
+    for (int j = threadIdx.x; j < a.classes; j += kThreads) dl[j] = from_float<T>(r.gradient(to_float(lg[j])));
     asm volatile("s_waitcnt vmcnt(0)" ::: "memory");  // the row is stored before single values of it are replaced
     __syncthreads();
-    finish_entries<kThreads>(a, c, lg, dl, r, share, id);
+    finish_entries<kThreads>(a, lg, dl, r, share, id);
     __syncthreads();  // the entries' LDS is free
   }
   finish_mean(a);
