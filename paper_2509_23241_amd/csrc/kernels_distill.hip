@@ -58,17 +58,22 @@ struct Team {
 // rounded once and its rounding, that of `max / T`, is large where all of a row's logits are: it cancels because every numerator, sum and
 // logarithm of both exponentials is formed from this one power.  (With labels alone c = log2(e) and the power is that of exp(z) itself.)
 // T = 3, logits around 1000 or 10000, the label's logarithm from z log2(e) - top log2(e) instead: cross entropy 4e-5 or 2e-4 off.
+// Where top c is so large that its rounding alone could take an exponential out of range (T = 1e-6, logits of some thousands) the maximum is
+// taken off the logits themselves first, at one more operation for each of them.
 struct Row {
-  float scale, shift;  // c and top c
+  float base;          // what is taken off every logit first: 0 or top
+  float scale, shift;  // c and top c, or 0 where top is taken off
   float to_hard;       // what turns the power into that of exp(z)
   float soft, hard;    // what the exponentials are multiplied with in the gradient
   __device__ __forceinline__ Row(const DistillArgs& a, float soft_scale, float top) {
     const bool only_hard = a.label_weight >= 1.f;
     scale = only_hard ? kLog2e : soft_scale;
     to_hard = only_hard ? 1.f : a.temperature;
-    shift = top * scale;
+    base = fabsf(top * scale) > 0x1p24f ? top : 0.f;  // from 2^24 on the rounding is 1 and more
+    shift = (top - base) * scale;
   }
-  __device__ __forceinline__ float power(float z) const { return fmaf(z, scale, -shift); }
+  __device__ __forceinline__ float power_of_rest(float z) const { return fmaf(z, scale, -shift); }  // base is taken off z
+  __device__ __forceinline__ float power(float z) const { return power_of_rest(z - base); }
   __device__ __forceinline__ float gradient(float z) const {
     const float p = power(z);
     float g = soft == 0.f ? 0.f : soft * __builtin_amdgcn_exp2f(p);
@@ -275,12 +280,18 @@ __global__ __launch_bounds__(Team<NT>::kThreads, HELD * kVec<T> == 64 ? 4 : 1) v
       for (int e = 0; e < V; ++e) top = fmaxf(top, x[i][e]);
     top = TM::over(top, sm, Max());
     Row r(a, soft_scale, top);
+    if (r.base != 0.f) {
+#pragma unroll
+      for (int i = 0; i < HELD; ++i)
+#pragma unroll
+        for (int e = 0; e < V; ++e) x[i][e] -= r.base;
+    }
     float soft = 0.f, hard = 0.f;
 #pragma unroll
     for (int i = 0; i < HELD; ++i)
 #pragma unroll
       for (int e = 0; e < V; ++e) {
-        const float power = r.power(x[i][e]), one = __builtin_amdgcn_exp2f(power);
+        const float power = r.power_of_rest(x[i][e]), one = __builtin_amdgcn_exp2f(power);
         soft += one;
         if constexpr (EXPS == kTwo) {
           hard += __builtin_amdgcn_exp2f(power * r.to_hard);

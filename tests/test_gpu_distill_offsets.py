@@ -75,3 +75,42 @@ def test_the_error_does_not_grow_with_what_all_logits_have_in_common(classes, dt
         assert off <= eloss + F * abs(want), (t, w)
         assert share <= 1.0, (t, w)
     st.close()
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("classes", [20, 1500, 40001, 140000])
+@pytest.mark.parametrize("t,offset", [(1e-6, 2000.0), (1e-6, 30000.0), (1e-5, 1e6), (1e-6, -30000.0), (1e-6, 1e12)])
+def test_logits_far_beyond_the_temperature(t, offset, classes, dtype):
+    """All probability on the largest logit, whatever max / T is rounded by.  The loss of an entry that lies `gap` below is T gap, the gradient
+    T on the one class and -T on the other; each is a product of five rounded factors at most."""
+    import torch
+    rows = 5
+    tt = torch.float32 if dtype == "f32" else torch.bfloat16
+    base = torch.tensor(offset).to(tt).double()
+    step = 2.0 ** (math.floor(math.log2(abs(offset))) - (6 if dtype == "bf16" else 20))
+    z = (base - step * (2 + torch.arange(classes).double() % 3)).repeat(rows, 1)
+    best, entry = torch.arange(rows) + 3, torch.arange(rows) + 11
+    z[torch.arange(rows), best] = base
+    z[torch.arange(rows), entry] = base - 3 * step
+    stored = z.to(tt)
+    assert bool((stored.double() == z).all())
+    st = _stage(dtype, rows, classes)
+    teacher = torch.zeros(rows, 2, device="cuda")
+    ids = torch.stack([entry, torch.full((rows,), -1)], 1).to(torch.int32).contiguous().cuda()
+    for w in (0.0, 0.5):
+        labels = entry.to(torch.int32).cuda()
+        loss, grad = st.loss_distill(0, stored.cuda(), teacher, ids, temperature=t, labels=labels, label_weight=w)
+        hard = torch.exp(z - base).sum(1).log() + 3 * step       # of the labels' softmax: the classes within some 100 of the maximum
+        want = (1 - w) * t * 3 * step + w * float(hard.mean())
+        # chain of its sum and one logarithm, as above, and the exponents of classes that count (within 18 of the maximum)
+        eloss = 16 * F * want + w * F * (min(classes, 64) + 24 + classes / 256 + 4 * 18 + 2 * (1 + math.log2(classes)))
+        assert abs(float(loss) - want) <= eloss, (w, float(loss), want, eloss)
+        if w == 0.0:
+            dwant = torch.zeros(rows, classes, dtype=torch.float64)
+            dwant[torch.arange(rows), best] = t / rows
+            dwant[torch.arange(rows), entry] = -t / rows
+            off = (grad.double().cpu() - dwant).abs()
+            assert bool((off <= dwant.abs() * (16 * F + (2.0 ** -8 if dtype == "bf16" else 0))).all())
+        else:
+            assert bool(torch.isfinite(grad).all())
+    st.close()
