@@ -311,7 +311,8 @@ int stage_loss_softmax_ce(tp_stage* st, uint64_t mb_id, const void* logits_dev,
  *   row = label_weight * -log s[label] + (1 - label_weight) * temperature^2 * sum over entries of p (log p - log q[id]),
  * the loss is the mean over the rows (row values in fp32, added up in fp64), dlogits_dev its gradient.
  * teacher_logits_dev: float[rows * k], teacher_ids_dev: int32[rows * k], the class of each entry, negative: no entry (a row may
- * have fewer than k, or none: then, or if all its teacher logits are -inf, it has no second term).  An entry twice counts twice.
+ * have fewer than k, or none: then, or if all its teacher logits are -inf, it has no second term, and with label_weight 0 a loss and
+ * gradient of 0 whatever its logits hold).  An entry twice counts twice.
  * labels_dev: int32[rows]; with label_weight 0 it is not read and may be NULL, with label_weight 1 the teacher has no part.
  * A class or label that does not exist (id >= classes; label outside 0 .. classes - 1) makes the loss NaN; the gradient is that
  * of the other terms.  logits_dev and dlogits_dev must not overlap.  TP_EINVAL: k outside 1 .. TP_MAX_TEACHER_ENTRIES, a

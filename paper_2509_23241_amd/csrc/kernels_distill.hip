@@ -305,6 +305,12 @@ __global__ __launch_bounds__(Team<NT>::kThreads, HELD * kVec<T> == 64 ? 4 : 1) v
     const float loss = entries<NT>(a, soft_scale, row, lg, entry, hard, soft, sm, share, id, &r);
     if (thread == 0) publish(a.row_loss + row, loss);
     const float one = r.soft + r.hard;  // kOne: both are of the same exponential
+    if (EXPS == kOne && one == 0.f) {   // a row without a term (a padded one, say) has no gradient, whatever its logits hold
+#pragma unroll
+      for (int i = 0; i < HELD; ++i)
+#pragma unroll
+        for (int e = 0; e < V; ++e) x[i][e] = 0.f;
+    }
 #pragma unroll
     for (int i = 0; i < HELD; ++i) {
       const int u = thread + NT * i;
