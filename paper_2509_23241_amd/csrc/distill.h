@@ -16,6 +16,7 @@ struct DistillArgs {
   float* row_loss;          // scratch, [rows]
   uint32_t* counter;        // zero before the launch and after it
   float* loss;
+  int first_row = 0;        // of this launch
 };
 hipError_t launch_distill(hipStream_t s, int elt, const DistillArgs& a);
 

@@ -240,7 +240,7 @@ __global__ __launch_bounds__(Team<NT>::kThreads, HELD * kVec<T> == 64 ? 4 : 1) v
   constexpr int V = kVec<T>;
   __shared__ float sm_all[TM::kThreads / 64];
   extern __shared__ float entry_lds[];  // for each row [k + 1] shares, [k + 1] classes
-  const int thread = TM::thread(), row = blockIdx.x * TM::kRows + TM::which();
+  const int thread = TM::thread(), row = a.first_row + blockIdx.x * TM::kRows + TM::which();
   float* sm = sm_all;
   float* share = entry_lds + TM::which() * 2 * (a.k + 1);
   int* id = reinterpret_cast<int*>(share + a.k + 1);
@@ -350,7 +350,8 @@ __global__ __launch_bounds__(kThreads) void distill_rows_kernel(DistillArgs a) {
   int* id = reinterpret_cast<int*>(share + a.k + 1);
   const float soft_scale = kLog2e / a.temperature;
   const bool labels = a.label_weight > 0.f;
-  for (int row = blockIdx.x; row < a.rows; row += gridDim.x) {
+  for (long at = blockIdx.x; at < a.rows; at += gridDim.x) {
+    const int row = (int)at;
     const T* lg = (const T*)a.logits + (size_t)row * a.classes;
     T* dl = (T*)a.dlogits + (size_t)row * a.classes;
     First entry(a, row, threadIdx.x);
@@ -383,7 +384,7 @@ constexpr int kMeanThreads = 1024;
 __global__ __launch_bounds__(kMeanThreads) void distill_mean_kernel(const float* __restrict__ row_loss, int rows, float* __restrict__ loss) {
   __shared__ double sums[kMeanThreads / 64];
   double s = 0.0;
-  int i = threadIdx.x;
+  long i = threadIdx.x;
   for (; i + 7 * kMeanThreads < rows; i += 8 * kMeanThreads) {  // eight loads on their way
     float v[8];
 #pragma unroll
@@ -412,12 +413,17 @@ hipError_t finish(hipStream_t s, const DistillArgs& a) {
 template <typename T, int NT, int HELD>
 hipError_t launch_held(hipStream_t s, DistillArgs a) {
   using TM = Team<NT>;
-  const unsigned blocks = (unsigned)((a.rows + TM::kRows - 1) / TM::kRows);
+  const long blocks = ((long)a.rows + TM::kRows - 1) / TM::kRows;
   if (blocks > kCounted) a.counter = nullptr;
   const size_t lds = (size_t)TM::kRows * 2 * (a.k + 1) * sizeof(float);
   const bool one = a.label_weight <= 0.f || a.label_weight >= 1.f || a.temperature == 1.f;
   auto kernel = one ? distill_held_kernel<T, NT, HELD, kOne> : distill_held_kernel<T, NT, HELD, kTwo>;
-  hipLaunchKernelGGL(kernel, dim3(blocks), dim3(TM::kThreads), lds, s, a);
+  // a launch takes fewer than 2^32 threads, and drops what a grid has beyond
+  const long most = UINT32_MAX / TM::kThreads;
+  for (long from = 0; from < blocks; from += most) {
+    a.first_row = (int)(from * TM::kRows);
+    hipLaunchKernelGGL(kernel, dim3((unsigned)std::min(most, blocks - from)), dim3(TM::kThreads), lds, s, a);
+  }
   return finish(s, a);
 }
 
