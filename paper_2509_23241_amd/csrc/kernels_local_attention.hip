@@ -18,6 +18,33 @@
 
 namespace tp {
 
+namespace {
+
+// A whole number, 32 bits a word, lowest first: up to 64 factors of at most 2^20.
+struct Whole {
+  uint32_t word[41] = {1};
+  int words = 1;
+  void times(uint32_t factor, int how_often) {
+    for (; how_often > 0; --how_often) {
+      uint64_t carry = 0;
+      for (int i = 0; i < words; ++i) {
+        carry += (uint64_t)word[i] * factor;
+        word[i] = (uint32_t)carry;
+        carry >>= 32;
+      }
+      if (carry) word[words++] = (uint32_t)carry;
+    }
+  }
+  bool operator<(const Whole& b) const {
+    if (words != b.words) return words < b.words;
+    for (int i = words - 1; i >= 0; --i)
+      if (word[i] != b.word[i]) return word[i] < b.word[i];
+    return false;
+  }
+};
+
+}  // namespace
+
 DistanceBuckets make_distance_buckets(int buckets, int max_distance) {
   DistanceBuckets d{};
   d.count = buckets;
@@ -25,14 +52,22 @@ DistanceBuckets make_distance_buckets(int buckets, int max_distance) {
   d.half = buckets / 2;
   const int n = buckets - d.half;
   d.ratio = (float)(n / std::log2((double)max_distance / d.half));
-  for (int b = 0; b < d.half; ++b) d.first[b] = b;
-  for (int t = 0; t < n; ++t) {
-    // logarithms of both sides of d^n >= half^(n - t) max_distance^t: equal ones differ by a few units of 2^-64 of their size, others
-    // by 1e-9 or more at these sizes
-    const long double want = (n - t) * std::log((long double)d.half) + t * std::log((long double)max_distance);
-    long at = std::max<long>(d.half, (long)std::exp(want / n) - 2);
-    while (n * std::log((long double)at) < want - 1e-13L * std::max(1.0L, want)) ++at;
-    d.first[d.half + t] = (int)at;
+  for (int b = 0; b <= d.half; ++b) d.first[b] = b;
+  const double step = std::log((double)max_distance / d.half) / n;
+  for (int t = 1; t < n; ++t) {
+    // The border is off by less than 1e-8 here.  Where a whole number is nearer than that could decide (borders come as close as 1e-9), whole
+    // numbers do: the smallest d with d^n >= half^(n - t) max_distance^t.
+    const double border = d.half * std::exp(step * t);
+    const int near = (int)std::lround(border);
+    if (std::fabs(border - near) > 1e-6) {
+      d.first[d.half + t] = (int)std::ceil(border);
+    } else {
+      Whole at, want;
+      at.times((uint32_t)near, n);
+      want.times((uint32_t)d.half, n - t);
+      want.times((uint32_t)max_distance, t);
+      d.first[d.half + t] = at < want ? near + 1 : near;
+    }
   }
   return d;
 }
