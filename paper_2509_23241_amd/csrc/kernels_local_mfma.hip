@@ -1089,7 +1089,19 @@ __global__ __launch_bounds__(64 * NW, sizeof(T) == 2 || DHP == 64 ? 2 : 1) void 
             for (int w = 0; w < 4; ++w) {
               const int r = 8 * v + 4 * q + w;
               pe[w] = __builtin_amdgcn_exp2f((BIAS ? fmaf(sacc[r], scale_log2, bias[w]) : sacc[r] * scale_log2) - l2v[w]);
-              de[w] = pe[w] * (pacc[r] - dlv[w]);  // a pair that does not count has p = 0 and a finite dP here
+              de[w] = pe[w] * (pacc[r] - dlv[w]);
+            }
+            // A pair that does not count has p = 0 and a finite dP here, but its query's lse and delta may be infinite or NaN: the rows of dK and
+            // dV are formed again then, the sums of the table cannot be.
+            if constexpr (BIAS) {
+              if (masked) {
+#pragma unroll
+                for (int w = 0; w < 4; ++w) {
+                  const bool counts = (row + w >= d_from - d0) & (row + w < d_end - d0);
+                  pe[w] = counts ? pe[w] : 0.f;
+                  de[w] = counts ? de[w] : 0.f;
+                }
+              }
             }
             if constexpr (BIAS) add_to_table(sums[wave], far_sum, diagonals, tb, first, p.db.count, d0 + row, lane, de);
             ph[q] = TY::half(pe);
