@@ -129,7 +129,8 @@ enum tp_layer_type {
                              [heads x buckets] and fp32 in every mode, is the layer's only parameter (where a dense layer keeps W;
                              it has no b).  The backward pass forms the probabilities of the forward pass again, with the table
                              that pass read (a copy is kept), under every policy.  May be the last layer of a stage.  Keys that a
-                             query does not see do not reach its results, whatever they hold */
+                             query does not see do not reach its results, whatever they hold, nor do entries of the table that
+                             none of its pairs has */
 };
 
 #define TP_MAX_LAYERS 64

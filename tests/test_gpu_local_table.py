@@ -77,3 +77,24 @@ def test_a_query_reaches_the_buckets_of_its_pairs_only(case, dtype, odd):
                 off = (got.double() - clean["dtable"].double()).abs()
                 assert bool((off <= apart)[:, ~hit].all()), (i, where, bad)
                 assert not bool(torch.isfinite(got).all()), (i, where, bad)
+
+
+@pytest.mark.parametrize("odd", [False, True])
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("case", [c for c in CASES if c["sinks"] == 0] + [dict(tokens=500, heads=2, kv=2, dh=64, window=200, sinks=0, buckets=16, reach=400)], ids=ids)
+def test_entries_that_no_visible_pair_has(case, dtype, odd):
+    """Entries of distances beyond the window hold anything: same bits everywhere, and a gradient of 0 for them."""
+    import torch
+    from oracle.layers import distance_buckets
+    c = dict(case, dtype=dtype)
+    x, dy, table = _inputs(c, seqs=2)
+    used = int(distance_buckets(c["tokens"], c["buckets"], c["reach"])[c["window"] - 1]) + 1
+    assert used < c["buckets"]
+    clean = _run(c, x, dy, table, odd)
+    assert bool((clean["dtable"][:, used:] == 0).all()) and all(bool(torch.isfinite(t).all()) for t in clean.values())
+    for value in (np.nan, np.inf, -np.inf, 3e38):
+        other = table.clone()
+        other[:, used:] = value
+        got = _run(c, x, dy, other, odd)
+        for k in clean:
+            assert torch.equal(got[k], clean[k]), (value, k)
