@@ -276,6 +276,7 @@ __device__ __forceinline__ void load_borders(const DistanceBuckets& d, int* firs
 // Buckets b0 .. b1 of a tile's distances dmin .. dmax, wave uniform; b0 = -1: near ones, by distance.
 struct TileBuckets {
   int b0 = -1, b1 = -1;
+  __device__ TileBuckets() {}
   __device__ __forceinline__ TileBuckets(const DistanceBuckets& d, const int* first, int dmin, int dmax) {
     const int last = d.first[d.count - 1];
     if (dmin < kNear && dmin < last) return;
@@ -1076,7 +1077,8 @@ __global__ __launch_bounds__(64 * NW, sizeof(T) == 2 || DHP == 64 ? 2 : 1) void 
             }
           }
         }
-        const TileBuckets tb(p.db, first, BIAS ? tlo : 0, thi);
+        TileBuckets tb;
+        if constexpr (BIAS) tb = TileBuckets(p.db, first, tlo, thi);  // without a bias there are no borders to look at
         if constexpr (BIAS) far_sum.start_tile(sums[wave], tb, lane);
         Diagonals diagonals;
 #pragma unroll
