@@ -20,6 +20,7 @@
 #include <stdint.h>
 
 #include <algorithm>
+#include <type_traits>
 
 #include "device_utils.h"
 #include "kernels.h"
@@ -754,36 +755,19 @@ __global__ __launch_bounds__(64 * NW, sizeof(T) == 2 || DHP == 64 ? 2 : 1) void 
   asm volatile("" : "+v"(l2), "+v"(delta));
 
   floatx16 acc[TN];
-#pragma unroll
-  for (int j = 0; j < TN; ++j)
-#pragma unroll
-    for (int r = 0; r < 16; ++r) acc[j][r] = 0.f;
   float total = 0.f;
   const int q_last = min(qw + 31, S - 1);
   const float scale_log2 = p.scale * kLog2e;
-  // The delta of the stored y is off by what rounded y, 2^-9 of it: of a query with few keys that is as much as dS itself is rounded by, and
-  // their tiles are walked over once before to correct it.  (bf16, 2 and 8 keys: dq 0.0038
-  // and 0.0027 of its norm off, so 0.0023 and 0.0024; the rounding of what is stored alone is 0.0017.  From 40 keys on it makes no difference.)
-  const bool twice = min(S, a.window + a.sinks) <= 32;
-  for (int pass = twice ? 0 : 1; pass < 2; ++pass) {
-    if (twice && pass == 1) {
-      float* totals = reinterpret_cast<float*>(lds);
-      lds_barrier();
-      totals[threadIdx.x] = total;
-      lds_barrier();
-      if (TEAMS == 2) total += totals[threadIdx.x ^ (64 * NW / 2)];
-      lds_barrier();
-      delta += over_halves(total, Add());
-      total = 0.f;
-      if (it.count > 0) issue(0);
-    }
-    for (int t = 0; t < it.count; ++t) {
+  // Over the first `steps` blocks, the first of which is on its way; waves of queries below q_end.  With products, or the sums of dS alone.
+  auto walk = [&](auto products, int steps, int q_end) __attribute__((always_inline)) {
+    constexpr bool kProducts = decltype(products)::value;
+    for (int t = 0; t < steps; ++t) {
       wait_vmcnt<0>();
       lds_barrier();
-      if (t + 1 < it.count) issue(t + 1);
+      if (t + 1 < steps) issue(t + 1);
       constexpr int kMine = BR / TEAMS;  // the wave's rows of the block
       const int skip = TEAMS == 1 ? 0 : team * 32, kb = it.block(t) * BR + skip;
-      if (!active || qw >= S || kb > q_last || (kb >= a.sinks && kb + kMine - 1 <= qw - a.window)) continue;
+      if (!active || qw >= q_end || kb > q_last || (kb >= a.sinks && kb + kMine - 1 <= qw - a.window)) continue;
       const uint32_t stage = lds0 + (t & 1) * 2 * TL::kBytes + skip * 128, lk = stage + row_at, lkc = stage + col_at;
       const int d0 = query - kb - 4 * half, sink0 = a.sinks - kb - 4 * half;
 #pragma unroll
@@ -803,8 +787,10 @@ __global__ __launch_bounds__(64 * NW, sizeof(T) == 2 || DHP == 64 ? 2 : 1) void 
                             else sacc = TY::mma(f, qf[i >> 1], sacc);
                           });
         auto k_frag = [&](int i) { return TL::col_frag(lkc, i % TN, 2 * u + i / TN); };
+        if constexpr (kProducts) {
 #pragma unroll
-        for (int i = 0; i < TY::kAhead; ++i) ahead[i] = k_frag(i);
+          for (int i = 0; i < TY::kAhead; ++i) ahead[i] = k_frag(i);
+        }
         __builtin_amdgcn_sched_barrier(0);
         if constexpr (BIAS) {  // ahead of the mask: an entry of the table that only hidden pairs have may hold anything
           float bias[16];
@@ -835,10 +821,33 @@ __global__ __launch_bounds__(64 * NW, sizeof(T) == 2 || DHP == 64 ? 2 : 1) void 
           }
           dsf[g] = TY::pack(e);
         }
-        if (pass == 1) pipelined<2 * TN>(ahead, k_frag, [&](int i, const typename TY::Frag& f) { if (!TY::skips(32 * (i % TN), dh)) acc[i % TN] = TY::mma(f, dsf[i / TN], acc[i % TN]); }, true);
+        if constexpr (kProducts) pipelined<2 * TN>(ahead, k_frag, [&](int i, const typename TY::Frag& f) { if (!TY::skips(32 * (i % TN), dh)) acc[i % TN] = TY::mma(f, dsf[i / TN], acc[i % TN]); }, true);
       }
     }
+  };
+  // The delta of the stored y is off by what rounded y, 2^-9 of it: of a query with few keys that is as much as dS itself is rounded by, and
+  // their tiles are walked over once before to correct it.  (bf16, 2 and 8 keys: dq 0.0038
+  // and 0.0027 of its norm off, so 0.0023 and 0.0024; the rounding of what is stored alone is 0.0017.  From 40 keys on it makes no difference.)
+  // A walk of its own, before there are sums: as a second pass of the other it took the 128-wide heads' kernel 15 registers and spilled.
+  if (min(S, a.window + a.sinks) <= 32) {
+    walk(std::false_type(), it.count, S);
+    lds_barrier();
+    if constexpr (TEAMS == 2) {
+      float* totals = reinterpret_cast<float*>(lds);
+      totals[threadIdx.x] = total;
+      lds_barrier();
+      total += totals[threadIdx.x ^ (64 * NW / 2)];
+      lds_barrier();
+    }
+    if (it.count > 0) issue(0);
+    delta += over_halves(total, Add());
+    total = 0.f;
   }
+#pragma unroll
+  for (int j = 0; j < TN; ++j)
+#pragma unroll
+    for (int r = 0; r < 16; ++r) acc[j][r] = 0.f;
+  walk(std::true_type(), it.count, S);
   lds_barrier();
   if constexpr (TEAMS == 2) {  // the second team's sums to the first
     floatx4* mine = reinterpret_cast<floatx4*>(lds) + (size_t)(wave % (NW / TEAMS)) * TN * 4 * 64 + lane;
