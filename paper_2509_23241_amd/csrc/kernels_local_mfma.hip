@@ -825,23 +825,30 @@ __global__ __launch_bounds__(64 * NW, sizeof(T) == 2 || DHP == 64 ? 2 : 1) void 
       }
     }
   };
-  // The delta of the stored y is off by what rounded y, 2^-9 of it: of a query with few keys that is as much as dS itself is rounded by, and
-  // their tiles are walked over once before to correct it.  (bf16, 2 and 8 keys: dq 0.0038
-  // and 0.0027 of its norm off, so 0.0023 and 0.0024; the rounding of what is stored alone is 0.0017.  From 40 keys on it makes no difference.)
-  // A walk of its own, before there are sums: as a second pass of the other it took the 128-wide heads' kernel 15 registers and spilled.
-  if (min(S, a.window + a.sinks) <= 32) {
-    walk(std::false_type(), it.count, S);
-    lds_barrier();
-    if constexpr (TEAMS == 2) {
-      float* totals = reinterpret_cast<float*>(lds);
-      totals[threadIdx.x] = total;
-      lds_barrier();
-      total += totals[threadIdx.x ^ (64 * NW / 2)];
-      lds_barrier();
+  // The delta of the stored y is off by what rounded y to bf16, 2^-9 of it: of a query with few keys that is as much as dS itself is rounded
+  // by.  Queries that see at most 32 keys, the first 32 of a sequence among them, are walked over once before to correct it; the others' dS are
+  // off by it, on average over their keys.  (2 and 8 keys: dq 0.0038 and 0.0027 of its norm off, so 0.0023 and 0.0024; the rounding of what is
+  // stored alone is 0.0017.  From 40 keys on it makes no difference.)  A walk of its own, before there are sums: as a second pass of the other
+  // it took the 128-wide heads' kernel 15 registers, and spilled.
+  if constexpr (sizeof(T) == 2) {
+    const bool all = a.window + a.sinks <= 32;
+    if (all || it.q_lo == 0) {
+      // of a sequence's first queries the first block of keys has all they see, and only the first team's tile of it
+      walk(std::false_type(), all ? it.count : min(1, it.count), all ? S : 32);
+      if (all) {
+        lds_barrier();
+        if constexpr (TEAMS == 2) {
+          float* totals = reinterpret_cast<float*>(lds);
+          totals[threadIdx.x] = total;
+          lds_barrier();
+          total += totals[threadIdx.x ^ (64 * NW / 2)];
+          lds_barrier();
+        }
+        if (it.count > 0) issue(0);
+      }
+      delta += over_halves(total, Add());
+      total = 0.f;
     }
-    if (it.count > 0) issue(0);
-    delta += over_halves(total, Add());
-    total = 0.f;
   }
 #pragma unroll
   for (int j = 0; j < TN; ++j)
