@@ -238,46 +238,59 @@ __global__ __launch_bounds__(kThreads) void local_dq_any_kernel(Shape a, int til
     for (int c = 0; c < kND; ++c) dq[r][c] = 0.f;
   }
   const int last = q0 + nq - 1, lo = max(0, q0 - a.window + 1);
-  for (int k0 = 0; k0 <= last; k0 += tile) {
-    if (k0 >= a.sinks && k0 + tile <= lo) {
-      k0 = lo / tile * tile - tile;
-      continue;
+  auto walk = [&](bool products) {  // with products, or the sums of dS alone
+    for (int k0 = 0; k0 <= last; k0 += tile) {
+      if (k0 >= a.sinks && k0 + tile <= lo) {
+        k0 = lo / tile * tile - tile;
+        continue;
+      }
+      const int nk = min(tile, S - k0);
+      __syncthreads();
+      stage_rows(ks, kbase + (size_t)k0 * ld, ld, nk, dh);
+      stage_rows(vs, vbase + (size_t)k0 * ld, ld, nk, dh);
+      __syncthreads();
+#pragma unroll
+      for (int r = 0; r < kRW; ++r) {
+        const int qi = wave * kRW + r, i = q0 + qi, j = k0 + lane;
+        if (qi >= nq || k0 > i) continue;
+        float ds = 0.f;
+        const bool sees = lane < nk && a.sees(i, j);
+        if (sees) {
+          float sc = 0.f, dp = 0.f;
+          for (int d = 0; d < dh; ++d) {
+            sc = fmaf(qs[qi * (dh + 1) + d], ks[lane * (dh + 1) + d], sc);
+            dp = fmaf(dos[qi * (dh + 1) + d], vs[lane * (dh + 1) + d], dp);
+          }
+          float e = sc * scale * kLog2e - l2[r];
+          if (db.count) e += bias.value[bucket_of(db, bias.first, i - j)];
+          ds = __builtin_amdgcn_exp2f(e) * (dp - dl[r]);
+          total[r] += ds;
+        }
+        if (!products) continue;
+        const uint64_t seen = __builtin_amdgcn_ballot_w64(sees);
+#pragma unroll
+        for (int c = 0; c < kND; ++c) {
+          const int d = lane + 64 * c;
+          if (64 * c >= dh) continue;
+          for (uint64_t left = seen; left; left &= left - 1) {
+            const int jj = __builtin_ctzll(left);
+            const float v = lane_value(ds, jj);
+            if (d < dh) dq[r][c] = fmaf(v, ks[jj * (dh + 1) + d], dq[r][c]);
+          }
+        }
+      }
     }
-    const int nk = min(tile, S - k0);
-    __syncthreads();
-    stage_rows(ks, kbase + (size_t)k0 * ld, ld, nk, dh);
-    stage_rows(vs, vbase + (size_t)k0 * ld, ld, nk, dh);
-    __syncthreads();
+  };
+  // Queries of at most 32 keys: what y was rounded to bf16 by is as much in dS as what rounds dS, and is taken out of delta ahead.
+  if (sizeof(T) == 2 && (a.window + a.sinks <= 32 || q0 < 32)) {
+    walk(false);
 #pragma unroll
     for (int r = 0; r < kRW; ++r) {
-      const int qi = wave * kRW + r, i = q0 + qi, j = k0 + lane;
-      if (qi >= nq || k0 > i) continue;
-      float ds = 0.f;
-      const bool sees = lane < nk && a.sees(i, j);
-      if (sees) {
-        float sc = 0.f, dp = 0.f;
-        for (int d = 0; d < dh; ++d) {
-          sc = fmaf(qs[qi * (dh + 1) + d], ks[lane * (dh + 1) + d], sc);
-          dp = fmaf(dos[qi * (dh + 1) + d], vs[lane * (dh + 1) + d], dp);
-        }
-        float e = sc * scale * kLog2e - l2[r];
-        if (db.count) e += bias.value[bucket_of(db, bias.first, i - j)];
-        ds = __builtin_amdgcn_exp2f(e) * (dp - dl[r]);
-        total[r] += ds;
-      }
-      const uint64_t seen = __builtin_amdgcn_ballot_w64(sees);
-#pragma unroll
-      for (int c = 0; c < kND; ++c) {
-        const int d = lane + 64 * c;
-        if (64 * c >= dh) continue;
-        for (uint64_t left = seen; left; left &= left - 1) {
-          const int jj = __builtin_ctzll(left);
-          const float v = lane_value(ds, jj);
-          if (d < dh) dq[r][c] = fmaf(v, ks[jj * (dh + 1) + d], dq[r][c]);
-        }
-      }
+      dl[r] += sum_over_lanes(total[r]);
+      total[r] = 0.f;
     }
   }
+  walk(true);
 #pragma unroll
   for (int r = 0; r < kRW; ++r) {
     const int qi = wave * kRW + r, i = q0 + qi;

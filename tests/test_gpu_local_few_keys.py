@@ -94,3 +94,15 @@ ids = lambda c: "-".join(str(v) for v in c.values())
 @pytest.mark.parametrize("case", CASES, ids=ids)
 def test_queries_of_few_keys(case, dtype):
     _check(dict(case, dtype=dtype))
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("case", [_case(1, dh=20), _case(33, dh=20), _case(40, dh=200), _case(90, dh=256, window=20, sinks=2, buckets=8, reach=30),
+                                  _case(130, heads=4, kv=2, dh=7, window=9), _case(300, heads=3, kv=1, dh=136, window=60, sinks=1)], ids=ids)
+def test_queries_of_few_keys_in_other_heads(case, dtype):
+    _check(dict(case, dtype=dtype))
+
+
+@pytest.mark.parametrize("case", [_case(33), _case(200, heads=4, kv=2, dh=128, window=12, sinks=3, buckets=8, reach=30), _case(150, window=90)], ids=ids)
+def test_queries_of_few_keys_at_any_address(case):
+    _check(dict(case, dtype="bf16"), odd=True)
