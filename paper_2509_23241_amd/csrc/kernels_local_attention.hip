@@ -11,6 +11,7 @@
 #include <stdint.h>
 
 #include <algorithm>
+#include <type_traits>
 
 #include "device_utils.h"
 #include "kernels.h"
@@ -198,7 +199,7 @@ __global__ __launch_bounds__(kThreads) void local_fwd_any_kernel(Shape a, int ti
 
 // dq; delta[(b*heads + h)*S + i], corrected by what the row's dS add up to
 template <typename T>
-__global__ __launch_bounds__(kThreads) void local_dq_any_kernel(Shape a, int tile, DistanceBuckets db, int seqs_per_table,
+__global__ __launch_bounds__(kThreads, 6) void local_dq_any_kernel(Shape a, int tile, DistanceBuckets db, int seqs_per_table,
                                                                 const T* __restrict__ x, const T* __restrict__ out,
                                                                 const T* __restrict__ dout, const float* __restrict__ lse,
                                                                 const float* __restrict__ kept, T* __restrict__ dx,
@@ -238,7 +239,7 @@ __global__ __launch_bounds__(kThreads) void local_dq_any_kernel(Shape a, int til
     for (int c = 0; c < kND; ++c) dq[r][c] = 0.f;
   }
   const int last = q0 + nq - 1, lo = max(0, q0 - a.window + 1);
-  auto walk = [&](bool products) {  // with products, or the sums of dS alone
+  auto walk = [&](auto products) {  // with products, or the sums of dS alone
     for (int k0 = 0; k0 <= last; k0 += tile) {
       if (k0 >= a.sinks && k0 + tile <= lo) {
         k0 = lo / tile * tile - tile;
@@ -266,7 +267,7 @@ __global__ __launch_bounds__(kThreads) void local_dq_any_kernel(Shape a, int til
           ds = __builtin_amdgcn_exp2f(e) * (dp - dl[r]);
           total[r] += ds;
         }
-        if (!products) continue;
+        if constexpr (!decltype(products)::value) continue;
         const uint64_t seen = __builtin_amdgcn_ballot_w64(sees);
 #pragma unroll
         for (int c = 0; c < kND; ++c) {
@@ -283,14 +284,14 @@ __global__ __launch_bounds__(kThreads) void local_dq_any_kernel(Shape a, int til
   };
   // Queries of at most 32 keys: what y was rounded to bf16 by is as much in dS as what rounds dS, and is taken out of delta ahead.
   if (sizeof(T) == 2 && (a.window + a.sinks <= 32 || q0 < 32)) {
-    walk(false);
+    walk(std::false_type());
 #pragma unroll
     for (int r = 0; r < kRW; ++r) {
       dl[r] += sum_over_lanes(total[r]);
       total[r] = 0.f;
     }
   }
-  walk(true);
+  walk(std::true_type());
 #pragma unroll
   for (int r = 0; r < kRW; ++r) {
     const int qi = wave * kRW + r, i = q0 + qi;
