@@ -119,7 +119,7 @@ enum tp_layer_type {
   TP_LAYER_AVGPOOL = 8,   /* global average pooling, no parameters: a sample of [positions x C] values becomes the C
                              means over its positions; in_features = out_features = C, geom = {positions} */
   TP_LAYER_LOCAL_ATTENTION = 9 /* causal multi-head self-attention over a window of keys: geom = {tokens, heads, kv heads, window,
-                             sinks}; out_features = heads * dh (dh: 1 .. 256), in_features = (heads + 2 * kv heads) * dh (queries | keys |
+                             sinks}; out_features = heads * dh (dh: 1 .. 256; at most 65535 heads, and 2^23 blocks of 16 tokens in a mini-batch), in_features = (heads + 2 * kv heads) * dh (queries | keys |
                              values; kv heads divide heads, query head h reads key head h / (heads / kv heads)).  Query i sees key
                              j <= i where i - j < window (0: every j <= i) or j < sinks (0 without a window).  rel = {buckets,
                              max distance} adds a learned bias table[h][bucket(i - j)] to the scaled scores, {0, 0}: none.  2 .. 128

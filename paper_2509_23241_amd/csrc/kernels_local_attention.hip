@@ -307,8 +307,9 @@ __global__ __launch_bounds__(kThreads, 6) void local_dq_any_kernel(Shape a, int 
 }
 
 // dk, dv, and the partial sums of dtable, [workgroups of x][heads][buckets]: a workgroup takes row blocks blockIdx.x, + gridDim.x, ..
-// of key head blockIdx.y
-template <typename T>
+// of key head blockIdx.y.  The LDS holds the table's sums of all heads of the key head or, where those do not fit (BY_HEAD), of one, whose sums
+// over a row block are added to the workgroup's own partial sums.  (Heads one by one where all would fit: 32 x 200 tokens, 8 heads of 20, 233 -> 265 us.)
+template <typename T, bool BY_HEAD>
 __global__ __launch_bounds__(kThreads) void local_dkv_any_kernel(Shape a, int tile, DistanceBuckets db, int seqs, int seqs_per_table,
                                                                  const T* __restrict__ x, const T* __restrict__ dout,
                                                                  const float* __restrict__ lse, const float* __restrict__ kept,
@@ -325,8 +326,12 @@ __global__ __launch_bounds__(kThreads) void local_dkv_any_kernel(Shape a, int ti
   float* dos = qs + tile * (dh + 1);
   float* dl = dos + tile * (dh + 1);     // [tile]
   float* ls = dl + tile;                 // [tile]
-  float* sums = ls + tile;               // [4 waves][group][buckets]
-  for (int t = threadIdx.x; t < 4 * group * db.count; t += kThreads) sums[t] = 0.f;
+  float* sums = ls + tile;               // [4 waves][group, or 1][buckets]
+  float* table_sums = partials + ((size_t)blockIdx.x * a.heads + (size_t)kvh * group) * db.count;
+  for (int t = threadIdx.x; t < 4 * (BY_HEAD ? 1 : group) * db.count; t += kThreads) sums[t] = 0.f;
+  static_assert(kMaxBuckets <= kThreads, "a thread for each bucket of a head");
+  if (BY_HEAD && (int)threadIdx.x < db.count)
+    for (int n = 0; n < group; ++n) table_sums[(size_t)n * db.count + threadIdx.x] = 0.f;
   for (int at = blockIdx.x; at < seqs * blocks; at += gridDim.x) {
     const int b = at / blocks, j0 = (at - b * blocks) * kRows;
     const T* base = x + (size_t)b * S * ld;
@@ -386,7 +391,7 @@ __global__ __launch_bounds__(kThreads) void local_dkv_any_kernel(Shape a, int ti
               const int which = __builtin_amdgcn_readlane(bucket, __builtin_ctzll(left));
               left &= ~__builtin_amdgcn_ballot_w64(bucket == which);
               const float s = sum_over_lanes(bucket == which ? ds : 0.f);
-              if (lane == 0) sums[(wave * group + n) * db.count + which] += s;
+              if (lane == 0) sums[(BY_HEAD ? wave : wave * group + n) * db.count + which] += s;
             }
           }
 #pragma unroll
@@ -402,6 +407,17 @@ __global__ __launch_bounds__(kThreads) void local_dkv_any_kernel(Shape a, int ti
               }
             }
           }
+        }
+      }
+      if (BY_HEAD) {  // this head's sums to memory, and the LDS free for the next head's
+        __syncthreads();
+        if ((int)threadIdx.x < db.count) {
+          float t = 0.f;
+          for (int w = 0; w < 4; ++w) {
+            t += sums[w * db.count + threadIdx.x];
+            sums[w * db.count + threadIdx.x] = 0.f;
+          }
+          table_sums[(size_t)n * db.count + threadIdx.x] += t;
         }
       }
     }
@@ -420,11 +436,12 @@ __global__ __launch_bounds__(kThreads) void local_dkv_any_kernel(Shape a, int ti
       }
     }
   }
+  if (BY_HEAD) return;
   __syncthreads();
   for (int t = threadIdx.x; t < group * db.count; t += kThreads) {
     float s = 0.f;
     for (int w = 0; w < 4; ++w) s += sums[w * group * db.count + t];
-    partials[((size_t)blockIdx.x * a.heads + (size_t)kvh * group) * db.count + t] = s;
+    table_sums[t] = s;
   }
 }
 
@@ -434,10 +451,11 @@ inline int any_dkv_blocks(const LocalAttention& a) {
   return (int)(a.buckets ? std::min<long>(kAnyTableRows, any_blocks(a)) : any_blocks(a));
 }
 // LDS of the last kernel, which needs most
-inline size_t any_lds(const LocalAttention& a) {
+inline size_t any_lds(const LocalAttention& a, int table_heads) {
   const int tile = tile_rows(a.dh);
-  return ((size_t)(2 * kRows + 2 * tile) * (a.dh + 1) + 2 * tile + (size_t)4 * (a.heads / a.kv) * a.buckets) * sizeof(float);
+  return ((size_t)(2 * kRows + 2 * tile) * (a.dh + 1) + 2 * tile + (size_t)4 * table_heads * a.buckets) * sizeof(float);
 }
+inline bool tables_fit(const LocalAttention& a) { return any_lds(a, a.heads / a.kv) <= 156 * 1024; }
 
 template <typename T>
 hipError_t any_fwd(hipStream_t s, const LocalAttention& a, const T* x, const float* table, float* kept, T* out, T* out2, float* lse) {
@@ -460,15 +478,19 @@ hipError_t any_bwd(hipStream_t s, const LocalAttention& a, const T* x, const T* 
   const size_t lds_q = (size_t)(2 * kRows + 2 * tile) * (a.dh + 1) * sizeof(float);
   static hipError_t attr_q = hipFuncSetAttribute(reinterpret_cast<const void*>(local_dq_any_kernel<T>),
                                                  hipFuncAttributeMaxDynamicSharedMemorySize, 158 * 1024);
-  static hipError_t attr_kv = hipFuncSetAttribute(reinterpret_cast<const void*>(local_dkv_any_kernel<T>),
+  auto dkv = tables_fit(a) ? local_dkv_any_kernel<T, false> : local_dkv_any_kernel<T, true>;
+  static hipError_t attr_kv = hipFuncSetAttribute(reinterpret_cast<const void*>(local_dkv_any_kernel<T, false>),
                                                   hipFuncAttributeMaxDynamicSharedMemorySize, 158 * 1024);
+  static hipError_t attr_by_head = hipFuncSetAttribute(reinterpret_cast<const void*>(local_dkv_any_kernel<T, true>),
+                                                       hipFuncAttributeMaxDynamicSharedMemorySize, 158 * 1024);
   if (attr_q != hipSuccess) return attr_q;
   if (attr_kv != hipSuccess) return attr_kv;
+  if (attr_by_head != hipSuccess) return attr_by_head;
   hipLaunchKernelGGL(local_dq_any_kernel<T>, dim3((unsigned)any_blocks(a), a.heads), dim3(kThreads), lds_q, s, shape_of(a), tile, db,
                      a.seqs_per_table, x, out, dout, lse, kept, dx, delta, scale);
   hipError_t e = hipGetLastError();
   if (e != hipSuccess) return e;
-  hipLaunchKernelGGL(local_dkv_any_kernel<T>, dim3(any_dkv_blocks(a), a.kv), dim3(kThreads), any_lds(a), s, shape_of(a), tile, db,
+  hipLaunchKernelGGL(dkv, dim3(any_dkv_blocks(a), a.kv), dim3(kThreads), any_lds(a, tables_fit(a) ? a.heads / a.kv : 1), s, shape_of(a), tile, db,
                      a.seqs, a.seqs_per_table, x, dout, lse, kept, delta, dx, partials, scale);
   return hipGetLastError();
 }
@@ -477,7 +499,7 @@ hipError_t any_bwd(hipStream_t s, const LocalAttention& a, const T* x, const T* 
 
 bool local_attention_supported(const LocalAttention& a) {
   return a.S >= 1 && a.dh >= 1 && a.dh <= kMaxDh && a.kv >= 1 && a.heads >= a.kv && a.heads % a.kv == 0 && a.heads <= 65535 &&
-         any_blocks(a) <= (1 << 23) && any_lds(a) <= 156 * 1024;
+         any_blocks(a) <= (1 << 23);
 }
 
 size_t local_attention_scratch_bytes(int elt, const LocalAttention& a) {
