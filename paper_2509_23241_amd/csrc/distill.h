@@ -12,6 +12,7 @@ struct DistillArgs {
   const int32_t* ids;       // [rows x k], negative: no entry
   const int32_t* labels;    // [rows], or null where label_weight is 0
   float temperature, label_weight;
+  float teacher_weight;     // 1 - the labels' weight, taken before either is rounded to 32 bits: next to 1 that rounding is much of what is left
   void* dlogits;            // [rows x classes] in elt
   float* row_loss;          // scratch, [rows]
   uint32_t* counter;        // zero before the launch and after it

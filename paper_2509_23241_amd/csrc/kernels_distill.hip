@@ -66,7 +66,7 @@ struct Row {
   float to_hard;       // what turns the power into that of exp(z)
   float soft, hard;    // what the exponentials are multiplied with in the gradient
   __device__ __forceinline__ Row(const DistillArgs& a, float soft_scale, float top) {
-    const bool only_hard = a.label_weight >= 1.f;
+    const bool only_hard = a.teacher_weight <= 0.f;
     scale = only_hard ? kLog2e : soft_scale;
     to_hard = only_hard ? 1.f : a.temperature;
     base = fabsf(top * scale) > 0x1p24f ? top : 0.f;  // from 2^24 on the rounding is 1 and more
@@ -119,12 +119,12 @@ __device__ __forceinline__ float entries(const DistillArgs& a, float soft_scale,
     tm = fmaxf(tm, share[e] == share[e] ? share[e] : INFINITY);  // a NaN is an entry, too, and makes the sum NaN
   }
   tm = TM::over(tm, sm, Max());
-  const bool has = tm != -INFINITY && a.label_weight < 1.f;
+  const bool has = tm != -INFINITY && a.teacher_weight > 0.f;
   float total = 0.f;
   for (int e = thread; e < a.k; e += NT) total += has ? __builtin_amdgcn_exp2f((share[e] - tm) * soft_scale) : 0.f;
   total = TM::over(total, sm, Add());
   const float log_total = __builtin_amdgcn_logf(total), log_soft = __builtin_amdgcn_logf(sum_soft);  // base 2
-  const float weight = (1.f - a.label_weight) * a.temperature * inv_rows;
+  const float weight = a.teacher_weight * a.temperature * inv_rows;
   float kl = 0.f;
   for (int e = thread; e < a.k; e += NT) {
     const float log_p = has ? (share[e] - tm) * soft_scale - log_total : -INFINITY;
@@ -139,7 +139,7 @@ __device__ __forceinline__ float entries(const DistillArgs& a, float soft_scale,
     }
   }
   kl = TM::over(kl, sm, Add()) * kLn2;
-  float loss = a.label_weight < 1.f ? (1.f - a.label_weight) * a.temperature * a.temperature * kl : 0.f;
+  float loss = a.teacher_weight > 0.f ? a.teacher_weight * a.temperature * a.temperature * kl : 0.f;
   if (a.label_weight > 0.f) {
     const bool known = (unsigned)f.label < (unsigned)a.classes;
     const float ce = known ? __builtin_amdgcn_logf(sum_hard) - r->power(f.z_label) * r->to_hard : __builtin_nanf("");
@@ -416,7 +416,7 @@ hipError_t launch_held(hipStream_t s, DistillArgs a) {
   const long blocks = ((long)a.rows + TM::kRows - 1) / TM::kRows;
   if (blocks > kCounted) a.counter = nullptr;
   const size_t lds = (size_t)TM::kRows * 2 * (a.k + 1) * sizeof(float);
-  const bool one = a.label_weight <= 0.f || a.label_weight >= 1.f || a.temperature == 1.f;
+  const bool one = a.label_weight <= 0.f || a.teacher_weight <= 0.f || a.temperature == 1.f;
   auto kernel = one ? distill_held_kernel<T, NT, HELD, kOne> : distill_held_kernel<T, NT, HELD, kTwo>;
   // a launch takes fewer than 2^32 threads, and drops what a grid has beyond
   const long most = UINT32_MAX / TM::kThreads;

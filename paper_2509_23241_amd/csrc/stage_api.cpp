@@ -1234,6 +1234,7 @@ int stage_loss_distill(tp_stage* st, uint64_t mb_id, const void* logits_dev, con
   a.labels = labels_dev;
   a.temperature = (float)temperature;
   a.label_weight = (float)label_weight;
+  a.teacher_weight = (float)(1.0 - label_weight);
   a.dlogits = dlogits_dev;
   a.row_loss = st->partials();
   a.counter = st->counter(tp_stage::kCountLoss);

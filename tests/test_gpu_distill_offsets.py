@@ -114,3 +114,29 @@ def test_logits_far_beyond_the_temperature(t, offset, classes, dtype):
         else:
             assert bool(torch.isfinite(grad).all())
     st.close()
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("classes", [20, 1500, 40001, 140000])
+def test_labels_that_have_nearly_all_the_weight(classes, dtype):
+    """What is left for the teacher, 1 - label_weight, is right to a rounding of its own; the label's own term is next to nothing here."""
+    import torch
+    rows, k = 6, 4
+    g = torch.Generator(device="cuda")
+    g.manual_seed(classes)
+    z = 0.25 * torch.randint(-3, 1, (rows, classes), generator=g, device="cuda").double()
+    ids = torch.rand(rows, classes, generator=g, device="cuda").topk(k, 1).indices.to(torch.int32)
+    labels = (ids[:, 0] + 1) % classes
+    z[torch.arange(rows, device="cuda"), labels.long()] = 64.0
+    stored = z.to(torch.float32 if dtype == "f32" else torch.bfloat16)
+    teacher = torch.randn(rows, k, generator=g, device="cuda")
+    st = _stage(dtype, rows, classes)
+    for t, w in ((1.5, 0.999), (3.0, 0.9999), (1.0, 0.9999), (2.0, 1 - 2.0 ** -30)):
+        loss, grad = st.loss_distill(0, stored, teacher, ids, temperature=t, labels=labels, label_weight=w)
+        want, dwant, eloss, egrad = _want(z, teacher, ids, t, labels, w)
+        bound = egrad + (2.0 ** -8 if dtype == "bf16" else F) * (dwant.abs() + egrad) + 2.0 ** -126
+        share = float(((grad.double() - dwant).abs() / bound).max())
+        print("T", t, "w", w, "loss off %.1e of %.1e" % (abs(float(loss) - want), eloss + F * abs(want)), "gradient %.2f of its bound" % share)
+        assert abs(float(loss) - want) <= eloss + F * abs(want), (t, w)
+        assert share <= 1.0, (t, w)
+    st.close()
