@@ -446,7 +446,7 @@ __global__ __launch_bounds__(kThreads) void local_dkv_any_kernel(Shape a, int ti
 }
 
 constexpr int kAnyTableRows = 512;  // partial sums of a table that the kernels above leave, at most
-inline long any_blocks(const LocalAttention& a) { return (long)a.seqs * ((a.S + kRows - 1) / kRows); }
+inline long any_blocks(const LocalAttention& a) { return a.seqs * (((long)a.S + kRows - 1) / kRows); }
 inline int any_dkv_blocks(const LocalAttention& a) {
   return (int)(a.buckets ? std::min<long>(kAnyTableRows, any_blocks(a)) : any_blocks(a));
 }

@@ -21,3 +21,15 @@ def test_more_heads_than_a_grid_has_rows():
     with pytest.raises(B.StageLibError) as e:
         _query(("local", 65536, 65536, 8, 1, 3, 1), "bf16")
     assert e.value.code == B.TP_EINVAL
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+def test_numbers_of_tokens_next_to_the_limits(dtype):
+    """2^23 blocks of 16 tokens and no more, up to the largest number a description holds."""
+    for tokens, mb in ((1 << 27, 1), (1 << 24, 8), (16, 1 << 23)):
+        _query(("local", 4, 4, tokens, 2, 3, 1), dtype, mb=mb, n=1)
+    for tokens, mb in (((1 << 27) + 1, 1), ((1 << 24) + 1, 8), (17, 1 << 23), ((1 << 31) - 16, 1), ((1 << 31) - 15, 1), ((1 << 31) - 1, 1),
+                       ((1 << 31) - 1, 1 << 24)):
+        with pytest.raises(B.StageLibError) as e:
+            _query(("local", 4, 4, tokens, 2, 3, 1), dtype, mb=mb, n=1)
+        assert e.value.code == B.TP_EINVAL, (tokens, mb)
