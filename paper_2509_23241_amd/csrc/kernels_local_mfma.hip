@@ -1275,6 +1275,8 @@ constexpr int kWaves = 4;
 //   1 x 16384, 8 heads of 128 on 2, window 1024: one part 257, two 246, four 232, eight 290; two teams 253, 224, 231, 318
 //   4 x 777, 6 heads of 80 on 2, window 300, a bias: one team, one part 172, four parts 67; two teams 97 and 52; far pairs in place 65
 //   32 x 200, 8 heads of 64, window 64, a bias: far pairs in place 29, far workgroups 44
+// and in fp32 the whole backward pass, planned with two workgroups a CU and with the one that heads above 64 leave room for:
+//   8 x 300, 8 heads of 128, all keys: 190 and 157; 1 x 4096, 4 heads of 128 on one, window 512: 315 and 250; 4 x 512, 2 x 2048, 4 x 1024: the same
 struct DkvPlan {
   int teams = 1, parts = 1;
   int far_blocks = 0, chunks = 0;  // workgroups for the far pairs of the first keys; none: those keys' own workgroups take them
@@ -1283,15 +1285,17 @@ struct DkvPlan {
 template <typename T, int DHP>
 DkvPlan dkv_plan(const LocalAttention& a) {
   constexpr int BR = kBlockRows<T, DHP>;
-  constexpr double kSlots = 512;  // workgroups the chip runs at a time, two on a CU
+  // workgroups the chip runs at a time: two on a CU, but one of fp32 heads above 64, whose waves take 384 registers
+  constexpr double kSlots = sizeof(T) == 4 && DHP == 128 ? 256 : 512;
+  // a step of a workgroup whose waves each take whole blocks; in fp32 its matrix instructions alone, at either width
+  constexpr double kStep = sizeof(T) == 4 ? 7.0e-6 : 2.6e-6 * DHP / 128;
   const long nz = (long)a.seqs * a.kv, group = a.heads / a.kv;
   const bool causal = a.window >= a.S;
   DkvPlan best;
   double best_time = 0;
   for (int teams = 1; teams <= BR / 32; ++teams) {
     const int own = 128 / teams, blocks = (a.S + own - 1) / own;
-    // Times in steps of a workgroup whose waves each take whole blocks (about 2.6 us for 128-wide heads); starting and ending one cost
-    // three, and a step of two teams 0.6.
+    // Times in steps; starting and ending a workgroup cost three, and a step of two teams 0.6.
     auto steps = [&](long queries) { return (double)((std::min<long>(a.S, queries) + BR - 1) / BR * group); };
     const double step = teams == 1 ? 1.0 : 0.6, walk = steps((long)own + a.window), far_walk = steps(a.S - a.window);
     for (int parts = 1; parts <= 16 && (parts == 1 || walk >= 4 * parts); ++parts) {
@@ -1314,7 +1318,7 @@ DkvPlan dkv_plan(const LocalAttention& a) {
         double time = causal ? std::max(one, all * (3 + step * walk / parts / 2) / kSlots)
                              : std::max(first, std::ceil((firsts * first / one + all - firsts) / kSlots) * one);
         // parts meet in memory: written and read at some 4 TB/s, and a launch
-        if (parts > 1 || apart) time += 1 + (parts > 1 ? (double)parts * nz * a.S * 2 * a.dh * 8 / 4e12 / (2.6e-6 * DHP / 128) : 0.0);
+        if (parts > 1 || apart) time += 1 + (parts > 1 ? (double)parts * nz * a.S * 2 * a.dh * 8 / 4e12 / kStep : 0.0);
         if (best.rows == 0 || time < best_time) {
           best = f;
           best_time = time;

@@ -44,3 +44,13 @@ def test_windowed_attention_dq_keeps_its_registers(tmp_path):
         assert int(k["vgpr_spill_count"]) == 0 and int(k["private_segment_fixed_size"]) == 0, (name, k)
         if "IfLi128" not in name:
             assert int(k["vgpr_count"]) <= (168 if "ItLi64" in name else 256), (name, k["vgpr_count"])
+
+
+@pytest.mark.skipif(not os.path.exists(READELF), reason="no llvm-readelf")
+def test_windowed_attention_dkv_workgroups_on_a_cu(tmp_path):
+    """What the launch is cut up for: two workgroups of four waves on a CU, one of fp32 heads above 64 (512 registers a SIMD)."""
+    kernels = {k: v for k, v in _kernels(tmp_path).items() if "local_dkv_kernel" in k}
+    assert len(kernels) >= 14
+    for name, k in kernels.items():
+        assert 512 // int(k["vgpr_count"]) >= 2 or "IfLi128" in name, (name, k["vgpr_count"])
+        assert 512 // int(k["vgpr_count"]) == 1 or "IfLi128" not in name, (name, k["vgpr_count"])
