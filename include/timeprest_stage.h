@@ -119,8 +119,9 @@ enum tp_layer_type {
   TP_LAYER_AVGPOOL = 8,   /* global average pooling, no parameters: a sample of [positions x C] values becomes the C
                              means over its positions; in_features = out_features = C, geom = {positions} */
   TP_LAYER_LOCAL_ATTENTION = 9 /* causal multi-head self-attention over a window of keys: geom = {tokens, heads, kv heads, window,
-                             sinks}; out_features = heads * dh (dh: 1 .. 256; at most 65535 heads, and 2^23 blocks of 16 tokens in a mini-batch), in_features = (heads + 2 * kv heads) * dh (queries | keys |
-                             values; kv heads divide heads, query head h reads key head h / (heads / kv heads)).  Query i sees key
+                             sinks}; out_features = heads * dh (dh: 1 .. 256; at most 65535 heads, and 2^23 blocks of 16 tokens in a
+                             mini-batch), in_features = (heads + 2 * kv heads) * dh (queries | keys | values; kv heads divide heads,
+                             query head h reads key head h / (heads / kv heads)).  Query i sees key
                              j <= i where i - j < window (0: every j <= i) or j < sinks (0 without a window).  rel = {buckets,
                              max distance} adds a learned bias table[h][bucket(i - j)] to the scaled scores, {0, 0}: none.  2 .. 128
                              buckets: distances 0 .. half - 1 have one each (half = buckets / 2, rounded down, < max distance <=
@@ -130,7 +131,9 @@ enum tp_layer_type {
                              it has no b).  The backward pass forms the probabilities of the forward pass again, with the table
                              that pass read (a copy is kept), under every policy.  May be the last layer of a stage.  Keys that a
                              query does not see do not reach its results, whatever they hold, nor do entries of the table that
-                             none of its pairs has */
+                             none of its pairs has.  In bf16 probabilities and gradients of scores are rounded to bf16 where they
+                             enter a product, sums are fp32, and the gradient of queries that see more than 32 keys is formed with
+                             their output as it was rounded */
 };
 
 #define TP_MAX_LAYERS 64
