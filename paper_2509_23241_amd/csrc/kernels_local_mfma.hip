@@ -1117,11 +1117,13 @@ __global__ __launch_bounds__(64 * NW, sizeof(T) == 2 || DHP == 64 ? 2 : 1) void 
             }
             if constexpr (BIAS) {
               // Here for the table's sums, which are not formed again: p = dS = 0 whatever the score, the bias, dP and the query's lse and delta
-              // are.  (As a second selection behind the other: 32 x 200 tokens 27 -> 30 us.)
+              // are.  (As a second selection behind the other: 32 x 200 tokens 27 -> 30 us.)  128-wide heads have no registers for what it takes of the
+              // lane, and work it out here: 33 spilled ones -> 23, 8 x 1024 tokens, all keys, 158 -> 154 us.
               if (masked) {
+                const int l = DHP == 128 ? afresh(lane) : lane, j = kw + (l & 31), at = qb - j + 4 * (l >> 5) + row, end = min(end_of(j), S - j);
 #pragma unroll
                 for (int w = 0; w < 4; ++w) {
-                  const bool counts = (row + w >= d_from - d0) & (row + w < d_end - d0);
+                  const bool counts = (at + w >= d_from) & (at + w < end);
                   pe[w] = counts ? pe[w] : 0.f;
                   de[w] = counts ? de[w] : 0.f;
                 }
