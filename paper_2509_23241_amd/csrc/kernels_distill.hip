@@ -58,7 +58,7 @@ struct Team {
 // rounded once and its rounding, that of `max / T`, is large where all of a row's logits are: it cancels because every numerator, sum and
 // logarithm of both exponentials is formed from this one power.  (With labels alone c = log2(e) and the power is that of exp(z) itself.)
 // T = 3, logits around 1000 or 10000, the label's logarithm from z log2(e) - top log2(e) instead: cross entropy 4e-5 or 2e-4 off.
-// Where top c is so large that its rounding alone could take an exponential out of range (T = 1e-6, logits of some thousands) the maximum is
+// Where top c is so large that its rounding alone could take an exponential out of range (T = 1e-6, logits of some thousands; T = 1e6, logits of 1e12) the maximum is
 // taken off the logits themselves first, at one more operation for each of them.
 struct Row {
   float base;          // what is taken off every logit first: 0 or top
@@ -69,7 +69,8 @@ struct Row {
     const bool only_hard = a.teacher_weight <= 0.f;
     scale = only_hard ? kLog2e : soft_scale;
     to_hard = only_hard ? 1.f : a.temperature;
-    base = fabsf(top * scale) > 0x1p24f ? top : 0.f;  // from 2^24 on the rounding is 1 and more
+    // From 2^24 on the rounding is 1 and more; it counts T times in exp(z).  (The second product may overflow to infinity, which is as good.)
+    base = fabsf(top * scale) * fmaxf(1.f, to_hard) > 0x1p24f ? top : 0.f;
     shift = (top - base) * scale;
   }
   __device__ __forceinline__ float power_of_rest(float z) const { return fmaf(z, scale, -shift); }  // base is taken off z

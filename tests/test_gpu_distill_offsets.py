@@ -140,3 +140,37 @@ def test_labels_that_have_nearly_all_the_weight(classes, dtype):
         assert abs(float(loss) - want) <= eloss + F * abs(want), (t, w)
         assert share <= 1.0, (t, w)
     st.close()
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("classes", [20, 1500, 40001, 140000])
+@pytest.mark.parametrize("t,offset", [(1e6, 1e12), (1e6, -1e12), (50.0, 1e10), (1e3, 3e8)])
+def test_large_logits_at_high_temperatures(t, offset, classes, dtype):
+    """What max / T is rounded by counts T times in the labels' softmax, which has all its probability on the largest logit here: its terms are off by
+    8 roundings.  The teacher's are bounded as above."""
+    import torch
+    rows, k = 5, 4
+    tt = torch.float32 if dtype == "f32" else torch.bfloat16
+    base = torch.tensor(offset).to(tt).double()
+    step = 2.0 ** (math.floor(math.log2(abs(offset))) - (6 if dtype == "bf16" else 20))
+    assert step >= 128
+    at = torch.arange(rows)
+    z = (base - step * (1 + torch.arange(classes).double() % 3)).repeat(rows, 1)
+    z[at, at + 3] = base
+    stored = z.to(tt)
+    assert bool((stored.double() == z).all())
+    g = torch.Generator().manual_seed(classes)
+    ids = torch.rand(rows, classes, generator=g).topk(k, 1).indices.to(torch.int32).cuda()
+    teacher, labels = torch.randn(rows, k, generator=g).cuda(), (at + 5).to(torch.int32).cuda()
+    z = z.cuda()
+    st = _stage(dtype, rows, classes)
+    for w in (0.0, 0.5, 1.0):
+        loss, grad = st.loss_distill(0, stored.cuda(), teacher, ids, temperature=t, labels=labels, label_weight=w)
+        want, dwant, eloss, egrad = _want(z, teacher, ids, t, labels, w)
+        assert abs(float(loss) - want) <= eloss + F * abs(want), w
+        if w > 0:   # without the labels' exponents in the bound: their probabilities are 0 and 1
+            _, _, _, teachers = _want(z, teacher, ids, t, labels, 0.0)
+            egrad = (1 - w) * teachers + w * (dwant != 0) * 8 * F / rows
+        bound = egrad + (2.0 ** -8 if dtype == "bf16" else F) * (dwant.abs() + egrad) + 2.0 ** -126
+        assert bool(((grad.double() - dwant).abs() <= bound).all()), w
+    st.close()
