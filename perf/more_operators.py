@@ -1,0 +1,503 @@
+"""Operators of a decoder stage that is tuned on preferences and rewards, as timed cases: each in a plain form of elementary torch
+operations (`own` false) and through the library's stages (`own` true).
+
+  gated       the first half of a gated feed-forward block, act(x Wg^T + bg) (x Wu^T + bu), forward and backward: a stage of one such
+              layer, its forward pass, backward pass and update (learning rate 0, so that passes on one state repeat)
+  rotary      rotary positions on the queries and keys of packed queries | keys | values, forward and backward: a stage of one such
+              layer; pairs of neighbours or of halves, a part of each head, frequencies scaled for long contexts
+  logprobs    the log probability of one given class of each row, as a reference or a sampling policy stores them
+  policy      the clipped policy loss with a KL term against a reference at a last stage, with its gradient
+  preference  the loss on pairs of sequences, chosen and rejected, by their log ratios to a reference, with its gradient
+
+The ranges (`draw`), on which the listed cases are points:
+  gated       1 .. 16384 rows, 64 .. 4096 values in, 64 .. 16384 out, odd ones among them, four activations; bf16, and fp32 at a
+              sixteenth of the work
+  rotary      1 .. 64 sequences of 1 .. 32768 tokens, 1 .. 32 heads 16 .. 128 wide, key heads that divide them, a half to all of each
+              head, first positions up to a million; bf16 and fp32
+  losses      1 .. 64 sequences (pairs: an even number) of 1 .. 4096 tokens, 10 .. 64000 classes, prompts and padding without a
+              term; bf16 and fp32
+"""
+import math
+
+import torch
+
+DEVICE = "cuda:0"
+own = False  # set by whoever imports the file
+
+
+# ---- the cases -----------------------------------------------------------------------------------------------------
+
+def _gated(seqs, tokens, width, inner, act, dtype):
+    return dict(kind="gated", seqs=seqs, tokens=tokens, width=width, inner=inner, act=act, dtype=dtype)
+
+
+def _rotary(seqs, tokens, heads, kv_heads, head, rotated, layout, dtype, first=0, factor=1.0, original=0):
+    return dict(kind="rotary", seqs=seqs, tokens=tokens, heads=heads, kv_heads=kv_heads, head=head, rotated=rotated, layout=layout,
+                base=10000.0, first=first, factor=factor, original=original, low=1.0 if original else 0.0,
+                high=4.0 if original else 0.0, amplitude=1.125 if original else 1.0, dtype=dtype)
+
+
+def _rows(kind, seqs, tokens, classes, dtype):
+    c = dict(kind=kind, seqs=seqs, tokens=tokens, classes=classes, dtype=dtype)
+    if kind == "policy":
+        c.update(clip_low=0.2, clip_high=0.25, kl_weight=0.05)
+    if kind == "preference":
+        c.update(beta=0.1, label_smoothing=0.1)
+    return c
+
+
+def listed():
+    return [
+        # a single token: launches and the weights' way from memory
+        dict(_gated(1, 1, 512, 1408, "silu", "bf16"), name="gated_bf16_1"),
+        # the transformer configuration's feed-forward width, one micro-batch of 8 x 1024 tokens
+        dict(_gated(8, 1024, 2048, 8192, "silu", "bf16"), name="gated_bf16_8192"),
+        # a small model in single precision, an inner width that fills no tile
+        dict(_gated(4, 333, 512, 1365, "gelu", "f32"), name="gated_f32_1332"),
+        # one new token far into a long context
+        dict(_rotary(1, 1, 16, 4, 128, 128, "halves", "bf16", first=100000, factor=8.0, original=8192), name="rotary_bf16_1"),
+        # the transformer configuration's attention, 16 heads of 128
+        dict(_rotary(8, 1024, 16, 16, 128, 128, "halves", "bf16"), name="rotary_bf16_8192"),
+        # shared key heads of another width, neighbours as pairs, a part of each head
+        dict(_rotary(4, 777, 6, 2, 80, 40, "pairs", "f32"), name="rotary_f32_3108"),
+        # a small vocabulary in single precision
+        dict(_rows("logprobs", 4, 250, 1000, "f32"), name="logprobs_f32_1000"),
+        # the decoder's vocabulary, one micro-batch of 8 x 1024 tokens
+        dict(_rows("logprobs", 8, 1024, 32000, "bf16"), name="logprobs_bf16_32000"),
+        # the smallest policy: 32 actions of 10 kinds
+        dict(_rows("policy", 32, 1, 10, "f32"), name="policy_f32_10"),
+        dict(_rows("policy", 8, 1024, 32000, "bf16"), name="policy_bf16_32000"),
+        # three pairs of odd length, an odd number of classes, in single precision
+        dict(_rows("preference", 6, 167, 32003, "f32"), name="preference_f32_32003"),
+        dict(_rows("preference", 8, 1024, 32000, "bf16"), name="preference_bf16_32000"),
+    ]
+
+
+def _log(rng, lo, hi):
+    return math.exp(rng.uniform(math.log(lo), math.log(hi)))
+
+
+def _int(rng, lo, hi):
+    return min(hi, max(lo, int(round(_log(rng, lo, hi)))))
+
+
+def _draw_once(rng):
+    dtype = rng.choice(["bf16", "bf16", "bf16", "f32"])
+    kind = rng.choice(["gated", "gated", "rotary", "rotary", "logprobs", "policy", "preference"])
+    if kind == "gated":
+        width, inner, rows = _int(rng, 64, 4096), _int(rng, 64, 16384), _int(rng, 1, 16384)
+        if rng.random() < 0.6:
+            width, inner = max(64, width // 64 * 64), max(64, inner // 64 * 64)
+        return _gated(1, rows, width, inner, rng.choice(["silu", "silu", "gelu", "relu", "none"]), dtype)
+    if kind == "rotary":
+        kv_heads, group = rng.choice([(1, 1), (2, 1), (4, 1), (8, 1), (16, 1), (32, 1), (1, 4), (2, 4), (4, 2), (3, 2), (1, 7), (8, 4)])
+        head = rng.choice([16, 32, 64, 64, 80, 96, 128, 128])
+        rotated = rng.choice([head, head, head // 2])
+        scaled = rng.random() < 0.4
+        return _rotary(_int(rng, 1, 64), _int(rng, 1, 32768), kv_heads * group, kv_heads, head, rotated, rng.choice(["halves", "pairs"]),
+                       dtype, first=rng.choice([0, 0, _int(rng, 1, 1000000)]), factor=rng.choice([2.0, 8.0]) if scaled else 1.0,
+                       original=rng.choice([0, 4096, 8192]) if scaled else 0)
+    classes = _int(rng, 10, 64000)
+    if rng.random() < 0.5:
+        classes = max(16, classes // 8 * 8)
+    seqs = _int(rng, 1, 64)
+    if kind == "preference":
+        seqs += seqs % 2
+    return _rows(kind, seqs, _int(rng, 1, 4096), classes, dtype)
+
+
+def draw(rng):
+    """Sizes are redrawn until the case costs no more than the largest listed one of its operators: operations for the gated
+    layer (fp32 a sixteenth of them), values for the others (fp32 half as many)."""
+    while True:
+        c = _draw_once(rng)
+        half = 1 if c["dtype"] == "bf16" else 2
+        if c["kind"] == "gated":
+            if work(c)["flops"] <= 12 * 8192 * 2048 * 8192 / (1 if c["dtype"] == "bf16" else 16):
+                return c
+        elif c["kind"] == "rotary":
+            if c["seqs"] * c["tokens"] * _packed(c) * half <= 8192 * 48 * 128:
+                return c
+        elif c["seqs"] * c["tokens"] * c["classes"] * half <= 8192 * 32000:
+            return c
+
+
+# ---- what a pass has to do -------------------------------------------------------------------------------------------
+
+def _packed(c):
+    return (c["heads"] + 2 * c["kv_heads"]) * c["head"]
+
+
+def work(case):
+    c = case
+    es = 2 if c["dtype"] == "bf16" else 4
+    rows = c["seqs"] * c["tokens"]
+    if c["kind"] == "gated":
+        # three products over both projections; input, output and their gradients once; each weight read, its gradient written, and
+        # the update: momentum and master in and out, in bf16 the compute copy out
+        params = 2 * c["inner"] * (c["width"] + 1)
+        return {"bytes": 2 * rows * (c["width"] + c["inner"]) * es + params * (es + 4 + 16 + (2 if es == 2 else 0)),
+                "flops": 12 * rows * c["width"] * c["inner"]}
+    if c["kind"] == "rotary":
+        turned = (c["heads"] + c["kv_heads"]) * c["rotated"]
+        return {"bytes": 4 * rows * _packed(c) * es, "flops": 6 * rows * turned}
+    logits = rows * c["classes"]
+    if c["kind"] == "logprobs":
+        return {"bytes": logits * es + 8 * rows, "flops": 4 * logits}
+    if c["kind"] == "policy":
+        return {"bytes": 2 * logits * es + 28 * rows, "flops": 6 * logits}
+    return {"bytes": 2 * logits * es + 12 * rows + 4 * c["seqs"], "flops": 6 * logits}
+
+
+# ---- inputs ----------------------------------------------------------------------------------------------------------
+
+def _type(c):
+    return torch.bfloat16 if c["dtype"] == "bf16" else torch.float32
+
+
+def _inputs(c, seed):
+    gen = torch.Generator(device=DEVICE)
+    gen.manual_seed(seed)
+
+    def normal(*shape):
+        return torch.randn(shape, generator=gen, device=DEVICE)
+
+    def uniform(*shape):
+        return torch.rand(shape, generator=gen, device=DEVICE)
+
+    s = {"case": c}
+    n, t = c["seqs"], c["tokens"]
+    if c["kind"] == "gated":
+        d, f = c["width"], c["inner"]
+        s["x"] = normal(n, t * d).to(_type(c))
+        s["dy"] = normal(n, t * f).to(_type(c))
+        # in bf16 the products read the weights in that type: masters that have it exactly
+        s["w"] = (normal(2 * f, d) * (1.5 / math.sqrt(d))).to(_type(c)).float()
+        s["b"] = 0.2 * normal(2 * f)
+        s["momentum"] = torch.zeros_like(s["w"])
+        return s
+    if c["kind"] == "rotary":
+        s["x"] = normal(n, t * _packed(c)).to(_type(c))
+        s["dy"] = normal(n, t * _packed(c)).to(_type(c))
+        return s
+    rows = n * t
+    z = 2.5 * normal(rows, c["classes"])
+    s["logits"] = z.to(_type(c))
+    ids = (z - (-uniform(*z.shape).clamp(1e-7, 1 - 1e-7).log()).log()).argmax(1)  # drawn from softmax(z)
+    # a prompt in front, which has no term, and padding behind
+    prompt = torch.randint(0, t // 4 + 1, (n, 1), generator=gen, device=DEVICE)
+    length = torch.randint(min(t, 3 * t // 4 + 1), t + 1, (n, 1), generator=gen, device=DEVICE)
+    at = torch.arange(t, device=DEVICE)[None]
+    counted = ((at >= prompt) & (at < length)).view(-1)
+    s["ids"] = torch.where(counted, ids, -1).to(torch.int32)
+    if c["kind"] == "logprobs":
+        return s
+    logp = torch.zeros(rows, dtype=torch.float64, device=DEVICE)
+    step = max(1, 2 ** 26 // c["classes"])
+    for a in range(0, rows, step):
+        logp[a:a + step] = s["logits"][a:a + step].double().log_softmax(1).gather(1, ids[a:a + step, None])[:, 0]
+    if c["kind"] == "policy":
+        s["advantages"] = normal(rows)
+        s["weights"] = counted / counted.sum().clamp(min=1)
+        moved = 0.25 * normal(rows).double()
+        # which side of a clip border a ratio is on is not left to the last bit
+        for border in (math.log1p(-c["clip_low"]), math.log1p(c["clip_high"])):
+            moved += torch.where((moved - border).abs() < 1e-3, 4e-3, 0.0)
+        s["old"] = (logp - moved).float()
+        s["ref"] = (logp + 0.3 * normal(rows)).float()
+        return s
+    s["weights"] = torch.ones(rows, device=DEVICE)
+    s["ref"] = ((logp * counted).view(n, t).sum(1) + 8 * normal(n)).float()
+    return s
+
+
+def prepare(case, seed):
+    s = _inputs(case, seed)
+    if own:
+        _attach_stage(s)
+    return s
+
+
+def _attach_stage(s):
+    """The stage that a user's program keeps, with its input where the stage wants it."""
+    from paper_2509_23241_amd.runner import GpuStage
+    import numpy as np
+    c = s["case"]
+    common = dict(dtype=c["dtype"], mb=c["seqs"], n=1, stage_index=1, num_stages=2, policy="latest", lam=0.1, lr=0.0, momentum=0.0,
+                  ring_capacity=1, max_in_flight=1, device=DEVICE)
+    if c["kind"] in ("gated", "rotary"):
+        if c["kind"] == "gated":
+            layer = ("gated", c["width"], c["inner"], c["act"], c["tokens"])
+            params = [s["w"].cpu().numpy(), s["b"].cpu().numpy()]
+        else:
+            layer = ("rotary", c["heads"], c["kv_heads"], c["head"], c["tokens"], c["rotated"], c["layout"], c["base"], c["first"],
+                     c["factor"], c["original"], c["low"], c["high"], c["amplitude"])
+            params = []
+        s["stage"] = st = GpuStage([layer], params, **common)
+        view = st.input_view(0, 0)
+        view.copy_(s["x"])
+        s["x"], s["j"] = view, 0
+        s["y"], s["dx"] = torch.empty_like(s["dy"]), torch.empty_like(view)
+        return
+    s["stage"] = st = GpuStage([(8, c["classes"], "none", c["tokens"])],
+                               [np.zeros((c["classes"], 8), np.float32), np.zeros(c["classes"], np.float32)], **common)
+    # a loss belongs to a mini-batch in flight
+    st.forward(0, 0, torch.zeros(c["seqs"], c["tokens"] * 8, dtype=st.tdtype, device=DEVICE))
+
+
+# ---- one pass --------------------------------------------------------------------------------------------------------
+
+def run(state):
+    kind = state["case"]["kind"]
+    if own:
+        return {"gated": _own_layer, "rotary": _own_layer, "logprobs": _own_logprobs, "policy": _own_policy,
+                "preference": _own_preference}[kind](state)
+    return {"gated": _plain_gated, "rotary": _plain_rotary, "logprobs": _plain_logprobs, "policy": _plain_policy,
+            "preference": _plain_preference}[kind](state)
+
+
+def _own_layer(s):
+    st, j, c = s["stage"], s["j"], s["case"]
+    s["j"] += 1
+    st.forward(j, 0, s["x"], s["y"])
+    st.backward(j, s["dy"], s["dx"])
+    st.blend_update(j)
+    out = {"y": s["y"], "dx": s["dx"]}
+    if c["kind"] == "gated":
+        # in the type that workers exchange them in
+        w, b = st.sizes.w_offset[0], st.sizes.b_offset[0]
+        out["dw"] = st.grad[w: w + s["w"].numel()].view_as(s["w"]).to(_type(c))
+        out["db"] = st.grad[b: b + s["b"].numel()].to(_type(c))
+    return out
+
+
+def _own_logprobs(s):
+    return {"logp": s["stage"].logprobs(s["logits"], s["ids"])}
+
+
+def _own_policy(s):
+    c = s["case"]
+    loss, dlogits, logp = s["stage"].loss_policy(0, s["logits"], s["ids"], s["old"], s["advantages"], weights=s["weights"],
+                                                 ref_logp=s["ref"], clip_low=c["clip_low"], clip_high=c["clip_high"],
+                                                 kl_weight=c["kl_weight"])
+    return {"loss": loss, "dlogits": dlogits, "logp": logp}
+
+
+def _own_preference(s):
+    c = s["case"]
+    loss, dlogits, logp = s["stage"].loss_preference(0, s["logits"], s["ids"], s["ref"], weights=s["weights"], beta=c["beta"],
+                                                     label_smoothing=c["label_smoothing"])
+    return {"loss": loss, "dlogits": dlogits, "logp": logp}
+
+
+def _plain_gated(s):
+    c = s["case"]
+    f, kind = c["inner"], c["act"]
+    x = s["x"].view(-1, c["width"]).float()
+    dy = s["dy"].view(-1, f).float()
+    z = x @ s["w"].t() + s["b"]
+    gate, up = z[:, :f], z[:, f:]
+    if kind == "silu":
+        sig = 1 / (1 + torch.exp(-gate))
+        act, slope = gate * sig, sig * (1 + gate * (1 - sig))
+    elif kind == "gelu":
+        cdf = 0.5 * (1 + torch.erf(gate / math.sqrt(2)))
+        act, slope = gate * cdf, cdf + gate * torch.exp(-0.5 * gate * gate) / math.sqrt(2 * math.pi)
+    elif kind == "relu":
+        act, slope = gate.clamp(min=0), (gate > 0).float()
+    else:
+        act, slope = gate, torch.ones_like(gate)
+    y = act * up
+    dz = torch.cat([dy * up * slope, dy * act], 1)
+    dx = dz @ s["w"]
+    dw = dz.t() @ x
+    db = dz.sum(0)
+    s["momentum"].mul_(0.0).add_(dw)
+    s["w"].sub_(s["momentum"], alpha=0.0)
+    t = _type(c)
+    return {"y": y.to(t).view_as(s["dy"]), "dx": dx.to(t).view_as(s["x"]), "dw": dw.to(t), "db": db.to(t)}
+
+
+def _angles(c):
+    """Of every position and pair, in 64 bits."""
+    half = c["rotated"] // 2
+    speed = c["base"] ** (-torch.arange(half, dtype=torch.float64, device=DEVICE) / half)
+    if c["original"]:
+        keep = ((speed * c["original"] / (2 * math.pi) - c["low"]) / (c["high"] - c["low"])).clamp(0, 1)
+        speed = speed * ((1 - keep) / c["factor"] + keep)
+    else:
+        speed = speed / c["factor"]
+    at = torch.arange(c["tokens"], dtype=torch.float64, device=DEVICE) + c["first"]
+    return at[:, None] * speed
+
+
+def _turn(x, c, cos, sin):
+    half, heads = c["rotated"] // 2, c["heads"] + c["kv_heads"]
+    v = x.view(c["seqs"], c["tokens"], -1, c["head"]).float()
+    out = v.clone()
+    part = v[:, :, :heads, :c["rotated"]]
+    if c["layout"] == "pairs":
+        a, b = part[..., 0::2], part[..., 1::2]
+        turned = torch.stack([a * cos - b * sin, a * sin + b * cos], -1).flatten(-2)
+    else:
+        a, b = part[..., :half], part[..., half:]
+        turned = torch.cat([a * cos - b * sin, a * sin + b * cos], -1)
+    out[:, :, :heads, :c["rotated"]] = turned
+    return out.to(_type(c)).view_as(x)
+
+
+def _plain_rotary(s):
+    c = s["case"]
+    angle = _angles(c)
+    cos = (angle.cos() * c["amplitude"]).float()[:, None]
+    sin = (angle.sin() * c["amplitude"]).float()[:, None]
+    return {"y": _turn(s["x"], c, cos, sin), "dx": _turn(s["dy"], c, cos, -sin)}
+
+
+def _log_softmax_parts(s):
+    """Of each row: exp(z - top), their sum in 64 bits, whether it counts, its class and that class's log probability."""
+    z = s["logits"].float()
+    counts = s["ids"] >= 0
+    ids = s["ids"].long().clamp(min=0)[:, None]
+    top = z.amax(1, keepdim=True)
+    mine = (z.gather(1, ids) - top)[:, 0].double()
+    e = torch.exp(z - top)
+    total = e.sum(1, dtype=torch.float64)
+    return e, total, counts, ids, torch.where(counts, mine - total.log(), 0.0)
+
+
+def _plain_logprobs(s):
+    return {"logp": _log_softmax_parts(s)[4].float()}
+
+
+def _row_gradient(e, total, ids, dlogp, dtype):
+    """d logp / dz = [j = id] - softmax(z), times dlogp of the row."""
+    dlogp = dlogp[:, None]
+    grad = e * (-dlogp / total[:, None]).float()
+    grad.scatter_add_(1, ids, dlogp.float())
+    return grad.to(dtype)
+
+
+def _plain_policy(s):
+    c = s["case"]
+    e, total, counts, ids, logp = _log_softmax_parts(s)
+    weight = s["weights"].double() * counts
+    advantage = s["advantages"].double()
+    moved = torch.where(counts, logp - s["old"].double(), 0.0)
+    ratio = moved.exp()
+    gain = ratio * advantage
+    clipped = ratio.clamp(1 - c["clip_low"], 1 + c["clip_high"]) * advantage
+    away = torch.where(counts, s["ref"].double() - logp, 0.0)
+    kl = away.exp() - 1 - away
+    loss = (weight * (c["kl_weight"] * kl - torch.minimum(gain, clipped))).sum()
+    dlogp = weight * (c["kl_weight"] * (1 - away.exp()) - gain * (gain <= clipped))
+    return {"loss": loss.float().view(1), "dlogits": _row_gradient(e, total, ids, dlogp, _type(c)), "logp": logp.float()}
+
+
+def _plain_preference(s):
+    c = s["case"]
+    e, total, counts, ids, logp = _log_softmax_parts(s)
+    weight = s["weights"].double() * counts
+    ratio = (weight * logp).view(c["seqs"], c["tokens"]).sum(1) - s["ref"].double()
+    margin = c["beta"] * (ratio[0::2] - ratio[1::2])
+    smooth, pairs = c["label_smoothing"], c["seqs"] // 2
+    right = 1 / (1 + torch.exp(-margin))
+    loss = -((1 - smooth) * right.log() + smooth * (1 - right).log()).sum() / pairs
+    pull = c["beta"] / pairs * (smooth * right - (1 - smooth) * (1 - right))
+    by_seq = torch.stack([pull, -pull], 1).view(-1, 1)
+    dlogp = (by_seq * weight.view(c["seqs"], c["tokens"])).view(-1)
+    return {"loss": loss.float().view(1), "dlogits": _row_gradient(e, total, ids, dlogp, _type(c)), "logp": logp.float()}
+
+
+# ---- the definitions in 64 bits --------------------------------------------------------------------------------------
+
+def exact(case, seed):
+    c, s = case, _inputs(case, seed)
+    if c["kind"] == "gated":
+        return _exact_gated(c, s)
+    if c["kind"] == "rotary":
+        return _exact_rotary(c, s)
+    return _exact_rows(c, s)
+
+
+def _exact_gated(c, s):
+    """The output as defined, its gradients by differentiating it, some rows at a time."""
+    rows, d, f = c["seqs"] * c["tokens"], c["width"], c["inner"]
+    x, dy = s["x"].view(rows, d), s["dy"].view(rows, f)
+    w, b = s["w"].double().requires_grad_(True), s["b"].double().requires_grad_(True)
+    act = {"silu": torch.nn.functional.silu, "gelu": torch.nn.functional.gelu, "relu": torch.relu, "none": lambda v: v}[c["act"]]
+    y = torch.empty(rows, f, dtype=torch.float64, device=DEVICE)
+    dx = torch.empty(rows, d, dtype=torch.float64, device=DEVICE)
+    dw, db = torch.zeros_like(w), torch.zeros_like(b)
+    for a in range(0, rows, 2048):
+        at = slice(a, a + 2048)
+        xi = x[at].double().requires_grad_(True)
+        z = torch.nn.functional.linear(xi, w, b)
+        gate, up = z.split(f, 1)
+        out = act(gate) * up
+        gx, gw, gb = torch.autograd.grad(out, [xi, w, b], dy[at].double())
+        y[at], dx[at] = out.detach(), gx
+        dw += gw
+        db += gb
+    return {"y": y.view_as(s["dy"]), "dx": dx.view_as(s["x"]), "dw": dw.detach(), "db": db.detach()}
+
+
+def _exact_rotary(c, s):
+    """Pairs as complex numbers, turned by a factor of their own."""
+    half, heads = c["rotated"] // 2, c["heads"] + c["kv_heads"]
+    pair = torch.arange(half, dtype=torch.float64, device=DEVICE)
+    speed = torch.exp(-math.log(c["base"]) * 2 * pair / c["rotated"])
+    if c["original"]:
+        turns = c["original"] * speed / (2 * math.pi)
+        share = torch.clip((turns - c["low"]) / (c["high"] - c["low"]), 0, 1)
+        speed = torch.lerp(speed / c["factor"], speed, share)
+    else:
+        speed = speed / c["factor"]
+    at = torch.arange(c["first"], c["first"] + c["tokens"], dtype=torch.float64, device=DEVICE)
+    by = torch.polar(torch.full((c["tokens"], half), c["amplitude"], dtype=torch.float64, device=DEVICE), torch.outer(at, speed))
+
+    def turn(x, by):
+        out = x.double().view(c["seqs"], c["tokens"], -1, c["head"])
+        part = out[:, :, :heads, :c["rotated"]]
+        if c["layout"] == "halves":
+            turned = torch.complex(part[..., :half].contiguous(), part[..., half:].contiguous()) * by[:, None]
+            out[:, :, :heads, :half], out[:, :, :heads, half:c["rotated"]] = turned.real, turned.imag
+        else:
+            turned = torch.complex(part[..., ::2].contiguous(), part[..., 1::2].contiguous()) * by[:, None]
+            out[:, :, :heads, 0:c["rotated"]:2], out[:, :, :heads, 1:c["rotated"]:2] = turned.real, turned.imag
+        return out.view_as(x)
+
+    return {"y": turn(s["x"], by), "dx": turn(s["dy"], by.conj())}
+
+
+def _exact_rows(c, s):
+    """Log probabilities some rows at a time; the loss as a function of them, differentiated; then the rows again."""
+    rows = c["seqs"] * c["tokens"]
+    counts, ids = s["ids"] >= 0, s["ids"].long().clamp(min=0)
+    step = max(1, 2 ** 25 // c["classes"])
+    logp = torch.cat([s["logits"][a:a + step].double().log_softmax(1).gather(1, ids[a:a + step, None])[:, 0]
+                      for a in range(0, rows, step)])
+    logp = torch.where(counts, logp, 0.0).requires_grad_(True)
+    out = {"logp": logp.detach()}
+    if c["kind"] == "logprobs":
+        return out
+    if c["kind"] == "policy":
+        ratio = torch.exp(torch.where(counts, logp - s["old"].double(), 0.0))
+        inside = torch.clamp(ratio, 1 - c["clip_low"], 1 + c["clip_high"])
+        advantage = s["advantages"].double()
+        away = torch.where(counts, s["ref"].double() - logp, 0.0)
+        each = c["kl_weight"] * (torch.expm1(away) - away) - torch.minimum(ratio * advantage, inside * advantage)
+        loss = (s["weights"].double() * counts * each).sum()
+    else:
+        sums = (s["weights"].double() * counts * logp).view(c["seqs"], c["tokens"]).sum(1) - s["ref"].double()
+        margin = c["beta"] * (sums.view(-1, 2)[:, 0] - sums.view(-1, 2)[:, 1])
+        log_sig = torch.nn.functional.logsigmoid
+        loss = -((1 - c["label_smoothing"]) * log_sig(margin) + c["label_smoothing"] * log_sig(-margin)).mean()
+    by_row = torch.autograd.grad(loss, logp)[0]
+    grad = torch.empty(s["logits"].shape, dtype=torch.float64, device=DEVICE)
+    for a in range(0, rows, step):
+        b = slice(a, a + step)
+        part = s["logits"][b].double().softmax(1).mul_(-by_row[b, None])
+        grad[b] = part.scatter_add_(1, ids[b, None], by_row[b, None])
+    out.update(loss=loss.detach().view(1), dlogits=grad)
+    return out
