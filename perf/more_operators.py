@@ -2,7 +2,8 @@
 operations (`own` false) and through the library's stages (`own` true).
 
   gated       the first half of a gated feed-forward block, act(x Wg^T + bg) (x Wu^T + bu), forward and backward: a stage of one such
-              layer, its forward pass, backward pass and update (learning rate 0, so that passes on one state repeat)
+              layer (rows of W: gate and other factor of each value in turn), its forward pass, backward pass and update (learning
+              rate 0, so that passes on one state repeat)
   rotary      rotary positions on the queries and keys of packed queries | keys | values, forward and backward: a stage of one such
               layer; pairs of neighbours or of halves, a part of each head, frequencies scaled for long contexts
   logprobs    the log probability of one given class of each row, as a reference or a sampling policy stores them
@@ -296,7 +297,7 @@ def _plain_gated(s):
     x = s["x"].view(-1, c["width"]).float()
     dy = s["dy"].view(-1, f).float()
     z = x @ s["w"].t() + s["b"]
-    gate, up = z[:, :f], z[:, f:]
+    gate, up = z[:, 0::2], z[:, 1::2]
     if kind == "silu":
         sig = 1 / (1 + torch.exp(-gate))
         act, slope = gate * sig, sig * (1 + gate * (1 - sig))
@@ -308,7 +309,7 @@ def _plain_gated(s):
     else:
         act, slope = gate, torch.ones_like(gate)
     y = act * up
-    dz = torch.cat([dy * up * slope, dy * act], 1)
+    dz = torch.stack([dy * up * slope, dy * act], 2).view(-1, 2 * f)
     dx = dz @ s["w"]
     dw = dz.t() @ x
     db = dz.sum(0)
@@ -433,7 +434,7 @@ def _exact_gated(c, s):
         at = slice(a, a + 2048)
         xi = x[at].double().requires_grad_(True)
         z = torch.nn.functional.linear(xi, w, b)
-        gate, up = z.split(f, 1)
+        gate, up = z.view(-1, f, 2).unbind(2)
         out = act(gate) * up
         gx, gw, gb = torch.autograd.grad(out, [xi, w, b], dy[at].double())
         y[at], dx[at] = out.detach(), gx
