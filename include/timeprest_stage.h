@@ -81,7 +81,7 @@ enum tp_policy {
 };
 
 enum tp_dtype { TP_F32 = 0, TP_BF16 = 1 };
-enum tp_act { TP_ACT_NONE = 0, TP_ACT_RELU = 1, TP_ACT_GELU = 2 /* exact erf form */ };
+enum tp_act { TP_ACT_NONE = 0, TP_ACT_RELU = 1, TP_ACT_GELU = 2 /* exact erf form */, TP_ACT_SILU = 3 /* z / (1 + e^-z); gated layers */ };
 enum tp_layer_type {
   TP_LAYER_DENSE = 0,    /* z = x W^T + b, a = act(z);  W[out x in].  geom[0] = token positions per sample
                             (0 or 1: one): the layer is applied to every position of a [tokens x in] sample */
@@ -118,7 +118,7 @@ enum tp_layer_type {
                              C * element size a multiple of 16 bytes */
   TP_LAYER_AVGPOOL = 8,   /* global average pooling, no parameters: a sample of [positions x C] values becomes the C
                              means over its positions; in_features = out_features = C, geom = {positions} */
-  TP_LAYER_LOCAL_ATTENTION = 9 /* causal multi-head self-attention over a window of keys: geom = {tokens, heads, kv heads, window,
+  TP_LAYER_LOCAL_ATTENTION = 9, /* causal multi-head self-attention over a window of keys: geom = {tokens, heads, kv heads, window,
                              sinks}; out_features = heads * dh (dh: 1 .. 256; at most 65535 heads, and 2^23 blocks of 16 tokens in a
                              mini-batch), in_features = (heads + 2 * kv heads) * dh (queries | keys | values; kv heads divide heads,
                              query head h reads key head h / (heads / kv heads)).  Query i sees key
@@ -134,6 +134,22 @@ enum tp_layer_type {
                              none of its pairs has.  In bf16 probabilities and gradients of scores are rounded to bf16 where they
                              enter a product, sums are fp32, and the gradient of queries that see more than 32 keys is formed with
                              their output as it was rounded */
+  TP_LAYER_GATED = 10,    /* both projections of a gated feed-forward block, their activation and product: a[f] = act(z[2f]) *
+                             z[2f + 1], z = x W^T + b, applied to every position of a [tokens x in] sample; in_features,
+                             out_features = F, geom = {tokens}; W[2F x in] and b[2F], whose rows are the gate (2f) and the other
+                             factor (2f + 1) of each output in turn; any activation.  Kept for the backward pass, in the
+                             activation type: z[2f + 1] act'(z[2f]) and act(z[2f]) */
+  TP_LAYER_ROTARY = 11    /* rotary positions, no parameters: in_features = out_features = (heads + 2 kv heads) * dh (queries | keys |
+                             values, as the attention layers take them), geom = {tokens, heads, kv heads, rotated, layout}.  In every
+                             query and key head the first `rotated` values (even, 2 .. dh <= 256) are turned in pairs: value 2i with
+                             2i + 1 (layout 0) or i with i + rotated / 2 (layout 1); the rest and the values pass unchanged.  Pair i
+                             at position p of a sample: (u, v) -> amplitude * (u cos t - v sin t, u sin t + v cos t), t = (first + p) *
+                             speed_i.  rel = {first, original}, rope = {base, factor, low, high, amplitude}; with s = base^(-2i /
+                             rotated), speed_i = s / factor where original = 0 (low = high = 0), else s * ((1 - g) / factor + g), g =
+                             (original * s / 2pi - low) / (high - low) held to 0 .. 1: pairs that turn less than `low` times over
+                             `original` positions are slowed down, those of more than `high` are not.  Angles are formed in fp64.
+                             The backward pass turns back (times amplitude).  Between a dense layer without activation and an
+                             attention layer the turn is made in place */
 };
 
 #define TP_MAX_LAYERS 64
@@ -146,9 +162,13 @@ typedef struct tp_layer_desc {
   int32_t out_features; /* dense: columns of the layer output; conv/pool: output channels; others: see the type */
   int32_t geom[5];      /* conv: {H, W, kernel, stride, pad}; pool: {H, W, 0, 0, 0}; dense, layer norm: {tokens};
                            attention: {tokens, heads}; windowed attention: {tokens, heads, kv heads, window, sinks}; residual: {tokens, mark[, tokens out]}; batch norm: {positions};
+                           gated: {tokens}; rotary: {tokens, heads, kv heads, rotated, layout};
                            subsampling: {H, W}; average pooling: {positions}; unused entries zero */
-  int32_t rel[2];       /* windowed attention: {buckets, max distance} of a position bias; others: zero */
-  int32_t reserved[5];  /* must be zero */
+  int32_t rel[2];       /* windowed attention: {buckets, max distance} of a position bias; rotary: {first, original}; others: zero */
+  union {
+    int32_t reserved[5]; /* must be zero */
+    float rope[5];       /* rotary: {base, factor, low, high, amplitude} */
+  };
 } tp_layer_desc;
 
 typedef struct tp_stage_desc {
@@ -246,7 +266,7 @@ int stage_forward(tp_stage* st, uint64_t mb_id, uint32_t ub_idx, const void* x_d
                   uint64_t* version_used);
 
 /* All n micro-batches of mini-batch mb_id, none of which has been forwarded yet: x_dev and y_dev hold [n*mb x ...], micro-batch by
- * micro-batch.  What n calls of stage_forward do; stages of dense, normalisation (per token) and residual layers without forward
+ * micro-batch.  What n calls of stage_forward do; stages of dense, gated, rotary, normalisation (per token) and residual layers without forward
  * streams take one kernel per layer for all of them.  Outputs and saved tensors are the same bits, with one exception: TP_BF16 stages
  * of dense layers alone (one token position each, in_features a multiple of 8) without forward streams.  There a product of at most
  * 256 tiles of 32 x 32 outputs sums over in_features in four parts, any other in one chain, so that a sum of this call's n*mb rows may
@@ -275,7 +295,7 @@ int stage_forward_on(tp_stage* st, uint64_t mb_id, uint32_t ub_idx, uint64_t ver
  *   - stage_backward / stage_backward_on make the stage's stream wait for the forward passes of THEIR mini-batch
  *     and for no others: forwards of later mini-batches enqueued before the call keep running beside the backward
  *     pass;
- *   - every other call that enqueues work or hands out results (stage_blend_update[_noalloc], stage_loss_softmax_ce, stage_loss_distill,
+ *   - every other call that enqueues work or hands out results (stage_blend_update[_noalloc], stage_loss_*, stage_logprobs,
  *     stage_saved_input_ptr, stage_export_params, stage_profile_begin, stage_forward_join) first makes the stage's
  *     stream wait for all forward streams.  Read y_dev on the stage's stream only after one of them.
  * Refused (TP_EINVAL) for stages with TP_LAYER_ATTENTION layers, whose forward kernels share their scratch memory, and under
@@ -296,7 +316,8 @@ int stage_input_ptr(tp_stage* st, uint64_t mb_id, uint32_t ub_idx, void** x_dev)
  * stage and must not be written.  Valid from that micro-batch's stage_forward until the mini-batch's
  * stage_backward.  Not every layer's input is materialised: the input of a residual add whose producer formed
  * the sum in its own kernel, and of a few-channel first convolution (kept padded to 8 channels elsewhere), are
- * never written -- the contents behind their pointers are unspecified.  bytes (optional) receives the size.
+ * never written -- the contents behind their pointers are unspecified, as for a rotary layer at the start of a stage; where such a
+ * layer works in place, its output lies there.  bytes (optional) receives the size.
  * TP_ESTATE: that micro-batch is not in flight. */
 int stage_saved_input_ptr(tp_stage* st, uint64_t mb_id, uint32_t ub_idx, int32_t layer, void** x_dev,
                           uint64_t* bytes);
@@ -325,6 +346,39 @@ int stage_loss_softmax_ce(tp_stage* st, uint64_t mb_id, const void* logits_dev,
 int stage_loss_distill(tp_stage* st, uint64_t mb_id, const void* logits_dev, const float* teacher_logits_dev,
                        const int32_t* teacher_ids_dev, int32_t k, double temperature, const int32_t* labels_dev,
                        double label_weight, void* dlogits_dev, float* loss_dev);
+
+/* Log probabilities of one given class per row: logp[r] = log softmax(logits[r])[id[r]], as a sampling policy or a reference stores them
+ * for the two losses below.  Any `rows` rows of the stage's classes (out_features of its dense last layer) in the activation type,
+ * of whichever pass: no mini-batch has to be in flight.  ids_dev: int32[rows]; a negative one: no token, logp 0 whatever its logits hold;
+ * one past the classes: NaN.  logp_dev: float[rows].  rows = 0 does nothing; TP_EINVAL beyond 2^31 - 1. */
+int stage_logprobs(tp_stage* st, const void* logits_dev, const int32_t* ids_dev, uint64_t rows, float* logp_dev);
+
+/* The clipped policy loss at the last stage and its gradient; stands in for stage_loss_softmax_ce.  rows = n*mb * token positions of
+ * the (dense) last layer; per row, with l = log softmax(logits)[action], r = exp(l - old_logp), d = ref_logp - l:
+ *   row = -min(r A, clip(r, 1 - clip_low, 1 + clip_high) A) + kl_weight * (exp(d) - d - 1),   loss = sum of weight * row
+ * (row values in fp32, added up in fp64), dlogits_dev its gradient; where both sides of the minimum are equal it is that of r A.
+ * actions_dev: int32[rows]; a negative one (a prompt, padding) or a weight of 0: no term, and a gradient of 0 whatever the row's
+ * logits and other values hold.  An action past the classes makes the loss and its logp NaN; its row has no gradient.
+ * old_logp_dev, advantages_dev: float[rows].  weights_dev: float[rows], or NULL: 1 / rows each.  ref_logp_dev: float[rows]; with
+ * kl_weight 0 it is not read and may be NULL.  logp_dev: float[rows], receives l (0 where there is no term), or NULL.
+ * logits_dev and dlogits_dev must not overlap.  TP_EINVAL: clip_low outside 0 .. 1, clip_high or kl_weight outside 0 .. 1e6. */
+int stage_loss_policy(tp_stage* st, uint64_t mb_id, const void* logits_dev, const int32_t* actions_dev, const float* old_logp_dev,
+                      const float* advantages_dev, const float* weights_dev, const float* ref_logp_dev, double clip_low,
+                      double clip_high, double kl_weight, void* dlogits_dev, float* logp_dev, float* loss_dev);
+
+/* The loss on pairs of sequences at the last stage and its gradient; stands in for stage_loss_softmax_ce.  Samples 2i and 2i + 1 of
+ * the mini-batch (n*mb of them, an even number) are the chosen and the rejected sequence of pair i.  With l_t = log softmax(logits_t)
+ * [target_t] at token position t of a sample, s = sum of weight_t l_t over its positions (in fp64):
+ *   m = beta * ((s_chosen - ref_chosen) - (s_rejected - ref_rejected)),
+ *   loss = mean over pairs of -(1 - label_smoothing) log sigmoid(m) - label_smoothing log sigmoid(-m),  dlogits_dev its gradient.
+ * targets_dev: int32[rows]; a negative one (a prompt, padding) or a weight of 0: no term, as above; one past the classes makes the
+ * loss, its logp and the gradients of its pair's rows NaN.  weights_dev: float[rows], or NULL: 1 each.  ref_logp_dev: float[n*mb],
+ * the reference's s of each sample.  logp_dev: float[rows], receives l (0 where there is no term); the passes of this call read it
+ * again.  logits_dev and dlogits_dev must not overlap.  TP_EINVAL: an odd number of samples, beta outside 0 .. 1e6, label_smoothing
+ * outside 0 .. 1. */
+int stage_loss_preference(tp_stage* st, uint64_t mb_id, const void* logits_dev, const int32_t* targets_dev, const float* weights_dev,
+                          const float* ref_logp_dev, double beta, double label_smoothing, void* dlogits_dev, float* logp_dev,
+                          float* loss_dev);
 
 /* The one backward pass of mini-batch `mb_id` over all its n micro-batches (Section
  * "Methodology"), on W_b = alpha(delta) W[v_f] + beta(delta) W[latest] with
@@ -430,7 +484,7 @@ enum tp_kernel_class {
   TP_K_COPY = 8,     /* device-to-device copies and conversions      */
   TP_K_POOL = 9,     /* max pooling forward / backward               */
   TP_K_NORM = 10,    /* layer normalisation forward / backward       */
-  TP_K_ATTN = 11,    /* attention forward / backward                 */
+  TP_K_ATTN = 11,    /* attention forward / backward, rotary turns   */
   TP_K_ADD = 12,     /* residual additions                           */
   TP_K_SUMS = 13,    /* a backward pass's sums of partials, one launch */
   TP_K_CLASSES = 14

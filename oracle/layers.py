@@ -24,6 +24,8 @@ def act_forward(z, act):
         return np.maximum(z, 0.0)
     if act == "gelu":
         return 0.5 * z * (1.0 + erf(z / _SQRT2))          # exact (erf) form
+    if act == "silu":
+        return z / (1.0 + np.exp(-z))
     if act == "none":
         return z
     raise ValueError(act)
@@ -34,6 +36,9 @@ def act_derivative(z, act):
         return (z > 0.0).astype(np.float64)                # derivative 0 at z = 0
     if act == "gelu":
         return 0.5 * (1.0 + erf(z / _SQRT2)) + z * _INV_SQRT_2PI * np.exp(-0.5 * z * z)
+    if act == "silu":
+        s = 1.0 / (1.0 + np.exp(-z))
+        return s * (1.0 + z * (1.0 - s))
     if act == "none":
         return np.ones_like(z)
     raise ValueError(act)
@@ -50,6 +55,91 @@ def dense_backward(dz, x, W_b):
     """
     dz2, x2 = dz.reshape(-1, dz.shape[-1]), x.reshape(-1, x.shape[-1])
     return dz2.T @ x2, dz2.sum(axis=0), dz @ W_b
+
+
+def gated_forward(z, act):
+    """Output f of a gated layer: act(z[2f]) * z[2f + 1], z the dense product with its 2F rows of weights."""
+    return act_forward(z[..., 0::2], act) * z[..., 1::2]
+
+
+def gated_backward(dy, z, act):
+    """dL/dz given dy = dL/doutput."""
+    dz = np.empty_like(z)
+    dz[..., 0::2] = dy * z[..., 1::2] * act_derivative(z[..., 0::2], act)
+    dz[..., 1::2] = dy * act_forward(z[..., 0::2], act)
+    return dz
+
+
+def rotary_speeds(spec):
+    """Angle of each pair per position: base^(-2i / rotated), slowed down by `factor`; with an original length by parts: pairs that
+    turn fewer than `low` times over it fully, those of more than `high` turns not at all."""
+    s = float(spec.base) ** (-2.0 * np.arange(spec.rotated // 2) / spec.rotated)
+    if not spec.original:
+        return s / spec.factor
+    g = np.clip((spec.original * s / (2 * np.pi) - spec.low) / (spec.high - spec.low), 0.0, 1.0)
+    return s * ((1.0 - g) / spec.factor + g)
+
+
+def rotary(x, spec, back=False):
+    """x: [B, S, (heads + 2 kv_heads) * head] = (queries | keys | values); the first `rotated` values of every query and key head
+    turned by the angles of their positions (back: the other way, which is the gradient)."""
+    B, S, _ = x.shape
+    v = np.array(x.reshape(B, S, -1, spec.head))
+    angle = (spec.first + np.arange(S))[:, None] * rotary_speeds(spec)
+    cos, sin = (spec.amplitude * f(angle)[None, :, None] for f in (np.cos, np.sin))
+    if back:
+        sin = -sin
+    heads, half = spec.heads + spec.kv_heads, spec.rotated // 2
+    first = slice(0, half) if spec.layout == "halves" else slice(0, spec.rotated, 2)
+    second = slice(half, spec.rotated) if spec.layout == "halves" else slice(1, spec.rotated, 2)
+    a, b = v[:, :, :heads, first].copy(), v[:, :, :heads, second].copy()
+    v[:, :, :heads, first] = a * cos - b * sin
+    v[:, :, :heads, second] = a * sin + b * cos
+    return v.reshape(x.shape)
+
+
+def policy_loss(logits, actions, old, advantages, weights=None, ref=None, clip_low=0.2, clip_high=0.2, kl_weight=0.0):
+    """(loss, dlogits, logp): sum over rows with an action of weight * (-min(r A, clip(r) A) + kl_weight (e^d - d - 1)), r = e^(logp -
+    old), d = ref - logp; weights None: 1 / rows."""
+    rows = logits.shape[0]
+    weights = np.full(rows, 1.0 / rows) if weights is None else weights
+    loss, logp, dz = 0.0, np.zeros(rows), np.zeros_like(logits)
+    for r in range(rows):
+        if actions[r] < 0 or weights[r] == 0:
+            continue
+        p = np.exp(logits[r] - logits[r].max())
+        p /= p.sum()
+        logp[r] = np.log(p[actions[r]])
+        ratio = np.exp(logp[r] - old[r])
+        inside = min(max(ratio, 1 - clip_low), 1 + clip_high)
+        loss -= weights[r] * min(ratio * advantages[r], inside * advantages[r])
+        slope = -ratio * advantages[r] if ratio * advantages[r] <= inside * advantages[r] else 0.0
+        if kl_weight > 0:
+            d = ref[r] - logp[r]
+            loss += weights[r] * kl_weight * (np.exp(d) - d - 1)
+            slope += kl_weight * (1 - np.exp(d))
+        dz[r] = -weights[r] * slope * p
+        dz[r, actions[r]] += weights[r] * slope
+    return loss, dz, logp
+
+
+def preference_loss(logits, targets, ref, tokens, weights=None, beta=0.1, smoothing=0.0):
+    """(loss, dlogits, logp): rows are samples of `tokens` positions, samples 2i and 2i + 1 the chosen and the rejected one of a pair;
+    mean of -(1 - smoothing) log sig(m) - smoothing log sig(-m), m = beta ((s_c - ref_c) - (s_r - ref_r)), s a sample's weighted sum."""
+    rows, pairs = logits.shape[0], logits.shape[0] // (2 * tokens)
+    weights = np.where(np.asarray(targets) < 0, 0.0, 1.0 if weights is None else weights)
+    z = logits - logits.max(axis=1, keepdims=True)
+    p = np.exp(z) / np.exp(z).sum(axis=1, keepdims=True)
+    at = np.maximum(targets, 0)
+    logp = np.where(weights != 0, np.log(p[np.arange(rows), at]), 0.0)
+    s = (weights * logp).reshape(pairs, 2, tokens).sum(axis=2) - np.asarray(ref).reshape(pairs, 2)
+    m = beta * (s[:, 0] - s[:, 1])
+    loss = ((1 - smoothing) * np.logaddexp(0, -m) + smoothing * np.logaddexp(0, m)).mean()
+    pull = beta / pairs * (smoothing / (1 + np.exp(-m)) - (1 - smoothing) / (1 + np.exp(m)))
+    slope = (np.stack([pull, -pull], axis=1).reshape(-1, 1) * weights.reshape(-1, tokens)).reshape(-1)
+    dz = -slope[:, None] * p
+    dz[np.arange(rows), at] += slope
+    return loss, dz, logp
 
 
 def softmax_cross_entropy(logits, labels, denom):

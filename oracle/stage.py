@@ -56,7 +56,7 @@ class Stage:
         self.pidx, nxt = [], 0
         for spec in self.specs:
             kind = getattr(spec, "kind", "dense")
-            if kind in ("pool", "attn", "res", "sub", "swap", "avg") or (kind == "local" and not spec.buckets):
+            if kind in ("pool", "attn", "res", "sub", "swap", "avg", "rotary") or (kind == "local" and not spec.buckets):
                 self.pidx.append(None)
             else:
                 self.pidx.append(nxt)
@@ -177,6 +177,17 @@ class Stage:
                 a = self.q(L.local_attention_forward(a, spec, table))
                 outs.append(a)
                 continue
+            if kind == "rotary":
+                saved.append(None)
+                a = self.q(L.rotary(a, spec))
+                outs.append(a)
+                continue
+            if kind == "gated":
+                z = L.dense_forward(a, W[pi], W[pi + 1])
+                saved.append((a, z))
+                a = self.q(L.gated_forward(z, spec.act))
+                outs.append(a)
+                continue
             if kind == "conv":
                 z = L.conv2d_forward(a, W[pi], W[pi + 1], spec.stride, spec.pad)
             else:
@@ -285,7 +296,16 @@ class Stage:
                         g[pi] += dtable
                     da = self.q(da)
                     continue
+                if kind == "rotary":
+                    da = self.q(L.rotary(da, spec, back=True))
+                    continue
                 x_in, z = saved[li]
+                if kind == "gated":
+                    dW, db, da = L.dense_backward(self.q(L.gated_backward(da, z, spec.act)), x_in, W_b[pi])
+                    g[pi] += dW
+                    g[pi + 1] += db
+                    da = self.q(da)
+                    continue
                 dz = self.q(da * L.act_derivative(z, spec.act))
                 if kind == "conv":
                     dW, db, da = L.conv2d_backward(dz, x_in, W_b[pi], spec.stride, spec.pad)

@@ -9,11 +9,13 @@ from .build import lib_path
 TP_OK, TP_EINVAL, TP_ESTATE, TP_ENOVERSION, TP_EFULL, TP_EBUSY, TP_EHIP = 0, -1, -2, -3, -4, -5, -6
 TP_LATEST, TP_INTERMEDIATE_EQ1, TP_INTERMEDIATE_CONVEX, TP_STASHED, TP_TIMEPREST = 0, 1, 2, 3, 4
 TP_F32, TP_BF16 = 0, 1
-TP_ACT_NONE, TP_ACT_RELU, TP_ACT_GELU = 0, 1, 2
+TP_ACT_NONE, TP_ACT_RELU, TP_ACT_GELU, TP_ACT_SILU = 0, 1, 2, 3
 TP_LAYER_DENSE, TP_LAYER_CONV2D, TP_LAYER_MAXPOOL2, TP_LAYER_LAYERNORM, TP_LAYER_ATTENTION, TP_LAYER_RESIDUAL, TP_LAYER_BATCHNORM = 0, 1, 2, 3, 4, 5, 6
 TP_LAYER_SUBSAMPLE2 = 7
 TP_LAYER_AVGPOOL = 8
 TP_LAYER_LOCAL_ATTENTION = 9
+TP_LAYER_GATED = 10
+TP_LAYER_ROTARY = 11
 TP_MAX_LAYERS, TP_MAX_SLOTS, TP_MAX_IN_FLIGHT = 64, 16, 16
 TP_NONE = (1 << 64) - 1
 TP_MAX_TEACHER_ENTRIES = 1024
@@ -21,18 +23,24 @@ TP_DIAG_GRAD_SQ, TP_DIAG_WEIGHT_SQ, TP_DIAG_DRIFT_SQ, TP_DIAG_WB_SQ, TP_DIAG_COU
 
 POLICY = {"latest": TP_LATEST, "eq1": TP_INTERMEDIATE_EQ1, "convex": TP_INTERMEDIATE_CONVEX, "stashed": TP_STASHED,
           "timeprest": TP_TIMEPREST}
-ACT = {"none": TP_ACT_NONE, "relu": TP_ACT_RELU, "gelu": TP_ACT_GELU}
+ACT = {"none": TP_ACT_NONE, "relu": TP_ACT_RELU, "gelu": TP_ACT_GELU, "silu": TP_ACT_SILU}
+ROTARY_LAYOUT = {"pairs": 0, "halves": 1}
 DTYPE = {"f32": TP_F32, "bf16": TP_BF16}
 
 EXPORTS = ["stage_workspace_query", "stage_init", "stage_destroy", "stage_set_forward_streams", "stage_forward_join", "stage_forward", "stage_forward_minibatch", "stage_forward_on", "stage_backward_on", "stage_input_ptr", "stage_saved_input_ptr",
-           "stage_loss_softmax_ce", "stage_loss_distill", "stage_backward", "stage_blend_update", "stage_blend_update_noalloc", "stash_push", "stash_evict",
+           "stage_loss_softmax_ce", "stage_loss_distill", "stage_logprobs", "stage_loss_policy", "stage_loss_preference", "stage_backward", "stage_blend_update", "stage_blend_update_noalloc", "stash_push", "stash_evict",
            "stage_query", "stage_export_params", "tp_blend_coefficients", "tp_schedule_events", "tp_schedule_microbatch_events",
            "stage_profile_begin", "stage_profile_end", "tp_last_error"]
 
 
+class _tp_layer_tail(C.Union):
+    _fields_ = [("reserved", C.c_int32 * 5), ("rope", C.c_float * 5)]
+
+
 class tp_layer_desc(C.Structure):
+    _anonymous_ = ("tail",)
     _fields_ = [("type", C.c_int32), ("act", C.c_int32), ("in_features", C.c_int32), ("out_features", C.c_int32),
-                ("geom", C.c_int32 * 5), ("rel", C.c_int32 * 2), ("reserved", C.c_int32 * 5)]
+                ("geom", C.c_int32 * 5), ("rel", C.c_int32 * 2), ("tail", _tp_layer_tail)]
 
 
 class tp_stage_desc(C.Structure):
@@ -110,6 +118,9 @@ lib.stage_forward_join.argtypes = [_vp]
 lib.stage_saved_input_ptr.argtypes = [_vp, _u64, _u32, _i32, C.POINTER(_vp), C.POINTER(_u64)]
 lib.stage_loss_softmax_ce.argtypes = [_vp, _u64, _vp, _vp, _vp, _vp]
 lib.stage_loss_distill.argtypes = [_vp, _u64, _vp, _vp, _vp, _i32, C.c_double, _vp, C.c_double, _vp, _vp]
+lib.stage_logprobs.argtypes = [_vp, _vp, _vp, _u64, _vp]
+lib.stage_loss_policy.argtypes = [_vp, _u64, _vp, _vp, _vp, _vp, _vp, _vp, C.c_double, C.c_double, C.c_double, _vp, _vp, _vp]
+lib.stage_loss_preference.argtypes = [_vp, _u64, _vp, _vp, _vp, _vp, C.c_double, C.c_double, _vp, _vp, _vp]
 lib.stage_backward.argtypes = [_vp, _u64, _vp, _vp, C.POINTER(_u32)]
 lib.stage_blend_update.argtypes = [_vp, _u64, _u64, C.POINTER(_u64)]
 lib.stage_blend_update_noalloc.argtypes = [_vp, _u64, _u64, C.POINTER(_u64)]
@@ -145,7 +156,9 @@ def make_desc(layers, *, dtype, mb, n, stage_index, num_stages, ring_capacity, m
     global average pooling, ("ln", D, tokens), ("attn", D, heads, tokens),
     ("res", D, tokens, "begin" | "add"[, act-name]), ("swap", D_in, tokens_in, D_out, tokens_out) for the residual
     mark that starts a projection shortcut, ("bn", C, positions, act-name), ("local", D, heads, tokens, kv_heads, window, sinks[,
-    buckets, max_distance]) for windowed attention with D = heads * head width."""
+    buckets, max_distance]) for windowed attention with D = heads * head width, ("gated", in, out, act-name, tokens), ("rotary", heads,
+    kv_heads, head width, tokens, rotated, "pairs" | "halves"[, base, first, factor, original, low, high, amplitude]) for rotary
+    positions on the queries and keys in front of attention."""
     if len(layers) > TP_MAX_LAYERS:
         raise ValueError(f"{len(layers)} layers: a stage takes at most {TP_MAX_LAYERS}")
     d = tp_stage_desc()
@@ -201,6 +214,19 @@ def make_desc(layers, *, dtype, mb, n, stage_index, num_stages, ring_capacity, m
             L.geom[0], L.geom[1], L.geom[2], L.geom[3], L.geom[4] = tokens, heads, kv_heads, window, sinks
             if len(spec) > 7:
                 L.rel[0], L.rel[1] = spec[7], spec[8]
+        elif spec[0] == "gated":
+            _, fin, fout, act, tokens = spec
+            L.type, L.in_features, L.out_features = TP_LAYER_GATED, fin, fout
+            L.geom[0] = tokens
+        elif spec[0] == "rotary":
+            _, heads, kv_heads, dh, tokens, rotated, layout = spec[:7]
+            base, first, factor, original, low, high, amplitude = tuple(spec[7:]) + ROTARY_DEFAULTS[len(spec) - 7:]
+            act = "none"
+            L.type, L.in_features, L.out_features = TP_LAYER_ROTARY, layer_width(spec), layer_width(spec)
+            L.geom[0], L.geom[1], L.geom[2], L.geom[3] = tokens, heads, kv_heads, rotated
+            L.geom[4] = ROTARY_LAYOUT[layout] if isinstance(layout, str) else layout
+            L.rel[0], L.rel[1] = first, original
+            L.rope[0], L.rope[1], L.rope[2], L.rope[3], L.rope[4] = base, factor, low, high, amplitude
         elif spec[0] == "res":
             _, dm, tokens, mark = spec[:4]
             act = spec[4] if len(spec) > 4 else "none"
@@ -216,6 +242,14 @@ def make_desc(layers, *, dtype, mb, n, stage_index, num_stages, ring_capacity, m
             L.geom[0] = spec[3] if len(spec) > 3 and spec[3] > 1 else 0
         L.act = ACT[act] if isinstance(act, str) else act
     return d
+
+
+ROTARY_DEFAULTS = (10000.0, 0, 1.0, 0, 0.0, 0.0, 1.0)
+
+
+def layer_width(spec) -> int:
+    """Values per token of a rotary layer: queries, keys and values of its heads."""
+    return (spec[1] + 2 * spec[2]) * spec[3]
 
 
 def _local_in_features(spec) -> int:
@@ -237,6 +271,10 @@ def layer_in_elems(spec) -> int:
         return _local_in_features(spec) * spec[3]
     if spec[0] == "res":
         return spec[1] * spec[2]
+    if spec[0] == "gated":
+        return spec[1] * spec[4]
+    if spec[0] == "rotary":
+        return layer_width(spec) * spec[4]
     return spec[0] * (spec[3] if len(spec) > 3 else 1)
 
 
@@ -256,6 +294,10 @@ def layer_out_elems(spec) -> int:
         return spec[1] * spec[3]
     if spec[0] == "res":
         return spec[1] * spec[2]
+    if spec[0] == "gated":
+        return spec[2] * spec[4]
+    if spec[0] == "rotary":
+        return layer_width(spec) * spec[4]
     return spec[1] * (spec[3] if len(spec) > 3 else 1)
 
 
@@ -263,8 +305,10 @@ def layer_param_shapes(spec):
     if spec[0] == "conv":
         k = spec[7] if len(spec) > 7 else 3
         return [(spec[2], k, k, spec[1]), (spec[2],)]
-    if spec[0] in ("pool", "attn", "res", "sub", "swap", "avg"):
+    if spec[0] in ("pool", "attn", "res", "sub", "swap", "avg", "rotary"):
         return []
+    if spec[0] == "gated":
+        return [(2 * spec[2], spec[1]), (2 * spec[2],)]   # gate and other factor of each output in turn
     if spec[0] == "local":
         return [(spec[2], spec[7]), (0,)] if len(spec) > 7 and spec[7] else []   # the table, and no second tensor
     if spec[0] in ("ln", "bn"):
@@ -350,6 +394,29 @@ def stage_loss_distill(st, mb_id: int, logits_dev: int, teacher_logits_dev: int,
                        labels_dev: int, label_weight: float, dlogits_dev: int, loss_dev: int):
     rc = lib.stage_loss_distill(st, mb_id, logits_dev, teacher_logits_dev, teacher_ids_dev, k, temperature, labels_dev, label_weight,
                                 dlogits_dev, loss_dev)
+    if rc:
+        _check(rc)
+
+
+def stage_logprobs(st, logits_dev: int, ids_dev: int, rows: int, logp_dev: int):
+    rc = lib.stage_logprobs(st, logits_dev, ids_dev, rows, logp_dev)
+    if rc:
+        _check(rc)
+
+
+def stage_loss_policy(st, mb_id: int, logits_dev: int, actions_dev: int, old_logp_dev: int, advantages_dev: int, weights_dev: int,
+                      ref_logp_dev: int, clip_low: float, clip_high: float, kl_weight: float, dlogits_dev: int, logp_dev: int,
+                      loss_dev: int):
+    rc = lib.stage_loss_policy(st, mb_id, logits_dev, actions_dev, old_logp_dev, advantages_dev, weights_dev, ref_logp_dev, clip_low,
+                               clip_high, kl_weight, dlogits_dev, logp_dev, loss_dev)
+    if rc:
+        _check(rc)
+
+
+def stage_loss_preference(st, mb_id: int, logits_dev: int, targets_dev: int, weights_dev: int, ref_logp_dev: int, beta: float,
+                          label_smoothing: float, dlogits_dev: int, logp_dev: int, loss_dev: int):
+    rc = lib.stage_loss_preference(st, mb_id, logits_dev, targets_dev, weights_dev, ref_logp_dev, beta, label_smoothing, dlogits_dev,
+                                   logp_dev, loss_dev)
     if rc:
         _check(rc)
 

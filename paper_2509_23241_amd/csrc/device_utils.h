@@ -110,6 +110,33 @@ __device__ __forceinline__ void act_pairs_fast(const float (&z)[N], int act, flo
   else each(0);
 }
 
+// The same for the gate of a gated layer, which SiLU may be, too: z s with s = 1 / (1 + exp(-z)), s (1 + z (1 - s)).  EXACT: the library's
+// exponential and a division, for fp32; else the hardware's, each an ulp off.
+template <bool EXACT>
+__device__ __forceinline__ ActPair gate_pair(float z, int act) {
+  if (act == 3) {
+    const float s = EXACT ? 1.f / (1.f + expf(-z)) : __builtin_amdgcn_rcpf(1.f + __builtin_amdgcn_exp2f(z * -1.4426950408889634f));
+    return ActPair{z * s, s * fmaf(z, 1.f - s, 1.f)};
+  }
+  if constexpr (EXACT) return ActPair{act_forward(z, act), act_derivative(z, act)};
+  else return act_pair_fast(z, act);
+}
+template <bool EXACT, int N>
+__device__ __forceinline__ void gate_pairs(const float (&z)[N], int act, float (&a)[N], float (&d)[N]) {
+  auto each = [&](int kind) {
+#pragma unroll
+    for (int j = 0; j < N; ++j) {
+      const ActPair p = gate_pair<EXACT>(z[j], kind);
+      a[j] = p.a;
+      d[j] = p.d;
+    }
+  };
+  if (act == 3) each(3);
+  else if (act == 2) each(2);
+  else if (act == 1) each(1);
+  else each(0);
+}
+
 // Butterflies over the lanes of a wave in vector instructions.  __shfl_xor goes through LDS, some 120 cycles for each of the six
 // dependent steps; a rotation within a row of 16 lanes is an operand of the addition itself, and rows and halves swap in one
 // instruction.  A rotation by O stands for lane ^ O where the lanes that differ in 2 O, 4 O, .. below 16 already agree, so the

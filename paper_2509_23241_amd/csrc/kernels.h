@@ -13,7 +13,7 @@ enum Elt : int { ELT_F32 = 0, ELT_BF16 = 1 };
 // SPREAD_CHAINS: on smaller tiles; SPREAD_PARTS: on smaller tiles, the sum over k in four parts, where it otherwise is one ascending
 // chain for every output, whatever the number of rows.
 enum Spread : int { SPREAD_NONE = 0, SPREAD_CHAINS = 1, SPREAD_PARTS = 2 };
-enum Act : int { ACT_NONE = 0, ACT_RELU = 1, ACT_GELU = 2 };
+enum Act : int { ACT_NONE = 0, ACT_RELU = 1, ACT_GELU = 2, ACT_SILU = 3 };  // SILU: gated layers alone
 
 // z = x W^T + bias ; a = act(z) ; d = act'(z).   x:[M x K] W:[N x K] (elt), bias: fp32[N].
 // d_out (what the backward pass multiplies with) may be null; a_out is always written.
@@ -26,6 +26,13 @@ hipError_t launch_fprop(hipStream_t s, int elt, int M, int N, int K, const void*
                         const float* bias, int act, void* d_out, void* a_out, void* x_copy, const void* addend = nullptr,
                         int spread = SPREAD_NONE);
 bool fprop_add_supported(int elt, int M, int N, int K);
+// A gated layer's forward product, z = x W^T + bias over N = 2 F columns, those of output f being 2f and 2f + 1: a[f] = act(z[2f]) z[2f+1]
+// into a_out [M x F]; what dy[f] is multiplied with to give the gradients of z[2f] and z[2f + 1] into d_out [M x N].
+hipError_t launch_gated_fprop(hipStream_t s, int elt, int M, int N, int K, const void* x, const void* W, const float* bias, int act,
+                              void* d_out, void* a_out, void* x_copy, int spread);
+// dz[2f] = dy[f] d[2f], dz[2f + 1] = dy[f] d[2f + 1], and gb = column sums of dz as stored; N = 2 F columns of dz.
+// partials: scratch of colsum_scratch_floats(M, N) floats.
+hipError_t launch_gated_backward(hipStream_t s, int elt, int M, int N, const void* dy, const void* d, void* dz, float* gb, float* partials);
 
 // out = (dz W_b) (.) d_prev   dz:[M x N] W_b:[N x K] d_prev:[M x K] saved act'(z), or null.
 hipError_t launch_dgrad(hipStream_t s, int elt, int M, int N, int K, const void* dz, const void* Wb,

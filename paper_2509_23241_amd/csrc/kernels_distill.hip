@@ -14,45 +14,13 @@
 #include "device_utils.h"
 #include "distill.h"
 #include "kernels.h"
+#include "row_device.h"
 
 namespace tp {
 
 namespace {
 
-constexpr float kLog2e = 1.4426950408889634f, kLn2 = 0.6931471805599453f;
-
-// The threads of a row: a wave, or a whole workgroup.
-template <int NT>
-struct Team {
-  static constexpr int kRows = NT == 64 ? 4 : 1;         // rows of a workgroup
-  static constexpr int kThreads = NT == 64 ? 256 : NT;
-  static __device__ __forceinline__ int thread() { return NT == 64 ? threadIdx.x & 63 : threadIdx.x; }
-  static __device__ __forceinline__ int which() { return NT == 64 ? threadIdx.x >> 6 : 0; }
-  // what the others have written to LDS and memory is there
-  static __device__ __forceinline__ void sync() {
-    if constexpr (NT == 64) {
-      __builtin_amdgcn_fence(__ATOMIC_RELEASE, "wavefront");
-      __builtin_amdgcn_wave_barrier();
-      __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "wavefront");
-    } else {
-      __syncthreads();
-    }
-  }
-  // sm: NT / 64 floats, free on both sides
-  template <class Op>
-  static __device__ __forceinline__ float over(float v, float* sm, const Op& op) {
-    v = over_lanes<32>(v, op);
-    if constexpr (NT > 64) {
-      if ((threadIdx.x & 63) == 0) sm[threadIdx.x >> 6] = v;
-      __syncthreads();
-      v = sm[0];
-#pragma unroll
-      for (int i = 1; i < NT / 64; ++i) v = op(v, sm[i]);
-      __syncthreads();
-    }
-    return v;
-  }
-};
+constexpr float kLn2 = 0.6931471805599453f;
 
 // Exponents: exp(z / T) = 2^(power), power = z c - top c with c = log2(e) / T and the row's maximum `top`; exp(z) = 2^(T power).  top c is
 // rounded once and its rounding, that of `max / T`, is large where all of a row's logits are: it cancels because every numerator, sum and
@@ -195,29 +163,6 @@ __device__ __forceinline__ void finish_mean(const DistillArgs& a) {
     __syncthreads();
   }
   if (threadIdx.x == 0) *a.loss = (float)(sums[0] / (double)a.rows);
-}
-
-template <typename T>
-constexpr int kVec = 16 / sizeof(T);  // values of a 16-byte unit
-template <typename T>
-__device__ __forceinline__ void unpack(const uint4& u, float (&v)[kVec<T>]) {
-  const uint32_t w[4] = {u.x, u.y, u.z, u.w};
-#pragma unroll
-  for (int i = 0; i < 4; ++i) {
-    if constexpr (sizeof(T) == 2) {
-      v[2 * i] = __uint_as_float(w[i] << 16);
-      v[2 * i + 1] = __uint_as_float(w[i] & 0xffff0000u);
-    } else {
-      v[i] = __uint_as_float(w[i]);
-    }
-  }
-}
-template <typename T>
-__device__ __forceinline__ uint4 pack(const float (&v)[kVec<T>]) {
-  if constexpr (sizeof(T) == 2)
-    return make_uint4(pack_bf16x2(v[0], v[1]), pack_bf16x2(v[2], v[3]), pack_bf16x2(v[4], v[5]), pack_bf16x2(v[6], v[7]));
-  else
-    return make_uint4(__float_as_uint(v[0]), __float_as_uint(v[1]), __float_as_uint(v[2]), __float_as_uint(v[3]));
 }
 
 // A value of which the compiler forgets what has been worked out from it before, and holds none of that.

@@ -142,6 +142,74 @@ __global__ __launch_bounds__(kThreads) void act_backward_colsum_kernel(int M, in
   }
 }
 
+// The backward pass of a gated layer ahead of its products, with the structure of the kernel above over N = 2 F columns: dz of columns 2f
+// and 2f + 1 is dy[f] times what the forward pass kept there.  VEC: rows of whole 16-byte units, dy of 8-byte ones, aligned so.
+template <typename T, bool VEC>
+__global__ __launch_bounds__(kThreads) void gated_backward_kernel(int M, int N, ColsumShape cs, const T* __restrict__ dy,
+                                                                  const T* __restrict__ d, T* __restrict__ dz,
+                                                                  float* __restrict__ partials) {
+  constexpr int V = 16 / sizeof(T);
+  __shared__ float sm[kThreads * V];
+  const int lr = threadIdx.x % cs.lanes_per_row, rsub = threadIdx.x / cs.lanes_per_row;
+  const int col = (blockIdx.x * cs.lanes_per_row + lr) * V;
+  const int r0 = blockIdx.y * cs.chunk_rows;
+  const int r1 = min(M, r0 + cs.chunk_rows);
+  float s[V];
+#pragma unroll
+  for (int j = 0; j < V; ++j) s[j] = 0.f;
+  if (col < N) {
+    if constexpr (VEC) {
+#pragma unroll 4
+      for (int r = r0 + rsub; r < r1; r += cs.rows_per_iter) {
+        const size_t at = (size_t)r * N + col;
+        const uint2 a = *reinterpret_cast<const uint2*>(dy + at / 2);
+        const uint4 b = *reinterpret_cast<const uint4*>(d + at);
+        const uint32_t bw[4] = {b.x, b.y, b.z, b.w};
+        uint32_t ow[4];
+        if constexpr (sizeof(T) == 2) {
+          const float g[4] = {__uint_as_float(a.x << 16), __uint_as_float(a.x & 0xffff0000u), __uint_as_float(a.y << 16),
+                              __uint_as_float(a.y & 0xffff0000u)};
+#pragma unroll
+          for (int j = 0; j < 4; ++j) {
+            ow[j] = pack_bf16x2(g[j] * __uint_as_float(bw[j] << 16), g[j] * __uint_as_float(bw[j] & 0xffff0000u));
+            s[(2 * j) % V] += __uint_as_float(ow[j] << 16);
+            s[(2 * j + 1) % V] += __uint_as_float(ow[j] & 0xffff0000u);
+          }
+        } else {
+          const float g[2] = {__uint_as_float(a.x), __uint_as_float(a.y)};
+#pragma unroll
+          for (int j = 0; j < 4; ++j) {
+            const float o = g[j / 2] * __uint_as_float(bw[j]);
+            ow[j] = __float_as_uint(o);
+            s[j % V] += o;
+          }
+        }
+        *reinterpret_cast<uint4*>(dz + at) = make_uint4(ow[0], ow[1], ow[2], ow[3]);
+      }
+    } else {
+      for (int r = r0 + rsub; r < r1; r += cs.rows_per_iter)
+        for (int j = 0; j < V; ++j)
+          if (col + j < N) {
+            const size_t at = (size_t)r * N + col + j;
+            const T o = from_float<T>(to_float(dy[(size_t)r * (N / 2) + (col + j) / 2]) * to_float(d[at]));
+            dz[at] = o;
+            s[j] += to_float(o);
+          }
+    }
+  }
+#pragma unroll
+  for (int j = 0; j < V; ++j) sm[(rsub * cs.lanes_per_row + lr) * V + j] = s[j];
+  __syncthreads();
+  if (rsub == 0) {
+    for (int j = 0; j < V; ++j) {
+      if (col + j >= N) continue;
+      float t = 0.f;
+      for (int q = 0; q < cs.rows_per_iter; ++q) t += sm[(q * cs.lanes_per_row + lr) * V + j];
+      partials[(size_t)blockIdx.y * N + col + j] = t;
+    }
+  }
+}
+
 // Sum of partial results.  A block covers IL = 256/ZG consecutive outputs with ZG threads each:
 // thread (zg, il) adds partials zg, zg + ZG, ... of output il, the ZG sums are combined through LDS
 // in a fixed order.  Large outputs take few threads per output (whole cache lines per partial
@@ -274,6 +342,32 @@ hipError_t launch_fprop(hipStream_t s, int elt, int M, int N, int K, const void*
     return f32_fprop(s, M, N, K, (const float*)x, (const float*)W, bias, act, (float*)d_out, (float*)a_out, (float*)x_copy);
   return mfma_fprop(s, M, N, K, (const uint16_t*)x, (const uint16_t*)W, bias, act, (uint16_t*)d_out, (uint16_t*)a_out,
                     (uint16_t*)x_copy, (const uint16_t*)addend, spread);
+}
+
+hipError_t launch_gated_fprop(hipStream_t s, int elt, int M, int N, int K, const void* x, const void* W, const float* bias, int act,
+                              void* d_out, void* a_out, void* x_copy, int spread) {
+  if (elt == ELT_F32)
+    return f32_gated_fprop(s, M, N, K, (const float*)x, (const float*)W, bias, act, (float*)d_out, (float*)a_out, (float*)x_copy);
+  return mfma_gated_fprop(s, M, N, K, (const uint16_t*)x, (const uint16_t*)W, bias, act, (uint16_t*)d_out, (uint16_t*)a_out,
+                          (uint16_t*)x_copy, spread);
+}
+
+hipError_t launch_gated_backward(hipStream_t s, int elt, int M, int N, const void* dy, const void* d, void* dz, float* gb, float* partials) {
+  const int V = elt == ELT_BF16 ? 8 : 4;
+  const ColsumShape cs = colsum_shape(M, N, V);
+  const dim3 g1(cs.col_blocks, cs.chunks);
+  const bool vec = N % V == 0 && (((uintptr_t)d | (uintptr_t)dz) & 15) == 0 && ((uintptr_t)dy & 7) == 0;
+#define TP_GATED(T, VEC)                                                                                                    \
+  hipLaunchKernelGGL((gated_backward_kernel<T, VEC>), g1, dim3(kThreads), 0, s, M, N, cs, (const T*)dy, (const T*)d, (T*)dz, partials)
+  if (elt == ELT_BF16) {
+    if (vec) TP_GATED(uint16_t, true); else TP_GATED(uint16_t, false);
+  } else {
+    if (vec) TP_GATED(float, true); else TP_GATED(float, false);
+  }
+#undef TP_GATED
+  const hipError_t err = hipGetLastError();
+  if (err != hipSuccess) return err;
+  return launch_sum_partials(s, (size_t)N, cs.chunks, partials, gb);
 }
 
 hipError_t launch_dgrad(hipStream_t s, int elt, int M, int N, int K, const void* dz, const void* Wb, const void* d_prev,

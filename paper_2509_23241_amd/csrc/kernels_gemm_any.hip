@@ -480,6 +480,43 @@ struct EpiForward {
     finish(m, n, count, v, input(m, n, count));
   }
 };
+// A gated layer: see EpiGated of the bf16 kernels.
+struct EpiGatedF32 {
+  static constexpr int kPartK = 0;
+  static constexpr bool kSums = false;
+  const float* bias;
+  float *d_out, *a_out;
+  int act, ldc, vec;
+  __device__ __forceinline__ floatx4 input(int, int n, int count) const {
+    floatx4 b;
+#pragma unroll
+    for (int j = 0; j < 4; ++j) b[j] = bias[j < count ? n + j : n];
+    return b;
+  }
+  // count: 2 or 4
+  __device__ __forceinline__ void finish(int m, int n, int count, const floatx4& v, const floatx4& b) const {
+    const size_t i = (size_t)m * ldc + n;
+    const float gate[2] = {v[0] + b[0], v[2] + b[2]}, other[2] = {v[1] + b[1], v[3] + b[3]};
+    float a[2], slope[2];
+    gate_pairs<true>(gate, act, a, slope);
+    const float d[4] = {other[0] * slope[0], a[0], other[1] * slope[1], a[1]};
+    if (vec && count == 4) {
+      store4(d_out + i, d);
+      *reinterpret_cast<float2*>(a_out + i / 2) = make_float2(a[0] * other[0], a[1] * other[1]);
+    } else {
+#pragma unroll
+      for (int f = 0; f < 2; ++f)
+        if (2 * f < count) {
+          d_out[i + 2 * f] = d[2 * f];
+          d_out[i + 2 * f + 1] = d[2 * f + 1];
+          a_out[i / 2 + f] = a[f] * other[f];
+        }
+    }
+  }
+  __device__ __forceinline__ void quad(int m, int n, int count, const floatx4& v, int) const {
+    finish(m, n, count, v, input(m, n, count));
+  }
+};
 template <class T>
 struct EpiInputGrad {
   static constexpr int kPartK = 0;
@@ -1066,8 +1103,9 @@ inline bool whole_tiles(int K, int ld) { return K % kTileK<float> == 0 && ld < (
 }  // namespace
 
 // ---- dense, fp32 -------------------------------------------------------------------------------
-hipError_t f32_fprop(hipStream_t s, int M, int N, int K, const float* x, const float* W, const float* bias, int act, float* d_out,
-                     float* a_out, float* x_copy) {
+namespace {
+template <class Epi>
+hipError_t f32_product(hipStream_t s, int M, int N, int K, const float* x, const float* W, float* x_copy, const Epi& e) {
   SideCopy side{nullptr, nullptr, 0};
   if (x_copy) {
     // Behind the tiles the copy is hidden where one stream runs everything: a step of four micro-batches and two layers takes
@@ -1083,12 +1121,22 @@ hipError_t f32_fprop(hipStream_t s, int M, int N, int K, const float* x, const f
     }
   }
   const DenseDesc a{x, K, M, K}, b{W, K, N, K};
-  const EpiForward<float> e{bias, d_out, a_out, act, N, N % 4 == 0 && aligned16(d_out, a_out)};
   if (aligned16(x, W) && wave_ok(M, N, K, K))
     return launch_wave<WaveRow, WaveRow>(s, M, N, K, x, K, W, K, e, side);
   if (whole_tiles(K, K) && aligned16(x, W)) return run<float, Chain, FpropDenseWhole, 4>(s, M, N, K, a, b, e, false, side);
   if (K % 4 == 0 && aligned16(x, W)) return run<float, Chain, FpropDense, 4>(s, M, N, K, a, b, e, false, side);
   return run<float, Chain, FpropDense, 1>(s, M, N, K, a, b, e, false, side);
+}
+}  // namespace
+
+hipError_t f32_fprop(hipStream_t s, int M, int N, int K, const float* x, const float* W, const float* bias, int act, float* d_out,
+                     float* a_out, float* x_copy) {
+  return f32_product(s, M, N, K, x, W, x_copy, EpiForward<float>{bias, d_out, a_out, act, N, N % 4 == 0 && aligned16(d_out, a_out)});
+}
+
+hipError_t f32_gated_fprop(hipStream_t s, int M, int N, int K, const float* x, const float* W, const float* bias, int act, float* d_out,
+                           float* a_out, float* x_copy) {
+  return f32_product(s, M, N, K, x, W, x_copy, EpiGatedF32{bias, d_out, a_out, act, N, N % 4 == 0 && aligned16(d_out, a_out)});
 }
 
 hipError_t f32_dgrad(hipStream_t s, int M, int N, int K, const float* dz, const float* Wb, const float* d_prev, float* out,

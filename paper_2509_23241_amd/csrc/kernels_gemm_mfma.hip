@@ -839,8 +839,13 @@ hipError_t run(bool dma, hipStream_t s, int M, int N, int K, const uint16_t* A, 
 
 inline int store_width(const void* a, const void* b) { return aligned(16, a, b) ? 2 : aligned(8, a, b) ? 1 : 0; }
 
-hipError_t mfma_fprop(hipStream_t s, int M, int N, int K, const uint16_t* x, const uint16_t* W, const float* bias,
-                      int act, uint16_t* d_out, uint16_t* a_out, uint16_t* x_copy, const uint16_t* addend, int spread) {
+// a forward product's input, and its copy where the layer keeps one
+struct FpropInput {
+  const uint16_t* x;
+  SideCopy side;
+  bool dma;  // the operands suit the direct-to-LDS kernel
+};
+inline hipError_t fprop_input(hipStream_t s, int M, int N, int K, const uint16_t* x, const uint16_t* W, uint16_t* x_copy, FpropInput* in) {
   const bool fits = dma_ok(M, N, K, K, K, false, false) && aligned(16, W, x_copy);
   if (x_copy && !(fits && aligned(16, x))) {
     const hipError_t err = launch_copy(s, x, x_copy, (size_t)M * K * 2);
@@ -849,17 +854,34 @@ hipError_t mfma_fprop(hipStream_t s, int M, int N, int K, const uint16_t* x, con
   }
   const bool dma = fits && aligned(16, x);
   // whole 16-byte units with dma
-  const SideCopy side{(const uint4*)x, (uint4*)x_copy, dma && x_copy && x != x_copy ? (size_t)M * K / 8 : 0};
+  *in = FpropInput{x, SideCopy{(const uint4*)x, (uint4*)x_copy, dma && x_copy && x != x_copy ? (size_t)M * K / 8 : 0}, dma};
+  return hipSuccess;
+}
+template <class Epi>
+hipError_t fprop_product(hipStream_t s, int M, int N, int K, const FpropInput& in, const uint16_t* W, const Epi& e, int spread) {
+  if (in.dma && spread == SPREAD_PARTS && few_tiles(M, N)) return launch_skinny<false>(s, M, N, K, in.x, K, W, K, e, in.side);
+  if (in.dma && spread == SPREAD_CHAINS && few_tiles(M, N)) return launch_skinny<true>(s, M, N, K, in.x, K, W, K, e, in.side);
+  return run<false, false>(in.dma, s, M, N, K, in.x, K, W, K, e, in.side);
+}
+
+hipError_t mfma_fprop(hipStream_t s, int M, int N, int K, const uint16_t* x, const uint16_t* W, const float* bias,
+                      int act, uint16_t* d_out, uint16_t* a_out, uint16_t* x_copy, const uint16_t* addend, int spread) {
+  FpropInput in;
+  const hipError_t err = fprop_input(s, M, N, K, x, W, x_copy, &in);
+  if (err != hipSuccess) return err;
   const int wide = store_width(d_out, a_out);
   // contractions that are no multiple of 8 ran on fp32 FMAs with GELU from erff, and keep it
-  if (K % 8) return run_any<false, false>(s, M, N, K, x, K, W, K, EpiFpropExact{bias, d_out, a_out, act, N, nullptr, wide});
-  auto product = [&](const auto& e) {
-    if (dma && spread == SPREAD_PARTS && few_tiles(M, N)) return launch_skinny<false>(s, M, N, K, x, K, W, K, e, side);
-    if (dma && spread == SPREAD_CHAINS && few_tiles(M, N)) return launch_skinny<true>(s, M, N, K, x, K, W, K, e, side);
-    return run<false, false>(dma, s, M, N, K, x, K, W, K, e, side);
-  };
-  if (addend) return product(EpiFpropAdd{bias, d_out, a_out, act, N, addend, wide});
-  return product(EpiFprop{bias, d_out, a_out, act, N, nullptr, wide});
+  if (K % 8) return run_any<false, false>(s, M, N, K, in.x, K, W, K, EpiFpropExact{bias, d_out, a_out, act, N, nullptr, wide});
+  if (addend) return fprop_product(s, M, N, K, in, W, EpiFpropAdd{bias, d_out, a_out, act, N, addend, wide}, spread);
+  return fprop_product(s, M, N, K, in, W, EpiFprop{bias, d_out, a_out, act, N, nullptr, wide}, spread);
+}
+
+hipError_t mfma_gated_fprop(hipStream_t s, int M, int N, int K, const uint16_t* x, const uint16_t* W, const float* bias, int act,
+                            uint16_t* d_out, uint16_t* a_out, uint16_t* x_copy, int spread) {
+  FpropInput in;
+  const hipError_t err = fprop_input(s, M, N, K, x, W, x_copy, &in);
+  if (err != hipSuccess) return err;
+  return fprop_product(s, M, N, K, in, W, EpiGated{bias, d_out, a_out, act, N, store_width(d_out, a_out)}, spread);
 }
 
 int mfma_dgrad_sum_rows(int M, int K) {

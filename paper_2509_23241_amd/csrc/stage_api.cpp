@@ -18,6 +18,8 @@
 #include "conv.h"
 #include "distill.h"
 #include "local_attention.h"
+#include "logprob.h"
+#include "rotary.h"
 #include "transformer.h"
 #include "batchnorm.h"
 #include "kernels.h"
@@ -58,6 +60,9 @@ struct LayerPlan {
   int tokens = 1;                  // positions per sample (rows of the layer's matrices per sample)
   int skip_layer = -1;             // residual add: index of the layer that remembered the skip activation
   DeferredNeed need;
+  uint64_t pair_off = UINT64_MAX;  // gated: what the backward pass multiplies with, [rows x 2 outputs]
+  bool in_place = false;           // rotary: input and output are one tensor
+  tp::RotarySpeeds speeds;         // rotary
   bool relu_out = false;           // ReLU whose derivative is read off its saved OUTPUT (the next layer's input): no act' tensor
 };
 
@@ -104,6 +109,23 @@ tp::LocalAttention local_attention(const tp_layer_desc& L, int seqs, int per_tab
   return a;
 }
 
+tp::Rotary rotary(const tp_layer_desc& L, int seqs) {
+  tp::Rotary r;
+  r.seqs = seqs;
+  r.S = L.geom[0];
+  r.turned = L.geom[1] + L.geom[2];
+  r.all = r.turned + L.geom[2];
+  r.dh = L.in_features / r.all;
+  r.rotated = L.geom[3];
+  r.halves = L.geom[4] == 1;
+  r.first = L.rel[0];
+  r.amplitude = L.rope[4];
+  return r;
+}
+
+// Columns of the product a dense or gated layer's weights take part in.
+inline int product_columns(const tp_layer_desc& L) { return L.type == TP_LAYER_GATED ? 2 * L.out_features : L.out_features; }
+
 // output pixels per image of a convolution layer (geom: H, W, kernel, stride, pad)
 inline uint64_t conv_out_px(const tp_layer_desc& L) { return (uint64_t)(L.geom[0] / L.geom[3]) * (L.geom[1] / L.geom[3]); }
 
@@ -128,7 +150,8 @@ int check_desc(const tp_stage_desc* d) {
   int open_swap = -1;  // layer of the swap between that begin and its add, if there is one
   for (int l = 0; l < d->num_layers; ++l) {
     const tp_layer_desc& L = d->layers[l];
-    if (L.act < TP_ACT_NONE || L.act > TP_ACT_GELU) return fail(TP_EINVAL, "layer %d: unknown activation", l);
+    if (L.act < TP_ACT_NONE || L.act > (L.type == TP_LAYER_GATED ? TP_ACT_SILU : TP_ACT_GELU))
+      return fail(TP_EINVAL, "layer %d: unknown activation, or one that its type does not take", l);
     if (L.in_features < 1 || L.out_features < 1) return fail(TP_EINVAL, "layer %d: empty shape", l);
     uint64_t in_e, out_e;
     if (L.type == TP_LAYER_DENSE) {
@@ -138,6 +161,32 @@ int check_desc(const tp_stage_desc* d) {
       const uint64_t T = L.geom[0] > 1 ? L.geom[0] : 1;
       in_e = T * L.in_features;
       out_e = T * L.out_features;
+    } else if (L.type == TP_LAYER_GATED) {
+      for (int r = 1; r < 5; ++r)
+        if (L.geom[r] != 0) return fail(TP_EINVAL, "layer %d: geometry fields 1..4 must be zero for a gated layer", l);
+      if (L.geom[0] < 1 || L.out_features > (1 << 29)) return fail(TP_EINVAL, "layer %d: malformed gated layer", l);
+      in_e = (uint64_t)L.geom[0] * L.in_features;
+      out_e = (uint64_t)L.geom[0] * L.out_features;
+      if (2 * out_e > (1u << 30)) return fail(TP_EINVAL, "layer %d: sample too large", l);
+      if ((int64_t)d->mb * d->n * L.geom[0] > INT32_MAX) return fail(TP_EINVAL, "layer %d: mini-batch too large", l);
+    } else if (L.type == TP_LAYER_ROTARY) {
+      const int64_t all = (int64_t)L.geom[1] + 2 * (int64_t)L.geom[2];
+      if (L.geom[0] < 1 || L.geom[1] < 1 || L.geom[2] < 1 || all > L.in_features || L.in_features % all != 0 ||
+          L.in_features != L.out_features || L.act != TP_ACT_NONE)
+        return fail(TP_EINVAL, "layer %d: malformed rotary layer", l);
+      const int dh = (int)(L.in_features / all);
+      if (dh > 2 * tp::kMaxRotaryPairs || L.geom[3] < 2 || L.geom[3] > dh || (L.geom[3] & 1) || L.geom[4] < 0 || L.geom[4] > 1)
+        return fail(TP_EINVAL, "layer %d: rotary positions turn an even number of 2 .. %d values of heads of at most %d, in layout 0 or 1", l,
+                    dh, 2 * tp::kMaxRotaryPairs);
+      if (L.rel[0] < 0 || (int64_t)L.rel[0] + L.geom[0] > INT32_MAX || L.rel[1] < 0)
+        return fail(TP_EINVAL, "layer %d: rotary positions lie in 0 .. 2^31 - 2", l);
+      const float base = L.rope[0], factor = L.rope[1], low = L.rope[2], high = L.rope[3], amplitude = L.rope[4];
+      if (!(base > 0.f && std::isfinite(base) && factor > 0.f && std::isfinite(factor) && amplitude > 0.f && std::isfinite(amplitude)))
+        return fail(TP_EINVAL, "layer %d: base, factor and amplitude of rotary positions must be positive", l);
+      if (L.rel[1] == 0 ? low != 0.f || high != 0.f : !(low >= 0.f && high > low && std::isfinite(high)))
+        return fail(TP_EINVAL, "layer %d: scaling by parts needs an original length and 0 <= low < high, plain scaling none of them", l);
+      in_e = out_e = (uint64_t)L.geom[0] * L.in_features;
+      if ((int64_t)d->mb * d->n * L.geom[0] > INT32_MAX) return fail(TP_EINVAL, "layer %d: mini-batch too large", l);
     } else if (L.type == TP_LAYER_BATCHNORM) {
       if (L.geom[0] < 1 || L.in_features != L.out_features || L.geom[1] || L.geom[2] || L.geom[3] || L.geom[4])
         return fail(TP_EINVAL, "layer %d: malformed batch normalisation layer", l);
@@ -241,8 +290,8 @@ int check_desc(const tp_stage_desc* d) {
                   (unsigned long long)in_e, (unsigned long long)prev_out);
     prev_out = out_e;
     for (int r = 0; r < 5; ++r)
-      if (L.reserved[r] != 0) return fail(TP_EINVAL, "layer %d: reserved fields must be zero", l);
-    if (L.type != TP_LAYER_LOCAL_ATTENTION && (L.rel[0] != 0 || L.rel[1] != 0))
+      if (L.type != TP_LAYER_ROTARY && L.reserved[r] != 0) return fail(TP_EINVAL, "layer %d: reserved fields must be zero", l);
+    if (L.type != TP_LAYER_LOCAL_ATTENTION && L.type != TP_LAYER_ROTARY && (L.rel[0] != 0 || L.rel[1] != 0))
       return fail(TP_EINVAL, "layer %d: only windowed attention has a position bias", l);
   }
   if (open_skip >= 0) return fail(TP_EINVAL, "layer %d: residual begin without an add", open_skip);
@@ -264,7 +313,8 @@ uint64_t sum_rows_left(const tp_stage_desc& d, int l) {
   const tp_layer_desc& B = d.layers[l + 1];
   const int samples = d.mb * d.n;
   switch (B.type) {
-    case TP_LAYER_DENSE: return tp::dgrad_sum_rows(d.dtype, samples * std::max(1, B.geom[0]), B.in_features);
+    case TP_LAYER_DENSE:
+    case TP_LAYER_GATED: return tp::dgrad_sum_rows(d.dtype, samples * std::max(1, B.geom[0]), B.in_features);
     case TP_LAYER_CONV2D:
       return tp::conv_dgrad_sum_rows(d.dtype, samples, B.geom[0], B.geom[1], B.geom[2], B.geom[3], B.in_features, B.out_features);
     case TP_LAYER_MAXPOOL2: return tp::maxpool_sum_rows(d.dtype, samples, B.geom[0], B.geom[1], B.in_features);
@@ -287,6 +337,10 @@ DeferredNeed deferred_need(const tp_stage_desc& d, int l, const LayerPlan& lp) {
   uint64_t extra = 0;
   if (L.type == TP_LAYER_LOCAL_ATTENTION) {
     need.weight = round_up(tp::local_attention_table_floats(d.dtype, local_attention(L, d.mb * d.n, d.mb)), 64);
+  } else if (L.type == TP_LAYER_GATED) {
+    const int r = (int)(rows * lp.tokens), columns = product_columns(L);
+    need.bias = round_up(tp::colsum_scratch_floats(r, columns), 64);
+    need.weight = round_up(tp::wgrad_scratch_floats(d.dtype, r, columns, L.in_features), 64);
   } else if (L.type == TP_LAYER_LAYERNORM) {
     need.norm = round_up(tp::layernorm_scratch_floats(rows * lp.tokens, L.in_features), 64);
   } else if (L.type == TP_LAYER_BATCHNORM) {
@@ -334,6 +388,19 @@ int make_plan(const tp_stage_desc* d, Plan* p) {
       lp.out_elems = (uint64_t)lp.tokens * L.out_features;
       lp.w_elems = (uint64_t)L.in_features * L.out_features;
       p->any_order = p->any_order && lp.tokens == 1;
+    } else if (L.type == TP_LAYER_GATED) {
+      lp.tokens = L.geom[0];
+      lp.in_elems = (uint64_t)lp.tokens * L.in_features;
+      lp.out_elems = (uint64_t)lp.tokens * L.out_features;
+      lp.w_elems = 2 * (uint64_t)L.out_features * L.in_features;
+    } else if (L.type == TP_LAYER_ROTARY) {
+      lp.tokens = L.geom[0];
+      lp.in_elems = lp.out_elems = (uint64_t)lp.tokens * L.in_features;
+      lp.w_elems = 0;
+      tp::rotary_speeds(L.geom[3], L.rope[0], L.rope[1], L.rel[1], L.rope[2], L.rope[3], &lp.speeds);
+      // nobody reads the turned tensor's former self: a dense layer's backward pass needs its input alone
+      lp.in_place = l > 0 && l + 1 < d->num_layers && d->layers[l - 1].type == TP_LAYER_DENSE && d->layers[l - 1].act == TP_ACT_NONE &&
+                    (d->layers[l + 1].type == TP_LAYER_ATTENTION || d->layers[l + 1].type == TP_LAYER_LOCAL_ATTENTION);
     } else if (L.type == TP_LAYER_LAYERNORM) {
       lp.tokens = L.geom[0];
       lp.in_elems = lp.out_elems = (uint64_t)lp.tokens * L.in_features;
@@ -402,7 +469,7 @@ int make_plan(const tp_stage_desc* d, Plan* p) {
     if (lp.w_elems) {
       off += round_up(lp.w_elems, 64);
       lp.b_off = off;
-      if (L.type != TP_LAYER_LOCAL_ATTENTION) off += round_up((uint64_t)L.out_features, 64);
+      if (L.type != TP_LAYER_LOCAL_ATTENTION) off += round_up((uint64_t)product_columns(L), 64);
     }
     if (alias_of >= 0) {
       lp.x_off = p->layers[alias_of].x_off;
@@ -410,7 +477,7 @@ int make_plan(const tp_stage_desc* d, Plan* p) {
       lp.x_off = act;
       act += round_up(rows * lp.in_elems * p->elt_size, 256);
     }
-    alias_of = L.type != TP_LAYER_RESIDUAL ? -1 : L.geom[1] == 0 ? l : L.geom[1] == 2 ? lp.skip_layer : -1;
+    alias_of = lp.in_place ? l : L.type != TP_LAYER_RESIDUAL ? -1 : L.geom[1] == 0 ? l : L.geom[1] == 2 ? lp.skip_layer : -1;
     if (lp.stat_elems || lp.stat_bytes) {
       lp.stat_off = act;
       act += round_up(lp.stat_bytes ? lp.stat_bytes : rows * lp.stat_elems * 4, 256);
@@ -430,7 +497,13 @@ int make_plan(const tp_stage_desc* d, Plan* p) {
     // front of a residual add (the add may be formed in this layer's kernel, the bare output then never exists).
     const bool next_is_add = l + 1 < d->num_layers && d->layers[l + 1].type == TP_LAYER_RESIDUAL && d->layers[l + 1].geom[1] == 1;
     lp.relu_out = L.act == TP_ACT_RELU && l + 1 < d->num_layers && !next_is_add;
-    if (L.act != TP_ACT_NONE && !lp.relu_out) {
+    if (L.type == TP_LAYER_GATED) {
+      lp.relu_out = false;
+      lp.pair_off = act;
+      act += round_up(rows * 2 * lp.out_elems * p->elt_size, 256);
+      max_feat = std::max<uint64_t>(max_feat, 2 * lp.out_elems);
+      lp.z_off = UINT64_MAX;
+    } else if (L.act != TP_ACT_NONE && !lp.relu_out) {
       lp.z_off = act;
       act += round_up(rows * lp.out_elems * p->elt_size, 256);
     } else {
@@ -461,11 +534,19 @@ int make_plan(const tp_stage_desc* d, Plan* p) {
     // bias gradients: column sums over rows (dense) or over all pixels (conv)
     if (lp.d.type == TP_LAYER_LAYERNORM || lp.d.type == TP_LAYER_BATCHNORM || lp.d.type == TP_LAYER_LOCAL_ATTENTION) continue;
     const uint64_t r = lp.d.type == TP_LAYER_CONV2D ? rows * conv_out_px(lp.d) : rows * lp.tokens;
+    if (lp.d.type == TP_LAYER_GATED) {
+      wg = std::max<uint64_t>({wg, tp::colsum_scratch_floats((int)r, product_columns(lp.d)),
+                               tp::wgrad_scratch_floats(d->dtype, (int)r, product_columns(lp.d), lp.d.in_features)});
+      continue;
+    }
     wg = std::max<uint64_t>(wg, bias_partials(*d, l, r));
     if (lp.d.type == TP_LAYER_DENSE)
       wg = std::max<uint64_t>(wg, tp::wgrad_scratch_floats(d->dtype, (int)r, lp.d.out_features, lp.d.in_features));
   }
-  p->partial_floats = round_up(std::max<uint64_t>({wg, tp::update_scratch_floats(), rows * p->layers.back().tokens, conv_scratch, norm_scratch}), 64);
+  // the losses: a float per row, or (pairs of sequences) what a row's second pass needs and three floats per sample
+  const uint64_t loss_rows = rows * p->layers.back().tokens;
+  const uint64_t loss_floats = p->layers.back().d.type == TP_LAYER_DENSE && rows % 2 == 0 ? loss_rows * (sizeof(tp::RowStats) / 4) + 2 * rows : loss_rows;
+  p->partial_floats = round_up(std::max<uint64_t>({wg, tp::update_scratch_floats(), loss_floats, conv_scratch, norm_scratch}), 64);
   // Every sum of partials the backward pass needs (bias and split weight gradients, scale and shift gradients of the
   // normalisations) is put off to one launch at its end: each keeps partials of its own until then.  Where the line lies is
   // decided by what the sums need at least, so that column sums left by another layer's kernel, which take more rows than a
@@ -921,7 +1002,9 @@ int old_version_copy(tp_stage* st, uint64_t v, int slot, const char** out) {
 // Stages whose forward pass treats every sample apart with one kernel per layer: several micro-batches can pass in one call.
 bool row_by_row(const tp_stage* st) {
   for (const LayerPlan& lp : st->plan.layers)
-    if (lp.d.type != TP_LAYER_DENSE && lp.d.type != TP_LAYER_LAYERNORM && lp.d.type != TP_LAYER_RESIDUAL) return false;
+    if (lp.d.type != TP_LAYER_DENSE && lp.d.type != TP_LAYER_LAYERNORM && lp.d.type != TP_LAYER_RESIDUAL &&
+        lp.d.type != TP_LAYER_GATED && lp.d.type != TP_LAYER_ROTARY)
+      return false;
   return st->fwd_streams == 0;
 }
 
@@ -1048,6 +1131,18 @@ int forward_impl(tp_stage* st, uint64_t mb_id, uint32_t ub_idx, uint32_t ubs, co
       HIP_TRY(tp::launch_fprop(fs, d.dtype, mb * lp.tokens, lp.d.out_features, lp.d.in_features, x_in,
                                wcopy + lp.w_off * es, master + lp.b_off, lp.d.act, z_out, a_out,
                                need_copy ? x_saved : nullptr, nullptr, spread));
+      continue;
+    }
+    if (lp.d.type == TP_LAYER_GATED) {
+      ProfScope ps(st, TP_K_FPROP);
+      HIP_TRY(tp::launch_gated_fprop(fs, d.dtype, mb * lp.tokens, product_columns(lp.d), lp.d.in_features, x_in, wcopy + lp.w_off * es,
+                                     master + lp.b_off, lp.d.act, aslot + lp.pair_off + row0 * 2 * lp.out_elems * es, a_out,
+                                     need_copy ? x_saved : nullptr, spread));
+      continue;
+    }
+    if (lp.d.type == TP_LAYER_ROTARY) {  // its backward pass needs no input: none is kept
+      ProfScope ps(st, TP_K_ATTN);
+      HIP_TRY(tp::launch_rotary(fs, d.dtype, rotary(lp.d, mb), lp.speeds, false, x_in, a_out));
       continue;
     }
     if (lp.xpad_off != UINT64_MAX) {
@@ -1244,6 +1339,108 @@ int stage_loss_distill(tp_stage* st, uint64_t mb_id, const void* logits_dev, con
   return TP_OK;
 }
 
+namespace {
+// What the losses on log probabilities have in common: the mini-batch is whole, the last layer dense, its rows countable, the gradient apart.
+int loss_rows(tp_stage* st, uint64_t mb_id, const void* logits_dev, const void* dlogits_dev, int* rows) {
+  InFlight* f = st->find_mb(mb_id);
+  if (!f || f->forwards != (uint32_t)st->desc.n)
+    return fail(TP_ESTATE, "loss of mini-batch %llu needs all %d forwards", (unsigned long long)mb_id, st->desc.n);
+  const LayerPlan& last = st->plan.layers.back();
+  if (last.d.type != TP_LAYER_DENSE) return fail(TP_EINVAL, "the loss needs a dense last layer");
+  const int64_t all = (int64_t)st->desc.mb * st->desc.n * last.tokens;  // one for every token position
+  if (all > INT32_MAX) return fail(TP_EINVAL, "the loss takes at most 2^31 - 1 rows");
+  *rows = (int)all;
+  const size_t bytes = (size_t)all * last.d.out_features * st->plan.elt_size;
+  if (!st->dry && (const char*)logits_dev < (const char*)dlogits_dev + bytes && (const char*)dlogits_dev < (const char*)logits_dev + bytes)
+    return fail(TP_EINVAL, "the gradient must not overlap the logits");
+  return TP_OK;
+}
+}  // namespace
+
+int stage_logprobs(tp_stage* st, const void* logits_dev, const int32_t* ids_dev, uint64_t rows, float* logp_dev) {
+  if (!st) return fail(TP_EINVAL, "null stage");
+  if (st->plan.layers.back().d.type != TP_LAYER_DENSE) return fail(TP_EINVAL, "log probabilities need a dense last layer");
+  if (rows > INT32_MAX) return fail(TP_EINVAL, "log probabilities of at most 2^31 - 1 rows");
+  if (st->dry || rows == 0) return TP_OK;
+  if (!logits_dev || !ids_dev || !logp_dev) return fail(TP_EINVAL, "null pointer");
+  if (int rc = join_forwards(st)) return rc;
+  ProfScope ps(st, TP_K_LOSS);
+  HIP_TRY(tp::launch_logprobs(st->stream, st->desc.dtype,
+                              tp::LogprobArgs{(int)rows, st->plan.layers.back().d.out_features, logits_dev, ids_dev, logp_dev, nullptr, nullptr}));
+  return TP_OK;
+}
+
+int stage_loss_policy(tp_stage* st, uint64_t mb_id, const void* logits_dev, const int32_t* actions_dev, const float* old_logp_dev,
+                      const float* advantages_dev, const float* weights_dev, const float* ref_logp_dev, double clip_low,
+                      double clip_high, double kl_weight, void* dlogits_dev, float* logp_dev, float* loss_dev) {
+  if (!st) return fail(TP_EINVAL, "null stage");
+  if (!(clip_low >= 0.0 && clip_low <= 1.0) || !(clip_high >= 0.0 && clip_high <= 1e6))
+    return fail(TP_EINVAL, "ratios are clipped to 1 - (0 .. 1) and 1 + (0 .. 1e6)");
+  if (!(kl_weight >= 0.0 && kl_weight <= 1e6)) return fail(TP_EINVAL, "the weight of the KL term must be 0 .. 1e6");
+  int rows = 0;
+  if (int rc = loss_rows(st, mb_id, logits_dev, dlogits_dev, &rows)) return rc;
+  if (st->dry) return TP_OK;
+  if (!logits_dev || !actions_dev || !old_logp_dev || !advantages_dev || !dlogits_dev || !loss_dev || (kl_weight > 0.0 && !ref_logp_dev))
+    return fail(TP_EINVAL, "null pointer");
+  if (int rc = join_forwards(st)) return rc;
+  tp::PolicyArgs a;
+  a.rows = rows;
+  a.classes = st->plan.layers.back().d.out_features;
+  a.logits = logits_dev;
+  a.actions = actions_dev;
+  a.old_logp = old_logp_dev;
+  a.advantages = advantages_dev;
+  a.weights = weights_dev;
+  a.ref_logp = ref_logp_dev;
+  a.log_low = std::log1p(-clip_low);
+  a.log_high = std::log1p(clip_high);
+  a.clip_low = (float)clip_low;
+  a.clip_high = (float)clip_high;
+  a.kl_weight = (float)kl_weight;
+  a.dlogits = dlogits_dev;
+  a.logp = logp_dev;
+  a.row_loss = st->partials();
+  a.counter = st->counter(tp_stage::kCountLoss);
+  a.loss = loss_dev;
+  ProfScope ps(st, TP_K_LOSS);
+  HIP_TRY(tp::launch_policy(st->stream, st->desc.dtype, a));
+  return TP_OK;
+}
+
+int stage_loss_preference(tp_stage* st, uint64_t mb_id, const void* logits_dev, const int32_t* targets_dev, const float* weights_dev,
+                          const float* ref_logp_dev, double beta, double label_smoothing, void* dlogits_dev, float* logp_dev,
+                          float* loss_dev) {
+  if (!st) return fail(TP_EINVAL, "null stage");
+  if (!(beta >= 0.0 && beta <= 1e6)) return fail(TP_EINVAL, "beta must be 0 .. 1e6");
+  if (!(label_smoothing >= 0.0 && label_smoothing <= 1.0)) return fail(TP_EINVAL, "label smoothing must be 0 .. 1");
+  int rows = 0;
+  if (int rc = loss_rows(st, mb_id, logits_dev, dlogits_dev, &rows)) return rc;
+  const int samples = st->desc.mb * st->desc.n;
+  if (samples % 2) return fail(TP_EINVAL, "pairs of sequences need an even number of samples, not %d", samples);
+  if (st->dry) return TP_OK;
+  if (!logits_dev || !targets_dev || !ref_logp_dev || !dlogits_dev || !logp_dev || !loss_dev) return fail(TP_EINVAL, "null pointer");
+  if (int rc = join_forwards(st)) return rc;
+  tp::PreferenceArgs a;
+  a.pairs = samples / 2;
+  a.tokens = st->plan.layers.back().tokens;
+  a.classes = st->plan.layers.back().d.out_features;
+  a.logits = logits_dev;
+  a.targets = targets_dev;
+  a.weights = weights_dev;
+  a.ref_logp = ref_logp_dev;
+  a.beta = beta;
+  a.smoothing = label_smoothing;
+  a.dlogits = dlogits_dev;
+  a.logp = logp_dev;
+  a.stats = (tp::RowStats*)st->partials();
+  a.pull = (float*)(a.stats + rows);
+  a.pair_loss = a.pull + samples;
+  a.loss = loss_dev;
+  ProfScope ps(st, TP_K_LOSS);
+  HIP_TRY(tp::launch_preference(st->stream, st->desc.dtype, a));
+  return TP_OK;
+}
+
 }  // extern "C"
 
 namespace {
@@ -1344,7 +1541,7 @@ int backward_impl(tp_stage* st, uint64_t mb_id, const void* dy_dev, void* dx_dev
     float* bias_room = nullptr;  // where its partial column sums go, if that has been laid out already
     {
       const LayerPlan& last = st->plan.layers[L - 1];
-      if (last.d.act == TP_ACT_NONE) {
+      if (last.z_off == UINT64_MAX) {  // no activation, or a gated layer's, which its own step below passes
         dz = dy_dev;
       } else {
         ProfScope ps(st, TP_K_ACT_BWD);
@@ -1374,7 +1571,7 @@ int backward_impl(tp_stage* st, uint64_t mb_id, const void* dy_dev, void* dx_dev
       const bool to_caller = l == 0;
       const bool no_dx = to_caller && !d.needs_dx;
       if (no_dx && (lp.d.type == TP_LAYER_MAXPOOL2 || lp.d.type == TP_LAYER_SUBSAMPLE2 || lp.d.type == TP_LAYER_ATTENTION ||
-                    lp.d.type == TP_LAYER_AVGPOOL || (lp.d.type == TP_LAYER_LOCAL_ATTENTION && !lp.w_elems)))
+                    lp.d.type == TP_LAYER_AVGPOOL || lp.d.type == TP_LAYER_ROTARY || (lp.d.type == TP_LAYER_LOCAL_ATTENTION && !lp.w_elems)))
         break;
       // what the gradient w.r.t. this layer's input is multiplied with: the saved act'(z) of the previous layer, or
       // (dmask = 1) that layer's saved ReLU output, which is this layer's own saved input
@@ -1577,6 +1774,19 @@ int backward_impl(tp_stage* st, uint64_t mb_id, const void* dy_dev, void* dx_dev
         dz = dst;
         continue;
       }
+      if (lp.d.type == TP_LAYER_ROTARY) {
+        // in place where the gradient in hand is one of the temporaries and nobody else's
+        bool own = false;
+        for (int i = 0; i < 3; ++i) own = own || dz == st->dz_buf(i);
+        if (own && !to_caller && dz != pinned) dst = const_cast<void*>(dz);
+        {
+          ProfScope ps(st, TP_K_ATTN);
+          HIP_TRY(tp::launch_rotary(st->stream, d.dtype, rotary(lp.d, rows), lp.speeds, true, dz, dst));
+        }
+        if (int rc = through_activation(dst)) return rc;
+        dz = dst;
+        continue;
+      }
       if (lp.d.type == TP_LAYER_LOCAL_ATTENTION) {
         {
           ProfScope ps(st, TP_K_ATTN);
@@ -1593,6 +1803,19 @@ int backward_impl(tp_stage* st, uint64_t mb_id, const void* dy_dev, void* dx_dev
         continue;
       }
       const int grad_rows = lp.d.type == TP_LAYER_CONV2D ? rows * (int)conv_out_px(lp.d) : rows * lp.tokens;
+      if (lp.d.type == TP_LAYER_GATED) {
+        // from the gradient of the outputs to that of both products, and its column sums; dx may then take the former's place
+        void* dz2 = scratch_for(dz);
+        {
+          ProfScope ps(st, TP_K_ACT_BWD);
+          SumsDeferred later(sink);
+          HIP_TRY(tp::launch_gated_backward(st->stream, d.dtype, grad_rows, product_columns(lp.d), dz, aslot + lp.pair_off, dz2,
+                                            g + lp.b_off, hold(need.bias)));
+        }
+        bias_summed = true;
+        dz = dz2;
+        if (!to_caller || no_dx) dst = scratch_for(dz);
+      }
       if (!bias_summed) {
         ProfScope ps(st, TP_K_COLSUM);
         SumsDeferred later(sink);
@@ -1605,8 +1828,8 @@ int backward_impl(tp_stage* st, uint64_t mb_id, const void* dy_dev, void* dx_dev
         ProfScope ps(st, TP_K_WGRAD);
         SumsDeferred later(sink);
         float* part = hold(need.weight);
-        if (lp.d.type == TP_LAYER_DENSE)
-          HIP_TRY(tp::launch_wgrad(st->stream, d.dtype, grad_rows, lp.d.out_features, lp.d.in_features, dz, aslot + lp.x_off,
+        if (lp.d.type == TP_LAYER_DENSE || lp.d.type == TP_LAYER_GATED)
+          HIP_TRY(tp::launch_wgrad(st->stream, d.dtype, grad_rows, product_columns(lp.d), lp.d.in_features, dz, aslot + lp.x_off,
                                    g + lp.w_off, part));
         else if (lp.xpad_off != UINT64_MAX && lp.d.geom[2] == 7)
           HIP_TRY(tp::conv_stem_wgrad(st->stream, rows, lp.d.geom[0], lp.d.geom[1], lp.d.in_features, lp.d.out_features,
@@ -1624,8 +1847,8 @@ int backward_impl(tp_stage* st, uint64_t mb_id, const void* dy_dev, void* dx_dev
       if (no_dx) break;
       {
         ProfScope ps(st, TP_K_DGRAD);
-        if (lp.d.type == TP_LAYER_DENSE)
-          HIP_TRY(tp::launch_dgrad(st->stream, d.dtype, grad_rows, lp.d.out_features, lp.d.in_features, dz, wb + lp.w_off * es,
+        if (lp.d.type == TP_LAYER_DENSE || lp.d.type == TP_LAYER_GATED)
+          HIP_TRY(tp::launch_dgrad(st->stream, d.dtype, grad_rows, product_columns(lp.d), lp.d.in_features, dz, wb + lp.w_off * es,
                                    dprev, dst, dmask, bias_sums(), &bias_rows));
         else
           HIP_TRY(tp::launch_conv_dgrad(st->stream, d.dtype, rows, lp.d.geom[0], lp.d.geom[1], lp.d.geom[2], lp.d.geom[3],

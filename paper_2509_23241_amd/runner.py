@@ -35,6 +35,11 @@ def layer_tuple(spec) -> tuple:
         return ("attn", spec.d, spec.heads, spec.tokens)
     if kind == "local":
         return ("local", spec.d, spec.heads, spec.tokens, spec.kv_heads, spec.window, spec.sinks, spec.buckets, spec.max_distance)
+    if kind == "gated":
+        return ("gated", spec.in_features, spec.out_features, spec.act, spec.tokens)
+    if kind == "rotary":
+        return ("rotary", spec.heads, spec.kv_heads, spec.head, spec.tokens, spec.rotated, spec.layout, spec.base, spec.first, spec.factor,
+                spec.original, spec.low, spec.high, spec.amplitude)
     if kind == "res":
         return ("res", spec.d, spec.tokens, spec.mark, spec.act)
     if kind == "bn":
@@ -239,6 +244,61 @@ class GpuStage:
                              temperature, labels.data_ptr() if labels is not None else 0, label_weight, dlogits.data_ptr(),
                              loss.data_ptr())
         return loss, dlogits
+
+    def _row_count(self, logits: torch.Tensor) -> int:
+        """Rows of a mini-batch's logits, one for every sample or token position; checks the tensor."""
+        classes = self.layers[-1][1]
+        rows = self.mb * self.n * self.out_elems // classes
+        assert logits.numel() == rows * classes and logits.is_contiguous() and logits.dtype == self.tdtype
+        return rows
+
+    @staticmethod
+    def _row_values(count: int, dtype, *values: Optional[torch.Tensor]) -> List[int]:
+        """Addresses of tensors of `count` values each (0 for None)."""
+        for v in values:
+            assert v is None or (v.dtype == dtype and v.numel() == count and v.is_contiguous())
+        return [0 if v is None else v.data_ptr() for v in values]
+
+    def logprobs(self, logits: torch.Tensor, ids: torch.Tensor) -> torch.Tensor:
+        """Log probability of class ids[r] (int32; negative: no token, 0) in every row of `logits`, whose rows have the stage's classes; of
+        any pass and any number of rows."""
+        classes = self.layers[-1][1]
+        rows = logits.numel() // classes
+        assert logits.numel() == rows * classes and logits.is_contiguous() and logits.dtype == self.tdtype
+        at, = self._row_values(rows, torch.int32, ids)
+        logp = torch.empty(rows, dtype=torch.float32, device=self.device)
+        B.stage_logprobs(self.handle, logits.data_ptr(), at, rows, logp.data_ptr())
+        return logp
+
+    def loss_policy(self, mb_id: int, logits: torch.Tensor, actions: torch.Tensor, old_logp: torch.Tensor, advantages: torch.Tensor, *,
+                    weights: Optional[torch.Tensor] = None, ref_logp: Optional[torch.Tensor] = None, clip_low: float = 0.2,
+                    clip_high: float = 0.2, kl_weight: float = 0.0):
+        """The clipped policy loss with a KL term against a reference: one action (int32, negative: none), old log probability, advantage,
+        weight (None: a mean) and reference log probability (float32) for every sample or token position.  Returns the loss, its
+        gradient and the actions' log probabilities."""
+        rows = self._row_count(logits)
+        act, = self._row_values(rows, torch.int32, actions)
+        old, adv, wgt, ref = self._row_values(rows, torch.float32, old_logp, advantages, weights, ref_logp)
+        dlogits = torch.empty_like(logits)
+        loss, logp = (torch.empty(k, dtype=torch.float32, device=self.device) for k in (1, rows))
+        B.stage_loss_policy(self.handle, mb_id, logits.data_ptr(), act, old, adv, wgt, ref, clip_low, clip_high, kl_weight,
+                            dlogits.data_ptr(), logp.data_ptr(), loss.data_ptr())
+        return loss, dlogits, logp
+
+    def loss_preference(self, mb_id: int, logits: torch.Tensor, targets: torch.Tensor, ref_logp: torch.Tensor, *,
+                        weights: Optional[torch.Tensor] = None, beta: float = 0.1, label_smoothing: float = 0.0):
+        """The loss on pairs of sequences, samples 2i (chosen) and 2i + 1 (rejected): targets (int32, negative: none) and weights (float32,
+        None: 1) for every token position, ref_logp (float32) the reference's weighted sum of each sample.  Returns the loss, its
+        gradient and the targets' log probabilities."""
+        rows = self._row_count(logits)
+        tgt, = self._row_values(rows, torch.int32, targets)
+        wgt, = self._row_values(rows, torch.float32, weights)
+        ref, = self._row_values(self.mb * self.n, torch.float32, ref_logp)
+        dlogits = torch.empty_like(logits)
+        loss, logp = (torch.empty(k, dtype=torch.float32, device=self.device) for k in (1, rows))
+        B.stage_loss_preference(self.handle, mb_id, logits.data_ptr(), tgt, wgt, ref, beta, label_smoothing, dlogits.data_ptr(),
+                                logp.data_ptr(), loss.data_ptr())
+        return loss, dlogits, logp
 
     def backward(self, mb_id: int, dy: torch.Tensor, dx: Optional[torch.Tensor] = None):
         rows = self.mb * self.n

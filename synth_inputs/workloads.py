@@ -109,6 +109,61 @@ class Attention:
 
 
 @dataclass(frozen=True)
+class Gated:
+    """Both projections of a gated feed-forward block, act(gate) * other, on [tokens, in_features] -> [tokens, out_features]; the rows of
+    its weights are the gate and the other factor of each output in turn."""
+    in_features: int
+    out_features: int
+    act: str
+    tokens: int
+    kind: str = "gated"
+
+    def param_shapes(self):
+        return [(2 * self.out_features, self.in_features), (2 * self.out_features,)]
+
+    def in_shape(self):
+        return (self.tokens, self.in_features)
+
+    def out_shape(self):
+        return (self.tokens, self.out_features)
+
+    def out_dim(self):
+        return self.tokens * self.out_features
+
+
+@dataclass(frozen=True)
+class Rotary:
+    """Rotary positions on the queries and keys of [tokens, (heads + 2 kv_heads) * head] (queries | keys | values); no parameters."""
+    heads: int
+    kv_heads: int
+    head: int
+    tokens: int
+    rotated: int
+    layout: str = "halves"
+    base: float = 10000.0
+    first: int = 0
+    factor: float = 1.0
+    original: int = 0
+    low: float = 0.0
+    high: float = 0.0
+    amplitude: float = 1.0
+    kind: str = "rotary"
+    act: str = "none"
+
+    def param_shapes(self):
+        return []
+
+    def in_shape(self):
+        return (self.tokens, (self.heads + 2 * self.kv_heads) * self.head)
+
+    def out_shape(self):
+        return self.in_shape()
+
+    def out_dim(self):
+        return self.tokens * (self.heads + 2 * self.kv_heads) * self.head
+
+
+@dataclass(frozen=True)
 class LocalAttention:
     """Causal attention of `heads` query heads on `kv_heads` key heads over the last `window` keys (0: all) and the first `sinks`
     keys, on [tokens, d + 2 * kv_heads * (d / heads)] (queries | keys | values) -> [tokens, d]; parameters: with buckets a table
