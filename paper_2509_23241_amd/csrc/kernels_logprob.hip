@@ -12,6 +12,7 @@
 #include <stdint.h>
 
 #include <algorithm>
+#include <type_traits>
 
 #include "device_utils.h"
 #include "kernels.h"
@@ -151,8 +152,213 @@ __global__ __launch_bounds__(kThreads) void preference_rows_kernel(PreferenceArg
   }
 }
 
+// ---- rows that registers hold -------------------------------------------------------------------
+// A row is read once and held, HELD units of 16 bytes for each of its NT threads, and its gradient written once; rows may start at any
+// element (units lie at 16-byte addresses; the first and last, which other rows share, are read and written one by one).
+template <typename T, int NT, int HELD>
+struct Held {
+  using TM = Team<NT>;
+  static constexpr int V = kVec<T>;
+  const T* unit0;
+  int thread, classes, lead, whole_from, whole_to, units;
+  float x[HELD][V];
+
+  __device__ __forceinline__ Held(const T* lg, int classes_) : thread(TM::thread()), classes(classes_) {
+    lead = (int)((uintptr_t)lg % 16 / sizeof(T));  // values of the first unit that are another row's
+    whole_from = lead > 0;
+    whole_to = (lead + classes) / V;               // units that are this row's alone
+    units = (lead + classes + V - 1) / V;
+    unit0 = lg - lead;
+  }
+  __device__ __forceinline__ void read() {
+    uint4 raw[HELD];
+#pragma unroll
+    for (int i = 0; i < HELD; ++i) {
+      const int u = min(max(thread + NT * i, whole_from), whole_to - 1);
+      raw[i] = *reinterpret_cast<const uint4*>(unit0 + (size_t)u * V);
+    }
+#pragma unroll
+    for (int i = 0; i < HELD; ++i) {
+      const int u = thread + NT * i;
+      unpack<T>(raw[i], x[i]);
+      if (u < whole_from || u >= whole_to) {
+#pragma unroll
+        for (int e = 0; e < V; ++e) {
+          const int j = u * V + e - lead;
+          x[i][e] = u < units && j >= 0 && j < classes ? to_float(unit0[lead + j]) : -INFINITY;
+        }
+      }
+    }
+  }
+  __device__ __forceinline__ float top(float* sm) const {
+    float m = -INFINITY;
+#pragma unroll
+    for (int i = 0; i < HELD; ++i)
+#pragma unroll
+      for (int e = 0; e < V; ++e) m = fmaxf(m, x[i][e]);
+    return TM::over(m, sm, Max());
+  }
+  // every value becomes its exponential; this thread's sum of them
+  __device__ __forceinline__ float exponentials(const Exponents& ex) {
+    if (ex.base != 0.f) {
+#pragma unroll
+      for (int i = 0; i < HELD; ++i)
+#pragma unroll
+        for (int e = 0; e < V; ++e) x[i][e] -= ex.base;
+    }
+    float sum = 0.f;
+#pragma unroll
+    for (int i = 0; i < HELD; ++i)
+#pragma unroll
+      for (int e = 0; e < V; ++e) {
+        x[i][e] = __builtin_amdgcn_exp2f(fmaf(x[i][e], kLog2e, -ex.shift));
+        sum += x[i][e];
+      }
+    return sum;
+  }
+  // The exponentials times `scale`, and `own` in the place of class id's (none: a negative one).  The thread that stores a unit replaces a value
+  // of it, in program order.
+  __device__ __forceinline__ void write(T* dl, float scale, int id, float own) {
+#pragma unroll
+    for (int i = 0; i < HELD; ++i) {
+      const int u = thread + NT * i;
+#pragma unroll
+      for (int e = 0; e < V; ++e) x[i][e] *= scale;
+      store(dl, u, x[i]);
+    }
+    if (id >= 0 && (lead + id) / V % NT == thread) dl[id] = from_float<T>(own);
+  }
+  __device__ __forceinline__ void write_zeros(T* dl) {
+    const float none[V] = {};
+    for (int u = thread; u < units; u += NT) store(dl, u, none);
+  }
+  __device__ __forceinline__ void store(T* dl, int u, const float (&v)[V]) const {
+    if (u >= whole_from && u < whole_to) {
+      *reinterpret_cast<uint4*>(dl - lead + (size_t)u * V) = pack<T>(v);
+    } else if (u < units) {
+#pragma unroll
+      for (int e = 0; e < V; ++e) {
+        const int j = u * V + e - lead;
+        if (j >= 0 && j < classes) dl[j] = from_float<T>(v[e]);
+      }
+    }
+  }
+};
+// Of 64 values a thread, two workgroups of 512 threads on a CU.
+template <typename T, int HELD>
+constexpr int kWavesASimd = HELD * kVec<T> == 64 ? 4 : 1;
+
+template <typename T, int NT, int HELD>
+__global__ __launch_bounds__(Team<NT>::kThreads, (kWavesASimd<T, HELD>)) void logprob_held_kernel(LogprobArgs a, int first_row) {
+  using TM = Team<NT>;
+  __shared__ float sm[TM::kThreads / 64];
+  const int row = first_row + blockIdx.x * TM::kRows + TM::which();
+  if (row >= a.rows) return;
+  const int id = a.ids[row];
+  const bool counts = id >= 0 && (!a.weights || a.weights[row] != 0.f);
+  const T* lg = (const T*)a.logits + (size_t)row * a.classes;
+  RowStats r{0.f, 1.f};
+  float z = 0.f;
+  if (counts) {
+    if (id < a.classes) z = to_float(lg[id]);
+    Held<T, NT, HELD> h(lg, a.classes);
+    h.read();
+    r.top = h.top(sm);
+    r.sum = TM::over(h.exponentials(Exponents(r.top)), sm, Add());
+  }
+  if (TM::thread() == 0) {
+    a.logp[row] = !counts ? 0.f : id < a.classes ? (float)Exponents(r.top).log_probability(z, r.sum) : __builtin_nanf("");
+    if (a.stats) a.stats[row] = r;
+  }
+}
+
+// The sum of the row losses by the workgroup that arrives last, where a counter is given.
+__device__ __forceinline__ void finish_sum(uint32_t* counter, const float* row_loss, int rows, float* loss) {
+  __shared__ double sums[256];
+  __shared__ int finishes;
+  if (!counter) return;
+  asm volatile("s_waitcnt vmcnt(0)" ::: "memory");  // this wave's row losses have arrived
+  __syncthreads();
+  if (threadIdx.x == 0) finishes = last_to_arrive(counter, gridDim.x);
+  __syncthreads();
+  if (!finishes) return;
+  if (threadIdx.x < 256) {
+    double s = 0.0;
+    for (int i = threadIdx.x; i < rows; i += 256) s += (double)published(row_loss + i);
+    sums[threadIdx.x] = s;
+  }
+  __syncthreads();
+  for (int w = 128; w > 0; w >>= 1) {
+    if ((int)threadIdx.x < w) sums[threadIdx.x] += sums[threadIdx.x + w];
+    __syncthreads();
+  }
+  if (threadIdx.x == 0) *loss = (float)sums[0];
+}
+
+template <typename T, int NT, int HELD>
+__global__ __launch_bounds__(Team<NT>::kThreads, (kWavesASimd<T, HELD>)) void policy_held_kernel(PolicyArgs a) {
+  using TM = Team<NT>;
+  __shared__ float sm[TM::kThreads / 64];
+  const int row = a.first_row + blockIdx.x * TM::kRows + TM::which();
+  if (row < a.rows) {
+    const int id = a.actions[row];
+    const float weight = a.weights ? a.weights[row] : 1.f / (float)a.rows;
+    const bool counts = id >= 0 && weight != 0.f, known = id < a.classes;
+    const T* lg = (const T*)a.logits + (size_t)row * a.classes;
+    T* dl = (T*)a.dlogits + (size_t)row * a.classes;
+    Held<T, NT, HELD> h(lg, a.classes);
+    PolicyTerm t{0.f, 0.f};
+    double logp = 0.0;
+    if (counts && known) {
+      const float z = to_float(lg[id]);
+      h.read();
+      const Exponents ex(h.top(sm));
+      const float sum = TM::over(h.exponentials(ex), sm, Add());
+      logp = ex.log_probability(z, sum);
+      t = policy_term(a, row, weight, logp);
+      if (t.slope != 0.f) {
+        const float scale = -t.slope / sum;
+        h.write(dl, scale, id, t.slope + scale * __builtin_amdgcn_exp2f(ex.power(z)));
+      }
+    } else if (counts) {
+      logp = __builtin_nan("");
+      t.loss = __builtin_nanf("");
+    }
+    if (t.slope == 0.f) h.write_zeros(dl);
+    if (TM::thread() == 0) {
+      publish(a.row_loss + row, t.loss);
+      if (a.logp) a.logp[row] = (float)logp;
+    }
+  }
+  finish_sum(a.counter, a.row_loss, a.rows, a.loss);
+}
+
+template <typename T, int NT, int HELD>
+__global__ __launch_bounds__(Team<NT>::kThreads, (kWavesASimd<T, HELD>)) void preference_held_kernel(PreferenceArgs a, int first_row) {
+  using TM = Team<NT>;
+  const int row = first_row + blockIdx.x * TM::kRows + TM::which();
+  if (row >= 2 * a.pairs * a.tokens) return;
+  const int id = a.targets[row];
+  const float weight = a.weights ? a.weights[row] : 1.f;
+  const float slope = id >= 0 && weight != 0.f ? a.pull[row / a.tokens] * weight : 0.f;
+  const T* lg = (const T*)a.logits + (size_t)row * a.classes;
+  T* dl = (T*)a.dlogits + (size_t)row * a.classes;
+  Held<T, NT, HELD> h(lg, a.classes);
+  if (slope == 0.f) {
+    h.write_zeros(dl);
+    return;
+  }
+  const RowStats r = a.stats[row];
+  const Exponents ex(r.top);
+  const float scale = -slope / r.sum;
+  const float z = id < a.classes ? to_float(lg[id]) : 0.f;
+  h.read();
+  h.exponentials(ex);
+  h.write(dl, scale, id < a.classes ? id : -1, slope + scale * __builtin_amdgcn_exp2f(ex.power(z)));
+}
+
 // ---- the sums -----------------------------------------------------------------------------------
-// Of 1024 threads' values, in every thread of the first wave's first lane; sm: 16 doubles.
+// Of a workgroup's values, in every thread; sm: a double for each wave.
 constexpr int kSumThreads = 1024;
 __device__ __forceinline__ double block_sum(double s, double* sm) {
 #pragma unroll
@@ -219,32 +425,86 @@ hipError_t sum_losses(hipStream_t s, const float* v, long n, double by, float* o
   return hipGetLastError();
 }
 
-}  // namespace
+// Calls f with the threads of a row and the units each holds (two integral constants) and the workgroups, some of them at a time: a launch takes
+// fewer than 2^32 threads, and drops what a grid has beyond.  False: rows that are not held, of too few units or too many.
+template <typename T, class F>
+bool held(int rows, int classes, const F& f) {
+  constexpr int V = kVec<T>, W = 64 / V;  // units of 64 values
+  const long units = classes / V + 2;     // with a first and a last one that are shared
+  auto go = [&](auto nt, auto count) {
+    constexpr int NT = decltype(nt)::value;
+    const long blocks = ((long)rows + Team<NT>::kRows - 1) / Team<NT>::kRows, most = UINT32_MAX / Team<NT>::kThreads;
+    for (long from = 0; from < blocks; from += most)
+      f(nt, count, (unsigned)std::min(most, blocks - from), blocks, (int)(from * Team<NT>::kRows));
+    return true;
+  };
+  auto n = [](auto v) { return v; };
+#define TP_HELD(NT, COUNT) go(n(std::integral_constant<int, NT>()), n(std::integral_constant<int, COUNT>()))
+  if (classes < 2 * V) return false;
+  if (units <= 64) return TP_HELD(64, 1);
+  if (units <= 64 * 2) return TP_HELD(64, 2);
+  if (units <= 256) return TP_HELD(256, 1);
+  if (units <= 256 * W / 4) return TP_HELD(256, W / 4);
+  if (units <= 256 * W / 2) return TP_HELD(256, W / 2);
+  if (units <= 256 * W) return TP_HELD(256, W);
+  if (units <= 512 * W) return TP_HELD(512, W);
+  if (units <= 1024 * W) return TP_HELD(1024, W);
+#undef TP_HELD
+  return false;
+}
+inline bool alike(const void* a, const void* b) { return ((uintptr_t)a - (uintptr_t)b) % 16 == 0; }
 
-hipError_t launch_logprobs(hipStream_t s, int elt, const LogprobArgs& a) {
-  if (elt == ELT_BF16) hipLaunchKernelGGL(logprob_rows_kernel<uint16_t>, dim3(row_blocks(a.rows)), dim3(kThreads), 0, s, a);
-  else hipLaunchKernelGGL(logprob_rows_kernel<float>, dim3(row_blocks(a.rows)), dim3(kThreads), 0, s, a);
+constexpr int kCounted = 128;  // workgroups up to which the last of them adds up the row losses; more take a launch of their own
+
+template <typename T>
+hipError_t logprobs(hipStream_t s, const LogprobArgs& a) {
+  const bool done = held<T>(a.rows, a.classes, [&](auto nt, auto count, unsigned blocks, long, int first_row) {
+    constexpr int NT = decltype(nt)::value, HELD = decltype(count)::value;
+    hipLaunchKernelGGL((logprob_held_kernel<T, NT, HELD>), dim3(blocks), dim3(Team<NT>::kThreads), 0, s, a, first_row);
+  });
+  if (!done) hipLaunchKernelGGL(logprob_rows_kernel<T>, dim3(row_blocks(a.rows)), dim3(kThreads), 0, s, a);
   return hipGetLastError();
 }
 
-hipError_t launch_policy(hipStream_t s, int elt, const PolicyArgs& a) {
-  if (elt == ELT_BF16) hipLaunchKernelGGL(policy_rows_kernel<uint16_t>, dim3(row_blocks(a.rows)), dim3(kThreads), 0, s, a);
-  else hipLaunchKernelGGL(policy_rows_kernel<float>, dim3(row_blocks(a.rows)), dim3(kThreads), 0, s, a);
+template <typename T>
+hipError_t policy(hipStream_t s, PolicyArgs a) {
+  bool counted = false;
+  const bool done = alike(a.logits, a.dlogits) && held<T>(a.rows, a.classes, [&](auto nt, auto count, unsigned blocks, long all, int first_row) {
+    constexpr int NT = decltype(nt)::value, HELD = decltype(count)::value;
+    counted = all <= kCounted;
+    PolicyArgs part = a;
+    part.first_row = first_row;
+    if (!counted) part.counter = nullptr;
+    hipLaunchKernelGGL((policy_held_kernel<T, NT, HELD>), dim3(blocks), dim3(Team<NT>::kThreads), 0, s, part);
+  });
+  if (!done) hipLaunchKernelGGL(policy_rows_kernel<T>, dim3(row_blocks(a.rows)), dim3(kThreads), 0, s, a);
   const hipError_t e = hipGetLastError();
-  return e != hipSuccess ? e : sum_losses(s, a.row_loss, a.rows, 1.0, a.loss);
+  return e != hipSuccess || counted ? e : sum_losses(s, a.row_loss, a.rows, 1.0, a.loss);
 }
 
-hipError_t launch_preference(hipStream_t s, int elt, const PreferenceArgs& a) {
-  const long rows = 2l * a.pairs * a.tokens;
-  hipError_t e = launch_logprobs(s, elt, LogprobArgs{(int)rows, a.classes, a.logits, a.targets, a.logp, a.stats, a.weights});
+template <typename T>
+hipError_t preference(hipStream_t s, const PreferenceArgs& a) {
+  const int rows = 2 * a.pairs * a.tokens;
+  hipError_t e = logprobs<T>(s, LogprobArgs{rows, a.classes, a.logits, a.targets, a.logp, a.stats, a.weights});
   if (e != hipSuccess) return e;
   hipLaunchKernelGGL(preference_pairs_kernel, dim3(row_blocks(a.pairs)), dim3(kThreads), 0, s, a);
   e = hipGetLastError();
   if (e != hipSuccess) return e;
-  if (elt == ELT_BF16) hipLaunchKernelGGL(preference_rows_kernel<uint16_t>, dim3(row_blocks(rows)), dim3(kThreads), 0, s, a);
-  else hipLaunchKernelGGL(preference_rows_kernel<float>, dim3(row_blocks(rows)), dim3(kThreads), 0, s, a);
+  const bool done = alike(a.logits, a.dlogits) && held<T>(rows, a.classes, [&](auto nt, auto count, unsigned blocks, long, int first_row) {
+    constexpr int NT = decltype(nt)::value, HELD = decltype(count)::value;
+    hipLaunchKernelGGL((preference_held_kernel<T, NT, HELD>), dim3(blocks), dim3(Team<NT>::kThreads), 0, s, a, first_row);
+  });
+  if (!done) hipLaunchKernelGGL(preference_rows_kernel<T>, dim3(row_blocks(rows)), dim3(kThreads), 0, s, a);
   e = hipGetLastError();
   return e != hipSuccess ? e : sum_losses(s, a.pair_loss, a.pairs, (double)a.pairs, a.loss);
+}
+
+}  // namespace
+
+hipError_t launch_logprobs(hipStream_t s, int elt, const LogprobArgs& a) { return elt == ELT_BF16 ? logprobs<uint16_t>(s, a) : logprobs<float>(s, a); }
+hipError_t launch_policy(hipStream_t s, int elt, const PolicyArgs& a) { return elt == ELT_BF16 ? policy<uint16_t>(s, a) : policy<float>(s, a); }
+hipError_t launch_preference(hipStream_t s, int elt, const PreferenceArgs& a) {
+  return elt == ELT_BF16 ? preference<uint16_t>(s, a) : preference<float>(s, a);
 }
 
 }  // namespace tp
