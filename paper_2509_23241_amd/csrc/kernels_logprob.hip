@@ -272,8 +272,8 @@ __global__ __launch_bounds__(Team<NT>::kThreads, (kWavesASimd<T, HELD>)) void lo
   }
 }
 
-// The sum of the row losses by the workgroup that arrives last, where a counter is given.
-__device__ __forceinline__ void finish_sum(uint32_t* counter, const float* row_loss, int rows, float* loss) {
+// The sum of the losses, over `by`, by the workgroup that arrives last, where a counter is given.
+__device__ __forceinline__ void finish_sum(uint32_t* counter, const float* row_loss, int rows, double by, float* loss) {
   __shared__ double sums[256];
   __shared__ int finishes;
   if (!counter) return;
@@ -292,7 +292,7 @@ __device__ __forceinline__ void finish_sum(uint32_t* counter, const float* row_l
     if ((int)threadIdx.x < w) sums[threadIdx.x] += sums[threadIdx.x + w];
     __syncthreads();
   }
-  if (threadIdx.x == 0) *loss = (float)sums[0];
+  if (threadIdx.x == 0) *loss = (float)(sums[0] / by);
 }
 
 template <typename T, int NT, int HELD>
@@ -330,14 +330,17 @@ __global__ __launch_bounds__(Team<NT>::kThreads, (kWavesASimd<T, HELD>)) void po
       if (a.logp) a.logp[row] = (float)logp;
     }
   }
-  finish_sum(a.counter, a.row_loss, a.rows, a.loss);
+  finish_sum(a.counter, a.row_loss, a.rows, 1.0, a.loss);
 }
 
 template <typename T, int NT, int HELD>
 __global__ __launch_bounds__(Team<NT>::kThreads, (kWavesASimd<T, HELD>)) void preference_held_kernel(PreferenceArgs a, int first_row) {
   using TM = Team<NT>;
-  const int row = first_row + blockIdx.x * TM::kRows + TM::which();
-  if (row >= 2 * a.pairs * a.tokens) return;
+  const int rows = 2 * a.pairs * a.tokens;
+  const int at = first_row + blockIdx.x * TM::kRows + TM::which();
+  if (at >= rows) return;
+  // from the last row to the first: what the pass before read last is what the last-level cache still has
+  const int row = rows - 1 - at;
   const int id = a.targets[row];
   const float weight = a.weights ? a.weights[row] : 1.f;
   const float slope = id >= 0 && weight != 0.f ? a.pull[row / a.tokens] * weight : 0.f;
@@ -387,7 +390,8 @@ __global__ __launch_bounds__(kSumThreads) void loss_sum_kernel(const float* __re
   if (threadIdx.x == 0) *out = (float)(s / by);
 }
 
-// A workgroup a pair: the sums of its two sequences, its loss, and what a log probability of either weighs.
+// A workgroup a pair: the sums of its two sequences, its loss, and what a log probability of either weighs; the mean of the losses by the
+// workgroup that arrives last, where a counter is given.
 __global__ __launch_bounds__(kThreads) void preference_pairs_kernel(PreferenceArgs a) {
   __shared__ double sm[kThreads / 64];
   for (long pair = blockIdx.x; pair < a.pairs; pair += gridDim.x) {
@@ -411,11 +415,12 @@ __global__ __launch_bounds__(kThreads) void preference_pairs_kernel(PreferenceAr
       if (a.smoothing < 1.0) loss -= (1.0 - a.smoothing) * log_right;
       if (a.smoothing > 0.0) loss -= a.smoothing * log_wrong;
       const double pull = a.beta / a.pairs * (a.smoothing * right - (1.0 - a.smoothing) * wrong);
-      a.pair_loss[pair] = m == m ? (float)loss : __builtin_nanf("");
+      publish(a.pair_loss + pair, m == m ? (float)loss : __builtin_nanf(""));
       a.pull[2 * pair] = (float)pull;
       a.pull[2 * pair + 1] = (float)-pull;
     }
   }
+  finish_sum(a.counter, a.pair_loss, a.pairs, (double)a.pairs, a.loss);
 }
 
 unsigned row_blocks(long rows) { return (unsigned)std::min<long>(rows, 1 << 20); }
@@ -454,7 +459,7 @@ bool held(int rows, int classes, const F& f) {
 }
 inline bool alike(const void* a, const void* b) { return ((uintptr_t)a - (uintptr_t)b) % 16 == 0; }
 
-constexpr int kCounted = 128;  // workgroups up to which the last of them adds up the row losses; more take a launch of their own
+constexpr int kCounted = 128;  // workgroups up to which the last of them adds up the losses; more take a launch of their own
 
 template <typename T>
 hipError_t logprobs(hipStream_t s, const LogprobArgs& a) {
@@ -483,10 +488,12 @@ hipError_t policy(hipStream_t s, PolicyArgs a) {
 }
 
 template <typename T>
-hipError_t preference(hipStream_t s, const PreferenceArgs& a) {
+hipError_t preference(hipStream_t s, PreferenceArgs a) {
   const int rows = 2 * a.pairs * a.tokens;
   hipError_t e = logprobs<T>(s, LogprobArgs{rows, a.classes, a.logits, a.targets, a.logp, a.stats, a.weights});
   if (e != hipSuccess) return e;
+  const bool counted = a.pairs <= kCounted;
+  if (!counted) a.counter = nullptr;
   hipLaunchKernelGGL(preference_pairs_kernel, dim3(row_blocks(a.pairs)), dim3(kThreads), 0, s, a);
   e = hipGetLastError();
   if (e != hipSuccess) return e;
@@ -496,7 +503,7 @@ hipError_t preference(hipStream_t s, const PreferenceArgs& a) {
   });
   if (!done) hipLaunchKernelGGL(preference_rows_kernel<T>, dim3(row_blocks(rows)), dim3(kThreads), 0, s, a);
   e = hipGetLastError();
-  return e != hipSuccess ? e : sum_losses(s, a.pair_loss, a.pairs, (double)a.pairs, a.loss);
+  return e != hipSuccess || counted ? e : sum_losses(s, a.pair_loss, a.pairs, (double)a.pairs, a.loss);
 }
 
 }  // namespace

@@ -50,6 +50,7 @@ struct PreferenceArgs {
   RowStats* stats;        // scratch, [rows]
   float* pull;            // scratch, [2 pairs]: what a log probability of the sample weighs in the loss
   float* pair_loss;       // scratch, [pairs]
+  uint32_t* counter;      // zero before the launch and after it
   float* loss;
 };
 hipError_t launch_preference(hipStream_t s, int elt, const PreferenceArgs& a);

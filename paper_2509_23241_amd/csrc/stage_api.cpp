@@ -1435,6 +1435,7 @@ int stage_loss_preference(tp_stage* st, uint64_t mb_id, const void* logits_dev, 
   a.stats = (tp::RowStats*)st->partials();
   a.pull = (float*)(a.stats + rows);
   a.pair_loss = a.pull + samples;
+  a.counter = st->counter(tp_stage::kCountLoss);
   a.loss = loss_dev;
   ProfScope ps(st, TP_K_LOSS);
   HIP_TRY(tp::launch_preference(st->stream, st->desc.dtype, a));
