@@ -339,7 +339,9 @@ __global__ __launch_bounds__(Team<NT>::kThreads, (kWavesASimd<T, HELD>)) void pr
   const int rows = 2 * a.pairs * a.tokens;
   const int at = first_row + blockIdx.x * TM::kRows + TM::which();
   if (at >= rows) return;
-  // from the last row to the first: what the pass before read last is what the last-level cache still has
+  // From the last row to the first: what the pass before read last is what the last-level cache still has (8192 rows of 32000 classes in bf16
+  // 150 -> 146 us).  Both passes over a few pairs at a time, 131 MB of them or 262, find more there and lose it to the ends of twice as many
+  // launches: 250 us in all, 300 and 271 so.
   const int row = rows - 1 - at;
   const int id = a.targets[row];
   const float weight = a.weights ? a.weights[row] : 1.f;
@@ -400,8 +402,8 @@ __global__ __launch_bounds__(kThreads) void preference_pairs_kernel(PreferenceAr
       const size_t row0 = (size_t)(2 * pair + k) * a.tokens;
       double s = 0.0;
       for (int t = threadIdx.x; t < a.tokens; t += kThreads) {
-        const float weight = a.weights ? a.weights[row0 + t] : 1.f;
-        if (a.targets[row0 + t] >= 0 && weight != 0.f) s += (double)weight * (double)a.logp[row0 + t];
+        const float weight = a.weights ? a.weights[row0 + t] : 1.f, logp = a.logp[row0 + t];  // loaded side by side
+        s += a.targets[row0 + t] >= 0 && weight != 0.f ? (double)weight * (double)logp : 0.0;
       }
       ratio[k] = block_sum(s, sm) - (double)a.ref_logp[2 * pair + k];
     }

@@ -7,10 +7,12 @@
 #include <stdint.h>
 
 #include <algorithm>
+#include <type_traits>
 
 #include "device_utils.h"
 #include "kernels.h"
 #include "rotary.h"
+#include "row_device.h"
 
 namespace tp {
 
@@ -62,6 +64,154 @@ __global__ __launch_bounds__(kThreads) void rotary_any_kernel(Rotary r, RotarySp
   }
 }
 
+// ---- heads and their parts in whole 16-byte units ------------------------------------------------
+// A workgroup takes some tokens: sines and cosines go into LDS, one or a few a thread, while the first units are on their way; every
+// thread then turns several items at a time, all of them loaded before the first is used.  An item is two units of halves, whose values are
+// pairs across them, or one unit of neighbours.  What is not turned is copied likewise where the output lies elsewhere.  Value by value
+// (the kernel above) the same 8192 tokens take 127 us.
+struct RotaryShape {
+  int tokens;      // of a workgroup
+  int units;       // of a token
+  int head_units;  // of a head
+  int items;       // of a head
+  int rest;        // units of a turned head that are not turned
+  uint32_t by_items, by_turned, by_copies, by_rest;  // multipliers that divide by .., heads that are turned, units of a token that are copied, ..
+};
+// n / d by the multiplier of divisor(d), exact for n * d < 2^32
+inline uint32_t divisor(int d) { return d <= 1 ? 0u : (uint32_t)(((1ull << 32) + d - 1) / d); }
+__device__ __forceinline__ int divided(int n, uint32_t mul) { return mul ? (int)__umulhi((uint32_t)n, mul) : n; }
+constexpr int kMaxTokens = 8;
+
+template <typename T, bool HALVES, bool COPY>
+__global__ __launch_bounds__(kThreads) void rotary_units_kernel(Rotary r, RotaryShape sh, RotarySpeeds speeds, bool back, const T* x, T* out) {
+  constexpr int V = kVec<T>, ITEMS = HALVES ? 4 : 8;
+  __shared__ float2 turn[kMaxTokens * kMaxRotaryPairs];
+  const int half = r.rotated / 2;
+  const long token0 = (long)blockIdx.x * sh.tokens;
+  const int tokens = (int)min((long)sh.tokens, (long)r.seqs * r.S - token0);
+  const uint4* from = reinterpret_cast<const uint4*>(x) + token0 * sh.units;
+  uint4* to = reinterpret_cast<uint4*>(out) + token0 * sh.units;
+  // what is copied: a batch of it is under way while the turns are made, the rest follows them
+  const int values = sh.units - r.turned * sh.head_units, copies = COPY ? tokens * (values + r.turned * sh.rest) : 0;
+  auto copied = [&](int i) {
+    const int token = divided(i, sh.by_copies), u = i - token * (values + r.turned * sh.rest), head = divided(max(u - values, 0), sh.by_rest);
+    return token * sh.units + (u < values ? r.turned * sh.head_units + u : (head + 1) * sh.head_units - sh.rest + u - values - head * sh.rest);
+  };
+  constexpr int BATCH = COPY ? 4 : 1;
+  typedef uint32_t unit_t __attribute__((ext_vector_type(4)));  // (an array of uint4 written under a condition stays in memory)
+  unit_t kept[BATCH];
+  if constexpr (COPY) {
+#pragma unroll
+    for (int k = 0; k < BATCH; ++k) {
+      const int i = k * kThreads + (int)threadIdx.x;
+      kept[k] = i < copies ? *reinterpret_cast<const unit_t*>(from + copied(i)) : unit_t{0, 0, 0, 0};
+    }
+  }
+  const int items = tokens * r.turned * sh.items, other = half / V;
+  for (int i0 = 0; i0 < items; i0 += kThreads * ITEMS) {
+    uint4 a[ITEMS], b[HALVES ? ITEMS : 1];
+    int unit[ITEMS], at[ITEMS];
+#pragma unroll
+    for (int k = 0; k < ITEMS; ++k) {
+      const int i = i0 + k * kThreads + (int)threadIdx.x;
+      const int head_of_all = divided(i, sh.by_items), item = i - head_of_all * sh.items;
+      const int token = divided(head_of_all, sh.by_turned), head = head_of_all - token * r.turned;
+      unit[k] = token * sh.units + head * sh.head_units + item;
+      at[k] = token * half + item * (HALVES ? V : V / 2);
+      if (i < items) {
+        a[k] = from[unit[k]];
+        if constexpr (HALVES) b[k] = from[unit[k] + other];
+      }
+    }
+    if (i0 == 0) {
+      for (int i = threadIdx.x; i < tokens * half; i += kThreads) {
+        const int token = i / half, pair = i - token * half;
+        turn[i] = turn_of(speeds.turns[pair], r.first + (int)((token0 + token) % r.S), r.amplitude, back);
+      }
+      __syncthreads();
+    }
+#pragma unroll
+    for (int k = 0; k < ITEMS; ++k) {
+      if (i0 + k * kThreads + (int)threadIdx.x < items) {
+        float u[V], p[V];
+        unpack<T>(a[k], u);
+        if constexpr (HALVES) {
+          float v[V], q[V];
+          unpack<T>(b[k], v);
+#pragma unroll
+          for (int e = 0; e < V; ++e) {
+            const float2 t = turn[at[k] + e];
+            p[e] = u[e] * t.x - v[e] * t.y;
+            q[e] = u[e] * t.y + v[e] * t.x;
+          }
+          to[unit[k] + other] = pack<T>(q);
+        } else {
+#pragma unroll
+          for (int e = 0; e < V; e += 2) {
+            const float2 t = turn[at[k] + e / 2];
+            p[e] = u[e] * t.x - u[e + 1] * t.y;
+            p[e + 1] = u[e] * t.y + u[e + 1] * t.x;
+          }
+        }
+        to[unit[k]] = pack<T>(p);
+      }
+    }
+  }
+  if constexpr (COPY) {
+#pragma unroll
+    for (int k = 0; k < BATCH; ++k) {
+      const int i = k * kThreads + (int)threadIdx.x;
+      if (i < copies) *reinterpret_cast<unit_t*>(to + copied(i)) = kept[k];
+    }
+    for (int i = BATCH * kThreads + (int)threadIdx.x; i < copies; i += kThreads) {
+      const int u = copied(i);
+      to[u] = from[u];
+    }
+  }
+}
+
+// Rotary layers whose parts of heads are whole units at 16-byte addresses; false: others, and tokens of too many units for the divisions.
+template <typename T>
+bool launch_units(hipStream_t s, const Rotary& r, const RotarySpeeds& speeds, bool back, const T* x, T* out) {
+  constexpr int V = kVec<T>;
+  const int half = r.rotated / 2;
+  if (r.dh % V || (r.halves ? half : r.rotated) % V || (((uintptr_t)x | (uintptr_t)out) & 15)) return false;
+  if ((long)r.all * r.dh / V * kMaxTokens * std::max(r.all, r.dh / V) >= (1l << 31)) return false;
+  const long all = (long)r.seqs * r.S;
+  RotaryShape sh;
+  sh.head_units = r.dh / V;
+  sh.units = r.all * sh.head_units;
+  // Four units a thread, as long as that leaves every CU two workgroups.  8192 tokens of 768 units, both ways with the values copied: 79 us with one token a
+  // workgroup (403 MB, at 5.1 TB/s the rate of a copy), 95 with two, 112 with four; 3108 tokens of 200 units 15.4 with five, 22 with one.
+  sh.tokens = (int)std::min<long>(kMaxTokens, std::max<long>(1, std::min<long>(all / 512, 1024 / sh.units)));
+  sh.items = (r.halves ? half : r.rotated) / V;
+  sh.rest = (r.dh - r.rotated) / V;
+  const int copies = sh.units - r.turned * sh.head_units + r.turned * sh.rest;
+  sh.by_items = divisor(sh.items);
+  sh.by_turned = divisor(r.turned);
+  sh.by_copies = divisor(copies);
+  sh.by_rest = divisor(sh.rest);
+  const dim3 grid((unsigned)((all + sh.tokens - 1) / sh.tokens));
+  auto go = [&](auto halves, auto copy) {
+    hipLaunchKernelGGL((rotary_units_kernel<T, decltype(halves)::value, decltype(copy)::value>), grid, dim3(kThreads), 0, s, r, sh, speeds, back, x, out);
+  };
+  using Yes = std::true_type;
+  using No = std::false_type;
+  const bool copy = x != out;
+  if (r.halves) copy ? go(Yes(), Yes()) : go(Yes(), No());
+  else copy ? go(No(), Yes()) : go(No(), No());
+  return true;
+}
+
+template <typename T>
+hipError_t launch(hipStream_t s, const Rotary& r, const RotarySpeeds& speeds, bool back, const T* x, T* out) {
+  if (!launch_units<T>(s, r, speeds, back, x, out)) {
+    const unsigned blocks = (unsigned)std::min<long>((long)r.seqs * r.S, 1 << 20);
+    hipLaunchKernelGGL(rotary_any_kernel<T>, dim3(blocks), dim3(kThreads), 0, s, r, speeds, back, x, out);
+  }
+  return hipGetLastError();
+}
+
 }  // namespace
 
 void rotary_speeds(int rotated, double base, double factor, double original, double low, double high, RotarySpeeds* out) {
@@ -82,12 +232,8 @@ void rotary_speeds(int rotated, double base, double factor, double original, dou
 }
 
 hipError_t launch_rotary(hipStream_t s, int elt, const Rotary& r, const RotarySpeeds& speeds, bool back, const void* x, void* out) {
-  const unsigned blocks = (unsigned)std::min<long>((long)r.seqs * r.S, 1 << 20);
-  if (elt == ELT_BF16)
-    hipLaunchKernelGGL(rotary_any_kernel<uint16_t>, dim3(blocks), dim3(kThreads), 0, s, r, speeds, back, (const uint16_t*)x, (uint16_t*)out);
-  else
-    hipLaunchKernelGGL(rotary_any_kernel<float>, dim3(blocks), dim3(kThreads), 0, s, r, speeds, back, (const float*)x, (float*)out);
-  return hipGetLastError();
+  if (elt == ELT_BF16) return launch<uint16_t>(s, r, speeds, back, (const uint16_t*)x, (uint16_t*)out);
+  return launch<float>(s, r, speeds, back, (const float*)x, (float*)out);
 }
 
 }  // namespace tp
