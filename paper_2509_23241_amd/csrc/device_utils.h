@@ -25,6 +25,16 @@ __device__ __forceinline__ uint32_t pack_bf16x2(float lo, float hi) {
   return __builtin_bit_cast(uint32_t, __builtin_convertvector(f, bf16x2_t));
 }
 
+// Two values to 12 significant bits (halves away from zero: at most 2^-13 off): the upper halves of their fp32 words in `hi`, the second one's on
+// top, and the four bits below those in a byte, the first one's in its lower half.  Infinities and NaN stay what they are but for NaN whose
+// fraction is all ones.
+__device__ __forceinline__ uint32_t split12(float a, float b, uint32_t& hi) {
+  const uint32_t p = __float_as_uint(a) + 0x800u, q = __float_as_uint(b) + 0x800u;
+  hi = __builtin_amdgcn_perm(q, p, 0x07060302u);
+  return (p >> 12 & 15u) | (q >> 8 & 0xf0u);
+}
+__device__ __forceinline__ float joined12(uint32_t upper, uint32_t low) { return __uint_as_float(upper | (low << 12)); }
+
 __device__ __forceinline__ float to_float(float v) { return v; }
 __device__ __forceinline__ float to_float(uint16_t v) { return bf16_to_float(v); }
 

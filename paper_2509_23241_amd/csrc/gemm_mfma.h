@@ -15,7 +15,7 @@ hipError_t mfma_fprop(hipStream_t s, int M, int N, int K, const uint16_t* x, con
                       int spread = SPREAD_NONE);
 // A gated layer's, N = 2 outputs (launch_gated_fprop).
 hipError_t mfma_gated_fprop(hipStream_t s, int M, int N, int K, const uint16_t* x, const uint16_t* W, const float* bias, int act,
-                            uint16_t* d_out, uint16_t* a_out, uint16_t* x_copy, int spread);
+                            uint16_t* d_out, uint8_t* fine, uint16_t* a_out, uint16_t* x_copy, int spread);
 // out = (dz Wb) (.) d_prev, d_prev = saved act'(z) of the previous layer or null; relu_mask = 1: d_prev holds that layer's
 // ReLU output instead and the factor is (output > 0).
 hipError_t mfma_dgrad(hipStream_t s, int M, int N, int K, const uint16_t* dz, const uint16_t* Wb,

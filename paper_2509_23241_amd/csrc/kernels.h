@@ -27,12 +27,14 @@ hipError_t launch_fprop(hipStream_t s, int elt, int M, int N, int K, const void*
                         int spread = SPREAD_NONE);
 bool fprop_add_supported(int elt, int M, int N, int K);
 // A gated layer's forward product, z = x W^T + bias over N = 2 F columns, those of output f being 2f and 2f + 1: a[f] = act(z[2f]) z[2f+1]
-// into a_out [M x F]; what dy[f] is multiplied with to give the gradients of z[2f] and z[2f + 1] into d_out [M x N].
+// into a_out [M x F]; what dy[f] is multiplied with to give the gradients of z[2f] and z[2f + 1] into d_out [M x N] and (bf16, 4-byte
+// aligned) fine [M x F], four bits more of each value: rounded to bf16 they would add as much to the gradients' error as dz itself.
 hipError_t launch_gated_fprop(hipStream_t s, int elt, int M, int N, int K, const void* x, const void* W, const float* bias, int act,
-                              void* d_out, void* a_out, void* x_copy, int spread);
+                              void* d_out, uint8_t* fine, void* a_out, void* x_copy, int spread);
 // dz[2f] = dy[f] d[2f], dz[2f + 1] = dy[f] d[2f + 1], and gb = column sums of dz as stored; N = 2 F columns of dz.
 // partials: scratch of colsum_scratch_floats(M, N) floats.
-hipError_t launch_gated_backward(hipStream_t s, int elt, int M, int N, const void* dy, const void* d, void* dz, float* gb, float* partials);
+hipError_t launch_gated_backward(hipStream_t s, int elt, int M, int N, const void* dy, const void* d, const uint8_t* fine, void* dz, float* gb,
+                                 float* partials);
 
 // out = (dz W_b) (.) d_prev   dz:[M x N] W_b:[N x K] d_prev:[M x K] saved act'(z), or null.
 hipError_t launch_dgrad(hipStream_t s, int elt, int M, int N, int K, const void* dz, const void* Wb,

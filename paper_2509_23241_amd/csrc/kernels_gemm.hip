@@ -146,8 +146,8 @@ __global__ __launch_bounds__(kThreads) void act_backward_colsum_kernel(int M, in
 // and 2f + 1 is dy[f] times what the forward pass kept there.  VEC: rows of whole 16-byte units, dy of 8-byte ones, aligned so.
 template <typename T, bool VEC>
 __global__ __launch_bounds__(kThreads) void gated_backward_kernel(int M, int N, ColsumShape cs, const T* __restrict__ dy,
-                                                                  const T* __restrict__ d, T* __restrict__ dz,
-                                                                  float* __restrict__ partials) {
+                                                                  const T* __restrict__ d, const uint8_t* __restrict__ fine,
+                                                                  T* __restrict__ dz, float* __restrict__ partials) {
   constexpr int V = 16 / sizeof(T);
   __shared__ float sm[kThreads * V];
   const int lr = threadIdx.x % cs.lanes_per_row, rsub = threadIdx.x / cs.lanes_per_row;
@@ -167,11 +167,12 @@ __global__ __launch_bounds__(kThreads) void gated_backward_kernel(int M, int N, 
         const uint32_t bw[4] = {b.x, b.y, b.z, b.w};
         uint32_t ow[4];
         if constexpr (sizeof(T) == 2) {
+          const uint32_t low = *reinterpret_cast<const uint32_t*>(fine + at / 2);
           const float g[4] = {__uint_as_float(a.x << 16), __uint_as_float(a.x & 0xffff0000u), __uint_as_float(a.y << 16),
                               __uint_as_float(a.y & 0xffff0000u)};
 #pragma unroll
           for (int j = 0; j < 4; ++j) {
-            ow[j] = pack_bf16x2(g[j] * __uint_as_float(bw[j] << 16), g[j] * __uint_as_float(bw[j] & 0xffff0000u));
+            ow[j] = pack_bf16x2(g[j] * joined12(bw[j] << 16, (low >> (8 * j)) & 15u), g[j] * joined12(bw[j] & 0xffff0000u, (low >> (8 * j + 4)) & 15u));
             s[(2 * j) % V] += __uint_as_float(ow[j] << 16);
             s[(2 * j + 1) % V] += __uint_as_float(ow[j] & 0xffff0000u);
           }
@@ -191,7 +192,9 @@ __global__ __launch_bounds__(kThreads) void gated_backward_kernel(int M, int N, 
         for (int j = 0; j < V; ++j)
           if (col + j < N) {
             const size_t at = (size_t)r * N + col + j;
-            const T o = from_float<T>(to_float(dy[(size_t)r * (N / 2) + (col + j) / 2]) * to_float(d[at]));
+            float kept = to_float(d[at]);
+            if constexpr (sizeof(T) == 2) kept = joined12(__float_as_uint(kept), (fine[at / 2] >> (4 * (j & 1))) & 15u);
+            const T o = from_float<T>(to_float(dy[at / 2]) * kept);
             dz[at] = o;
             s[j] += to_float(o);
           }
@@ -345,20 +348,22 @@ hipError_t launch_fprop(hipStream_t s, int elt, int M, int N, int K, const void*
 }
 
 hipError_t launch_gated_fprop(hipStream_t s, int elt, int M, int N, int K, const void* x, const void* W, const float* bias, int act,
-                              void* d_out, void* a_out, void* x_copy, int spread) {
+                              void* d_out, uint8_t* fine, void* a_out, void* x_copy, int spread) {
   if (elt == ELT_F32)
     return f32_gated_fprop(s, M, N, K, (const float*)x, (const float*)W, bias, act, (float*)d_out, (float*)a_out, (float*)x_copy);
-  return mfma_gated_fprop(s, M, N, K, (const uint16_t*)x, (const uint16_t*)W, bias, act, (uint16_t*)d_out, (uint16_t*)a_out,
+  return mfma_gated_fprop(s, M, N, K, (const uint16_t*)x, (const uint16_t*)W, bias, act, (uint16_t*)d_out, fine, (uint16_t*)a_out,
                           (uint16_t*)x_copy, spread);
 }
 
-hipError_t launch_gated_backward(hipStream_t s, int elt, int M, int N, const void* dy, const void* d, void* dz, float* gb, float* partials) {
+hipError_t launch_gated_backward(hipStream_t s, int elt, int M, int N, const void* dy, const void* d, const uint8_t* fine, void* dz, float* gb,
+                                 float* partials) {
   const int V = elt == ELT_BF16 ? 8 : 4;
   const ColsumShape cs = colsum_shape(M, N, V);
   const dim3 g1(cs.col_blocks, cs.chunks);
   const bool vec = N % V == 0 && (((uintptr_t)d | (uintptr_t)dz) & 15) == 0 && ((uintptr_t)dy & 7) == 0;
 #define TP_GATED(T, VEC)                                                                                                    \
-  hipLaunchKernelGGL((gated_backward_kernel<T, VEC>), g1, dim3(kThreads), 0, s, M, N, cs, (const T*)dy, (const T*)d, (T*)dz, partials)
+  hipLaunchKernelGGL((gated_backward_kernel<T, VEC>), g1, dim3(kThreads), 0, s, M, N, cs, (const T*)dy, (const T*)d, fine, (T*)dz, \
+                     partials)
   if (elt == ELT_BF16) {
     if (vec) TP_GATED(uint16_t, true); else TP_GATED(uint16_t, false);
   } else {

@@ -877,11 +877,11 @@ hipError_t mfma_fprop(hipStream_t s, int M, int N, int K, const uint16_t* x, con
 }
 
 hipError_t mfma_gated_fprop(hipStream_t s, int M, int N, int K, const uint16_t* x, const uint16_t* W, const float* bias, int act,
-                            uint16_t* d_out, uint16_t* a_out, uint16_t* x_copy, int spread) {
+                            uint16_t* d_out, uint8_t* fine, uint16_t* a_out, uint16_t* x_copy, int spread) {
   FpropInput in;
   const hipError_t err = fprop_input(s, M, N, K, x, W, x_copy, &in);
   if (err != hipSuccess) return err;
-  return fprop_product(s, M, N, K, in, W, EpiGated{bias, d_out, a_out, act, N, store_width(d_out, a_out)}, spread);
+  return fprop_product(s, M, N, K, in, W, EpiGated{bias, d_out, fine, a_out, act, N, store_width(d_out, a_out)}, spread);
 }
 
 int mfma_dgrad_sum_rows(int M, int K) {

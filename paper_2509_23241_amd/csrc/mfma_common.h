@@ -110,10 +110,10 @@ using EpiFprop = EpiFpropT<false>;
 using EpiFpropAdd = EpiFpropT<true>;
 using EpiFpropExact = EpiFpropT<false, true>;
 // A gated layer: columns 2f and 2f + 1 of the product are the gate and the other factor of output f, so that a lane's neighbouring columns
-// hold both and whichever tile a kernel has needs no exchange between lanes.  d_out [M x ldc]: what dy[f] is multiplied with for either
-// column; a_out [M x ldc / 2].
+// hold both and whichever tile a kernel has needs no exchange between lanes.  d_out [M x ldc] and fine [M x ldc / 2]: what dy[f] is
+// multiplied with for either column, to 12 bits (split12 in device_utils.h); a_out [M x ldc / 2].
 struct EpiGated {
-  const float* bias; uint16_t* d_out; uint16_t* a_out; int act; int ldc;
+  const float* bias; uint16_t* d_out; uint8_t* fine; uint16_t* a_out; int act; int ldc;
   int wide = 2;  // alignment of the outputs, as above
   static constexpr bool kSwap = true, kSums = false;
   struct Cols { float4 b0, b1; };
@@ -122,18 +122,20 @@ struct EpiGated {
   }
   __device__ __forceinline__ bool has_rows() const { return false; }
   __device__ __forceinline__ uint4 row_in(int, int) const { return make_uint4(0, 0, 0, 0); }
-  // the outputs of F pairs of columns and their factors, packed
+  // the outputs of F pairs of columns and their factors, packed, whose further bits are F bytes
   template <int F>
-  __device__ __forceinline__ void pairs(const float (&z)[2 * F], uint32_t (&d)[F], float (&a)[F]) const {
+  __device__ __forceinline__ uint32_t pairs(const float (&z)[2 * F], uint32_t (&d)[F], float (&a)[F]) const {
     float gate[F], slope[F];
 #pragma unroll
     for (int f = 0; f < F; ++f) gate[f] = z[2 * f];
     gate_pairs<false>(gate, act, a, slope);
+    uint32_t low = 0;
 #pragma unroll
     for (int f = 0; f < F; ++f) {
-      d[f] = pack_bf16x2(z[2 * f + 1] * slope[f], a[f]);
+      low |= split12(z[2 * f + 1] * slope[f], a[f], d[f]) << (8 * f);
       a[f] *= z[2 * f + 1];
     }
+    return low;
   }
   __device__ __forceinline__ uint4 row8(int m, int n, float (&v)[8], const Cols& c, const uint4&) const {
     const float b[8] = {c.b0.x, c.b0.y, c.b0.z, c.b0.w, c.b1.x, c.b1.y, c.b1.z, c.b1.w};
@@ -141,11 +143,12 @@ struct EpiGated {
     for (int j = 0; j < 8; ++j) v[j] += b[j];
     uint32_t d[4];
     float a[4];
-    pairs<4>(v, d, a);
+    const uint32_t low = pairs<4>(v, d, a);
     const size_t i = (size_t)m * ldc + n;
     const uint4 o = make_uint4(d[0], d[1], d[2], d[3]);
     *reinterpret_cast<uint4*>(d_out + i) = o;
     *reinterpret_cast<uint2*>(a_out + i / 2) = make_uint2(pack_bf16x2(a[0], a[1]), pack_bf16x2(a[2], a[3]));
+    *reinterpret_cast<uint32_t*>(fine + i / 2) = low;
     return o;
   }
   // count: 2 or 4
@@ -155,15 +158,17 @@ struct EpiGated {
     const float z[4] = {v0 + bias[n], v1 + bias[n + 1], v2 + bias[both ? n + 2 : n], v3 + bias[both ? n + 3 : n]};
     uint32_t d[2];
     float a[2];
-    pairs<2>(z, d, a);
+    const uint32_t low = pairs<2>(z, d, a);
     if (both && (ldc & 3) == 0 && wide) {
       *reinterpret_cast<uint2*>(d_out + i) = make_uint2(d[0], d[1]);
       *reinterpret_cast<uint32_t*>(a_out + i / 2) = pack_bf16x2(a[0], a[1]);
+      *reinterpret_cast<uint16_t*>(fine + i / 2) = (uint16_t)low;
     } else {
       for (int f = 0; f < count / 2; ++f) {
         d_out[i + 2 * f] = (uint16_t)d[f];
         d_out[i + 2 * f + 1] = (uint16_t)(d[f] >> 16);
         a_out[i / 2 + f] = float_to_bf16(a[f]);
+        fine[i / 2 + f] = (uint8_t)(low >> (8 * f));
       }
     }
   }

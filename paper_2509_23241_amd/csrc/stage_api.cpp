@@ -61,6 +61,7 @@ struct LayerPlan {
   int skip_layer = -1;             // residual add: index of the layer that remembered the skip activation
   DeferredNeed need;
   uint64_t pair_off = UINT64_MAX;  // gated: what the backward pass multiplies with, [rows x 2 outputs]
+  uint64_t fine_off = UINT64_MAX;  // and in bf16 four more bits of each, [rows x outputs] bytes
   bool in_place = false;           // rotary: input and output are one tensor
   tp::RotarySpeeds speeds;         // rotary
   bool relu_out = false;           // ReLU whose derivative is read off its saved OUTPUT (the next layer's input): no act' tensor
@@ -501,6 +502,10 @@ int make_plan(const tp_stage_desc* d, Plan* p) {
       lp.relu_out = false;
       lp.pair_off = act;
       act += round_up(rows * 2 * lp.out_elems * p->elt_size, 256);
+      if (d->dtype == TP_BF16) {
+        lp.fine_off = act;
+        act += round_up(rows * lp.out_elems, 256);
+      }
       max_feat = std::max<uint64_t>(max_feat, 2 * lp.out_elems);
       lp.z_off = UINT64_MAX;
     } else if (L.act != TP_ACT_NONE && !lp.relu_out) {
@@ -1135,8 +1140,9 @@ int forward_impl(tp_stage* st, uint64_t mb_id, uint32_t ub_idx, uint32_t ubs, co
     }
     if (lp.d.type == TP_LAYER_GATED) {
       ProfScope ps(st, TP_K_FPROP);
+      uint8_t* fine = lp.fine_off == UINT64_MAX ? nullptr : (uint8_t*)aslot + lp.fine_off + row0 * lp.out_elems;
       HIP_TRY(tp::launch_gated_fprop(fs, d.dtype, mb * lp.tokens, product_columns(lp.d), lp.d.in_features, x_in, wcopy + lp.w_off * es,
-                                     master + lp.b_off, lp.d.act, aslot + lp.pair_off + row0 * 2 * lp.out_elems * es, a_out,
+                                     master + lp.b_off, lp.d.act, aslot + lp.pair_off + row0 * 2 * lp.out_elems * es, fine, a_out,
                                      need_copy ? x_saved : nullptr, spread));
       continue;
     }
@@ -1810,8 +1816,8 @@ int backward_impl(tp_stage* st, uint64_t mb_id, const void* dy_dev, void* dx_dev
         {
           ProfScope ps(st, TP_K_ACT_BWD);
           SumsDeferred later(sink);
-          HIP_TRY(tp::launch_gated_backward(st->stream, d.dtype, grad_rows, product_columns(lp.d), dz, aslot + lp.pair_off, dz2,
-                                            g + lp.b_off, hold(need.bias)));
+          HIP_TRY(tp::launch_gated_backward(st->stream, d.dtype, grad_rows, product_columns(lp.d), dz, aslot + lp.pair_off,
+                                            lp.fine_off == UINT64_MAX ? nullptr : (const uint8_t*)aslot + lp.fine_off, dz2, g + lp.b_off, hold(need.bias)));
         }
         bias_summed = true;
         dz = dz2;
