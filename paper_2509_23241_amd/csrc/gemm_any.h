@@ -14,6 +14,10 @@ hipError_t f32_gated_fprop(hipStream_t s, int M, int N, int K, const float* x, c
                            float* a_out, float* x_copy);  // launch_gated_fprop
 hipError_t f32_dgrad(hipStream_t s, int M, int N, int K, const float* dz, const float* Wb, const float* d_prev, float* out,
                      int relu_mask, float* sums = nullptr);  // sums: column sums of every 16 rows of `out`, [(M + 15) / 16][K]
+// The gated layer's (launch_gated_dgrad, launch_gated_wgrad), summed in parts
+hipError_t f32_gated_dgrad(hipStream_t s, int M, int N, int K, const float* dz, int ldz, const float* Wb, const float* d_prev, float* out,
+                           int relu_mask, float* sums);
+hipError_t f32_gated_wgrad(hipStream_t s, int M, int N, int K, const float* dz, int ldz, const float* x, float* gW, float* partial);
 // partial: scratch of f32_wgrad_splits(M, N, K) * N * K floats where that is more than one range, or null
 hipError_t f32_wgrad(hipStream_t s, int M, int N, int K, const float* dz, const float* x, float* gW, float* partial);
 int f32_wgrad_splits(int M, int N, int K);

@@ -31,10 +31,16 @@ bool fprop_add_supported(int elt, int M, int N, int K);
 // aligned) fine [M x F], four bits more of each value: rounded to bf16 they would add as much to the gradients' error as dz itself.
 hipError_t launch_gated_fprop(hipStream_t s, int elt, int M, int N, int K, const void* x, const void* W, const float* bias, int act,
                               void* d_out, uint8_t* fine, void* a_out, void* x_copy, int spread);
-// dz[2f] = dy[f] d[2f], dz[2f + 1] = dy[f] d[2f + 1], and gb = column sums of dz as stored; N = 2 F columns of dz.
+// dz[2f] = dy[f] d[2f], dz[2f + 1] = dy[f] d[2f + 1], and gb = column sums of dz as stored; N = 2 F columns of dz, whose rows are
+// gated_pitch(elt, N) values apart (fp32: the next multiple of four, with zeros behind the columns, so that rows start at 16 bytes).
 // partials: scratch of colsum_scratch_floats(M, N) floats.
 hipError_t launch_gated_backward(hipStream_t s, int elt, int M, int N, const void* dy, const void* d, const uint8_t* fine, void* dz, float* gb,
                                  float* partials);
+int gated_pitch(int elt, int N);
+// launch_dgrad and launch_wgrad on that dz.
+hipError_t launch_gated_dgrad(hipStream_t s, int elt, int M, int N, int K, const void* dz, const void* Wb, const void* d_prev, void* out,
+                              int relu_mask, float* sums, int* sum_rows);
+hipError_t launch_gated_wgrad(hipStream_t s, int elt, int M, int N, int K, const void* dz, const void* x, float* gW, float* partial);
 
 // out = (dz W_b) (.) d_prev   dz:[M x N] W_b:[N x K] d_prev:[M x K] saved act'(z), or null.
 hipError_t launch_dgrad(hipStream_t s, int elt, int M, int N, int K, const void* dz, const void* Wb,

@@ -147,7 +147,7 @@ __global__ __launch_bounds__(kThreads) void act_backward_colsum_kernel(int M, in
 template <typename T, bool VEC>
 __global__ __launch_bounds__(kThreads) void gated_backward_kernel(int M, int N, ColsumShape cs, const T* __restrict__ dy,
                                                                   const T* __restrict__ d, const uint8_t* __restrict__ fine,
-                                                                  T* __restrict__ dz, float* __restrict__ partials) {
+                                                                  T* __restrict__ dz, int ldz, float* __restrict__ partials) {
   constexpr int V = 16 / sizeof(T);
   __shared__ float sm[kThreads * V];
   const int lr = threadIdx.x % cs.lanes_per_row, rsub = threadIdx.x / cs.lanes_per_row;
@@ -185,17 +185,19 @@ __global__ __launch_bounds__(kThreads) void gated_backward_kernel(int M, int N, 
             s[j % V] += o;
           }
         }
-        *reinterpret_cast<uint4*>(dz + at) = make_uint4(ow[0], ow[1], ow[2], ow[3]);
+        *reinterpret_cast<uint4*>(dz + at) = make_uint4(ow[0], ow[1], ow[2], ow[3]);  // (ldz = N)
       }
     } else {
       for (int r = r0 + rsub; r < r1; r += cs.rows_per_iter)
         for (int j = 0; j < V; ++j)
-          if (col + j < N) {
+          if (col + j >= N) {
+            if (col + j < ldz) dz[(size_t)r * ldz + col + j] = 0;
+          } else {
             const size_t at = (size_t)r * N + col + j;
             float kept = to_float(d[at]);
             if constexpr (sizeof(T) == 2) kept = joined12(__float_as_uint(kept), (fine[at / 2] >> (4 * (j & 1))) & 15u);
             const T o = from_float<T>(to_float(dy[at / 2]) * kept);
-            dz[at] = o;
+            dz[(size_t)r * ldz + col + j] = o;
             s[j] += to_float(o);
           }
     }
@@ -355,6 +357,21 @@ hipError_t launch_gated_fprop(hipStream_t s, int elt, int M, int N, int K, const
                           (uint16_t*)x_copy, spread);
 }
 
+int gated_pitch(int elt, int N) { return elt == ELT_F32 ? (N + 3) / 4 * 4 : N; }
+
+hipError_t launch_gated_dgrad(hipStream_t s, int elt, int M, int N, int K, const void* dz, const void* Wb, const void* d_prev, void* out,
+                              int relu_mask, float* sums, int* sum_rows) {
+  if (elt == ELT_BF16) return launch_dgrad(s, elt, M, N, K, dz, Wb, d_prev, out, relu_mask, sums, sum_rows);
+  if (sums) *sum_rows = dgrad_sum_rows(elt, M, K);
+  return f32_gated_dgrad(s, M, N, K, (const float*)dz, gated_pitch(elt, N), (const float*)Wb, (const float*)d_prev, (float*)out, relu_mask,
+                         sums && *sum_rows ? sums : nullptr);
+}
+
+hipError_t launch_gated_wgrad(hipStream_t s, int elt, int M, int N, int K, const void* dz, const void* x, float* gW, float* partial) {
+  if (elt == ELT_BF16) return launch_wgrad(s, elt, M, N, K, dz, x, gW, partial);
+  return f32_gated_wgrad(s, M, N, K, (const float*)dz, gated_pitch(elt, N), (const float*)x, gW, partial);
+}
+
 hipError_t launch_gated_backward(hipStream_t s, int elt, int M, int N, const void* dy, const void* d, const uint8_t* fine, void* dz, float* gb,
                                  float* partials) {
   const int V = elt == ELT_BF16 ? 8 : 4;
@@ -363,7 +380,7 @@ hipError_t launch_gated_backward(hipStream_t s, int elt, int M, int N, const voi
   const bool vec = N % V == 0 && (((uintptr_t)d | (uintptr_t)dz) & 15) == 0 && ((uintptr_t)dy & 7) == 0;
 #define TP_GATED(T, VEC)                                                                                                    \
   hipLaunchKernelGGL((gated_backward_kernel<T, VEC>), g1, dim3(kThreads), 0, s, M, N, cs, (const T*)dy, (const T*)d, fine, (T*)dz, \
-                     partials)
+                     gated_pitch(elt, N), partials)
   if (elt == ELT_BF16) {
     if (vec) TP_GATED(uint16_t, true); else TP_GATED(uint16_t, false);
   } else {

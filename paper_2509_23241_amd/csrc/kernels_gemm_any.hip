@@ -480,43 +480,6 @@ struct EpiForward {
     finish(m, n, count, v, input(m, n, count));
   }
 };
-// A gated layer: see EpiGated of the bf16 kernels.
-struct EpiGatedF32 {
-  static constexpr int kPartK = 0;
-  static constexpr bool kSums = false;
-  const float* bias;
-  float *d_out, *a_out;
-  int act, ldc, vec;
-  __device__ __forceinline__ floatx4 input(int, int n, int count) const {
-    floatx4 b;
-#pragma unroll
-    for (int j = 0; j < 4; ++j) b[j] = bias[j < count ? n + j : n];
-    return b;
-  }
-  // count: 2 or 4
-  __device__ __forceinline__ void finish(int m, int n, int count, const floatx4& v, const floatx4& b) const {
-    const size_t i = (size_t)m * ldc + n;
-    const float gate[2] = {v[0] + b[0], v[2] + b[2]}, other[2] = {v[1] + b[1], v[3] + b[3]};
-    float a[2], slope[2];
-    gate_pairs<true>(gate, act, a, slope);
-    const float d[4] = {other[0] * slope[0], a[0], other[1] * slope[1], a[1]};
-    if (vec && count == 4) {
-      store4(d_out + i, d);
-      *reinterpret_cast<float2*>(a_out + i / 2) = make_float2(a[0] * other[0], a[1] * other[1]);
-    } else {
-#pragma unroll
-      for (int f = 0; f < 2; ++f)
-        if (2 * f < count) {
-          d_out[i + 2 * f] = d[2 * f];
-          d_out[i + 2 * f + 1] = d[2 * f + 1];
-          a_out[i / 2 + f] = a[f] * other[f];
-        }
-    }
-  }
-  __device__ __forceinline__ void quad(int m, int n, int count, const floatx4& v, int) const {
-    finish(m, n, count, v, input(m, n, count));
-  }
-};
 template <class T>
 struct EpiInputGrad {
   static constexpr int kPartK = 0;
@@ -587,6 +550,51 @@ struct EpiPartial {
 // of 32 x 32, 64 channels: 2.9e-7 -> 4.4e-7).
 struct EpiPartialPixels : EpiPartial {
   static constexpr int kPartK = 256;
+};
+// A gated layer: see EpiGated of the bf16 kernels.  Its three products are summed in parts of 256: nothing holds them to the single chains of
+// dense layers, and those are up to three times further off fp64 (one of 4096 terms 1.7e-6 of the norm, in parts 5e-7).
+constexpr int kGatedPart = 256;
+struct EpiGatedF32 {
+  static constexpr int kPartK = kGatedPart;
+  static constexpr bool kSums = false;
+  const float* bias;
+  float *d_out, *a_out;
+  int act, ldc, vec;
+  __device__ __forceinline__ floatx4 input(int, int n, int count) const {
+    floatx4 b;
+#pragma unroll
+    for (int j = 0; j < 4; ++j) b[j] = bias[j < count ? n + j : n];
+    return b;
+  }
+  // count: 2 or 4
+  __device__ __forceinline__ void finish(int m, int n, int count, const floatx4& v, const floatx4& b) const {
+    const size_t i = (size_t)m * ldc + n;
+    const float gate[2] = {v[0] + b[0], v[2] + b[2]}, other[2] = {v[1] + b[1], v[3] + b[3]};
+    float a[2], slope[2];
+    gate_pairs<true>(gate, act, a, slope);
+    const float d[4] = {other[0] * slope[0], a[0], other[1] * slope[1], a[1]};
+    if (vec && count == 4) {
+      store4(d_out + i, d);
+      *reinterpret_cast<float2*>(a_out + i / 2) = make_float2(a[0] * other[0], a[1] * other[1]);
+    } else {
+#pragma unroll
+      for (int f = 0; f < 2; ++f)
+        if (2 * f < count) {
+          d_out[i + 2 * f] = d[2 * f];
+          d_out[i + 2 * f + 1] = d[2 * f + 1];
+          a_out[i / 2 + f] = a[f] * other[f];
+        }
+    }
+  }
+  __device__ __forceinline__ void quad(int m, int n, int count, const floatx4& v, int) const {
+    finish(m, n, count, v, input(m, n, count));
+  }
+};
+struct EpiInputGradParts : EpiInputGrad<float> {
+  static constexpr int kPartK = kGatedPart;
+};
+struct EpiPartialParts : EpiPartial {
+  static constexpr int kPartK = kGatedPart;
 };
 // ---- the kernel --------------------------------------------------------------------------------
 // grid = (output tiles, contraction ranges of `per` k tiles each).  U k tiles are multiplied between two barriers; NS runs of U
@@ -745,7 +753,7 @@ __global__ __launch_bounds__(64 * WGM * WGN) void gemm_any_kernel(int M, int N, 
       const int n = n0 + wn + 16 * j + 4 * (lane >> 4);
       if constexpr (Epi::kSums) {
         floatx4 o = {0.f, 0.f, 0.f, 0.f};
-        if (m < M && n < N) o = epi.quad(m, n, min(4, N - n), acc[i][j], blockIdx.y);
+        if (m < M && n < N) o = epi.quad(m, n, min(4, N - n), kPart > 0 ? parts[i][j] : acc[i][j], blockIdx.y);
         if (epi.sums) epi.store_sums(m, n, M, N, o);
       } else {
         if (m < M && n < N) epi.quad(m, n, min(4, N - n), kPart > 0 ? parts[i][j] : acc[i][j], blockIdx.y);
@@ -931,9 +939,19 @@ __global__ __launch_bounds__(64) void gemm_f32_wave_kernel(int M, int N, int KT,
       }
     }, std::make_integer_sequence<int, NS>{});
   };
+  // parts, where the epilogue wants them, are the tiles of one turn over the stages
+  static_assert(Epi::kPartK == 0 || Epi::kPartK == NS * 32, "a part is one turn");
+  floatx4 parts = {0.f, 0.f, 0.f, 0.f};
   int t0 = -skip;
-  for (; t0 + NS < KT; t0 += NS) all_stages(t0, std::false_type{});
+  for (; t0 + NS < KT; t0 += NS) {
+    all_stages(t0, std::false_type{});
+    if constexpr (Epi::kPartK > 0) {
+      parts += acc;
+      acc = floatx4{0.f, 0.f, 0.f, 0.f};
+    }
+  }
   all_stages(t0, std::true_type{});
+  if constexpr (Epi::kPartK > 0) acc += parts;
   if constexpr (Epi::kSums) {
     floatx4 o = {0.f, 0.f, 0.f, 0.f};
     if (m < M && n < N) o = epi.finish(m, n, min(4, N - n), acc, input);
@@ -1139,31 +1157,55 @@ hipError_t f32_gated_fprop(hipStream_t s, int M, int N, int K, const float* x, c
   return f32_product(s, M, N, K, x, W, x_copy, EpiGatedF32{bias, d_out, a_out, act, N, N % 4 == 0 && aligned16(d_out, a_out)});
 }
 
+namespace {
+// ldz: values from one row of dz to the next; those behind a row's N hold zeros up to a multiple of four, if ldz is one
+template <class Epi>
+hipError_t f32_dgrad_product(hipStream_t s, int M, int N, int K, const float* dz, int ldz, const float* Wb, const Epi& e) {
+  // out[M x K] = dz[M x N] . Wb[N x K]: contraction over N
+  const DenseDesc a{dz, ldz, M, N}, b{Wb, K, K, N};
+  if (K % 4 == 0 && aligned16(dz, Wb) && wave_ok(M, K, N, std::max(ldz, K)))
+    return launch_wave<WaveRow, WaveCol>(s, M, K, N, dz, ldz, Wb, K, e);
+  if (whole_tiles(N, std::max(ldz, K)) && K % 4 == 0 && aligned16(dz, Wb)) return run<float, Chain, DgradDenseWhole, 4>(s, M, K, N, a, b, e);
+  if (ldz % 4 == 0 && K % 4 == 0 && aligned16(dz, Wb)) return run<float, Chain, DgradDense, 4>(s, M, K, N, a, b, e);
+  return run<float, Chain, DgradDense, 1>(s, M, K, N, a, b, e);
+}
+template <class Epi>
+hipError_t f32_wgrad_product(hipStream_t s, int M, int N, int K, const float* dz, int ldz, const float* x, const Epi& e, bool split) {
+  // gW[N x K] = dz^T[N x M] . x[M x K]: contraction over M
+  const bool chunks = ldz % 4 == 0 && K % 4 == 0 && aligned16(dz, x);
+  const DenseDesc a{dz, ldz, chunks ? (N + 3) / 4 * 4 : N, M}, b{x, K, K, M};
+  if (chunks && whole_tiles(M, std::max(ldz, K))) return run<float, Chain, WgradDenseWhole, 4>(s, N, K, M, a, b, e, split);
+  if (chunks) return run<float, Chain, WgradDense, 4>(s, N, K, M, a, b, e, split);
+  return run<float, Chain, WgradDense, 1>(s, N, K, M, a, b, e, split);
+}
+}  // namespace
+
 hipError_t f32_dgrad(hipStream_t s, int M, int N, int K, const float* dz, const float* Wb, const float* d_prev, float* out,
                      int relu_mask, float* sums) {
-  // out[M x K] = dz[M x N] . Wb[N x K]: contraction over N
-  const DenseDesc a{dz, N, M, N}, b{Wb, K, K, N};
-  const EpiInputGrad<float> e{d_prev, out, K, relu_mask, K % 4 == 0 && aligned16(out), sums};
-  if (K % 4 == 0 && aligned16(dz, Wb) && wave_ok(M, K, N, std::max(N, K)))
-    return launch_wave<WaveRow, WaveCol>(s, M, K, N, dz, N, Wb, K, e);
-  if (whole_tiles(N, std::max(N, K)) && K % 4 == 0 && aligned16(dz, Wb)) return run<float, Chain, DgradDenseWhole, 4>(s, M, K, N, a, b, e);
-  if (N % 4 == 0 && K % 4 == 0 && aligned16(dz, Wb)) return run<float, Chain, DgradDense, 4>(s, M, K, N, a, b, e);
-  return run<float, Chain, DgradDense, 1>(s, M, K, N, a, b, e);
+  return f32_dgrad_product(s, M, N, K, dz, N, Wb, EpiInputGrad<float>{d_prev, out, K, relu_mask, K % 4 == 0 && aligned16(out), sums});
+}
+
+hipError_t f32_gated_dgrad(hipStream_t s, int M, int N, int K, const float* dz, int ldz, const float* Wb, const float* d_prev, float* out,
+                           int relu_mask, float* sums) {
+  return f32_dgrad_product(s, M, N, K, dz, ldz, Wb, EpiInputGradParts{{d_prev, out, K, relu_mask, K % 4 == 0 && aligned16(out), sums}});
 }
 
 int f32_wgrad_splits(int M, int N, int K) { return ranges_of<float, Chain>(N, K, M); }
 
 hipError_t f32_wgrad(hipStream_t s, int M, int N, int K, const float* dz, const float* x, float* gW, float* partial) {
-  // gW[N x K] = dz^T[N x M] . x[M x K]: contraction over M
-  const bool split = partial != nullptr;
-  const int splits = split ? f32_wgrad_splits(M, N, K) : 1;
-  const DenseDesc a{dz, N, N, M}, b{x, K, K, M};
+  const int splits = partial != nullptr ? f32_wgrad_splits(M, N, K) : 1;
   float* out = splits > 1 ? partial : gW;
   const EpiPartial e{out, K, K % 4 == 0 && aligned16(out), (size_t)N * K};
-  const bool chunks = N % 4 == 0 && K % 4 == 0 && aligned16(dz, x);
-  const hipError_t err = chunks && whole_tiles(M, std::max(N, K)) ? run<float, Chain, WgradDenseWhole, 4>(s, N, K, M, a, b, e, split)
-                         : chunks                                ? run<float, Chain, WgradDense, 4>(s, N, K, M, a, b, e, split)
-                                                                 : run<float, Chain, WgradDense, 1>(s, N, K, M, a, b, e, split);
+  const hipError_t err = f32_wgrad_product(s, M, N, K, dz, N, x, e, partial != nullptr);
+  if (err != hipSuccess || splits == 1) return err;
+  return launch_sum_partials(s, (size_t)N * K, splits, partial, gW);
+}
+
+hipError_t f32_gated_wgrad(hipStream_t s, int M, int N, int K, const float* dz, int ldz, const float* x, float* gW, float* partial) {
+  const int splits = partial != nullptr ? f32_wgrad_splits(M, N, K) : 1;
+  float* out = splits > 1 ? partial : gW;
+  const EpiPartialParts e{{out, K, K % 4 == 0 && aligned16(out), (size_t)N * K}};
+  const hipError_t err = f32_wgrad_product(s, M, N, K, dz, ldz, x, e, partial != nullptr);
   if (err != hipSuccess || splits == 1) return err;
   return launch_sum_partials(s, (size_t)N * K, splits, partial, gW);
 }

@@ -506,7 +506,7 @@ int make_plan(const tp_stage_desc* d, Plan* p) {
         lp.fine_off = act;
         act += round_up(rows * lp.out_elems, 256);
       }
-      max_feat = std::max<uint64_t>(max_feat, 2 * lp.out_elems);
+      max_feat = std::max<uint64_t>(max_feat, (uint64_t)lp.tokens * tp::gated_pitch(d->dtype, product_columns(L)));
       lp.z_off = UINT64_MAX;
     } else if (L.act != TP_ACT_NONE && !lp.relu_out) {
       lp.z_off = act;
@@ -1835,8 +1835,11 @@ int backward_impl(tp_stage* st, uint64_t mb_id, const void* dy_dev, void* dx_dev
         ProfScope ps(st, TP_K_WGRAD);
         SumsDeferred later(sink);
         float* part = hold(need.weight);
-        if (lp.d.type == TP_LAYER_DENSE || lp.d.type == TP_LAYER_GATED)
-          HIP_TRY(tp::launch_wgrad(st->stream, d.dtype, grad_rows, product_columns(lp.d), lp.d.in_features, dz, aslot + lp.x_off,
+        if (lp.d.type == TP_LAYER_GATED)
+          HIP_TRY(tp::launch_gated_wgrad(st->stream, d.dtype, grad_rows, product_columns(lp.d), lp.d.in_features, dz, aslot + lp.x_off,
+                                         g + lp.w_off, part));
+        else if (lp.d.type == TP_LAYER_DENSE)
+          HIP_TRY(tp::launch_wgrad(st->stream, d.dtype, grad_rows, lp.d.out_features, lp.d.in_features, dz, aslot + lp.x_off,
                                    g + lp.w_off, part));
         else if (lp.xpad_off != UINT64_MAX && lp.d.geom[2] == 7)
           HIP_TRY(tp::conv_stem_wgrad(st->stream, rows, lp.d.geom[0], lp.d.geom[1], lp.d.in_features, lp.d.out_features,
@@ -1854,8 +1857,11 @@ int backward_impl(tp_stage* st, uint64_t mb_id, const void* dy_dev, void* dx_dev
       if (no_dx) break;
       {
         ProfScope ps(st, TP_K_DGRAD);
-        if (lp.d.type == TP_LAYER_DENSE || lp.d.type == TP_LAYER_GATED)
-          HIP_TRY(tp::launch_dgrad(st->stream, d.dtype, grad_rows, product_columns(lp.d), lp.d.in_features, dz, wb + lp.w_off * es,
+        if (lp.d.type == TP_LAYER_GATED)
+          HIP_TRY(tp::launch_gated_dgrad(st->stream, d.dtype, grad_rows, product_columns(lp.d), lp.d.in_features, dz, wb + lp.w_off * es,
+                                         dprev, dst, dmask, bias_sums(), &bias_rows));
+        else if (lp.d.type == TP_LAYER_DENSE)
+          HIP_TRY(tp::launch_dgrad(st->stream, d.dtype, grad_rows, lp.d.out_features, lp.d.in_features, dz, wb + lp.w_off * es,
                                    dprev, dst, dmask, bias_sums(), &bias_rows));
         else
           HIP_TRY(tp::launch_conv_dgrad(st->stream, d.dtype, rows, lp.d.geom[0], lp.d.geom[1], lp.d.geom[2], lp.d.geom[3],
