@@ -27,7 +27,7 @@ hipError_t launch_fprop(hipStream_t s, int elt, int M, int N, int K, const void*
                         int spread = SPREAD_NONE);
 bool fprop_add_supported(int elt, int M, int N, int K);
 // A gated layer's forward product, z = x W^T + bias over N = 2 F columns, those of output f being 2f and 2f + 1: a[f] = act(z[2f]) z[2f+1]
-// into a_out [M x F]; what dy[f] is multiplied with to give the gradients of z[2f] and z[2f + 1] into d_out [M x N] and (bf16, 4-byte
+// into a_out [M x F]; what dy[f] is multiplied with to give the gradients of z[2f] and z[2f + 1] into d_out [M x gated_pitch(elt, N)] and (bf16, 4-byte
 // aligned) fine [M x F], four bits more of each value: rounded to bf16 they would add as much to the gradients' error as dz itself.
 hipError_t launch_gated_fprop(hipStream_t s, int elt, int M, int N, int K, const void* x, const void* W, const float* bias, int act,
                               void* d_out, uint8_t* fine, void* a_out, void* x_copy, int spread);

@@ -143,7 +143,8 @@ __global__ __launch_bounds__(kThreads) void act_backward_colsum_kernel(int M, in
 }
 
 // The backward pass of a gated layer ahead of its products, with the structure of the kernel above over N = 2 F columns: dz of columns 2f
-// and 2f + 1 is dy[f] times what the forward pass kept there.  VEC: rows of whole 16-byte units, dy of 8-byte ones, aligned so.
+// and 2f + 1 is dy[f] times what the forward pass kept there.  d and dz have rows of ldz values, zeros behind the columns of dz.  VEC: rows of whole
+// 16-byte units, aligned so, and in bf16 dy of 8-byte ones (in fp32 its values are fetched one by one).
 template <typename T, bool VEC>
 __global__ __launch_bounds__(kThreads) void gated_backward_kernel(int M, int N, ColsumShape cs, const T* __restrict__ dy,
                                                                   const T* __restrict__ d, const uint8_t* __restrict__ fine,
@@ -161,13 +162,13 @@ __global__ __launch_bounds__(kThreads) void gated_backward_kernel(int M, int N, 
     if constexpr (VEC) {
 #pragma unroll 4
       for (int r = r0 + rsub; r < r1; r += cs.rows_per_iter) {
-        const size_t at = (size_t)r * N + col;
-        const uint2 a = *reinterpret_cast<const uint2*>(dy + at / 2);
+        const size_t at = (size_t)r * ldz + col, from = ((size_t)r * N + col) / 2;
         const uint4 b = *reinterpret_cast<const uint4*>(d + at);
         const uint32_t bw[4] = {b.x, b.y, b.z, b.w};
         uint32_t ow[4];
         if constexpr (sizeof(T) == 2) {
-          const uint32_t low = *reinterpret_cast<const uint32_t*>(fine + at / 2);
+          const uint2 a = *reinterpret_cast<const uint2*>(dy + from);
+          const uint32_t low = *reinterpret_cast<const uint32_t*>(fine + from);
           const float g[4] = {__uint_as_float(a.x << 16), __uint_as_float(a.x & 0xffff0000u), __uint_as_float(a.y << 16),
                               __uint_as_float(a.y & 0xffff0000u)};
 #pragma unroll
@@ -177,27 +178,28 @@ __global__ __launch_bounds__(kThreads) void gated_backward_kernel(int M, int N, 
             s[(2 * j + 1) % V] += __uint_as_float(ow[j] & 0xffff0000u);
           }
         } else {
-          const float g[2] = {__uint_as_float(a.x), __uint_as_float(a.y)};
+          const bool both = col + 2 < N;
+          const float g[2] = {to_float(dy[from]), to_float(dy[both ? from + 1 : from])};
 #pragma unroll
           for (int j = 0; j < 4; ++j) {
-            const float o = g[j / 2] * __uint_as_float(bw[j]);
+            const float o = j < 2 || both ? g[j / 2] * __uint_as_float(bw[j]) : 0.f;
             ow[j] = __float_as_uint(o);
             s[j % V] += o;
           }
         }
-        *reinterpret_cast<uint4*>(dz + at) = make_uint4(ow[0], ow[1], ow[2], ow[3]);  // (ldz = N)
+        *reinterpret_cast<uint4*>(dz + at) = make_uint4(ow[0], ow[1], ow[2], ow[3]);
       }
     } else {
       for (int r = r0 + rsub; r < r1; r += cs.rows_per_iter)
         for (int j = 0; j < V; ++j)
           if (col + j >= N) {
-            if (col + j < ldz) dz[(size_t)r * ldz + col + j] = 0;
+            if (col + j < ldz) dz[(size_t)r * ldz + col + j] = from_float<T>(0.f);
           } else {
-            const size_t at = (size_t)r * N + col + j;
+            const size_t at = (size_t)r * ldz + col + j, from = ((size_t)r * N + col + j) / 2;
             float kept = to_float(d[at]);
-            if constexpr (sizeof(T) == 2) kept = joined12(__float_as_uint(kept), (fine[at / 2] >> (4 * (j & 1))) & 15u);
-            const T o = from_float<T>(to_float(dy[at / 2]) * kept);
-            dz[(size_t)r * ldz + col + j] = o;
+            if constexpr (sizeof(T) == 2) kept = joined12(__float_as_uint(kept), (fine[from] >> (4 * (j & 1))) & 15u);
+            const T o = from_float<T>(to_float(dy[from]) * kept);
+            dz[at] = o;
             s[j] += to_float(o);
           }
     }
@@ -377,7 +379,7 @@ hipError_t launch_gated_backward(hipStream_t s, int elt, int M, int N, const voi
   const int V = elt == ELT_BF16 ? 8 : 4;
   const ColsumShape cs = colsum_shape(M, N, V);
   const dim3 g1(cs.col_blocks, cs.chunks);
-  const bool vec = N % V == 0 && (((uintptr_t)d | (uintptr_t)dz) & 15) == 0 && ((uintptr_t)dy & 7) == 0;
+  const bool vec = gated_pitch(elt, N) % V == 0 && (((uintptr_t)d | (uintptr_t)dz) & 15) == 0 && (elt == ELT_F32 || ((uintptr_t)dy & 7) == 0);
 #define TP_GATED(T, VEC)                                                                                                    \
   hipLaunchKernelGGL((gated_backward_kernel<T, VEC>), g1, dim3(kThreads), 0, s, M, N, cs, (const T*)dy, (const T*)d, fine, (T*)dz, \
                      gated_pitch(elt, N), partials)

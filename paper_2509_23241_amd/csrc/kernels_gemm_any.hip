@@ -552,14 +552,14 @@ struct EpiPartialPixels : EpiPartial {
   static constexpr int kPartK = 256;
 };
 // A gated layer: see EpiGated of the bf16 kernels.  Its three products are summed in parts of 256: nothing holds them to the single chains of
-// dense layers, and those are up to three times further off fp64 (one of 4096 terms 1.7e-6 of the norm, in parts 5e-7).
+// dense layers, whose rounding grows with their length (input gradient over 2730 columns 1.0e-6 of its norm off fp64, in parts 4.4e-7).
 constexpr int kGatedPart = 256;
 struct EpiGatedF32 {
   static constexpr int kPartK = kGatedPart;
   static constexpr bool kSums = false;
   const float* bias;
   float *d_out, *a_out;
-  int act, ldc, vec;
+  int act, ldc, ldd, vec;  // ldd: values from one row of d_out to the next, a multiple of four (vec: 16-byte aligned)
   __device__ __forceinline__ floatx4 input(int, int n, int count) const {
     floatx4 b;
 #pragma unroll
@@ -568,21 +568,22 @@ struct EpiGatedF32 {
   }
   // count: 2 or 4
   __device__ __forceinline__ void finish(int m, int n, int count, const floatx4& v, const floatx4& b) const {
-    const size_t i = (size_t)m * ldc + n;
+    const size_t i = (size_t)m * ldd + n, o = ((size_t)m * ldc + n) / 2;
     const float gate[2] = {v[0] + b[0], v[2] + b[2]}, other[2] = {v[1] + b[1], v[3] + b[3]};
     float a[2], slope[2];
     gate_pairs<true>(gate, act, a, slope);
     const float d[4] = {other[0] * slope[0], a[0], other[1] * slope[1], a[1]};
     if (vec && count == 4) {
       store4(d_out + i, d);
-      *reinterpret_cast<float2*>(a_out + i / 2) = make_float2(a[0] * other[0], a[1] * other[1]);
+      a_out[o] = a[0] * other[0];
+      a_out[o + 1] = a[1] * other[1];
     } else {
 #pragma unroll
       for (int f = 0; f < 2; ++f)
         if (2 * f < count) {
           d_out[i + 2 * f] = d[2 * f];
           d_out[i + 2 * f + 1] = d[2 * f + 1];
-          a_out[i / 2 + f] = a[f] * other[f];
+          a_out[o + f] = a[f] * other[f];
         }
     }
   }
@@ -1154,7 +1155,7 @@ hipError_t f32_fprop(hipStream_t s, int M, int N, int K, const float* x, const f
 
 hipError_t f32_gated_fprop(hipStream_t s, int M, int N, int K, const float* x, const float* W, const float* bias, int act, float* d_out,
                            float* a_out, float* x_copy) {
-  return f32_product(s, M, N, K, x, W, x_copy, EpiGatedF32{bias, d_out, a_out, act, N, N % 4 == 0 && aligned16(d_out, a_out)});
+  return f32_product(s, M, N, K, x, W, x_copy, EpiGatedF32{bias, d_out, a_out, act, N, (N + 3) / 4 * 4, aligned16(d_out)});
 }
 
 namespace {

@@ -60,7 +60,8 @@ struct LayerPlan {
   int tokens = 1;                  // positions per sample (rows of the layer's matrices per sample)
   int skip_layer = -1;             // residual add: index of the layer that remembered the skip activation
   DeferredNeed need;
-  uint64_t pair_off = UINT64_MAX;  // gated: what the backward pass multiplies with, [rows x 2 outputs]
+  uint64_t pair_off = UINT64_MAX;  // gated: what the backward pass multiplies with, two values for each output
+  uint64_t pair_elems = 0;         // values per sample there
   uint64_t fine_off = UINT64_MAX;  // and in bf16 four more bits of each, [rows x outputs] bytes
   bool in_place = false;           // rotary: input and output are one tensor
   tp::RotarySpeeds speeds;         // rotary
@@ -501,12 +502,13 @@ int make_plan(const tp_stage_desc* d, Plan* p) {
     if (L.type == TP_LAYER_GATED) {
       lp.relu_out = false;
       lp.pair_off = act;
-      act += round_up(rows * 2 * lp.out_elems * p->elt_size, 256);
+      lp.pair_elems = (uint64_t)lp.tokens * tp::gated_pitch(d->dtype, product_columns(L));
+      act += round_up(rows * lp.pair_elems * p->elt_size, 256);
       if (d->dtype == TP_BF16) {
         lp.fine_off = act;
         act += round_up(rows * lp.out_elems, 256);
       }
-      max_feat = std::max<uint64_t>(max_feat, (uint64_t)lp.tokens * tp::gated_pitch(d->dtype, product_columns(L)));
+      max_feat = std::max<uint64_t>(max_feat, lp.pair_elems);
       lp.z_off = UINT64_MAX;
     } else if (L.act != TP_ACT_NONE && !lp.relu_out) {
       lp.z_off = act;
@@ -1142,7 +1144,7 @@ int forward_impl(tp_stage* st, uint64_t mb_id, uint32_t ub_idx, uint32_t ubs, co
       ProfScope ps(st, TP_K_FPROP);
       uint8_t* fine = lp.fine_off == UINT64_MAX ? nullptr : (uint8_t*)aslot + lp.fine_off + row0 * lp.out_elems;
       HIP_TRY(tp::launch_gated_fprop(fs, d.dtype, mb * lp.tokens, product_columns(lp.d), lp.d.in_features, x_in, wcopy + lp.w_off * es,
-                                     master + lp.b_off, lp.d.act, aslot + lp.pair_off + row0 * 2 * lp.out_elems * es, fine, a_out,
+                                     master + lp.b_off, lp.d.act, aslot + lp.pair_off + row0 * lp.pair_elems * es, fine, a_out,
                                      need_copy ? x_saved : nullptr, spread));
       continue;
     }
