@@ -16,6 +16,16 @@ hipError_t mfma_fprop(hipStream_t s, int M, int N, int K, const uint16_t* x, con
 // A gated layer's, N = 2 outputs (launch_gated_fprop).
 hipError_t mfma_gated_fprop(hipStream_t s, int M, int N, int K, const uint16_t* x, const uint16_t* W, const float* bias, int act,
                             uint16_t* d_out, uint8_t* fine, uint16_t* a_out, uint16_t* x_copy, int spread);
+// Its gradients: dz of rows that are N rounded up to eight values apart, zeros behind them; ldw, ldx: K, or that rounded up to eight, zeros
+// behind the rows of x and anything behind those of Wb.  partial: scratch of .._scratch_floats(M, N, K) floats.
+hipError_t mfma_gated_dgrad(hipStream_t s, int M, int N, int K, const uint16_t* dz, const uint16_t* Wb, int ldw, const uint16_t* d_prev,
+                            uint16_t* out, int relu_mask, float* sums, int* sum_rows, float* partial);
+hipError_t mfma_gated_wgrad(hipStream_t s, int M, int N, int K, const uint16_t* dz, const uint16_t* x, int ldx, float* gW, float* partial);
+size_t mfma_gated_dgrad_scratch_floats(int M, int N, int K);
+size_t mfma_gated_wgrad_scratch_floats(int M, int N, int K);
+// Whether x and the weights are to be copied into rows of K rounded up to eight values, and that copy.
+bool mfma_gated_padded(int M, int N, int K);
+hipError_t mfma_pad_rows(hipStream_t s, size_t rows, int cols, const uint16_t* src, uint16_t* dst);
 // out = (dz Wb) (.) d_prev, d_prev = saved act'(z) of the previous layer or null; relu_mask = 1: d_prev holds that layer's
 // ReLU output instead and the factor is (output > 0).
 hipError_t mfma_dgrad(hipStream_t s, int M, int N, int K, const uint16_t* dz, const uint16_t* Wb,

@@ -27,20 +27,27 @@ hipError_t launch_fprop(hipStream_t s, int elt, int M, int N, int K, const void*
                         int spread = SPREAD_NONE);
 bool fprop_add_supported(int elt, int M, int N, int K);
 // A gated layer's forward product, z = x W^T + bias over N = 2 F columns, those of output f being 2f and 2f + 1: a[f] = act(z[2f]) z[2f+1]
-// into a_out [M x F]; what dy[f] is multiplied with to give the gradients of z[2f] and z[2f + 1] into d_out [M x gated_pitch(elt, N)] and (bf16, 4-byte
-// aligned) fine [M x F], four bits more of each value: rounded to bf16 they would add as much to the gradients' error as dz itself.
+// into a_out [M x F]; what dy[f] is multiplied with to give the gradients of z[2f] and z[2f + 1] into d_out [M x gated_pitch(elt, N)] and (bf16)
+// fine [M x F], four bits more of each value: rounded to bf16 they would add as much to the gradients' error as dz itself.
+// x_pad, w_pad: where gated_padded, room for M and for N rows of gated_pitch(elt, K) values, else null.  x_pad is kept for the backward pass.
 hipError_t launch_gated_fprop(hipStream_t s, int elt, int M, int N, int K, const void* x, const void* W, const float* bias, int act,
-                              void* d_out, uint8_t* fine, void* a_out, void* x_copy, int spread);
+                              void* d_out, uint8_t* fine, void* a_out, void* x_copy, int spread, void* x_pad, void* w_pad);
+// Values from one row to the next of tensors of n columns that start each at 16 bytes.
+int gated_pitch(int elt, int n);
+// M: rows of the whole mini-batch
+bool gated_padded(int elt, int M, int N, int K);
 // dz[2f] = dy[f] d[2f], dz[2f + 1] = dy[f] d[2f + 1], and gb = column sums of dz as stored; N = 2 F columns of dz, whose rows are
-// gated_pitch(elt, N) values apart (fp32: the next multiple of four, with zeros behind the columns, so that rows start at 16 bytes).
+// gated_pitch(elt, N) values apart with zeros behind the columns.
 // partials: scratch of colsum_scratch_floats(M, N) floats.
 hipError_t launch_gated_backward(hipStream_t s, int elt, int M, int N, const void* dy, const void* d, const uint8_t* fine, void* dz, float* gb,
                                  float* partials);
-int gated_pitch(int elt, int N);
-// launch_dgrad and launch_wgrad on that dz.
-hipError_t launch_gated_dgrad(hipStream_t s, int elt, int M, int N, int K, const void* dz, const void* Wb, const void* d_prev, void* out,
-                              int relu_mask, float* sums, int* sum_rows);
-hipError_t launch_gated_wgrad(hipStream_t s, int elt, int M, int N, int K, const void* dz, const void* x, float* gW, float* partial);
+// launch_dgrad and launch_wgrad on that dz; partial: scratch of gated_.._scratch_floats floats.
+hipError_t launch_gated_dgrad(hipStream_t s, int elt, int M, int N, int K, const void* dz, const void* Wb, void* w_pad, const void* d_prev,
+                              void* out, int relu_mask, float* sums, int* sum_rows, float* partial);
+hipError_t launch_gated_wgrad(hipStream_t s, int elt, int M, int N, int K, const void* dz, const void* x, const void* x_pad, float* gW,
+                              float* partial);
+size_t gated_dgrad_scratch_floats(int elt, int M, int N, int K);
+size_t gated_wgrad_scratch_floats(int elt, int M, int N, int K);
 
 // out = (dz W_b) (.) d_prev   dz:[M x N] W_b:[N x K] d_prev:[M x K] saved act'(z), or null.
 hipError_t launch_dgrad(hipStream_t s, int elt, int M, int N, int K, const void* dz, const void* Wb,

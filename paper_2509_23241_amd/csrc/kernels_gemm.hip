@@ -143,12 +143,13 @@ __global__ __launch_bounds__(kThreads) void act_backward_colsum_kernel(int M, in
 }
 
 // The backward pass of a gated layer ahead of its products, with the structure of the kernel above over N = 2 F columns: dz of columns 2f
-// and 2f + 1 is dy[f] times what the forward pass kept there.  d and dz have rows of ldz values, zeros behind the columns of dz.  VEC: rows of whole
-// 16-byte units, aligned so, and in bf16 dy of 8-byte ones (in fp32 its values are fetched one by one).
-template <typename T, bool VEC>
+// and 2f + 1 is dy[f] times what the forward pass kept there.  d and dz have rows of `pitch` values, whole 16-byte units, zeros behind the
+// columns of dz; those of dy and `fine` start anywhere.  A unit takes 16 bytes of d, 8 of dy and in bf16 4 of `fine`, the last one of a row value by
+// value where it is not whole.  8192 x 16384 in bf16 (738 MB): 152 us, the rate of a copy.
+template <typename T>
 __global__ __launch_bounds__(kThreads) void gated_backward_kernel(int M, int N, ColsumShape cs, const T* __restrict__ dy,
                                                                   const T* __restrict__ d, const uint8_t* __restrict__ fine,
-                                                                  T* __restrict__ dz, int ldz, float* __restrict__ partials) {
+                                                                  T* __restrict__ dz, int pitch, float* __restrict__ partials) {
   constexpr int V = 16 / sizeof(T);
   __shared__ float sm[kThreads * V];
   const int lr = threadIdx.x % cs.lanes_per_row, rsub = threadIdx.x / cs.lanes_per_row;
@@ -158,51 +159,50 @@ __global__ __launch_bounds__(kThreads) void gated_backward_kernel(int M, int N, 
   float s[V];
 #pragma unroll
   for (int j = 0; j < V; ++j) s[j] = 0.f;
-  if (col < N) {
-    if constexpr (VEC) {
+  if (col + V <= N) {
 #pragma unroll 4
-      for (int r = r0 + rsub; r < r1; r += cs.rows_per_iter) {
-        const size_t at = (size_t)r * ldz + col, from = ((size_t)r * N + col) / 2;
-        const uint4 b = *reinterpret_cast<const uint4*>(d + at);
-        const uint32_t bw[4] = {b.x, b.y, b.z, b.w};
-        uint32_t ow[4];
-        if constexpr (sizeof(T) == 2) {
-          const uint2 a = *reinterpret_cast<const uint2*>(dy + from);
-          const uint32_t low = *reinterpret_cast<const uint32_t*>(fine + from);
-          const float g[4] = {__uint_as_float(a.x << 16), __uint_as_float(a.x & 0xffff0000u), __uint_as_float(a.y << 16),
-                              __uint_as_float(a.y & 0xffff0000u)};
+    for (int r = r0 + rsub; r < r1; r += cs.rows_per_iter) {
+      const size_t at = (size_t)r * pitch + col, from = ((size_t)r * N + col) / 2;
+      const uint4 b = *reinterpret_cast<const uint4*>(d + at);
+      uint2 a;
+      __builtin_memcpy(&a, dy + from, 8);
+      const uint32_t bw[4] = {b.x, b.y, b.z, b.w};
+      uint32_t ow[4];
+      if constexpr (sizeof(T) == 2) {
+        uint32_t low;
+        __builtin_memcpy(&low, fine + from, 4);
+        const float g[4] = {__uint_as_float(a.x << 16), __uint_as_float(a.x & 0xffff0000u), __uint_as_float(a.y << 16),
+                            __uint_as_float(a.y & 0xffff0000u)};
 #pragma unroll
-          for (int j = 0; j < 4; ++j) {
-            ow[j] = pack_bf16x2(g[j] * joined12(bw[j] << 16, (low >> (8 * j)) & 15u), g[j] * joined12(bw[j] & 0xffff0000u, (low >> (8 * j + 4)) & 15u));
-            s[(2 * j) % V] += __uint_as_float(ow[j] << 16);
-            s[(2 * j + 1) % V] += __uint_as_float(ow[j] & 0xffff0000u);
-          }
-        } else {
-          const bool both = col + 2 < N;
-          const float g[2] = {to_float(dy[from]), to_float(dy[both ? from + 1 : from])};
-#pragma unroll
-          for (int j = 0; j < 4; ++j) {
-            const float o = j < 2 || both ? g[j / 2] * __uint_as_float(bw[j]) : 0.f;
-            ow[j] = __float_as_uint(o);
-            s[j % V] += o;
-          }
+        for (int j = 0; j < 4; ++j) {
+          ow[j] = pack_bf16x2(g[j] * joined12(bw[j] << 16, (low >> (8 * j)) & 15u), g[j] * joined12(bw[j] & 0xffff0000u, (low >> (8 * j + 4)) & 15u));
+          s[(2 * j) % V] += __uint_as_float(ow[j] << 16);
+          s[(2 * j + 1) % V] += __uint_as_float(ow[j] & 0xffff0000u);
         }
-        *reinterpret_cast<uint4*>(dz + at) = make_uint4(ow[0], ow[1], ow[2], ow[3]);
+      } else {
+        const float g[2] = {__uint_as_float(a.x), __uint_as_float(a.y)};
+#pragma unroll
+        for (int j = 0; j < 4; ++j) {
+          const float o = g[j / 2] * __uint_as_float(bw[j]);
+          ow[j] = __float_as_uint(o);
+          s[j % V] += o;
+        }
       }
-    } else {
-      for (int r = r0 + rsub; r < r1; r += cs.rows_per_iter)
-        for (int j = 0; j < V; ++j)
-          if (col + j >= N) {
-            if (col + j < ldz) dz[(size_t)r * ldz + col + j] = from_float<T>(0.f);
-          } else {
-            const size_t at = (size_t)r * ldz + col + j, from = ((size_t)r * N + col + j) / 2;
-            float kept = to_float(d[at]);
-            if constexpr (sizeof(T) == 2) kept = joined12(__float_as_uint(kept), (fine[from] >> (4 * (j & 1))) & 15u);
-            const T o = from_float<T>(to_float(dy[from]) * kept);
-            dz[at] = o;
-            s[j] += to_float(o);
-          }
+      *reinterpret_cast<uint4*>(dz + at) = make_uint4(ow[0], ow[1], ow[2], ow[3]);
     }
+  } else if (col < N) {
+    for (int r = r0 + rsub; r < r1; r += cs.rows_per_iter)
+      for (int j = 0; j < V; ++j) {
+        const size_t at = (size_t)r * pitch + col + j, from = ((size_t)r * N + col + j) / 2;
+        T o = from_float<T>(0.f);
+        if (col + j < N) {
+          float kept = to_float(d[at]);
+          if constexpr (sizeof(T) == 2) kept = joined12(__float_as_uint(kept), (fine[from] >> (4 * (j & 1))) & 15u);
+          o = from_float<T>(to_float(dy[from]) * kept);
+          s[j] += to_float(o);
+        }
+        dz[at] = o;
+      }
   }
 #pragma unroll
   for (int j = 0; j < V; ++j) sm[(rsub * cs.lanes_per_row + lr) * V + j] = s[j];
@@ -351,47 +351,71 @@ hipError_t launch_fprop(hipStream_t s, int elt, int M, int N, int K, const void*
                     (uint16_t*)x_copy, (const uint16_t*)addend, spread);
 }
 
+int gated_pitch(int elt, int n) { return elt == ELT_BF16 ? (n + 7) / 8 * 8 : (n + 3) / 4 * 4; }
+bool gated_padded(int elt, int M, int N, int K) { return elt == ELT_BF16 && mfma_gated_padded(M, N, K); }
+
 hipError_t launch_gated_fprop(hipStream_t s, int elt, int M, int N, int K, const void* x, const void* W, const float* bias, int act,
-                              void* d_out, uint8_t* fine, void* a_out, void* x_copy, int spread) {
+                              void* d_out, uint8_t* fine, void* a_out, void* x_copy, int spread, void* x_pad, void* w_pad) {
   if (elt == ELT_F32)
     return f32_gated_fprop(s, M, N, K, (const float*)x, (const float*)W, bias, act, (float*)d_out, (float*)a_out, (float*)x_copy);
+  if (x_pad) {
+    hipError_t err = x_copy ? launch_copy(s, x, x_copy, (size_t)M * K * 2) : hipSuccess;
+    if (err == hipSuccess) err = mfma_pad_rows(s, M, K, (const uint16_t*)x, (uint16_t*)x_pad);
+    if (err == hipSuccess) err = mfma_pad_rows(s, N, K, (const uint16_t*)W, (uint16_t*)w_pad);
+    if (err != hipSuccess) return err;
+    x = x_pad;
+    W = w_pad;
+    x_copy = nullptr;
+    K = gated_pitch(elt, K);
+  }
   return mfma_gated_fprop(s, M, N, K, (const uint16_t*)x, (const uint16_t*)W, bias, act, (uint16_t*)d_out, fine, (uint16_t*)a_out,
                           (uint16_t*)x_copy, spread);
 }
 
-int gated_pitch(int elt, int N) { return elt == ELT_F32 ? (N + 3) / 4 * 4 : N; }
-
-hipError_t launch_gated_dgrad(hipStream_t s, int elt, int M, int N, int K, const void* dz, const void* Wb, const void* d_prev, void* out,
-                              int relu_mask, float* sums, int* sum_rows) {
-  if (elt == ELT_BF16) return launch_dgrad(s, elt, M, N, K, dz, Wb, d_prev, out, relu_mask, sums, sum_rows);
+hipError_t launch_gated_dgrad(hipStream_t s, int elt, int M, int N, int K, const void* dz, const void* Wb, void* w_pad, const void* d_prev,
+                              void* out, int relu_mask, float* sums, int* sum_rows, float* partial) {
+  if (elt == ELT_BF16) {
+    int ldw = K;
+    if (w_pad) {
+      const hipError_t err = mfma_pad_rows(s, N, K, (const uint16_t*)Wb, (uint16_t*)w_pad);
+      if (err != hipSuccess) return err;
+      Wb = w_pad;
+      ldw = gated_pitch(elt, K);
+    }
+    return mfma_gated_dgrad(s, M, N, K, (const uint16_t*)dz, (const uint16_t*)Wb, ldw, (const uint16_t*)d_prev, (uint16_t*)out, relu_mask, sums,
+                            sum_rows, partial);
+  }
   if (sums) *sum_rows = dgrad_sum_rows(elt, M, K);
   return f32_gated_dgrad(s, M, N, K, (const float*)dz, gated_pitch(elt, N), (const float*)Wb, (const float*)d_prev, (float*)out, relu_mask,
                          sums && *sum_rows ? sums : nullptr);
 }
 
-hipError_t launch_gated_wgrad(hipStream_t s, int elt, int M, int N, int K, const void* dz, const void* x, float* gW, float* partial) {
-  if (elt == ELT_BF16) return launch_wgrad(s, elt, M, N, K, dz, x, gW, partial);
+hipError_t launch_gated_wgrad(hipStream_t s, int elt, int M, int N, int K, const void* dz, const void* x, const void* x_pad, float* gW,
+                              float* partial) {
+  if (elt == ELT_BF16)
+    return mfma_gated_wgrad(s, M, N, K, (const uint16_t*)dz, (const uint16_t*)(x_pad ? x_pad : x), x_pad ? gated_pitch(elt, K) : K, gW, partial);
   return f32_gated_wgrad(s, M, N, K, (const float*)dz, gated_pitch(elt, N), (const float*)x, gW, partial);
+}
+
+size_t gated_dgrad_scratch_floats(int elt, int M, int N, int K) { return elt == ELT_BF16 ? mfma_gated_dgrad_scratch_floats(M, N, K) : 0; }
+size_t gated_wgrad_scratch_floats(int elt, int M, int N, int K) {
+  return elt == ELT_BF16 ? mfma_gated_wgrad_scratch_floats(M, N, K) : wgrad_scratch_floats(elt, M, N, K);
 }
 
 hipError_t launch_gated_backward(hipStream_t s, int elt, int M, int N, const void* dy, const void* d, const uint8_t* fine, void* dz, float* gb,
                                  float* partials) {
-  const int V = elt == ELT_BF16 ? 8 : 4;
-  const ColsumShape cs = colsum_shape(M, N, V);
+  const ColsumShape cs = colsum_shape(M, N, elt == ELT_BF16 ? 8 : 4);
   const dim3 g1(cs.col_blocks, cs.chunks);
-  const bool vec = gated_pitch(elt, N) % V == 0 && (((uintptr_t)d | (uintptr_t)dz) & 15) == 0 && (elt == ELT_F32 || ((uintptr_t)dy & 7) == 0);
-#define TP_GATED(T, VEC)                                                                                                    \
-  hipLaunchKernelGGL((gated_backward_kernel<T, VEC>), g1, dim3(kThreads), 0, s, M, N, cs, (const T*)dy, (const T*)d, fine, (T*)dz, \
-                     gated_pitch(elt, N), partials)
-  if (elt == ELT_BF16) {
-    if (vec) TP_GATED(uint16_t, true); else TP_GATED(uint16_t, false);
-  } else {
-    if (vec) TP_GATED(float, true); else TP_GATED(float, false);
-  }
-#undef TP_GATED
+  const int pitch = gated_pitch(elt, N);
+  float* sums = cs.chunks == 1 ? gb : partials;  // of one chunk of rows: the sums themselves
+  if (elt == ELT_BF16)
+    hipLaunchKernelGGL(gated_backward_kernel<uint16_t>, g1, dim3(kThreads), 0, s, M, N, cs, (const uint16_t*)dy, (const uint16_t*)d, fine,
+                       (uint16_t*)dz, pitch, sums);
+  else
+    hipLaunchKernelGGL(gated_backward_kernel<float>, g1, dim3(kThreads), 0, s, M, N, cs, (const float*)dy, (const float*)d, fine, (float*)dz,
+                       pitch, sums);
   const hipError_t err = hipGetLastError();
-  if (err != hipSuccess) return err;
-  return launch_sum_partials(s, (size_t)N, cs.chunks, partials, gb);
+  return err != hipSuccess || cs.chunks == 1 ? err : launch_sum_partials(s, (size_t)N, cs.chunks, partials, gb);
 }
 
 hipError_t launch_dgrad(hipStream_t s, int elt, int M, int N, int K, const void* dz, const void* Wb, const void* d_prev,

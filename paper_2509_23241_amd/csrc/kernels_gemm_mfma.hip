@@ -148,6 +148,14 @@ __device__ __forceinline__ EpiWgrad epi_of_split(const EpiWgradSplit& e, int spl
   return EpiWgrad{e.out + (size_t)split * e.split_stride, e.ldc};
 }
 
+struct EpiCutSplit {
+  float* out; int ldc; int rows, cols; size_t split_stride;
+  static constexpr bool kSwap = false;
+};
+__device__ __forceinline__ EpiCut epi_of_split(const EpiCutSplit& e, int split) {
+  return EpiCut{e.out + (size_t)split * e.split_stride, e.ldc, e.rows, e.cols};
+}
+
 // ---- any extents and alignment ------------------------------------------------------------------
 // Bound by the latency of its loads at the few workgroups it mostly has.  PF: k tiles in flight in registers (with one,
 // every k tile cost a memory latency: 0.7 us at 100 x 2000 x 2000).  Against bounds-checked fp32 FMAs: stage of width 2315
@@ -355,7 +363,7 @@ __global__ __launch_bounds__(64 * WGM * WGN) void gemm_bf16_dma_kernel(int M, in
   // rows of the wave tile stored whole, by 4 * TN lanes each
   constexpr bool kRowStores = Epi::kSwap && 64 % (4 * TN) == 0;
   bool whole = false;
-  if constexpr (kRowStores) whole = m0 + wm + WM <= M && n0 + wn + WN <= N && (N & 7) == 0 && epi.wide == 2;
+  if constexpr (kRowStores) whole = m0 + wm + WM <= M && n0 + wn + WN <= N && epi.whole_rows(N);
   typename EpiInputs<TM, TN, Epi, kRowStores>::type row_inputs;
 
   int kt0 = 0;
@@ -765,7 +773,8 @@ Tile pick(int M, int N, bool wgrad) {
 // five ranges do less of it: two decoder blocks of width 512 1.087 -> 1.039 ms; 2048 x 2048 over 32768 rows, 128x128 tiles
 // before, 256x256 over four ranges now: decoder block of width 2048 10.52 -> 10.45 ms.
 struct WgradPlan { Tile tile; int per; };
-WgradPlan wgrad_plan(int M, int N, int K, bool dma) {
+// square: only the three square tiles
+WgradPlan wgrad_plan(int M, int N, int K, bool dma, bool square = false) {
   const int kt = k_tiles(M);
   if (!dma) {
     const long blocks = (long)((N + 63) / 64) * ((K + 63) / 64);
@@ -773,12 +782,20 @@ WgradPlan wgrad_plan(int M, int N, int K, bool dma) {
     return {T64x64, ranges > 1 ? (kt + ranges - 1) / ranges : kt};
   }
   auto k_tile_us = [](const TileCost& t) { return 1.66 * t.bm * t.bn / 65536 * 100 / t.rate; };
+  auto is_square = [](const TileCost& t) { return t.t == T256x256 || t.t == T128x128 || t.t == T64x64; };
   WgradPlan best{pick(N, K, true), kt};
+  if (square) {
+    long cost = -1;
+    for (const TileCost& t : kTiles) {
+      const long c = (blocks_of(t, N, K) + 255) / 256 * t.bm * t.bn * 100 / t.rate;
+      if (is_square(t) && (cost < 0 || c < cost)) { cost = c; best.tile = t.t; }
+    }
+  }
   double best_us = -1;
   for (const TileCost& t : kTiles)
     if (t.t == best.tile) best_us = (double)((blocks_of(t, N, K) + 255) / 256) * k_tile_us(t) * kt;
   for (const TileCost& t : kTiles) {
-    if (t.t != T256x256 && t.t != T128x128 && t.t != T64x64) continue;
+    if (!is_square(t)) continue;
     const int ranges = (int)std::min<long>(256 / blocks_of(t, N, K), kt / 8);
     if (ranges < 2) continue;
     const int per = (kt + ranges - 1) / ranges;
@@ -876,12 +893,123 @@ hipError_t mfma_fprop(hipStream_t s, int M, int N, int K, const uint16_t* x, con
   return fprop_product(s, M, N, K, in, W, EpiFprop{bias, d_out, a_out, act, N, nullptr, wide}, spread);
 }
 
+// ---- the gated layer ----------------------------------------------------------------------------
+// Its products take the direct-to-LDS kernel whatever the widths: dz has rows of whole 16-byte units, and x and the weights are copied into
+// such rows where theirs are not, zeros behind them.
+namespace {
+__global__ __launch_bounds__(256) void pad_rows_kernel(size_t units, int cols, int pitch, const uint16_t* __restrict__ src, uint16_t* __restrict__ dst) {
+  const int per_row = pitch / 8;
+  for (size_t u = (size_t)blockIdx.x * 256 + threadIdx.x; u < units; u += (size_t)gridDim.x * 256) {
+    const size_t row = u / per_row;
+    const int col = (int)(u - row * per_row) * 8;
+    *reinterpret_cast<uint4*>(dst + row * pitch + col) = load8(src + row * cols + col, cols - col);
+  }
+}
+// Gradient of x from the partial sums of `ranges` contraction ranges
+__global__ __launch_bounds__(256) void dgrad_ranges_kernel(size_t count, int ranges, const float* __restrict__ partial,
+                                                           const uint16_t* __restrict__ d_prev, int relu_mask, uint16_t* __restrict__ out) {
+  for (size_t i = (size_t)blockIdx.x * 256 + threadIdx.x; i < count; i += (size_t)gridDim.x * 256) {
+    float s = 0.f;
+#pragma unroll 8
+    for (int r = 0; r < ranges; ++r) s += partial[(size_t)r * count + i];
+    if (d_prev) {
+      const float d = bf16_to_float(d_prev[i]);
+      s = relu_mask ? (d > 0.f ? s : 0.f) : s * d;
+    }
+    out[i] = float_to_bf16(s);
+  }
+}
+inline int pitch8(int n) { return (n + 7) / 8 * 8; }
+// where a product has too few tiles for the chip: ranges of its contraction, as a weight gradient's
+inline WgradPlan gated_dgrad_plan(int M, int N, int K) { return wgrad_plan(N, M, pitch8(K), true, true); }
+inline int ranges_of(const WgradPlan& p, int contraction) { return (k_tiles(contraction) + p.per - 1) / p.per; }
+inline bool in_reach(int rows, int ld) { return (size_t)std::min(rows, 384) * ld * 2 < (1ull << 31); }
+
+// One of the three square tiles
+template <bool A_COL, bool B_COL, class Epi>
+hipError_t run_square(Tile tile, hipStream_t s, int M, int N, int K, const uint16_t* A, int lda, const uint16_t* B, int ldb, const Epi& e, int per) {
+  const SideCopy none{nullptr, nullptr, 0};
+  auto go = [&](auto tail) {
+    constexpr bool T = decltype(tail)::value;
+    switch (tile) {
+      case T256x256: return launch_dma<256, 256, 2, 4, 2, A_COL, B_COL, false, true, T>(s, M, N, K, A, lda, B, ldb, e, none, per);
+      case T128x128: return launch_dma<128, 128, 2, 2, 3, A_COL, B_COL, false, true, T>(s, M, N, K, A, lda, B, ldb, e, none, per);
+      default: return launch_dma<64, 64, 2, 2, 4, A_COL, B_COL, true, false, T>(s, M, N, K, A, lda, B, ldb, e, none, per);
+    }
+  };
+  return K % DBK ? go(std::true_type{}) : go(std::false_type{});
+}
+}  // namespace
+
+hipError_t mfma_pad_rows(hipStream_t s, size_t rows, int cols, const uint16_t* src, uint16_t* dst) {
+  const size_t units = rows * (pitch8(cols) / 8);
+  hipLaunchKernelGGL(pad_rows_kernel, dim3((unsigned)std::min<size_t>((units + 255) / 256, 8192)), dim3(256), 0, s, units, cols, pitch8(cols), src, dst);
+  return hipGetLastError();
+}
+
+bool mfma_gated_padded(int M, int N, int K) { return K % 8 != 0 && in_reach(std::max(M, N), pitch8(K)) && in_reach(M, pitch8(N)); }
+
 hipError_t mfma_gated_fprop(hipStream_t s, int M, int N, int K, const uint16_t* x, const uint16_t* W, const float* bias, int act,
                             uint16_t* d_out, uint8_t* fine, uint16_t* a_out, uint16_t* x_copy, int spread) {
   FpropInput in;
   const hipError_t err = fprop_input(s, M, N, K, x, W, x_copy, &in);
   if (err != hipSuccess) return err;
-  return fprop_product(s, M, N, K, in, W, EpiGated{bias, d_out, fine, a_out, act, N, store_width(d_out, a_out)}, spread);
+  return fprop_product(s, M, N, K, in, W, EpiGated{bias, d_out, fine, a_out, act, N, pitch8(N), aligned(16, d_out) ? 2 : 0}, spread);
+}
+
+size_t mfma_gated_dgrad_scratch_floats(int M, int N, int K) {
+  const int ranges = ranges_of(gated_dgrad_plan(M, N, K), N);
+  return ranges > 1 ? (size_t)ranges * M * K : 0;
+}
+
+hipError_t mfma_gated_dgrad(hipStream_t s, int M, int N, int K, const uint16_t* dz, const uint16_t* Wb, int ldw, const uint16_t* d_prev,
+                            uint16_t* out, int relu_mask, float* sums, int* sum_rows, float* partial) {
+  const int ldz = pitch8(N);
+  if (sums) *sum_rows = 0;
+  // out[M x K] = dz[M x N] . Wb[N x K]: GEMM (M, K, contraction N); zeros behind a row of dz, none read behind the rows of Wb
+  if (ldw % 8 || !aligned(16, dz, Wb) || !in_reach(M, ldz) || !in_reach(64, ldw))
+    return run_any<false, true>(s, M, K, N, dz, ldz, Wb, ldw, EpiDgrad{d_prev, out, K, relu_mask, store_width(d_prev, out)});
+  const WgradPlan plan = gated_dgrad_plan(M, N, K);
+  const int ranges = ranges_of(plan, N);
+  if (ranges > 1) {
+    const hipError_t err = run_square<false, true>(plan.tile, s, M, ldw, N, dz, ldz, Wb, ldw, EpiCutSplit{partial, K, M, K, (size_t)M * K}, plan.per);
+    if (err != hipSuccess) return err;
+    const size_t count = (size_t)M * K;
+    hipLaunchKernelGGL(dgrad_ranges_kernel, dim3((unsigned)std::min<size_t>((count + 255) / 256, 4096)), dim3(256), 0, s, count, ranges, partial,
+                       d_prev, relu_mask, out);
+    return hipGetLastError();
+  }
+  if (ldw != K)
+    return run_square<false, true>(plan.tile, s, M, ldw, N, dz, ldz, Wb, ldw, EpiDgradCut{{d_prev, out, K, relu_mask, 0}, K}, plan.per);
+  EpiDgrad e{d_prev, out, K, relu_mask, store_width(d_prev, out)};
+  if (sums) {
+    *sum_rows = e.wide == 2 ? mfma_dgrad_sum_rows(M, K) : 0;
+    if (*sum_rows) e.sums = sums;
+  }
+  const SideCopy none{nullptr, nullptr, 0};
+  const Tile tile = pick(M, K, false);
+  return N % DBK ? run_dma<false, true, true>(tile, s, M, K, N, dz, ldz, Wb, ldw, e, none, k_tiles(N))
+                 : run_dma<false, true, false>(tile, s, M, K, N, dz, ldz, Wb, ldw, e, none, k_tiles(N));
+}
+
+size_t mfma_gated_wgrad_scratch_floats(int M, int N, int K) {
+  if (N % 8 == 0 && K % 8 == 0) return mfma_wgrad_scratch_floats(M, N, K);
+  const int ranges = ranges_of(wgrad_plan(M, pitch8(N), pitch8(K), true, true), M);
+  return ranges > 1 ? (size_t)ranges * N * K : 0;
+}
+
+hipError_t mfma_gated_wgrad(hipStream_t s, int M, int N, int K, const uint16_t* dz, const uint16_t* x, int ldx, float* gW, float* partial) {
+  const int ldz = pitch8(N);
+  if (ldz == N && K % 8 == 0) return mfma_wgrad(s, M, N, K, dz, x, gW, partial);
+  // gW[N x K] = dz^T[N x M] . x[M x K]: GEMM (N, K, contraction M)
+  if (ldx % 8 || !aligned(16, dz, x) || !in_reach(64, ldz) || !in_reach(64, ldx))
+    return run_any<true, true>(s, N, K, M, dz, ldz, x, ldx, EpiWgrad{gW, K});
+  const WgradPlan plan = wgrad_plan(M, ldz, ldx, true, true);
+  const int ranges = ranges_of(plan, M);
+  if (!partial || ranges == 1) return run_square<true, true>(plan.tile, s, ldz, ldx, M, dz, ldz, x, ldx, EpiCut{gW, K, N, K}, k_tiles(M));
+  const hipError_t err = run_square<true, true>(plan.tile, s, ldz, ldx, M, dz, ldz, x, ldx, EpiCutSplit{partial, K, N, K, (size_t)N * K}, plan.per);
+  if (err != hipSuccess) return err;
+  return launch_sum_partials(s, (size_t)N * K, ranges, partial, gW);
 }
 
 int mfma_dgrad_sum_rows(int M, int K) {

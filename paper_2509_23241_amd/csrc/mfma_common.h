@@ -34,6 +34,7 @@ struct EpiFpropT {
   const uint16_t* addend = nullptr;
   int wide = 2;  // 2: the outputs are 16-byte aligned (row8 may be used), 1: 8-byte, 0: not even that
   static constexpr bool kSwap = true, kSums = false;
+  __device__ __forceinline__ bool whole_rows(int N) const { return (N & 7) == 0 && wide == 2; }
   // what row8 below reads, as its own steps so that a wave can have all of it in flight before it needs any: the values
   // of columns n..n+7, and the 16 bytes that belong to row m there
   struct Cols { float4 b0, b1; };
@@ -112,10 +113,12 @@ using EpiFpropExact = EpiFpropT<false, true>;
 // A gated layer: columns 2f and 2f + 1 of the product are the gate and the other factor of output f, so that a lane's neighbouring columns
 // hold both and whichever tile a kernel has needs no exchange between lanes.  d_out [M x ldc] and fine [M x ldc / 2]: what dy[f] is
 // multiplied with for either column, to 12 bits (split12 in device_utils.h); a_out [M x ldc / 2].
+// Rows of d_out are ldd values apart, a multiple of eight; those of the other two start at any address.
 struct EpiGated {
-  const float* bias; uint16_t* d_out; uint8_t* fine; uint16_t* a_out; int act; int ldc;
-  int wide = 2;  // alignment of the outputs, as above
+  const float* bias; uint16_t* d_out; uint8_t* fine; uint16_t* a_out; int act; int ldc; int ldd;
+  int wide = 2;  // 2: d_out is 16-byte aligned
   static constexpr bool kSwap = true, kSums = false;
+  __device__ __forceinline__ bool whole_rows(int) const { return wide == 2; }
   struct Cols { float4 b0, b1; };
   __device__ __forceinline__ Cols cols(int n) const {
     return Cols{*reinterpret_cast<const float4*>(bias + n), *reinterpret_cast<const float4*>(bias + n + 4)};
@@ -144,31 +147,34 @@ struct EpiGated {
     uint32_t d[4];
     float a[4];
     const uint32_t low = pairs<4>(v, d, a);
-    const size_t i = (size_t)m * ldc + n;
+    const size_t f = ((size_t)m * ldc + n) / 2;
     const uint4 o = make_uint4(d[0], d[1], d[2], d[3]);
-    *reinterpret_cast<uint4*>(d_out + i) = o;
-    *reinterpret_cast<uint2*>(a_out + i / 2) = make_uint2(pack_bf16x2(a[0], a[1]), pack_bf16x2(a[2], a[3]));
-    *reinterpret_cast<uint32_t*>(fine + i / 2) = low;
+    *reinterpret_cast<uint4*>(d_out + (size_t)m * ldd + n) = o;
+    const uint2 y = make_uint2(pack_bf16x2(a[0], a[1]), pack_bf16x2(a[2], a[3]));
+    __builtin_memcpy(a_out + f, &y, 8);
+    __builtin_memcpy(fine + f, &low, 4);
     return o;
   }
   // count: 2 or 4
   __device__ __forceinline__ void quad(int m, int n, int count, float v0, float v1, float v2, float v3) const {
-    const size_t i = (size_t)m * ldc + n;
+    const size_t i = (size_t)m * ldd + n, o = ((size_t)m * ldc + n) / 2;
     const bool both = count == 4;
     const float z[4] = {v0 + bias[n], v1 + bias[n + 1], v2 + bias[both ? n + 2 : n], v3 + bias[both ? n + 3 : n]};
     uint32_t d[2];
     float a[2];
     const uint32_t low = pairs<2>(z, d, a);
-    if (both && (ldc & 3) == 0 && wide) {
+    if (both && wide) {
       *reinterpret_cast<uint2*>(d_out + i) = make_uint2(d[0], d[1]);
-      *reinterpret_cast<uint32_t*>(a_out + i / 2) = pack_bf16x2(a[0], a[1]);
-      *reinterpret_cast<uint16_t*>(fine + i / 2) = (uint16_t)low;
+      const uint32_t y = pack_bf16x2(a[0], a[1]);
+      const uint16_t lo = (uint16_t)low;
+      __builtin_memcpy(a_out + o, &y, 4);
+      __builtin_memcpy(fine + o, &lo, 2);
     } else {
       for (int f = 0; f < count / 2; ++f) {
         d_out[i + 2 * f] = (uint16_t)d[f];
         d_out[i + 2 * f + 1] = (uint16_t)(d[f] >> 16);
-        a_out[i / 2 + f] = float_to_bf16(a[f]);
-        fine[i / 2 + f] = (uint8_t)(low >> (8 * f));
+        a_out[o + f] = float_to_bf16(a[f]);
+        fine[o + f] = (uint8_t)(low >> (8 * f));
       }
     }
   }
@@ -181,6 +187,7 @@ struct EpiDgrad {
   // every wave stores its rows whole.
   float* sums = nullptr;
   static constexpr bool kSwap = true, kSums = true;
+  __device__ __forceinline__ bool whole_rows(int N) const { return (N & 7) == 0 && wide == 2; }
   __device__ __forceinline__ float through(float v, float d) const { return relu_mask ? (d > 0.f ? v : 0.f) : v * d; }
   struct Cols {};
   __device__ __forceinline__ Cols cols(int) const { return Cols{}; }
@@ -228,6 +235,20 @@ struct EpiWgrad {
   float* out; int ldc;
   static constexpr bool kSwap = false;
   __device__ __forceinline__ void elem(int m, int n, float v) const { out[(size_t)m * ldc + n] = v; }
+};
+// Of operands that are padded to whole 16-byte units: the rows and columns that are there.
+struct EpiDgradCut : EpiDgrad {  // (wide is 0: no rows are stored whole)
+  int there;  // columns
+  __device__ __forceinline__ void quad(int m, int n, int count, float v0, float v1, float v2, float v3) const {
+    if (n < there) EpiDgrad::quad(m, n, min(count, there - n), v0, v1, v2, v3);
+  }
+};
+struct EpiCut {
+  float* out; int ldc; int rows, cols;
+  static constexpr bool kSwap = false;
+  __device__ __forceinline__ void elem(int m, int n, float v) const {
+    if (m < rows && n < cols) out[(size_t)m * ldc + n] = v;
+  }
 };
 
 // Accumulator element r of a lane sits at tile row 8*(r/4) + 4*(lane/32) + r%4, tile column

@@ -62,6 +62,8 @@ struct LayerPlan {
   DeferredNeed need;
   uint64_t pair_off = UINT64_MAX;  // gated: what the backward pass multiplies with, two values for each output
   uint64_t pair_elems = 0;         // values per sample there
+  uint64_t wide_off = UINT64_MAX;  // gated: the input again, in rows of whole 16-byte units, where its own are not
+  uint64_t wide_elems = 0;
   uint64_t fine_off = UINT64_MAX;  // and in bf16 four more bits of each, [rows x outputs] bytes
   bool in_place = false;           // rotary: input and output are one tensor
   tp::RotarySpeeds speeds;         // rotary
@@ -90,6 +92,7 @@ struct Plan {
   uint64_t partial_floats = 0; // reduction partials
   uint64_t deferred_floats = 0; // behind them: partials of the backward pass's sums, which one launch forms at its end
   uint64_t fwd2_floats = 0;     // behind those: scratch of the normalisation forward kernels on a second forward stream
+  uint64_t gated_pad_bytes = 0;     // behind the attention's: weights of a gated layer in rows of whole 16-byte units, for every stream that forwards run on
   uint64_t attn_scratch_bytes = 0;  // transient score matrices of the matrix-core attention
   size_t elt_size = 4;
   bool any_order = true;  // dense layers of whole samples alone: no normalisation follows whose results hang on an ulp of its input
@@ -342,7 +345,7 @@ DeferredNeed deferred_need(const tp_stage_desc& d, int l, const LayerPlan& lp) {
   } else if (L.type == TP_LAYER_GATED) {
     const int r = (int)(rows * lp.tokens), columns = product_columns(L);
     need.bias = round_up(tp::colsum_scratch_floats(r, columns), 64);
-    need.weight = round_up(tp::wgrad_scratch_floats(d.dtype, r, columns, L.in_features), 64);
+    need.weight = round_up(tp::gated_wgrad_scratch_floats(d.dtype, r, columns, L.in_features), 64);
   } else if (L.type == TP_LAYER_LAYERNORM) {
     need.norm = round_up(tp::layernorm_scratch_floats(rows * lp.tokens, L.in_features), 64);
   } else if (L.type == TP_LAYER_BATCHNORM) {
@@ -509,6 +512,13 @@ int make_plan(const tp_stage_desc* d, Plan* p) {
         act += round_up(rows * lp.out_elems, 256);
       }
       max_feat = std::max<uint64_t>(max_feat, lp.pair_elems);
+      if (tp::gated_padded(d->dtype, (int)(rows * lp.tokens), product_columns(L), L.in_features)) {
+        const uint64_t pitch = tp::gated_pitch(d->dtype, L.in_features);
+        lp.wide_off = act;
+        lp.wide_elems = lp.tokens * pitch;
+        act += round_up(rows * lp.wide_elems * p->elt_size, 256);
+        p->gated_pad_bytes = std::max<uint64_t>(p->gated_pad_bytes, round_up(product_columns(L) * pitch * p->elt_size, 256));
+      }
       lp.z_off = UINT64_MAX;
     } else if (L.act != TP_ACT_NONE && !lp.relu_out) {
       lp.z_off = act;
@@ -543,7 +553,8 @@ int make_plan(const tp_stage_desc* d, Plan* p) {
     const uint64_t r = lp.d.type == TP_LAYER_CONV2D ? rows * conv_out_px(lp.d) : rows * lp.tokens;
     if (lp.d.type == TP_LAYER_GATED) {
       wg = std::max<uint64_t>({wg, tp::colsum_scratch_floats((int)r, product_columns(lp.d)),
-                               tp::wgrad_scratch_floats(d->dtype, (int)r, product_columns(lp.d), lp.d.in_features)});
+                               tp::gated_wgrad_scratch_floats(d->dtype, (int)r, product_columns(lp.d), lp.d.in_features),
+                               tp::gated_dgrad_scratch_floats(d->dtype, (int)r, product_columns(lp.d), lp.d.in_features)});
       continue;
     }
     wg = std::max<uint64_t>(wg, bias_partials(*d, l, r));
@@ -574,7 +585,8 @@ int make_plan(const tp_stage_desc* d, Plan* p) {
   s.wfwd_bytes = d->dtype == TP_BF16 ? P * 2 : 0;
   s.wbwd_bytes = d->policy == TP_LATEST ? 0 : P * p->elt_size;  // V-TiMePReSt never builds intermediate weights
   s.act_bytes = (uint64_t)d->max_in_flight * act;
-  s.scratch_bytes = 3 * p->dz_bytes + (p->partial_floats + p->deferred_floats + TP_MAX_FORWARD_STREAMS * p->fwd2_floats) * 4 + 512 + p->attn_scratch_bytes;  // + an aligned block of 256 zero bytes (conv padding)
+  s.scratch_bytes = 3 * p->dz_bytes + (p->partial_floats + p->deferred_floats + TP_MAX_FORWARD_STREAMS * p->fwd2_floats) * 4 + 512 +
+                    round_up(p->attn_scratch_bytes, 256) + (1 + TP_MAX_FORWARD_STREAMS) * p->gated_pad_bytes;  // + an aligned block of 256 zero bytes (conv padding)
   s.diag_bytes = TP_DIAG_COUNT * sizeof(double);
   return TP_OK;
 }
@@ -656,6 +668,8 @@ struct tp_stage {
   enum Counter { kCountUpdate, kCountLoss };
   uint32_t* counter(Counter c) const { return (uint32_t*)((char*)zeros() + 128) + c; }
   void* attn_scratch() const { return plan.attn_scratch_bytes ? (char*)zeros() + 256 : nullptr; }
+  // k: -1 the stage's own stream, else a forward stream's index
+  void* gated_pad(int k) const { return (char*)zeros() + 256 + round_up(plan.attn_scratch_bytes, 256) + (uint64_t)(k + 1) * plan.gated_pad_bytes; }
   // drop a version that nobody needs any more
   void evict_if_unused(uint64_t v) {
     int s = find_slot(v);
@@ -1145,7 +1159,9 @@ int forward_impl(tp_stage* st, uint64_t mb_id, uint32_t ub_idx, uint32_t ubs, co
       uint8_t* fine = lp.fine_off == UINT64_MAX ? nullptr : (uint8_t*)aslot + lp.fine_off + row0 * lp.out_elems;
       HIP_TRY(tp::launch_gated_fprop(fs, d.dtype, mb * lp.tokens, product_columns(lp.d), lp.d.in_features, x_in, wcopy + lp.w_off * es,
                                      master + lp.b_off, lp.d.act, aslot + lp.pair_off + row0 * lp.pair_elems * es, fine, a_out,
-                                     need_copy ? x_saved : nullptr, spread));
+                                     need_copy ? x_saved : nullptr, spread,
+                                     lp.wide_off == UINT64_MAX ? nullptr : aslot + lp.wide_off + row0 * lp.wide_elems * es,
+                                     lp.wide_off == UINT64_MAX ? nullptr : st->gated_pad(fsk)));
       continue;
     }
     if (lp.d.type == TP_LAYER_ROTARY) {  // its backward pass needs no input: none is kept
@@ -1839,7 +1855,7 @@ int backward_impl(tp_stage* st, uint64_t mb_id, const void* dy_dev, void* dx_dev
         float* part = hold(need.weight);
         if (lp.d.type == TP_LAYER_GATED)
           HIP_TRY(tp::launch_gated_wgrad(st->stream, d.dtype, grad_rows, product_columns(lp.d), lp.d.in_features, dz, aslot + lp.x_off,
-                                         g + lp.w_off, part));
+                                         lp.wide_off == UINT64_MAX ? nullptr : aslot + lp.wide_off, g + lp.w_off, part));
         else if (lp.d.type == TP_LAYER_DENSE)
           HIP_TRY(tp::launch_wgrad(st->stream, d.dtype, grad_rows, lp.d.out_features, lp.d.in_features, dz, aslot + lp.x_off,
                                    g + lp.w_off, part));
@@ -1861,7 +1877,8 @@ int backward_impl(tp_stage* st, uint64_t mb_id, const void* dy_dev, void* dx_dev
         ProfScope ps(st, TP_K_DGRAD);
         if (lp.d.type == TP_LAYER_GATED)
           HIP_TRY(tp::launch_gated_dgrad(st->stream, d.dtype, grad_rows, product_columns(lp.d), lp.d.in_features, dz, wb + lp.w_off * es,
-                                         dprev, dst, dmask, bias_sums(), &bias_rows));
+                                         lp.wide_off == UINT64_MAX ? nullptr : st->gated_pad(-1), dprev, dst, dmask, bias_sums(), &bias_rows,
+                                         st->partials()));
         else if (lp.d.type == TP_LAYER_DENSE)
           HIP_TRY(tp::launch_dgrad(st->stream, d.dtype, grad_rows, lp.d.out_features, lp.d.in_features, dz, wb + lp.w_off * es,
                                    dprev, dst, dmask, bias_sums(), &bias_rows));
