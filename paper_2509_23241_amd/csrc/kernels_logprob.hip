@@ -81,7 +81,7 @@ __device__ __forceinline__ RowStats read_row(const T* lg, int classes, float* sm
   const Exponents e(top);
   float sum = 0.f;
   for (int j = threadIdx.x; j < classes; j += kThreads) sum += __builtin_amdgcn_exp2f(e.power(to_float(lg[j])));
-  return RowStats{top, TM::over(sum, sm, Add())};
+  return RowStats{top, TM::over(sum, sm, Add()), 0.0};
 }
 // slope ([j = id] - softmax(z)_j), or zeros (slope 0: whatever the logits hold)
 template <typename T>
@@ -105,10 +105,11 @@ __global__ __launch_bounds__(kThreads) void logprob_rows_kernel(LogprobArgs a) {
     const int id = a.ids[row];
     const bool counts = id >= 0 && (!a.weights || a.weights[row] != 0.f);
     const T* lg = (const T*)a.logits + (size_t)row * a.classes;
-    RowStats r{0.f, 1.f};
+    RowStats r{0.f, 1.f, 0.0};
     if (counts) r = read_row(lg, a.classes, sm);
     if (threadIdx.x == 0) {
-      a.logp[row] = !counts ? 0.f : id < a.classes ? (float)Exponents(r.top).log_probability(to_float(lg[id]), r.sum) : __builtin_nanf("");
+      if (counts) r.logp = id < a.classes ? Exponents(r.top).log_probability(to_float(lg[id]), r.sum) : __builtin_nan("");
+      if (a.logp) a.logp[row] = (float)r.logp;
       if (a.stats) a.stats[row] = r;
     }
   }
@@ -122,7 +123,7 @@ __global__ __launch_bounds__(kThreads) void policy_rows_kernel(PolicyArgs a) {
     const float weight = a.weights ? a.weights[row] : 1.f / (float)a.rows;
     const bool counts = id >= 0 && weight != 0.f, known = id < a.classes;
     const T* lg = (const T*)a.logits + (size_t)row * a.classes;
-    RowStats r{0.f, 1.f};
+    RowStats r{0.f, 1.f, 0.0};
     PolicyTerm t{0.f, 0.f};
     double logp = 0.0;
     if (counts && known) {
@@ -257,7 +258,7 @@ __global__ __launch_bounds__(Team<NT>::kThreads, (kWavesASimd<T, HELD>)) void lo
   const int id = a.ids[row];
   const bool counts = id >= 0 && (!a.weights || a.weights[row] != 0.f);
   const T* lg = (const T*)a.logits + (size_t)row * a.classes;
-  RowStats r{0.f, 1.f};
+  RowStats r{0.f, 1.f, 0.0};
   float z = 0.f;
   if (counts) {
     if (id < a.classes) z = to_float(lg[id]);
@@ -267,7 +268,8 @@ __global__ __launch_bounds__(Team<NT>::kThreads, (kWavesASimd<T, HELD>)) void lo
     r.sum = TM::over(h.exponentials(Exponents(r.top)), sm, Add());
   }
   if (TM::thread() == 0) {
-    a.logp[row] = !counts ? 0.f : id < a.classes ? (float)Exponents(r.top).log_probability(z, r.sum) : __builtin_nanf("");
+    if (counts) r.logp = id < a.classes ? Exponents(r.top).log_probability(z, r.sum) : __builtin_nan("");
+    if (a.logp) a.logp[row] = (float)r.logp;
     if (a.stats) a.stats[row] = r;
   }
 }
@@ -402,8 +404,9 @@ __global__ __launch_bounds__(kThreads) void preference_pairs_kernel(PreferenceAr
       const size_t row0 = (size_t)(2 * pair + k) * a.tokens;
       double s = 0.0;
       for (int t = threadIdx.x; t < a.tokens; t += kThreads) {
-        const float weight = a.weights ? a.weights[row0 + t] : 1.f, logp = a.logp[row0 + t];  // loaded side by side
-        s += a.targets[row0 + t] >= 0 && weight != 0.f ? (double)weight * (double)logp : 0.0;
+        const float weight = a.weights ? a.weights[row0 + t] : 1.f;  // loaded side by side
+        const double logp = a.stats[row0 + t].logp;
+        s += a.targets[row0 + t] >= 0 && weight != 0.f ? (double)weight * logp : 0.0;
       }
       ratio[k] = block_sum(s, sm) - (double)a.ref_logp[2 * pair + k];
     }

@@ -5,17 +5,19 @@
 
 namespace tp {
 
-// What the second pass over a row needs of the first: its maximum and the sum of exp(z_j - top).
+// What is needed of a row once it has been read: its maximum, the sum of exp(z_j - top), and the log probability of its class before it is
+// rounded to fp32: a sequence's sum of them is the difference that a margin is made of.
 struct RowStats {
   float top, sum;
+  double logp;
 };
 
 struct LogprobArgs {
   int rows, classes;
   const void* logits;   // [rows x classes] in elt
   const int32_t* ids;   // [rows], negative: no token
-  float* logp;          // [rows]
-  RowStats* stats;      // [rows], or null
+  float* logp;          // [rows], or null
+  RowStats* stats;      // [rows] at 16 bytes, or null
   const float* weights; // [rows], or null: rows of weight 0 are left out, too
 };
 hipError_t launch_logprobs(hipStream_t s, int elt, const LogprobArgs& a);
@@ -46,7 +48,7 @@ struct PreferenceArgs {
   const float* ref_logp;  // [2 pairs]
   double beta, smoothing;
   void* dlogits;
-  float* logp;            // [rows]
+  float* logp;            // [rows], or null
   RowStats* stats;        // scratch, [rows]
   float* pull;            // scratch, [2 pairs]: what a log probability of the sample weighs in the loss
   float* pair_loss;       // scratch, [pairs]

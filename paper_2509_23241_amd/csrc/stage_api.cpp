@@ -1442,7 +1442,7 @@ int stage_loss_preference(tp_stage* st, uint64_t mb_id, const void* logits_dev, 
   const int samples = st->desc.mb * st->desc.n;
   if (samples % 2) return fail(TP_EINVAL, "pairs of sequences need an even number of samples, not %d", samples);
   if (st->dry) return TP_OK;
-  if (!logits_dev || !targets_dev || !ref_logp_dev || !dlogits_dev || !logp_dev || !loss_dev) return fail(TP_EINVAL, "null pointer");
+  if (!logits_dev || !targets_dev || !ref_logp_dev || !dlogits_dev || !loss_dev) return fail(TP_EINVAL, "null pointer");
   if (int rc = join_forwards(st)) return rc;
   tp::PreferenceArgs a;
   a.pairs = samples / 2;
