@@ -207,15 +207,15 @@ struct Held {
 #pragma unroll
         for (int e = 0; e < V; ++e) x[i][e] -= ex.base;
     }
-    float sum = 0.f;
+    float sum[4] = {};  // short chains of additions
 #pragma unroll
     for (int i = 0; i < HELD; ++i)
 #pragma unroll
       for (int e = 0; e < V; ++e) {
         x[i][e] = __builtin_amdgcn_exp2f(fmaf(x[i][e], kLog2e, -ex.shift));
-        sum += x[i][e];
+        sum[e % 4] += x[i][e];
       }
-    return sum;
+    return (sum[0] + sum[1]) + (sum[2] + sum[3]);
   }
   // The exponentials times `scale`, and `own` in the place of class id's (none: a negative one).  The thread that stores a unit replaces a value
   // of it, in program order.
