@@ -14,10 +14,16 @@ hipError_t f32_gated_fprop(hipStream_t s, int M, int N, int K, const float* x, c
                            float* a_out, float* x_copy);  // launch_gated_fprop
 hipError_t f32_dgrad(hipStream_t s, int M, int N, int K, const float* dz, const float* Wb, const float* d_prev, float* out,
                      int relu_mask, float* sums = nullptr);  // sums: column sums of every 16 rows of `out`, [(M + 15) / 16][K]
-// The gated layer's (launch_gated_dgrad, launch_gated_wgrad), summed in parts
-hipError_t f32_gated_dgrad(hipStream_t s, int M, int N, int K, const float* dz, int ldz, const float* Wb, const float* d_prev, float* out,
-                           int relu_mask, float* sums);
-hipError_t f32_gated_wgrad(hipStream_t s, int M, int N, int K, const float* dz, int ldz, const float* x, float* gW, float* partial);
+// The gated layer's gradients (launch_gated_dgrad, launch_gated_wgrad): rows of dz are N rounded up to four values apart, zeros behind them;
+// ldw, ldx: K, or that rounded up to four, anything finite behind the rows.  partial: scratch of .._scratch_floats(M, N, K) floats
+hipError_t f32_gated_dgrad(hipStream_t s, int M, int N, int K, const float* dz, const float* Wb, int ldw, const float* d_prev, float* out,
+                           int relu_mask, float* sums, int* sum_rows, float* partial);
+hipError_t f32_gated_wgrad(hipStream_t s, int M, int N, int K, const float* dz, const float* x, int ldx, float* gW, float* partial);
+size_t f32_gated_dgrad_scratch_floats(int M, int N, int K);
+size_t f32_gated_wgrad_scratch_floats(int M, int N, int K);
+// Whether x and the weights are to be copied into rows of K rounded up to four values, zeros behind them, and that copy.
+bool f32_gated_padded(int M, int N, int K);
+hipError_t f32_pad_rows(hipStream_t s, size_t rows, int cols, const float* src, float* dst);
 // partial: scratch of f32_wgrad_splits(M, N, K) * N * K floats where that is more than one range, or null
 hipError_t f32_wgrad(hipStream_t s, int M, int N, int K, const float* dz, const float* x, float* gW, float* partial);
 int f32_wgrad_splits(int M, int N, int K);

@@ -352,54 +352,59 @@ hipError_t launch_fprop(hipStream_t s, int elt, int M, int N, int K, const void*
 }
 
 int gated_pitch(int elt, int n) { return elt == ELT_BF16 ? (n + 7) / 8 * 8 : (n + 3) / 4 * 4; }
-bool gated_padded(int elt, int M, int N, int K) { return elt == ELT_BF16 && mfma_gated_padded(M, N, K); }
+bool gated_padded(int elt, int M, int N, int K) { return elt == ELT_BF16 ? mfma_gated_padded(M, N, K) : f32_gated_padded(M, N, K); }
+namespace {
+hipError_t pad_rows(hipStream_t s, int elt, size_t rows, int cols, const void* src, void* dst) {
+  return elt == ELT_BF16 ? mfma_pad_rows(s, rows, cols, (const uint16_t*)src, (uint16_t*)dst) : f32_pad_rows(s, rows, cols, (const float*)src, (float*)dst);
+}
+}  // namespace
 
 hipError_t launch_gated_fprop(hipStream_t s, int elt, int M, int N, int K, const void* x, const void* W, const float* bias, int act,
                               void* d_out, uint8_t* fine, void* a_out, void* x_copy, int spread, void* x_pad, void* w_pad) {
-  if (elt == ELT_F32)
-    return f32_gated_fprop(s, M, N, K, (const float*)x, (const float*)W, bias, act, (float*)d_out, (float*)a_out, (float*)x_copy);
   if (x_pad) {
-    hipError_t err = x_copy ? launch_copy(s, x, x_copy, (size_t)M * K * 2) : hipSuccess;
-    if (err == hipSuccess) err = mfma_pad_rows(s, M, K, (const uint16_t*)x, (uint16_t*)x_pad);
-    if (err == hipSuccess) err = mfma_pad_rows(s, N, K, (const uint16_t*)W, (uint16_t*)w_pad);
+    hipError_t err = x_copy ? launch_copy(s, x, x_copy, (size_t)M * K * (elt == ELT_BF16 ? 2 : 4)) : hipSuccess;
+    if (err == hipSuccess) err = pad_rows(s, elt, M, K, x, x_pad);
+    if (err == hipSuccess) err = pad_rows(s, elt, N, K, W, w_pad);
     if (err != hipSuccess) return err;
     x = x_pad;
     W = w_pad;
     x_copy = nullptr;
     K = gated_pitch(elt, K);
   }
+  if (elt == ELT_F32)
+    return f32_gated_fprop(s, M, N, K, (const float*)x, (const float*)W, bias, act, (float*)d_out, (float*)a_out, (float*)x_copy);
   return mfma_gated_fprop(s, M, N, K, (const uint16_t*)x, (const uint16_t*)W, bias, act, (uint16_t*)d_out, fine, (uint16_t*)a_out,
                           (uint16_t*)x_copy, spread);
 }
 
 hipError_t launch_gated_dgrad(hipStream_t s, int elt, int M, int N, int K, const void* dz, const void* Wb, void* w_pad, const void* d_prev,
                               void* out, int relu_mask, float* sums, int* sum_rows, float* partial) {
-  if (elt == ELT_BF16) {
-    int ldw = K;
-    if (w_pad) {
-      const hipError_t err = mfma_pad_rows(s, N, K, (const uint16_t*)Wb, (uint16_t*)w_pad);
-      if (err != hipSuccess) return err;
-      Wb = w_pad;
-      ldw = gated_pitch(elt, K);
-    }
+  int ldw = K;
+  if (w_pad) {
+    const hipError_t err = pad_rows(s, elt, N, K, Wb, w_pad);
+    if (err != hipSuccess) return err;
+    Wb = w_pad;
+    ldw = gated_pitch(elt, K);
+  }
+  if (elt == ELT_BF16)
     return mfma_gated_dgrad(s, M, N, K, (const uint16_t*)dz, (const uint16_t*)Wb, ldw, (const uint16_t*)d_prev, (uint16_t*)out, relu_mask, sums,
                             sum_rows, partial);
-  }
-  if (sums) *sum_rows = dgrad_sum_rows(elt, M, K);
-  return f32_gated_dgrad(s, M, N, K, (const float*)dz, gated_pitch(elt, N), (const float*)Wb, (const float*)d_prev, (float*)out, relu_mask,
-                         sums && *sum_rows ? sums : nullptr);
+  return f32_gated_dgrad(s, M, N, K, (const float*)dz, (const float*)Wb, ldw, (const float*)d_prev, (float*)out, relu_mask, sums, sum_rows, partial);
 }
 
 hipError_t launch_gated_wgrad(hipStream_t s, int elt, int M, int N, int K, const void* dz, const void* x, const void* x_pad, float* gW,
                               float* partial) {
-  if (elt == ELT_BF16)
-    return mfma_gated_wgrad(s, M, N, K, (const uint16_t*)dz, (const uint16_t*)(x_pad ? x_pad : x), x_pad ? gated_pitch(elt, K) : K, gW, partial);
-  return f32_gated_wgrad(s, M, N, K, (const float*)dz, gated_pitch(elt, N), (const float*)x, gW, partial);
+  const int ldx = x_pad ? gated_pitch(elt, K) : K;
+  if (x_pad) x = x_pad;
+  if (elt == ELT_BF16) return mfma_gated_wgrad(s, M, N, K, (const uint16_t*)dz, (const uint16_t*)x, ldx, gW, partial);
+  return f32_gated_wgrad(s, M, N, K, (const float*)dz, (const float*)x, ldx, gW, partial);
 }
 
-size_t gated_dgrad_scratch_floats(int elt, int M, int N, int K) { return elt == ELT_BF16 ? mfma_gated_dgrad_scratch_floats(M, N, K) : 0; }
+size_t gated_dgrad_scratch_floats(int elt, int M, int N, int K) {
+  return elt == ELT_BF16 ? mfma_gated_dgrad_scratch_floats(M, N, K) : f32_gated_dgrad_scratch_floats(M, N, K);
+}
 size_t gated_wgrad_scratch_floats(int elt, int M, int N, int K) {
-  return elt == ELT_BF16 ? mfma_gated_wgrad_scratch_floats(M, N, K) : wgrad_scratch_floats(elt, M, N, K);
+  return elt == ELT_BF16 ? mfma_gated_wgrad_scratch_floats(M, N, K) : f32_gated_wgrad_scratch_floats(M, N, K);
 }
 
 hipError_t launch_gated_backward(hipStream_t s, int elt, int M, int N, const void* dy, const void* d, const uint8_t* fine, void* dz, float* gb,

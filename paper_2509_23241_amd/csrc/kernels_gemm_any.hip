@@ -266,6 +266,36 @@ struct DenseWhole {
   }
 };
 
+// And for contractions of any length: the k tiles that are whole are copied so, the last one with an address of each lane's own.  Which it
+// is, is known to the whole wave. 
+template <class T, class Sum, int R, int NW, bool COL>
+struct DenseMost : DenseWhole<T, Sum, R, NW, COL> {
+  using Whole = DenseWhole<T, Sum, R, NW, COL>;
+  using Desc = DenseDesc;
+  int K, wave, lane;
+  __device__ __forceinline__ void init(const Desc& d, int r0, int wave_, int lane_) {
+    Whole::init(d, r0, wave_, lane_);
+    K = d.K;
+    wave = wave_;
+    lane = lane_;
+  }
+  struct Tile {
+    const T* at;
+    int left;  // k values from here on
+  };
+  __device__ __forceinline__ Tile tile(int tile) const { return Tile{this->base + tile * this->step, K - tile * kTileK<T>}; }
+  __device__ __forceinline__ void copy(int t, Tile tile, uint32_t lds) const {
+    if (tile.left >= kTileK<T>) {
+      dma16(lds, tile.at, this->off[t]);
+    } else {
+      int r, k;
+      if constexpr (COL) Whole::Col::at(t, wave, lane, r, k);
+      else Whole::Row::at(t, wave, lane, r, k);
+      dma_addr<16>(lds, k < tile.left ? (const char*)tile.at + this->off[t] : zero_chunk());
+    }
+  }
+};
+
 // Quotient and remainder by a divisor known on the host: n * ceil(2^32 / div) >> 32 is exact for every n with
 // n * div < 2^32; mul = 0 where that does not cover the range (or div is 1): a division.
 struct FastDiv {
@@ -1074,6 +1104,18 @@ template <class T, class Sum, int> struct WgradDenseWhole {
   template <int R, int NW> using A = DenseWhole<T, Sum, R, NW, true>;
   template <int R, int NW> using B = DenseWhole<T, Sum, R, NW, true>;
 };
+template <class T, class Sum, int> struct FpropDenseMost {
+  template <int R, int NW> using A = DenseMost<T, Sum, R, NW, false>;
+  template <int R, int NW> using B = DenseMost<T, Sum, R, NW, false>;
+};
+template <class T, class Sum, int> struct DgradDenseMost {
+  template <int R, int NW> using A = DenseMost<T, Sum, R, NW, false>;
+  template <int R, int NW> using B = DenseMost<T, Sum, R, NW, true>;
+};
+template <class T, class Sum, int> struct WgradDenseMost {
+  template <int R, int NW> using A = DenseMost<T, Sum, R, NW, true>;
+  template <int R, int NW> using B = DenseMost<T, Sum, R, NW, true>;
+};
 template <class T, class Sum, int VEC> struct FpropConv {
   template <int R, int NW> using A = GatherRow<T, Sum, R, NW, VEC, false>;
   template <int R, int NW> using B = DenseRow<T, Sum, R, NW, VEC>;
@@ -1087,18 +1129,17 @@ template <class T, class Sum, int VEC> struct WgradConv {
   template <int R, int NW> using B = GatherCol<T, Sum, R, NW, VEC>;
 };
 
-template <class T, class Sum, template <class, class, int> class Product, int VEC, class AD, class BD, class Epi>
-hipError_t run(hipStream_t s, int M, int N, int K, const AD& ad, const BD& bd, const Epi& epi, bool split = false,
-               const SideCopy& side = SideCopy{nullptr, nullptr, 0}) {
+// LARGE: 128 x 128 among them
+template <class T, class Sum, template <class, class, int> class Product, int VEC, bool LARGE, class AD, class BD, class Epi>
+hipError_t run_tiles(Tile tile, int ranges, hipStream_t s, int M, int N, int KT, const AD& ad, const BD& bd, const Epi& epi, const SideCopy& side) {
   using P = Product<T, Sum, VEC>;
-  const int KT = (K + kTileK<T> - 1) / kTileK<T>;
-  int ranges = 1;
 #define TP_ANY(E, WGM, WGN, NS, U)                                                                                           \
   launch_any<T, Sum, E, E, WGM, WGN, NS, U, typename P::template A<E, WGM * WGN>, typename P::template B<E, WGM * WGN>>( \
       s, M, N, KT, ranges, ad, bd, epi, side)
-  switch (pick_tile<T, Sum>(M, N, KT, split, &ranges)) {
+  switch (tile) {
     case Tile::k128:
-      if constexpr (sizeof(T) == 4) return TP_ANY(128, 4, 2, 2, 2);
+      if constexpr (!LARGE) return hipErrorInvalidValue;
+      else if constexpr (sizeof(T) == 4) return TP_ANY(128, 4, 2, 2, 2);
       else if constexpr (__is_same(Sum, Free)) return TP_ANY(128, 4, 2, 3, 1);
       [[fallthrough]];  // not among those tiles
     case Tile::k64: return TP_ANY(64, 4, 2, 2, 2);
@@ -1108,6 +1149,14 @@ hipError_t run(hipStream_t s, int M, int N, int K, const AD& ad, const BD& bd, c
       return TP_ANY(32, 2, 2, 2, 2);
   }
 #undef TP_ANY
+}
+template <class T, class Sum, template <class, class, int> class Product, int VEC, class AD, class BD, class Epi>
+hipError_t run(hipStream_t s, int M, int N, int K, const AD& ad, const BD& bd, const Epi& epi, bool split = false,
+               const SideCopy& side = SideCopy{nullptr, nullptr, 0}) {
+  const int KT = (K + kTileK<T> - 1) / kTileK<T>;
+  int ranges = 1;
+  const Tile tile = pick_tile<T, Sum>(M, N, KT, split, &ranges);
+  return run_tiles<T, Sum, Product, VEC, true>(tile, ranges, s, M, N, KT, ad, bd, epi, side);
 }
 template <class T, class Sum>
 int ranges_of(int M, int N, int K) {
@@ -1123,9 +1172,9 @@ inline bool whole_tiles(int K, int ld) { return K % kTileK<float> == 0 && ld < (
 
 // ---- dense, fp32 -------------------------------------------------------------------------------
 namespace {
-template <class Epi>
-hipError_t f32_product(hipStream_t s, int M, int N, int K, const float* x, const float* W, float* x_copy, const Epi& e) {
-  SideCopy side{nullptr, nullptr, 0};
+// The copy of its input that a layer keeps: behind the product's tiles, or a launch of its own
+hipError_t f32_input_copy(hipStream_t s, int M, int K, const float* x, float* x_copy, SideCopy* side) {
+  *side = SideCopy{nullptr, nullptr, 0};
   if (x_copy) {
     // Behind the tiles the copy is hidden where one stream runs everything: a step of four micro-batches and two layers takes
     // 7 us less than with launches of its own at every size from 16 KB to 1 MB (32 x 512: 103 and 110 us; pipeline of
@@ -1133,12 +1182,21 @@ hipError_t f32_product(hipStream_t s, int M, int N, int K, const float* x, const
     // one: from process to process 4 us more to 17 us less at 64 KB, 17 us more to 3 us less at 512 KB.  The line lies at
     // 256 KB, in between.
     if (aligned16(x, x_copy) && (size_t)M * K % 4 == 0 && (size_t)M * K <= 65536) {
-      side = SideCopy{(const uint4*)x, (uint4*)x_copy, (size_t)M * K / 4};
+      *side = SideCopy{(const uint4*)x, (uint4*)x_copy, (size_t)M * K / 4};
     } else {
-      const hipError_t e = launch_copy(s, x, x_copy, (size_t)M * K * 4);
-      if (e != hipSuccess) return e;
+      return launch_copy(s, x, x_copy, (size_t)M * K * 4);
     }
   }
+  return hipSuccess;
+}
+}  // namespace
+
+hipError_t f32_fprop(hipStream_t s, int M, int N, int K, const float* x, const float* W, const float* bias, int act, float* d_out,
+                     float* a_out, float* x_copy) {
+  const EpiForward<float> e{bias, d_out, a_out, act, N, N % 4 == 0 && aligned16(d_out, a_out)};
+  SideCopy side;
+  const hipError_t err = f32_input_copy(s, M, K, x, x_copy, &side);
+  if (err != hipSuccess) return err;
   const DenseDesc a{x, K, M, K}, b{W, K, N, K};
   if (aligned16(x, W) && wave_ok(M, N, K, K))
     return launch_wave<WaveRow, WaveRow>(s, M, N, K, x, K, W, K, e, side);
@@ -1146,69 +1204,172 @@ hipError_t f32_product(hipStream_t s, int M, int N, int K, const float* x, const
   if (K % 4 == 0 && aligned16(x, W)) return run<float, Chain, FpropDense, 4>(s, M, N, K, a, b, e, false, side);
   return run<float, Chain, FpropDense, 1>(s, M, N, K, a, b, e, false, side);
 }
-}  // namespace
-
-hipError_t f32_fprop(hipStream_t s, int M, int N, int K, const float* x, const float* W, const float* bias, int act, float* d_out,
-                     float* a_out, float* x_copy) {
-  return f32_product(s, M, N, K, x, W, x_copy, EpiForward<float>{bias, d_out, a_out, act, N, N % 4 == 0 && aligned16(d_out, a_out)});
-}
-
-hipError_t f32_gated_fprop(hipStream_t s, int M, int N, int K, const float* x, const float* W, const float* bias, int act, float* d_out,
-                           float* a_out, float* x_copy) {
-  return f32_product(s, M, N, K, x, W, x_copy, EpiGatedF32{bias, d_out, a_out, act, N, (N + 3) / 4 * 4, aligned16(d_out)});
-}
-
-namespace {
-// ldz: values from one row of dz to the next; those behind a row's N hold zeros up to a multiple of four, if ldz is one
-template <class Epi>
-hipError_t f32_dgrad_product(hipStream_t s, int M, int N, int K, const float* dz, int ldz, const float* Wb, const Epi& e) {
-  // out[M x K] = dz[M x N] . Wb[N x K]: contraction over N
-  const DenseDesc a{dz, ldz, M, N}, b{Wb, K, K, N};
-  if (K % 4 == 0 && aligned16(dz, Wb) && wave_ok(M, K, N, std::max(ldz, K)))
-    return launch_wave<WaveRow, WaveCol>(s, M, K, N, dz, ldz, Wb, K, e);
-  if (whole_tiles(N, std::max(ldz, K)) && K % 4 == 0 && aligned16(dz, Wb)) return run<float, Chain, DgradDenseWhole, 4>(s, M, K, N, a, b, e);
-  if (ldz % 4 == 0 && K % 4 == 0 && aligned16(dz, Wb)) return run<float, Chain, DgradDense, 4>(s, M, K, N, a, b, e);
-  return run<float, Chain, DgradDense, 1>(s, M, K, N, a, b, e);
-}
-template <class Epi>
-hipError_t f32_wgrad_product(hipStream_t s, int M, int N, int K, const float* dz, int ldz, const float* x, const Epi& e, bool split) {
-  // gW[N x K] = dz^T[N x M] . x[M x K]: contraction over M
-  const bool chunks = ldz % 4 == 0 && K % 4 == 0 && aligned16(dz, x);
-  const DenseDesc a{dz, ldz, chunks ? (N + 3) / 4 * 4 : N, M}, b{x, K, K, M};
-  if (chunks && whole_tiles(M, std::max(ldz, K))) return run<float, Chain, WgradDenseWhole, 4>(s, N, K, M, a, b, e, split);
-  if (chunks) return run<float, Chain, WgradDense, 4>(s, N, K, M, a, b, e, split);
-  return run<float, Chain, WgradDense, 1>(s, N, K, M, a, b, e, split);
-}
-}  // namespace
 
 hipError_t f32_dgrad(hipStream_t s, int M, int N, int K, const float* dz, const float* Wb, const float* d_prev, float* out,
                      int relu_mask, float* sums) {
-  return f32_dgrad_product(s, M, N, K, dz, N, Wb, EpiInputGrad<float>{d_prev, out, K, relu_mask, K % 4 == 0 && aligned16(out), sums});
-}
-
-hipError_t f32_gated_dgrad(hipStream_t s, int M, int N, int K, const float* dz, int ldz, const float* Wb, const float* d_prev, float* out,
-                           int relu_mask, float* sums) {
-  return f32_dgrad_product(s, M, N, K, dz, ldz, Wb, EpiInputGradParts{{d_prev, out, K, relu_mask, K % 4 == 0 && aligned16(out), sums}});
+  // out[M x K] = dz[M x N] . Wb[N x K]: contraction over N
+  const EpiInputGrad<float> e{d_prev, out, K, relu_mask, K % 4 == 0 && aligned16(out), sums};
+  const DenseDesc a{dz, N, M, N}, b{Wb, K, K, N};
+  if (K % 4 == 0 && aligned16(dz, Wb) && wave_ok(M, K, N, std::max(N, K)))
+    return launch_wave<WaveRow, WaveCol>(s, M, K, N, dz, N, Wb, K, e);
+  if (whole_tiles(N, std::max(N, K)) && K % 4 == 0 && aligned16(dz, Wb)) return run<float, Chain, DgradDenseWhole, 4>(s, M, K, N, a, b, e);
+  if (N % 4 == 0 && K % 4 == 0 && aligned16(dz, Wb)) return run<float, Chain, DgradDense, 4>(s, M, K, N, a, b, e);
+  return run<float, Chain, DgradDense, 1>(s, M, K, N, a, b, e);
 }
 
 int f32_wgrad_splits(int M, int N, int K) { return ranges_of<float, Chain>(N, K, M); }
 
 hipError_t f32_wgrad(hipStream_t s, int M, int N, int K, const float* dz, const float* x, float* gW, float* partial) {
   const int splits = partial != nullptr ? f32_wgrad_splits(M, N, K) : 1;
+  const bool split = partial != nullptr;
   float* out = splits > 1 ? partial : gW;
   const EpiPartial e{out, K, K % 4 == 0 && aligned16(out), (size_t)N * K};
-  const hipError_t err = f32_wgrad_product(s, M, N, K, dz, N, x, e, partial != nullptr);
+  // gW[N x K] = dz^T[N x M] . x[M x K]: contraction over M
+  const DenseDesc a{dz, N, N, M}, b{x, K, K, M};
+  const bool chunks = N % 4 == 0 && K % 4 == 0 && aligned16(dz, x);
+  hipError_t err;
+  if (chunks && whole_tiles(M, std::max(N, K))) err = run<float, Chain, WgradDenseWhole, 4>(s, N, K, M, a, b, e, split);
+  else if (chunks) err = run<float, Chain, WgradDense, 4>(s, N, K, M, a, b, e, split);
+  else err = run<float, Chain, WgradDense, 1>(s, N, K, M, a, b, e, split);
   if (err != hipSuccess || splits == 1) return err;
   return launch_sum_partials(s, (size_t)N * K, splits, partial, gW);
 }
 
-hipError_t f32_gated_wgrad(hipStream_t s, int M, int N, int K, const float* dz, int ldz, const float* x, float* gW, float* partial) {
-  const int splits = partial != nullptr ? f32_wgrad_splits(M, N, K) : 1;
-  float* out = splits > 1 ? partial : gW;
+// ---- the gated layer, fp32 ----------------------------------------------------------------------
+namespace {
+// Tiles and contraction ranges of its products: the least time, with the partial results written and read again at 4.5 TB/s and a launch for
+// them.  ns: a k tile on a CU with one workgroup and with two, measured on these products, which sum in parts and are short (chains of long
+// products, above, take 10 to 30 % less).  1332 rows, 512 x 1365: input gradient 49 us in tiles of 32 x 32, 55 of 64 x 64, 39 + 5 of those over three
+// ranges, 49 + 5 of 128 x 128 over five; weight gradient 49, 51 and, over two, 43.  300 rows, 1500 x 2000: input gradient 55, 74 and, over four, 42 + 5.
+struct GatedRanges {
+  Tile tile;
+  int ranges;
+};
+GatedRanges gated_ranges(int M, int N, int contraction, int most) {
+  constexpr struct { Tile tile; int edge, one, two; } kCosts[] = {{Tile::k32, 32, 290, 450}, {Tile::k64, 64, 700, 1350}};
+  const int KT = (contraction + kTileK<float> - 1) / kTileK<float>;
+  GatedRanges best{Tile::k32, 1};
+  double best_ns = -1;
+  for (const auto& c : kCosts)
+    for (int r = 1; r <= most && (r == 1 || r * 8 <= KT); ++r) {
+      const int per = (KT + r - 1) / r;
+      if ((KT + per - 1) / per != r) continue;  // a range would be empty
+      const long all = blocks_of(c.edge, M, N) * r, rest = all % 512;
+      double ns = ((double)(all / 512) * c.two + (rest == 0 ? 0 : rest <= 256 ? c.one : c.two)) * per;
+      if (r > 1) ns += 3000 + (r + 1) * 4.0 * M * N / 4500;
+      if (best_ns < 0 || ns < best_ns) {
+        best_ns = ns;
+        best = GatedRanges{c.tile, r};
+      }
+    }
+  return best;
+}
+constexpr int kGatedRanges = 16;
+inline int pitch4(int n) { return (n + 3) / 4 * 4; }
+
+__global__ __launch_bounds__(256) void pad_rows_f32_kernel(size_t units, int cols, int pitch, const float* __restrict__ src, float* __restrict__ dst) {
+  const int per_row = pitch / 4;
+  for (size_t u = (size_t)blockIdx.x * 256 + threadIdx.x; u < units; u += (size_t)gridDim.x * 256) {
+    const size_t row = u / per_row;
+    const int col = (int)(u - row * per_row) * 4;
+    float v[4];
+#pragma unroll
+    for (int j = 0; j < 4; ++j) v[j] = col + j < cols ? src[row * cols + col + j] : 0.f;
+    *reinterpret_cast<float4*>(dst + row * pitch + col) = make_float4(v[0], v[1], v[2], v[3]);
+  }
+}
+// Gradient of x from the partial sums of `ranges` contraction ranges
+__global__ __launch_bounds__(256) void f32_dgrad_ranges_kernel(size_t count, int ranges, const float* __restrict__ partial,
+                                                               const float* __restrict__ d_prev, int relu_mask, float* __restrict__ out) {
+  for (size_t i = (size_t)blockIdx.x * 256 + threadIdx.x; i < count; i += (size_t)gridDim.x * 256) {
+    float s = 0.f;
+#pragma unroll 8
+    for (int r = 0; r < ranges; ++r) s += partial[(size_t)r * count + i];
+    if (d_prev) s = relu_mask ? (d_prev[i] > 0.f ? s : 0.f) : s * d_prev[i];
+    out[i] = s;
+  }
+}
+// rows of whole 16-byte units, 128 of which lie within 2 GiB
+inline bool unit_rows(int ld) { return ld % 4 == 0 && ld < (1 << 22); }
+}  // namespace
+
+hipError_t f32_pad_rows(hipStream_t s, size_t rows, int cols, const float* src, float* dst) {
+  const size_t units = rows * (pitch4(cols) / 4);
+  hipLaunchKernelGGL(pad_rows_f32_kernel, dim3((unsigned)std::min<size_t>((units + 255) / 256, 8192)), dim3(256), 0, s, units, cols, pitch4(cols), src, dst);
+  return hipGetLastError();
+}
+bool f32_gated_padded(int M, int N, int K) { return K % 4 != 0 && M >= 256 && unit_rows(pitch4(K)); }
+
+hipError_t f32_gated_fprop(hipStream_t s, int M, int N, int K, const float* x, const float* W, const float* bias, int act, float* d_out,
+                           float* a_out, float* x_copy) {
+  const EpiGatedF32 e{bias, d_out, a_out, act, N, pitch4(N), aligned16(d_out)};
+  SideCopy side;
+  const hipError_t err = f32_input_copy(s, M, K, x, x_copy, &side);
+  if (err != hipSuccess) return err;
+  const DenseDesc a{x, K, M, K}, b{W, K, N, K};
+  if (aligned16(x, W) && wave_ok(M, N, K, K)) return launch_wave<WaveRow, WaveRow>(s, M, N, K, x, K, W, K, e, side);
+  const Tile tile = gated_ranges(M, N, K, 1).tile;
+  const int KT = (K + 31) / 32;
+  if (unit_rows(K) && aligned16(x, W)) return run_tiles<float, Chain, FpropDenseMost, 4, false>(tile, 1, s, M, N, KT, a, b, e, side);
+  return run_tiles<float, Chain, FpropDense, 1, false>(tile, 1, s, M, N, KT, a, b, e, side);
+}
+
+size_t f32_gated_dgrad_scratch_floats(int M, int N, int K) {
+  const int ranges = gated_ranges(M, K, N, kGatedRanges).ranges;
+  return ranges > 1 ? (size_t)ranges * M * K : 0;
+}
+
+hipError_t f32_gated_dgrad(hipStream_t s, int M, int N, int K, const float* dz, const float* Wb, int ldw, const float* d_prev, float* out,
+                           int relu_mask, float* sums, int* sum_rows, float* partial) {
+  // out[M x K] = dz[M x N] . Wb[N x K]: contraction over N; a row of dz ends in zeros up to whole units
+  const int ldz = pitch4(N);
+  const DenseDesc a{dz, ldz, M, N}, b{Wb, ldw, ldw, N};
+  const bool units = unit_rows(ldz) && unit_rows(ldw) && aligned16(dz, Wb);
+  const GatedRanges plan = gated_ranges(M, K, N, kGatedRanges);
+  const int KT = (N + 31) / 32;
+  const SideCopy none{nullptr, nullptr, 0};
+  const bool wave = ldw == K && units && wave_ok(M, K, N, std::max(ldz, K));
+  if (sums) *sum_rows = 0;
+  if (plan.ranges > 1 && units && !wave) {
+    const EpiPartialParts e{{partial, K, K % 4 == 0 && aligned16(partial), (size_t)M * K}};
+    const hipError_t err = run_tiles<float, Chain, DgradDenseMost, 4, false>(plan.tile, plan.ranges, s, M, K, KT, a, b, e, none);
+    if (err != hipSuccess) return err;
+    const size_t count = (size_t)M * K;
+    hipLaunchKernelGGL(f32_dgrad_ranges_kernel, dim3((unsigned)std::min<size_t>((count + 255) / 256, 4096)), dim3(256), 0, s, count, plan.ranges,
+                       partial, d_prev, relu_mask, out);
+    return hipGetLastError();
+  }
+  EpiInputGradParts e{{d_prev, out, K, relu_mask, K % 4 == 0 && aligned16(out), nullptr}};
+  if (sums) {
+    *sum_rows = dgrad_sum_rows(ELT_F32, M, K);
+    if (*sum_rows) e.sums = sums;
+  }
+  if (wave) return launch_wave<WaveRow, WaveCol>(s, M, K, N, dz, ldz, Wb, K, e);
+  if (units) return run_tiles<float, Chain, DgradDenseMost, 4, false>(plan.tile, 1, s, M, K, KT, a, b, e, none);
+  return run_tiles<float, Chain, DgradDense, 1, false>(plan.tile, 1, s, M, K, KT, a, DenseDesc{Wb, ldw, K, N}, e, none);
+}
+
+size_t f32_gated_wgrad_scratch_floats(int M, int N, int K) {
+  const int ranges = gated_ranges(N, K, M, kGatedRanges).ranges;
+  return ranges > 1 ? (size_t)ranges * N * K : 0;
+}
+
+hipError_t f32_gated_wgrad(hipStream_t s, int M, int N, int K, const float* dz, const float* x, int ldx, float* gW, float* partial) {
+  // gW[N x K] = dz^T[N x M] . x[M x K]: contraction over M
+  const int ldz = pitch4(N);
+  const GatedRanges plan = gated_ranges(N, K, M, kGatedRanges);
+  const int ranges = partial ? plan.ranges : 1;
+  const SideCopy none{nullptr, nullptr, 0};
+  float* out = ranges > 1 ? partial : gW;
   const EpiPartialParts e{{out, K, K % 4 == 0 && aligned16(out), (size_t)N * K}};
-  const hipError_t err = f32_wgrad_product(s, M, N, K, dz, ldz, x, e, partial != nullptr);
-  if (err != hipSuccess || splits == 1) return err;
-  return launch_sum_partials(s, (size_t)N * K, splits, partial, gW);
+  const int KT = (M + 31) / 32;
+  hipError_t err;
+  if (unit_rows(ldz) && unit_rows(ldx) && aligned16(dz, x))
+    err = run_tiles<float, Chain, WgradDenseMost, 4, false>(plan.tile, ranges, s, N, K, KT, DenseDesc{dz, ldz, ldz, M}, DenseDesc{x, ldx, ldx, M}, e, none);
+  else
+    err = run_tiles<float, Chain, WgradDense, 1, false>(plan.tile, ranges, s, N, K, KT, DenseDesc{dz, ldz, N, M}, DenseDesc{x, ldx, K, M}, e, none);
+  if (err != hipSuccess || ranges == 1) return err;
+  return launch_sum_partials(s, (size_t)N * K, ranges, partial, gW);
 }
 
 // ---- convolutions ------------------------------------------------------------------------------
