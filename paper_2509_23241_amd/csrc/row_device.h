@@ -12,16 +12,17 @@ namespace {
 
 constexpr float kLog2e = 1.4426950408889634f;
 
-// The threads of a row: a wave, or a whole workgroup.
+// The threads of a row: a quarter or half of a wave, a wave, or a whole workgroup.
 template <int NT>
 struct Team {
-  static constexpr int kRows = NT == 64 ? 4 : 1;         // rows of a workgroup
-  static constexpr int kThreads = NT == 64 ? 256 : NT;
-  static __device__ __forceinline__ int thread() { return NT == 64 ? threadIdx.x & 63 : threadIdx.x; }
-  static __device__ __forceinline__ int which() { return NT == 64 ? threadIdx.x >> 6 : 0; }
+  static_assert(NT >= 16, "lanes of a row of 16 meet by rotations of it");
+  static constexpr int kRows = NT <= 64 ? 256 / NT : 1;  // rows of a workgroup
+  static constexpr int kThreads = NT <= 64 ? 256 : NT;
+  static __device__ __forceinline__ int thread() { return NT <= 64 ? threadIdx.x & (NT - 1) : threadIdx.x; }
+  static __device__ __forceinline__ int which() { return NT <= 64 ? threadIdx.x / NT : 0; }
   // what the others have written to LDS and memory is there
   static __device__ __forceinline__ void sync() {
-    if constexpr (NT == 64) {
+    if constexpr (NT <= 64) {
       __builtin_amdgcn_fence(__ATOMIC_RELEASE, "wavefront");
       __builtin_amdgcn_wave_barrier();
       __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "wavefront");
@@ -32,7 +33,7 @@ struct Team {
   // sm: NT / 64 floats, free on both sides
   template <class Op>
   static __device__ __forceinline__ float over(float v, float* sm, const Op& op) {
-    v = over_lanes<32>(v, op);
+    v = over_lanes<(NT < 64 ? NT / 2 : 32)>(v, op);
     if constexpr (NT > 64) {
       if ((threadIdx.x & 63) == 0) sm[threadIdx.x >> 6] = v;
       __syncthreads();

@@ -173,7 +173,8 @@ int check_desc(const tp_stage_desc* d) {
       in_e = (uint64_t)L.geom[0] * L.in_features;
       out_e = (uint64_t)L.geom[0] * L.out_features;
       if (2 * out_e > (1u << 30)) return fail(TP_EINVAL, "layer %d: sample too large", l);
-      if ((int64_t)d->mb * d->n * L.geom[0] > INT32_MAX) return fail(TP_EINVAL, "layer %d: mini-batch too large", l);
+      // tiles of 32 rows and up, 256 threads each: fewer than 2^32 of them in a launch
+      if ((int64_t)d->mb * d->n * L.geom[0] > (1 << 28)) return fail(TP_EINVAL, "layer %d: more than 2^28 token positions in a mini-batch", l);
     } else if (L.type == TP_LAYER_ROTARY) {
       const int64_t all = (int64_t)L.geom[1] + 2 * (int64_t)L.geom[2];
       if (L.geom[0] < 1 || L.geom[1] < 1 || L.geom[2] < 1 || all > L.in_features || L.in_features % all != 0 ||

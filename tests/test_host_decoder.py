@@ -137,3 +137,10 @@ def test_loss_refusals():
             call(st)
         assert e.value.code == B.TP_EINVAL
     B.stage_destroy(st)
+
+
+def test_rows_of_a_gated_layer():
+    _query([("gated", 1, 1, "silu", 1 << 20)], mb=256, n=1)
+    with pytest.raises(B.StageLibError) as e:
+        _query([("gated", 1, 1, "silu", (1 << 20) + 1)], mb=256, n=1)
+    assert e.value.code == B.TP_EINVAL
