@@ -12,7 +12,6 @@
 #include "device_utils.h"
 #include "kernels.h"
 #include "rotary.h"
-#include "row_device.h"
 
 namespace tp {
 
@@ -64,7 +63,7 @@ __global__ __launch_bounds__(kThreads) void rotary_any_kernel(Rotary r, RotarySp
   }
 }
 
-// ---- heads and their parts in whole 16-byte units ------------------------------------------------
+// ---- heads and their parts in whole units of 16 or 8 bytes -------------------------------------
 // A workgroup takes some tokens: sines and cosines go into LDS, one or a few a thread, while the first units are on their way; every
 // thread then turns several items at a time, all of them loaded before the first is used.  An item is two units of halves, whose values are
 // pairs across them, or one unit of neighbours.  What is not turned is copied likewise where the output lies elsewhere.  Value by value
@@ -80,17 +79,50 @@ struct RotaryShape {
 // n / d by the multiplier of divisor(d), exact for n * d < 2^32
 inline uint32_t divisor(int d) { return d <= 1 ? 0u : (uint32_t)(((1ull << 32) + d - 1) / d); }
 __device__ __forceinline__ int divided(int n, uint32_t mul) { return mul ? (int)__umulhi((uint32_t)n, mul) : n; }
-constexpr int kMaxTokens = 8;
+constexpr int kTurns = 1024;  // pairs of a workgroup's tokens
 
-template <typename T, bool HALVES, bool COPY>
+// (an array of uint4 written under a condition stays in memory)
+template <int BYTES>
+struct UnitOf {
+  typedef uint32_t kept __attribute__((ext_vector_type(BYTES / 4)));
+  typedef std::conditional_t<BYTES == 16, uint4, uint2> type;
+};
+template <typename T, int BYTES>
+__device__ __forceinline__ void values_of(const typename UnitOf<BYTES>::type& u, float (&v)[BYTES / sizeof(T)]) {
+#pragma unroll
+  for (int i = 0; i < BYTES / 4; ++i) {
+    const uint32_t w = reinterpret_cast<const uint32_t*>(&u)[i];
+    if constexpr (sizeof(T) == 2) {
+      v[2 * i] = __uint_as_float(w << 16);
+      v[2 * i + 1] = __uint_as_float(w & 0xffff0000u);
+    } else {
+      v[i] = __uint_as_float(w);
+    }
+  }
+}
+template <typename T, int BYTES>
+__device__ __forceinline__ typename UnitOf<BYTES>::type unit_of(const float (&v)[BYTES / sizeof(T)]) {
+  uint32_t w[BYTES / 4];
+#pragma unroll
+  for (int i = 0; i < BYTES / 4; ++i) {
+    if constexpr (sizeof(T) == 2) w[i] = pack_bf16x2(v[2 * i], v[2 * i + 1]);
+    else w[i] = __float_as_uint(v[i]);
+  }
+  if constexpr (BYTES == 16) return make_uint4(w[0], w[1], w[2], w[3]);
+  else return make_uint2(w[0], w[1]);
+}
+
+template <typename T, int BYTES, bool HALVES, bool COPY>
 __global__ __launch_bounds__(kThreads) void rotary_units_kernel(Rotary r, RotaryShape sh, RotarySpeeds speeds, bool back, const T* x, T* out) {
-  constexpr int V = kVec<T>, ITEMS = HALVES ? 4 : 8;
-  __shared__ float2 turn[kMaxTokens * kMaxRotaryPairs];
+  using unit_t = typename UnitOf<BYTES>::type;
+  using kept_t = typename UnitOf<BYTES>::kept;
+  constexpr int V = BYTES / sizeof(T), ITEMS = HALVES ? 4 : 8;
+  __shared__ float2 turn[kTurns];
   const int half = r.rotated / 2;
   const long token0 = (long)blockIdx.x * sh.tokens;
   const int tokens = (int)min((long)sh.tokens, (long)r.seqs * r.S - token0);
-  const uint4* from = reinterpret_cast<const uint4*>(x) + token0 * sh.units;
-  uint4* to = reinterpret_cast<uint4*>(out) + token0 * sh.units;
+  const unit_t* from = reinterpret_cast<const unit_t*>(x) + token0 * sh.units;
+  unit_t* to = reinterpret_cast<unit_t*>(out) + token0 * sh.units;
   // what is copied: a batch of it is under way while the turns are made, the rest follows them
   const int values = sh.units - r.turned * sh.head_units, copies = COPY ? tokens * (values + r.turned * sh.rest) : 0;
   auto copied = [&](int i) {
@@ -98,18 +130,17 @@ __global__ __launch_bounds__(kThreads) void rotary_units_kernel(Rotary r, Rotary
     return token * sh.units + (u < values ? r.turned * sh.head_units + u : (head + 1) * sh.head_units - sh.rest + u - values - head * sh.rest);
   };
   constexpr int BATCH = COPY ? 4 : 1;
-  typedef uint32_t unit_t __attribute__((ext_vector_type(4)));  // (an array of uint4 written under a condition stays in memory)
-  unit_t kept[BATCH];
+  kept_t kept[BATCH];
   if constexpr (COPY) {
 #pragma unroll
     for (int k = 0; k < BATCH; ++k) {
       const int i = k * kThreads + (int)threadIdx.x;
-      kept[k] = i < copies ? *reinterpret_cast<const unit_t*>(from + copied(i)) : unit_t{0, 0, 0, 0};
+      kept[k] = i < copies ? *reinterpret_cast<const kept_t*>(from + copied(i)) : kept_t(0);
     }
   }
   const int items = tokens * r.turned * sh.items, other = half / V;
   for (int i0 = 0; i0 < items; i0 += kThreads * ITEMS) {
-    uint4 a[ITEMS], b[HALVES ? ITEMS : 1];
+    unit_t a[ITEMS], b[HALVES ? ITEMS : 1];
     int unit[ITEMS], at[ITEMS];
 #pragma unroll
     for (int k = 0; k < ITEMS; ++k) {
@@ -134,17 +165,17 @@ __global__ __launch_bounds__(kThreads) void rotary_units_kernel(Rotary r, Rotary
     for (int k = 0; k < ITEMS; ++k) {
       if (i0 + k * kThreads + (int)threadIdx.x < items) {
         float u[V], p[V];
-        unpack<T>(a[k], u);
+        values_of<T, BYTES>(a[k], u);
         if constexpr (HALVES) {
           float v[V], q[V];
-          unpack<T>(b[k], v);
+          values_of<T, BYTES>(b[k], v);
 #pragma unroll
           for (int e = 0; e < V; ++e) {
             const float2 t = turn[at[k] + e];
             p[e] = u[e] * t.x - v[e] * t.y;
             q[e] = u[e] * t.y + v[e] * t.x;
           }
-          to[unit[k] + other] = pack<T>(q);
+          to[unit[k] + other] = unit_of<T, BYTES>(q);
         } else {
 #pragma unroll
           for (int e = 0; e < V; e += 2) {
@@ -153,7 +184,7 @@ __global__ __launch_bounds__(kThreads) void rotary_units_kernel(Rotary r, Rotary
             p[e + 1] = u[e] * t.y + u[e + 1] * t.x;
           }
         }
-        to[unit[k]] = pack<T>(p);
+        to[unit[k]] = unit_of<T, BYTES>(p);
       }
     }
   }
@@ -161,7 +192,7 @@ __global__ __launch_bounds__(kThreads) void rotary_units_kernel(Rotary r, Rotary
 #pragma unroll
     for (int k = 0; k < BATCH; ++k) {
       const int i = k * kThreads + (int)threadIdx.x;
-      if (i < copies) *reinterpret_cast<unit_t*>(to + copied(i)) = kept[k];
+      if (i < copies) *reinterpret_cast<kept_t*>(to + copied(i)) = kept[k];
     }
     for (int i = BATCH * kThreads + (int)threadIdx.x; i < copies; i += kThreads) {
       const int u = copied(i);
@@ -170,20 +201,21 @@ __global__ __launch_bounds__(kThreads) void rotary_units_kernel(Rotary r, Rotary
   }
 }
 
-// Rotary layers whose parts of heads are whole units at 16-byte addresses; false: others, and tokens of too many units for the divisions.
-template <typename T>
+// Rotary layers whose parts of heads are whole units at their addresses; false: others, and tokens of too many units for the divisions.
+template <typename T, int BYTES>
 bool launch_units(hipStream_t s, const Rotary& r, const RotarySpeeds& speeds, bool back, const T* x, T* out) {
-  constexpr int V = kVec<T>;
+  constexpr int V = BYTES / sizeof(T);
   const int half = r.rotated / 2;
-  if (r.dh % V || (r.halves ? half : r.rotated) % V || (((uintptr_t)x | (uintptr_t)out) & 15)) return false;
-  if ((long)r.all * r.dh / V * kMaxTokens * std::max(r.all, r.dh / V) >= (1l << 31)) return false;
-  const long all = (long)r.seqs * r.S;
-  RotaryShape sh;
-  sh.head_units = r.dh / V;
-  sh.units = r.all * sh.head_units;
+  if (r.dh % V || (r.halves ? half : r.rotated) % V || (((uintptr_t)x | (uintptr_t)out) & (BYTES - 1))) return false;
+  const long all = (long)r.seqs * r.S, units = (long)r.all * r.dh / V;
   // Four units a thread, as long as that leaves every CU two workgroups.  8192 tokens of 768 units, both ways with the values copied: 79 us with one token a
   // workgroup (403 MB, at 5.1 TB/s the rate of a copy), 95 with two, 112 with four; 3108 tokens of 200 units 15.4 with five, 22 with one.
-  sh.tokens = (int)std::min<long>(kMaxTokens, std::max<long>(1, std::min<long>(all / 512, 1024 / sh.units)));
+  const long tokens = std::max<long>(1, std::min({all / 512, 1024 / units, (long)kTurns / half}));
+  if ((tokens * units + 8 * kThreads) * units >= (1l << 32)) return false;
+  RotaryShape sh;
+  sh.tokens = (int)tokens;
+  sh.units = (int)units;
+  sh.head_units = r.dh / V;
   sh.items = (r.halves ? half : r.rotated) / V;
   sh.rest = (r.dh - r.rotated) / V;
   const int copies = sh.units - r.turned * sh.head_units + r.turned * sh.rest;
@@ -191,9 +223,10 @@ bool launch_units(hipStream_t s, const Rotary& r, const RotarySpeeds& speeds, bo
   sh.by_turned = divisor(r.turned);
   sh.by_copies = divisor(copies);
   sh.by_rest = divisor(sh.rest);
-  const dim3 grid((unsigned)((all + sh.tokens - 1) / sh.tokens));
   auto go = [&](auto halves, auto copy) {
-    hipLaunchKernelGGL((rotary_units_kernel<T, decltype(halves)::value, decltype(copy)::value>), grid, dim3(kThreads), 0, s, r, sh, speeds, back, x, out);
+    // (a workgroup with a token or a thousand units has 4 KB and more: the 2^24 that a launch takes have more than there is)
+    hipLaunchKernelGGL((rotary_units_kernel<T, BYTES, decltype(halves)::value, decltype(copy)::value>), dim3((unsigned)((all + tokens - 1) / tokens)),
+                       dim3(kThreads), 0, s, r, sh, speeds, back, x, out);
   };
   using Yes = std::true_type;
   using No = std::false_type;
@@ -205,7 +238,7 @@ bool launch_units(hipStream_t s, const Rotary& r, const RotarySpeeds& speeds, bo
 
 template <typename T>
 hipError_t launch(hipStream_t s, const Rotary& r, const RotarySpeeds& speeds, bool back, const T* x, T* out) {
-  if (!launch_units<T>(s, r, speeds, back, x, out)) {
+  if (!launch_units<T, 16>(s, r, speeds, back, x, out) && !launch_units<T, 8>(s, r, speeds, back, x, out)) {
     const unsigned blocks = (unsigned)std::min<long>((long)r.seqs * r.S, 1 << 20);
     hipLaunchKernelGGL(rotary_any_kernel<T>, dim3(blocks), dim3(kThreads), 0, s, r, speeds, back, x, out);
   }
