@@ -21,9 +21,8 @@ hipError_t f32_gated_dgrad(hipStream_t s, int M, int N, int K, const float* dz, 
 hipError_t f32_gated_wgrad(hipStream_t s, int M, int N, int K, const float* dz, const float* x, int ldx, float* gW, float* partial);
 size_t f32_gated_dgrad_scratch_floats(int M, int N, int K);
 size_t f32_gated_wgrad_scratch_floats(int M, int N, int K);
-// Whether x and the weights are to be copied into rows of K rounded up to four values, zeros behind them, and that copy.
+// Whether x and the weights are to be copied into rows of K rounded up to four values, zeros behind them.
 bool f32_gated_padded(int M, int N, int K);
-hipError_t f32_pad_rows(hipStream_t s, size_t rows, int cols, const float* src, float* dst);
 // partial: scratch of f32_wgrad_splits(M, N, K) * N * K floats where that is more than one range, or null
 hipError_t f32_wgrad(hipStream_t s, int M, int N, int K, const float* dz, const float* x, float* gW, float* partial);
 int f32_wgrad_splits(int M, int N, int K);

@@ -23,9 +23,8 @@ hipError_t mfma_gated_dgrad(hipStream_t s, int M, int N, int K, const uint16_t* 
 hipError_t mfma_gated_wgrad(hipStream_t s, int M, int N, int K, const uint16_t* dz, const uint16_t* x, int ldx, float* gW, float* partial);
 size_t mfma_gated_dgrad_scratch_floats(int M, int N, int K);
 size_t mfma_gated_wgrad_scratch_floats(int M, int N, int K);
-// Whether x and the weights are to be copied into rows of K rounded up to eight values, and that copy.
+// Whether x and the weights are to be copied into rows of K rounded up to eight values.
 bool mfma_gated_padded(int M, int N, int K);
-hipError_t mfma_pad_rows(hipStream_t s, size_t rows, int cols, const uint16_t* src, uint16_t* dst);
 // out = (dz Wb) (.) d_prev, d_prev = saved act'(z) of the previous layer or null; relu_mask = 1: d_prev holds that layer's
 // ReLU output instead and the factor is (output > 0).
 hipError_t mfma_dgrad(hipStream_t s, int M, int N, int K, const uint16_t* dz, const uint16_t* Wb,

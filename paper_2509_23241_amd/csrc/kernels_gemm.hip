@@ -354,8 +354,47 @@ hipError_t launch_fprop(hipStream_t s, int elt, int M, int N, int K, const void*
 int gated_pitch(int elt, int n) { return elt == ELT_BF16 ? (n + 7) / 8 * 8 : (n + 3) / 4 * 4; }
 bool gated_padded(int elt, int M, int N, int K) { return elt == ELT_BF16 ? mfma_gated_padded(M, N, K) : f32_gated_padded(M, N, K); }
 namespace {
-hipError_t pad_rows(hipStream_t s, int elt, size_t rows, int cols, const void* src, void* dst) {
-  return elt == ELT_BF16 ? mfma_pad_rows(s, rows, cols, (const uint16_t*)src, (uint16_t*)dst) : f32_pad_rows(s, rows, cols, (const float*)src, (float*)dst);
+// A matrix in rows of `pitch` values, whole 16-byte units, zeros behind its columns
+template <typename T>
+struct Padded {
+  const T* src;
+  T* dst;
+  size_t units;  // 0: none
+};
+// One matrix, or two of as many columns one behind the other
+template <typename T>
+__global__ __launch_bounds__(256) void pad_rows_kernel(int cols, int pitch, Padded<T> one, Padded<T> two) {
+  constexpr int V = 16 / sizeof(T);
+  const int per_row = pitch / V;
+  for (size_t i = (size_t)blockIdx.x * 256 + threadIdx.x; i < one.units + two.units; i += (size_t)gridDim.x * 256) {
+    const bool first = i < one.units;
+    const size_t u = first ? i : i - one.units, row = u / per_row;
+    const int col = (int)(u - row * per_row) * V;
+    const T* from = (first ? one.src : two.src) + row * cols + col;
+    T v[V];
+    if (col + V <= cols) {
+      __builtin_memcpy(v, from, 16);
+    } else {
+#pragma unroll
+      for (int j = 0; j < V; ++j) v[j] = col + j < cols ? from[j] : T(0);
+    }
+    uint4 w;
+    __builtin_memcpy(&w, v, 16);
+    *reinterpret_cast<uint4*>((first ? one.dst : two.dst) + row * pitch + col) = w;
+  }
+}
+template <typename T>
+hipError_t pad_rows(hipStream_t s, int cols, int pitch, size_t rows1, const void* src1, void* dst1, size_t rows2, const void* src2, void* dst2) {
+  const size_t per_row = pitch * sizeof(T) / 16, units = (rows1 + rows2) * per_row;
+  hipLaunchKernelGGL(pad_rows_kernel<T>, dim3((unsigned)std::min<size_t>((units + 255) / 256, 8192)), dim3(256), 0, s, cols, pitch,
+                     Padded<T>{(const T*)src1, (T*)dst1, rows1 * per_row}, Padded<T>{(const T*)src2, (T*)dst2, rows2 * per_row});
+  return hipGetLastError();
+}
+hipError_t pad_rows(hipStream_t s, int elt, int cols, size_t rows1, const void* src1, void* dst1, size_t rows2 = 0, const void* src2 = nullptr,
+                    void* dst2 = nullptr) {
+  const int pitch = gated_pitch(elt, cols);
+  return elt == ELT_BF16 ? pad_rows<uint16_t>(s, cols, pitch, rows1, src1, dst1, rows2, src2, dst2)
+                         : pad_rows<float>(s, cols, pitch, rows1, src1, dst1, rows2, src2, dst2);
 }
 }  // namespace
 
@@ -363,8 +402,7 @@ hipError_t launch_gated_fprop(hipStream_t s, int elt, int M, int N, int K, const
                               void* d_out, uint8_t* fine, void* a_out, void* x_copy, int spread, void* x_pad, void* w_pad) {
   if (x_pad) {
     hipError_t err = x_copy ? launch_copy(s, x, x_copy, (size_t)M * K * (elt == ELT_BF16 ? 2 : 4)) : hipSuccess;
-    if (err == hipSuccess) err = pad_rows(s, elt, M, K, x, x_pad);
-    if (err == hipSuccess) err = pad_rows(s, elt, N, K, W, w_pad);
+    if (err == hipSuccess) err = pad_rows(s, elt, K, M, x, x_pad, N, W, w_pad);
     if (err != hipSuccess) return err;
     x = x_pad;
     W = w_pad;
@@ -381,7 +419,7 @@ hipError_t launch_gated_dgrad(hipStream_t s, int elt, int M, int N, int K, const
                               void* out, int relu_mask, float* sums, int* sum_rows, float* partial) {
   int ldw = K;
   if (w_pad) {
-    const hipError_t err = pad_rows(s, elt, N, K, Wb, w_pad);
+    const hipError_t err = pad_rows(s, elt, K, N, Wb, w_pad);
     if (err != hipSuccess) return err;
     Wb = w_pad;
     ldw = gated_pitch(elt, K);

@@ -1244,12 +1244,12 @@ namespace {
 struct GatedRanges {
   Tile tile;
   int ranges;
+  double ns;
 };
 GatedRanges gated_ranges(int M, int N, int contraction, int most) {
   constexpr struct { Tile tile; int edge, one, two; } kCosts[] = {{Tile::k32, 32, 290, 450}, {Tile::k64, 64, 700, 1350}};
   const int KT = (contraction + kTileK<float> - 1) / kTileK<float>;
-  GatedRanges best{Tile::k32, 1};
-  double best_ns = -1;
+  GatedRanges best{Tile::k32, 1, -1};
   for (const auto& c : kCosts)
     for (int r = 1; r <= most && (r == 1 || r * 8 <= KT); ++r) {
       const int per = (KT + r - 1) / r;
@@ -1257,27 +1257,13 @@ GatedRanges gated_ranges(int M, int N, int contraction, int most) {
       const long all = blocks_of(c.edge, M, N) * r, rest = all % 512;
       double ns = ((double)(all / 512) * c.two + (rest == 0 ? 0 : rest <= 256 ? c.one : c.two)) * per;
       if (r > 1) ns += 3000 + (r + 1) * 4.0 * M * N / 4500;
-      if (best_ns < 0 || ns < best_ns) {
-        best_ns = ns;
-        best = GatedRanges{c.tile, r};
-      }
+      if (best.ns < 0 || ns < best.ns) best = GatedRanges{c.tile, r, ns};
     }
   return best;
 }
-constexpr int kGatedRanges = 16;
+constexpr int kGatedRanges = 32;
 inline int pitch4(int n) { return (n + 3) / 4 * 4; }
 
-__global__ __launch_bounds__(256) void pad_rows_f32_kernel(size_t units, int cols, int pitch, const float* __restrict__ src, float* __restrict__ dst) {
-  const int per_row = pitch / 4;
-  for (size_t u = (size_t)blockIdx.x * 256 + threadIdx.x; u < units; u += (size_t)gridDim.x * 256) {
-    const size_t row = u / per_row;
-    const int col = (int)(u - row * per_row) * 4;
-    float v[4];
-#pragma unroll
-    for (int j = 0; j < 4; ++j) v[j] = col + j < cols ? src[row * cols + col + j] : 0.f;
-    *reinterpret_cast<float4*>(dst + row * pitch + col) = make_float4(v[0], v[1], v[2], v[3]);
-  }
-}
 // Gradient of x from the partial sums of `ranges` contraction ranges
 __global__ __launch_bounds__(256) void f32_dgrad_ranges_kernel(size_t count, int ranges, const float* __restrict__ partial,
                                                                const float* __restrict__ d_prev, int relu_mask, float* __restrict__ out) {
@@ -1293,11 +1279,6 @@ __global__ __launch_bounds__(256) void f32_dgrad_ranges_kernel(size_t count, int
 inline bool unit_rows(int ld) { return ld % 4 == 0 && ld < (1 << 22); }
 }  // namespace
 
-hipError_t f32_pad_rows(hipStream_t s, size_t rows, int cols, const float* src, float* dst) {
-  const size_t units = rows * (pitch4(cols) / 4);
-  hipLaunchKernelGGL(pad_rows_f32_kernel, dim3((unsigned)std::min<size_t>((units + 255) / 256, 8192)), dim3(256), 0, s, units, cols, pitch4(cols), src, dst);
-  return hipGetLastError();
-}
 bool f32_gated_padded(int M, int N, int K) { return K % 4 != 0 && M >= 256 && unit_rows(pitch4(K)); }
 
 hipError_t f32_gated_fprop(hipStream_t s, int M, int N, int K, const float* x, const float* W, const float* bias, int act, float* d_out,
@@ -1328,11 +1309,15 @@ hipError_t f32_gated_dgrad(hipStream_t s, int M, int N, int K, const float* dz, 
   const GatedRanges plan = gated_ranges(M, K, N, kGatedRanges);
   const int KT = (N + 31) / 32;
   const SideCopy none{nullptr, nullptr, 0};
-  const bool wave = ldw == K && units && wave_ok(M, K, N, std::max(ldz, K));
+  // a wave for each 16 x 16 outputs takes 140 ns for a k tile: one row, 512 x 1408 14 -> 6 + 3 us; 188 rows,
+  // 192 x 10304 84 -> 19 + 5
+  const bool wave = ldw == K && units && wave_ok(M, K, N, std::max(ldz, K)) && 140.0 * KT <= plan.ns;
   if (sums) *sum_rows = 0;
-  if (plan.ranges > 1 && units && !wave) {
+  if (plan.ranges > 1 && !wave) {
     const EpiPartialParts e{{partial, K, K % 4 == 0 && aligned16(partial), (size_t)M * K}};
-    const hipError_t err = run_tiles<float, Chain, DgradDenseMost, 4, false>(plan.tile, plan.ranges, s, M, K, KT, a, b, e, none);
+    const hipError_t err =
+        units ? run_tiles<float, Chain, DgradDenseMost, 4, false>(plan.tile, plan.ranges, s, M, K, KT, a, b, e, none)
+              : run_tiles<float, Chain, DgradDense, 1, false>(plan.tile, plan.ranges, s, M, K, KT, a, DenseDesc{Wb, ldw, K, N}, e, none);
     if (err != hipSuccess) return err;
     const size_t count = (size_t)M * K;
     hipLaunchKernelGGL(f32_dgrad_ranges_kernel, dim3((unsigned)std::min<size_t>((count + 255) / 256, 4096)), dim3(256), 0, s, count, plan.ranges,

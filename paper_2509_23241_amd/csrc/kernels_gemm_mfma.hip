@@ -897,14 +897,6 @@ hipError_t mfma_fprop(hipStream_t s, int M, int N, int K, const uint16_t* x, con
 // Its products take the direct-to-LDS kernel whatever the widths: dz has rows of whole 16-byte units, and x and the weights are copied into
 // such rows where theirs are not, zeros behind them.
 namespace {
-__global__ __launch_bounds__(256) void pad_rows_kernel(size_t units, int cols, int pitch, const uint16_t* __restrict__ src, uint16_t* __restrict__ dst) {
-  const int per_row = pitch / 8;
-  for (size_t u = (size_t)blockIdx.x * 256 + threadIdx.x; u < units; u += (size_t)gridDim.x * 256) {
-    const size_t row = u / per_row;
-    const int col = (int)(u - row * per_row) * 8;
-    *reinterpret_cast<uint4*>(dst + row * pitch + col) = load8(src + row * cols + col, cols - col);
-  }
-}
 // Gradient of x from the partial sums of `ranges` contraction ranges
 __global__ __launch_bounds__(256) void dgrad_ranges_kernel(size_t count, int ranges, const float* __restrict__ partial,
                                                            const uint16_t* __restrict__ d_prev, int relu_mask, uint16_t* __restrict__ out) {
@@ -940,12 +932,6 @@ hipError_t run_square(Tile tile, hipStream_t s, int M, int N, int K, const uint1
   return K % DBK ? go(std::true_type{}) : go(std::false_type{});
 }
 }  // namespace
-
-hipError_t mfma_pad_rows(hipStream_t s, size_t rows, int cols, const uint16_t* src, uint16_t* dst) {
-  const size_t units = rows * (pitch8(cols) / 8);
-  hipLaunchKernelGGL(pad_rows_kernel, dim3((unsigned)std::min<size_t>((units + 255) / 256, 8192)), dim3(256), 0, s, units, cols, pitch8(cols), src, dst);
-  return hipGetLastError();
-}
 
 bool mfma_gated_padded(int M, int N, int K) { return K % 8 != 0 && in_reach(std::max(M, N), pitch8(K)) && in_reach(M, pitch8(N)); }
 
