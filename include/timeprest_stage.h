@@ -374,8 +374,9 @@ int stage_loss_policy(tp_stage* st, uint64_t mb_id, const void* logits_dev, cons
  *   loss = mean over pairs of -(1 - label_smoothing) log sigmoid(m) - label_smoothing log sigmoid(-m),  dlogits_dev its gradient.
  * targets_dev: int32[rows]; a negative one (a prompt, padding) or a weight of 0: no term, as above; one past the classes makes the
  * loss, its logp and the gradients of its pair's rows NaN.  weights_dev: float[rows], or NULL: 1 each.  ref_logp_dev: float[n*mb],
- * the reference's s of each sample.  logp_dev: float[rows], receives l (0 where there is no term), or NULL.  logits_dev and
- * dlogits_dev must not overlap.  TP_EINVAL: an odd number of samples, beta outside 0 .. 1e6, label_smoothing outside 0 .. 1. */
+ * the reference's s of each sample.  logp_dev: float[rows], receives l (0 where there is no term); the passes of this call read it
+ * again.  logits_dev and dlogits_dev must not overlap.  TP_EINVAL: an odd number of samples, beta outside 0 .. 1e6, label_smoothing
+ * outside 0 .. 1. */
 int stage_loss_preference(tp_stage* st, uint64_t mb_id, const void* logits_dev, const int32_t* targets_dev, const float* weights_dev,
                           const float* ref_logp_dev, double beta, double label_smoothing, void* dlogits_dev, float* logp_dev,
                           float* loss_dev);

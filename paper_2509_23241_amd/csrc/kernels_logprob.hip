@@ -81,7 +81,7 @@ __device__ __forceinline__ RowStats read_row(const T* lg, int classes, float* sm
   const Exponents e(top);
   float sum = 0.f;
   for (int j = threadIdx.x; j < classes; j += kThreads) sum += __builtin_amdgcn_exp2f(e.power(to_float(lg[j])));
-  return RowStats{top, TM::over(sum, sm, Add()), 0.0};
+  return RowStats{top, TM::over(sum, sm, Add())};
 }
 // slope ([j = id] - softmax(z)_j), or zeros (slope 0: whatever the logits hold)
 template <typename T>
@@ -98,6 +98,15 @@ __device__ __forceinline__ void write_row(const RowStats& r, const T* lg, T* dl,
   }
 }
 
+__device__ __forceinline__ void store_row(const LogprobArgs& a, long row, const RowStats& r, double logp) {
+  const float stored = (float)logp;
+  a.logp[row] = stored;
+  if (a.stats) {
+    a.stats[row] = r;
+    a.logp_rest[row] = float_to_bf16(fabsf(stored) < INFINITY ? (float)(logp - (double)stored) : 0.f);
+  }
+}
+
 template <typename T>
 __global__ __launch_bounds__(kThreads) void logprob_rows_kernel(LogprobArgs a) {
   __shared__ float sm[kThreads / 64];
@@ -105,12 +114,10 @@ __global__ __launch_bounds__(kThreads) void logprob_rows_kernel(LogprobArgs a) {
     const int id = a.ids[row];
     const bool counts = id >= 0 && (!a.weights || a.weights[row] != 0.f);
     const T* lg = (const T*)a.logits + (size_t)row * a.classes;
-    RowStats r{0.f, 1.f, 0.0};
+    RowStats r{0.f, 1.f};
     if (counts) r = read_row(lg, a.classes, sm);
     if (threadIdx.x == 0) {
-      if (counts) r.logp = id < a.classes ? Exponents(r.top).log_probability(to_float(lg[id]), r.sum) : __builtin_nan("");
-      if (a.logp) a.logp[row] = (float)r.logp;
-      if (a.stats) a.stats[row] = r;
+      store_row(a, row, r, !counts ? 0.0 : id < a.classes ? Exponents(r.top).log_probability(to_float(lg[id]), r.sum) : __builtin_nan(""));
     }
   }
 }
@@ -123,7 +130,7 @@ __global__ __launch_bounds__(kThreads) void policy_rows_kernel(PolicyArgs a) {
     const float weight = a.weights ? a.weights[row] : 1.f / (float)a.rows;
     const bool counts = id >= 0 && weight != 0.f, known = id < a.classes;
     const T* lg = (const T*)a.logits + (size_t)row * a.classes;
-    RowStats r{0.f, 1.f, 0.0};
+    RowStats r{0.f, 1.f};
     PolicyTerm t{0.f, 0.f};
     double logp = 0.0;
     if (counts && known) {
@@ -259,7 +266,7 @@ __global__ __launch_bounds__(Team<NT>::kThreads, (kWavesASimd<T, HELD>)) void lo
   const int id = a.ids[row];
   const bool counts = id >= 0 && (!a.weights || a.weights[row] != 0.f);
   const T* lg = (const T*)a.logits + (size_t)row * a.classes;
-  RowStats r{0.f, 1.f, 0.0};
+  RowStats r{0.f, 1.f};
   float z = 0.f;
   if (counts) {
     if (id < a.classes) z = to_float(lg[id]);
@@ -269,9 +276,7 @@ __global__ __launch_bounds__(Team<NT>::kThreads, (kWavesASimd<T, HELD>)) void lo
     r.sum = TM::over(h.exponentials(Exponents(r.top)), sm, Add());
   }
   if (TM::thread() == 0) {
-    if (counts) r.logp = id < a.classes ? Exponents(r.top).log_probability(z, r.sum) : __builtin_nan("");
-    if (a.logp) a.logp[row] = (float)r.logp;
-    if (a.stats) a.stats[row] = r;
+    store_row(a, row, r, !counts ? 0.0 : id < a.classes ? Exponents(r.top).log_probability(z, r.sum) : __builtin_nan(""));
   }
 }
 
@@ -379,26 +384,40 @@ __device__ __forceinline__ double block_sum(double s, double* sm) {
   __syncthreads();
   return s;
 }
-// out = sum of n values, over `by`
-__global__ __launch_bounds__(kSumThreads) void loss_sum_kernel(const float* __restrict__ v, long n, double by, float* __restrict__ out) {
+// out = sum of n values, over `by`: workgroups of 8192 values and up, their sums added up by the one that arrives last, in their order.
+// (128000 values by one workgroup 14 us, by 15 4.6.)
+__global__ __launch_bounds__(kSumThreads) void loss_sum_kernel(const float* __restrict__ v, long n, double by, double* parts, uint32_t* counter,
+                                                               float* __restrict__ out) {
   __shared__ double sm[kSumThreads / 64];
+  __shared__ int finishes;
+  const long step = (long)gridDim.x * kSumThreads;
   double s = 0.0;
-  long i = threadIdx.x;
-  for (; i + 7 * kSumThreads < n; i += 8 * kSumThreads) {  // eight loads on their way
+  long i = (long)blockIdx.x * kSumThreads + threadIdx.x;
+  for (; i + 7 * step < n; i += 8 * step) {  // eight loads on their way
     float x[8];
 #pragma unroll
-    for (int u = 0; u < 8; ++u) x[u] = v[i + u * kSumThreads];
+    for (int u = 0; u < 8; ++u) x[u] = v[i + u * step];
 #pragma unroll
     for (int u = 0; u < 8; ++u) s += (double)x[u];
   }
-  for (; i < n; i += kSumThreads) s += (double)v[i];
+  for (; i < n; i += step) s += (double)v[i];
   s = block_sum(s, sm);
+  if (gridDim.x > 1) {
+    if (threadIdx.x == 0) {
+      __hip_atomic_store(parts + blockIdx.x, s, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+      finishes = last_to_arrive(counter, gridDim.x);
+    }
+    __syncthreads();
+    if (!finishes) return;
+    s = block_sum(threadIdx.x < gridDim.x ? __hip_atomic_load(parts + threadIdx.x, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT) : 0.0, sm);
+  }
   if (threadIdx.x == 0) *out = (float)(s / by);
 }
 
 // A workgroup a pair: the sums of its two sequences, whose rows lie one behind the other, its loss, and what a log probability of either weighs; the
-// mean of the losses by the workgroup that arrives last, where a counter is given.  A thread has four rows on their way at a time: of 2 x 1024 rows
-// each waits once (28736 rows of 592 classes, eight pairs: 9.5 -> 7.1 us).
+// mean of the losses by the workgroup that arrives last, where a counter is given.  What rounding log
+// probabilities to fp32 has left over is added: without it results of 1002 rows of 32003 classes were 4.5e-7 of their norm off, 6e-8 with it.  A thread has
+// four rows on their way at a time (28736 rows of 592 classes, eight pairs: 7 us, row after row 9.5; log probabilities formed again in fp64 11.6).
 __global__ __launch_bounds__(kSumThreads) void preference_pairs_kernel(PreferenceArgs a) {
   __shared__ double sm[kSumThreads / 64];
   for (long pair = blockIdx.x; pair < a.pairs; pair += gridDim.x) {
@@ -408,19 +427,19 @@ __global__ __launch_bounds__(kSumThreads) void preference_pairs_kernel(Preferenc
     double s[2] = {0.0, 0.0};
     for (long i = threadIdx.x; i < rows; i += 4 * kSumThreads) {
       int id[4];
-      float weight[4];
-      double logp[4];
+      float weight[4], logp[4], rest[4];
 #pragma unroll
       for (int u = 0; u < 4; ++u) {
         const size_t row = row0 + std::min(i + u * kSumThreads, rows - 1);
         id[u] = a.targets[row];
         weight[u] = a.weights ? a.weights[row] : 1.f;
-        logp[u] = a.stats[row].logp;
+        logp[u] = a.logp[row];
+        rest[u] = to_float(a.logp_rest[row]);
       }
 #pragma unroll
       for (int u = 0; u < 4; ++u) {
         const long t = i + u * kSumThreads;
-        const double term = t < rows && id[u] >= 0 && weight[u] != 0.f ? (double)weight[u] * logp[u] : 0.0;
+        const double term = t < rows && id[u] >= 0 && weight[u] != 0.f ? (double)weight[u] * ((double)logp[u] + (double)rest[u]) : 0.0;
         if (t < a.tokens) s[0] += term;
         else s[1] += term;
       }
@@ -447,8 +466,9 @@ __global__ __launch_bounds__(kSumThreads) void preference_pairs_kernel(Preferenc
 
 unsigned row_blocks(long rows) { return (unsigned)std::min<long>(rows, 1 << 20); }
 
-hipError_t sum_losses(hipStream_t s, const float* v, long n, double by, float* out) {
-  hipLaunchKernelGGL(loss_sum_kernel, dim3(1), dim3(kSumThreads), 0, s, v, n, by, out);
+hipError_t sum_losses(hipStream_t s, const float* v, long n, double by, double* parts, uint32_t* counter, float* out) {
+  const long blocks = std::max<long>(1, std::min<long>(kSumParts, n / (8 * kSumThreads)));
+  hipLaunchKernelGGL(loss_sum_kernel, dim3((unsigned)blocks), dim3(kSumThreads), 0, s, v, n, by, parts, counter, out);
   return hipGetLastError();
 }
 
@@ -512,15 +532,16 @@ hipError_t policy(hipStream_t s, PolicyArgs a) {
   });
   if (!done) hipLaunchKernelGGL(policy_rows_kernel<T>, dim3(row_blocks(a.rows)), dim3(kThreads), 0, s, a);
   const hipError_t e = hipGetLastError();
-  return e != hipSuccess || counted ? e : sum_losses(s, a.row_loss, a.rows, 1.0, a.loss);
+  return e != hipSuccess || counted ? e : sum_losses(s, a.row_loss, a.rows, 1.0, a.parts, a.counter, a.loss);
 }
 
 template <typename T>
 hipError_t preference(hipStream_t s, PreferenceArgs a) {
   const int rows = 2 * a.pairs * a.tokens;
-  hipError_t e = logprobs<T>(s, LogprobArgs{rows, a.classes, a.logits, a.targets, a.logp, a.stats, a.weights});
+  hipError_t e = logprobs<T>(s, LogprobArgs{rows, a.classes, a.logits, a.targets, a.logp, a.stats, a.logp_rest, a.weights});
   if (e != hipSuccess) return e;
   const bool counted = a.pairs <= kCounted;
+  uint32_t* const counter = a.counter;
   if (!counted) a.counter = nullptr;
   hipLaunchKernelGGL(preference_pairs_kernel, dim3(row_blocks(a.pairs)), dim3(kSumThreads), 0, s, a);
   e = hipGetLastError();
@@ -531,7 +552,7 @@ hipError_t preference(hipStream_t s, PreferenceArgs a) {
   });
   if (!done) hipLaunchKernelGGL(preference_rows_kernel<T>, dim3(row_blocks(rows)), dim3(kThreads), 0, s, a);
   e = hipGetLastError();
-  return e != hipSuccess || counted ? e : sum_losses(s, a.pair_loss, a.pairs, (double)a.pairs, a.loss);
+  return e != hipSuccess || counted ? e : sum_losses(s, a.pair_loss, a.pairs, (double)a.pairs, a.parts, counter, a.loss);
 }
 
 }  // namespace

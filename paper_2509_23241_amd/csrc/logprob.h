@@ -5,22 +5,24 @@
 
 namespace tp {
 
-// What is needed of a row once it has been read: its maximum, the sum of exp(z_j - top), and the log probability of its class before it is
-// rounded to fp32: a sequence's sum of them is the difference that a margin is made of.
+// What is needed of a row once it has been read: its maximum and the sum of exp(z_j - top).
 struct RowStats {
   float top, sum;
-  double logp;
 };
 
 struct LogprobArgs {
   int rows, classes;
   const void* logits;   // [rows x classes] in elt
   const int32_t* ids;   // [rows], negative: no token
-  float* logp;          // [rows], or null
-  RowStats* stats;      // [rows] at 16 bytes, or null
+  float* logp;          // [rows]
+  RowStats* stats;      // [rows], or null
+  uint16_t* logp_rest;  // [rows] with stats: bf16, what rounding logp to fp32 has left over
   const float* weights; // [rows], or null: rows of weight 0 are left out, too
 };
 hipError_t launch_logprobs(hipStream_t s, int elt, const LogprobArgs& a);
+
+// Partial sums of many losses
+constexpr int kSumParts = 64;
 
 struct PolicyArgs {
   int rows, classes;
@@ -34,6 +36,7 @@ struct PolicyArgs {
   void* dlogits;
   float* logp;            // or null
   float* row_loss;        // scratch, [rows]
+  double* parts;          // scratch, [kSumParts]
   uint32_t* counter;      // zero before the launch and after it
   float* loss;
   int first_row = 0;      // of this launch
@@ -48,10 +51,12 @@ struct PreferenceArgs {
   const float* ref_logp;  // [2 pairs]
   double beta, smoothing;
   void* dlogits;
-  float* logp;            // [rows], or null
+  float* logp;            // [rows]
   RowStats* stats;        // scratch, [rows]
+  uint16_t* logp_rest;    // scratch, [rows]
   float* pull;            // scratch, [2 pairs]: what a log probability of the sample weighs in the loss
   float* pair_loss;       // scratch, [pairs]
+  double* parts;          // scratch, [kSumParts]
   uint32_t* counter;      // zero before the launch and after it
   float* loss;
 };

@@ -562,10 +562,12 @@ int make_plan(const tp_stage_desc* d, Plan* p) {
     if (lp.d.type == TP_LAYER_DENSE)
       wg = std::max<uint64_t>(wg, tp::wgrad_scratch_floats(d->dtype, (int)r, lp.d.out_features, lp.d.in_features));
   }
-  // the losses: a float per row, or (pairs of sequences) what a row's second pass needs and three floats per sample
+  // the losses: a float per row, or (pairs of sequences) what a row's second pass needs, two bytes a row and three
+  // floats per sample
   const uint64_t loss_rows = rows * p->layers.back().tokens;
-  const uint64_t loss_floats = p->layers.back().d.type == TP_LAYER_DENSE && rows % 2 == 0 ? loss_rows * (sizeof(tp::RowStats) / 4) + 2 * rows : loss_rows;
-  p->partial_floats = round_up(std::max<uint64_t>({wg, tp::update_scratch_floats(), loss_floats, conv_scratch, norm_scratch}), 64);
+  const uint64_t loss_floats = p->layers.back().d.type == TP_LAYER_DENSE && rows % 2 == 0 ? loss_rows * (sizeof(tp::RowStats) / 4) + (loss_rows + 1) / 2 + 2 * rows : loss_rows;
+  const uint64_t loss_parts = 2 * tp::kSumParts;  // in front of them
+  p->partial_floats = round_up(std::max<uint64_t>({wg, tp::update_scratch_floats(), loss_parts + loss_floats, conv_scratch, norm_scratch}), 64);
   // Every sum of partials the backward pass needs (bias and split weight gradients, scale and shift gradients of the
   // normalisations) is put off to one launch at its end: each keeps partials of its own until then.  Where the line lies is
   // decided by what the sums need at least, so that column sums left by another layer's kernel, which take more rows than a
@@ -1391,7 +1393,7 @@ int stage_logprobs(tp_stage* st, const void* logits_dev, const int32_t* ids_dev,
   if (int rc = join_forwards(st)) return rc;
   ProfScope ps(st, TP_K_LOSS);
   HIP_TRY(tp::launch_logprobs(st->stream, st->desc.dtype,
-                              tp::LogprobArgs{(int)rows, st->plan.layers.back().d.out_features, logits_dev, ids_dev, logp_dev, nullptr, nullptr}));
+                              tp::LogprobArgs{(int)rows, st->plan.layers.back().d.out_features, logits_dev, ids_dev, logp_dev, nullptr, nullptr, nullptr}));
   return TP_OK;
 }
 
@@ -1424,7 +1426,8 @@ int stage_loss_policy(tp_stage* st, uint64_t mb_id, const void* logits_dev, cons
   a.kl_weight = (float)kl_weight;
   a.dlogits = dlogits_dev;
   a.logp = logp_dev;
-  a.row_loss = st->partials();
+  a.parts = (double*)st->partials();
+  a.row_loss = (float*)(a.parts + tp::kSumParts);
   a.counter = st->counter(tp_stage::kCountLoss);
   a.loss = loss_dev;
   ProfScope ps(st, TP_K_LOSS);
@@ -1443,7 +1446,7 @@ int stage_loss_preference(tp_stage* st, uint64_t mb_id, const void* logits_dev, 
   const int samples = st->desc.mb * st->desc.n;
   if (samples % 2) return fail(TP_EINVAL, "pairs of sequences need an even number of samples, not %d", samples);
   if (st->dry) return TP_OK;
-  if (!logits_dev || !targets_dev || !ref_logp_dev || !dlogits_dev || !loss_dev) return fail(TP_EINVAL, "null pointer");
+  if (!logits_dev || !targets_dev || !ref_logp_dev || !dlogits_dev || !logp_dev || !loss_dev) return fail(TP_EINVAL, "null pointer");
   if (int rc = join_forwards(st)) return rc;
   tp::PreferenceArgs a;
   a.pairs = samples / 2;
@@ -1457,9 +1460,11 @@ int stage_loss_preference(tp_stage* st, uint64_t mb_id, const void* logits_dev, 
   a.smoothing = label_smoothing;
   a.dlogits = dlogits_dev;
   a.logp = logp_dev;
-  a.stats = (tp::RowStats*)st->partials();
+  a.parts = (double*)st->partials();
+  a.stats = (tp::RowStats*)(a.parts + tp::kSumParts);
   a.pull = (float*)(a.stats + rows);
   a.pair_loss = a.pull + samples;
+  a.logp_rest = (uint16_t*)(a.pair_loss + a.pairs);
   a.counter = st->counter(tp_stage::kCountLoss);
   a.loss = loss_dev;
   ProfScope ps(st, TP_K_LOSS);
