@@ -144,8 +144,9 @@ __global__ __launch_bounds__(kThreads) void act_backward_colsum_kernel(int M, in
 
 // The backward pass of a gated layer ahead of its products, with the structure of the kernel above over N = 2 F columns: dz of columns 2f
 // and 2f + 1 is dy[f] times what the forward pass kept there.  d and dz have rows of `pitch` values, whole 16-byte units, zeros behind the
-// columns of dz; those of dy and `fine` start anywhere.  A unit takes 16 bytes of d, 8 of dy and in bf16 4 of `fine`, the last one of a row value by
-// value where it is not whole.  8192 x 16384 in bf16 (738 MB): 152 us, the rate of a copy.
+// columns of dz; those of dy and `fine` start anywhere.  A unit takes 16 bytes of d, 8 of dy and in bf16 4 of `fine`, the last one of a row what
+// there is of it.  8192 x 16384 in bf16 (738 MB): 152 us, the rate of a copy;
+// 13558 x 17898 (1.33 GB, rows of dy at odd addresses) 387.
 template <typename T>
 __global__ __launch_bounds__(kThreads) void gated_backward_kernel(int M, int N, ColsumShape cs, const T* __restrict__ dy,
                                                                   const T* __restrict__ d, const uint8_t* __restrict__ fine,
@@ -159,23 +160,35 @@ __global__ __launch_bounds__(kThreads) void gated_backward_kernel(int M, int N, 
   float s[V];
 #pragma unroll
   for (int j = 0; j < V; ++j) s[j] = 0.f;
-  if (col + V <= N) {
+  const int left = min(V, N - col);  // columns of this unit: an even number
+  if (left > 0) {
 #pragma unroll 4
     for (int r = r0 + rsub; r < r1; r += cs.rows_per_iter) {
       const size_t at = (size_t)r * pitch + col, from = ((size_t)r * N + col) / 2;
       const uint4 b = *reinterpret_cast<const uint4*>(d + at);
-      uint2 a;
-      __builtin_memcpy(&a, dy + from, 8);
+      uint2 a = make_uint2(0, 0);
+      uint32_t low = 0;
+      if (left == V) {
+        __builtin_memcpy(&a, dy + from, 8);
+        if constexpr (sizeof(T) == 2) __builtin_memcpy(&low, fine + from, 4);
+      } else {  // (side by side with the other lanes' loads: value by value in a loop of its own it held up the whole launch)
+        T v[V / 2];
+#pragma unroll
+        for (int j = 0; j < V / 2; ++j) {
+          v[j] = 2 * j < left ? dy[from + j] : T(0);
+          if constexpr (sizeof(T) == 2) low |= 2 * j < left ? (uint32_t)fine[from + j] << (8 * j) : 0u;
+        }
+        __builtin_memcpy(&a, v, 8);
+      }
       const uint32_t bw[4] = {b.x, b.y, b.z, b.w};
       uint32_t ow[4];
       if constexpr (sizeof(T) == 2) {
-        uint32_t low;
-        __builtin_memcpy(&low, fine + from, 4);
         const float g[4] = {__uint_as_float(a.x << 16), __uint_as_float(a.x & 0xffff0000u), __uint_as_float(a.y << 16),
                             __uint_as_float(a.y & 0xffff0000u)};
 #pragma unroll
         for (int j = 0; j < 4; ++j) {
           ow[j] = pack_bf16x2(g[j] * joined12(bw[j] << 16, (low >> (8 * j)) & 15u), g[j] * joined12(bw[j] & 0xffff0000u, (low >> (8 * j + 4)) & 15u));
+          if (2 * j >= left) ow[j] = 0;
           s[(2 * j) % V] += __uint_as_float(ow[j] << 16);
           s[(2 * j + 1) % V] += __uint_as_float(ow[j] & 0xffff0000u);
         }
@@ -183,26 +196,13 @@ __global__ __launch_bounds__(kThreads) void gated_backward_kernel(int M, int N, 
         const float g[2] = {__uint_as_float(a.x), __uint_as_float(a.y)};
 #pragma unroll
         for (int j = 0; j < 4; ++j) {
-          const float o = g[j / 2] * __uint_as_float(bw[j]);
+          const float o = j < left ? g[j / 2] * __uint_as_float(bw[j]) : 0.f;
           ow[j] = __float_as_uint(o);
           s[j % V] += o;
         }
       }
       *reinterpret_cast<uint4*>(dz + at) = make_uint4(ow[0], ow[1], ow[2], ow[3]);
     }
-  } else if (col < N) {
-    for (int r = r0 + rsub; r < r1; r += cs.rows_per_iter)
-      for (int j = 0; j < V; ++j) {
-        const size_t at = (size_t)r * pitch + col + j, from = ((size_t)r * N + col + j) / 2;
-        T o = from_float<T>(0.f);
-        if (col + j < N) {
-          float kept = to_float(d[at]);
-          if constexpr (sizeof(T) == 2) kept = joined12(__float_as_uint(kept), (fine[from] >> (4 * (j & 1))) & 15u);
-          o = from_float<T>(to_float(dy[from]) * kept);
-          s[j] += to_float(o);
-        }
-        dz[at] = o;
-      }
   }
 #pragma unroll
   for (int j = 0; j < V; ++j) sm[(rsub * cs.lanes_per_row + lr) * V + j] = s[j];
