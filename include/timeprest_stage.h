@@ -357,7 +357,7 @@ int stage_logprobs(tp_stage* st, const void* logits_dev, const int32_t* ids_dev,
 /* The clipped policy loss at the last stage and its gradient; stands in for stage_loss_softmax_ce.  rows = n*mb * token positions of
  * the (dense) last layer; per row, with l = log softmax(logits)[action], r = exp(l - old_logp), d = ref_logp - l:
  *   row = -min(r A, clip(r, 1 - clip_low, 1 + clip_high) A) + kl_weight * (exp(d) - d - 1),   loss = sum of weight * row
- * (row values in fp32, added up in fp64), dlogits_dev its gradient; where both sides of the minimum are equal it is that of r A.
+ * (row values in fp64), dlogits_dev its gradient; where both sides of the minimum are equal it is that of r A.
  * actions_dev: int32[rows]; a negative one (a prompt, padding) or a weight of 0: no term, and a gradient of 0 whatever the row's
  * logits and other values hold.  An action past the classes makes the loss and its logp NaN; its row has no gradient.
  * old_logp_dev, advantages_dev: float[rows].  weights_dev: float[rows], or NULL: 1 / rows each.  ref_logp_dev: float[rows]; with

@@ -38,36 +38,31 @@ struct Exponents {
   }
 };
 
-// A row's term of the policy loss: its value and what it changes by with the log probability, both times the row's weight.
+// A row's term of the policy loss: its value and what it changes by with the log probability, both times the row's weight.  In fp64, whose
+// instructions take no longer than fp32's here: rows of both signs cancel, and a sum of rows rounded to fp32 was up to six times further off than
+// one of fp32 exponentials.
 struct PolicyTerm {
-  float loss, slope;
+  double loss;
+  float slope;
 };
-__device__ __forceinline__ PolicyTerm policy_term(const PolicyArgs& a, int row, float weight, double logp) {
-  const float advantage = a.advantages[row];
+__device__ __forceinline__ PolicyTerm policy_term(const PolicyArgs& a, int row, double weight, double logp) {
+  const double advantage = (double)a.advantages[row];
   const double moved = logp - (double)a.old_logp[row];
-  // which side of a border the ratio is on is decided before anything is rounded to fp32
-  const bool above = advantage > 0.f && moved > a.log_high, below = advantage < 0.f && moved < a.log_low;
-  const float gain = advantage == 0.f ? 0.f : expf((float)moved) * advantage;
-  PolicyTerm t;
-  t.loss = -(above ? (1.f + a.clip_high) * advantage : below ? (1.f - a.clip_low) * advantage : gain);
-  t.slope = above || below ? 0.f : -gain;
-  if (a.kl_weight > 0.f) {
-    const float x = (float)((double)a.ref_logp[row] - logp), grown = expm1f(x);
-    // exp(x) - 1 - x: its series where the difference would lose more than an ulp or two (x = 1/2: the ninth term is 3e-9 of it)
-    float tail = fmaf(x, 1.f / 362880.f, 1.f / 40320.f);
-    tail = fmaf(x, tail, 1.f / 5040.f);
-    tail = fmaf(x, tail, 1.f / 720.f);
-    tail = fmaf(x, tail, 1.f / 120.f);
-    tail = fmaf(x, tail, 1.f / 24.f);
-    tail = fmaf(x, tail, 1.f / 6.f);
-    tail = fmaf(x, tail, 0.5f);
-    t.loss = fmaf(a.kl_weight, fabsf(x) < 0.5f ? x * x * tail : grown - x, t.loss);
-    t.slope = fmaf(-a.kl_weight, grown, t.slope);
+  const bool above = advantage > 0.0 && moved > a.log_high, below = advantage < 0.0 && moved < a.log_low;
+  const double gain = advantage == 0.0 ? 0.0 : exp(moved) * advantage;
+  double loss = -(above ? (1.0 + a.clip_high) * advantage : below ? (1.0 - a.clip_low) * advantage : gain);
+  double slope = above || below ? 0.0 : -gain;
+  if (a.kl_weight > 0.0) {
+    const double x = (double)a.ref_logp[row] - logp, grown = expm1(x);
+    loss += a.kl_weight * (grown - x);
+    slope -= a.kl_weight * grown;
   }
-  t.loss *= weight;
-  t.slope *= weight;
-  return t;
+  return PolicyTerm{loss * weight, (float)(slope * weight)};
 }
+
+// row losses go as doubles
+__device__ __forceinline__ void publish(double* p, double v) { __hip_atomic_store(p, v, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT); }
+__device__ __forceinline__ double published(const double* p) { return __hip_atomic_load(p, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT); }
 
 // ---- any row, by a workgroup of its own ---------------------------------------------------------
 constexpr int kThreads = 256;
@@ -127,11 +122,11 @@ __global__ __launch_bounds__(kThreads) void policy_rows_kernel(PolicyArgs a) {
   __shared__ float sm[kThreads / 64];
   for (long at = blockIdx.x; at < a.rows; at += gridDim.x) {
     const int row = (int)at, id = a.actions[row];
-    const float weight = a.weights ? a.weights[row] : 1.f / (float)a.rows;
-    const bool counts = id >= 0 && weight != 0.f, known = id < a.classes;
+    const double weight = a.weights ? (double)a.weights[row] : 1.0 / a.rows;
+    const bool counts = id >= 0 && weight != 0.0, known = id < a.classes;
     const T* lg = (const T*)a.logits + (size_t)row * a.classes;
     RowStats r{0.f, 1.f};
-    PolicyTerm t{0.f, 0.f};
+    PolicyTerm t{0.0, 0.f};
     double logp = 0.0;
     if (counts && known) {
       r = read_row(lg, a.classes, sm);
@@ -139,7 +134,7 @@ __global__ __launch_bounds__(kThreads) void policy_rows_kernel(PolicyArgs a) {
       t = policy_term(a, row, weight, logp);
     } else if (counts) {
       logp = __builtin_nan("");
-      t.loss = __builtin_nanf("");
+      t.loss = __builtin_nan("");
     }
     if (threadIdx.x == 0) {
       a.row_loss[row] = t.loss;
@@ -281,7 +276,7 @@ __global__ __launch_bounds__(Team<NT>::kThreads, (kWavesASimd<T, HELD>)) void lo
 }
 
 // The sum of the losses, over `by`, by the workgroup that arrives last, where a counter is given.
-__device__ __forceinline__ void finish_sum(uint32_t* counter, const float* row_loss, int rows, double by, float* loss) {
+__device__ __forceinline__ void finish_sum(uint32_t* counter, const double* row_loss, int rows, double by, float* loss) {
   __shared__ double sums[256];
   __shared__ int finishes;
   if (!counter) return;
@@ -292,7 +287,7 @@ __device__ __forceinline__ void finish_sum(uint32_t* counter, const float* row_l
   if (!finishes) return;
   if (threadIdx.x < 256) {
     double s = 0.0;
-    for (int i = threadIdx.x; i < rows; i += 256) s += (double)published(row_loss + i);
+    for (int i = threadIdx.x; i < rows; i += 256) s += published(row_loss + i);
     sums[threadIdx.x] = s;
   }
   __syncthreads();
@@ -311,12 +306,12 @@ __global__ __launch_bounds__(Team<NT>::kThreads, (kWavesASimd<T, HELD>)) void po
   if (at < a.rows) {
     const int row = (int)at;
     const int id = a.actions[row];
-    const float weight = a.weights ? a.weights[row] : 1.f / (float)a.rows;
-    const bool counts = id >= 0 && weight != 0.f, known = id < a.classes;
+    const double weight = a.weights ? (double)a.weights[row] : 1.0 / a.rows;
+    const bool counts = id >= 0 && weight != 0.0, known = id < a.classes;
     const T* lg = (const T*)a.logits + (size_t)row * a.classes;
     T* dl = (T*)a.dlogits + (size_t)row * a.classes;
     Held<T, NT, HELD> h(lg, a.classes);
-    PolicyTerm t{0.f, 0.f};
+    PolicyTerm t{0.0, 0.f};
     double logp = 0.0;
     if (counts && known) {
       const float z = to_float(lg[id]);
@@ -331,7 +326,7 @@ __global__ __launch_bounds__(Team<NT>::kThreads, (kWavesASimd<T, HELD>)) void po
       }
     } else if (counts) {
       logp = __builtin_nan("");
-      t.loss = __builtin_nanf("");
+      t.loss = __builtin_nan("");
     }
     if (t.slope == 0.f) h.write_zeros(dl);
     if (TM::thread() == 0) {
@@ -386,7 +381,7 @@ __device__ __forceinline__ double block_sum(double s, double* sm) {
 }
 // out = sum of n values, over `by`: workgroups of 8192 values and up, their sums added up by the one that arrives last, in their order.
 // (128000 values by one workgroup 14 us, by 15 4.6.)
-__global__ __launch_bounds__(kSumThreads) void loss_sum_kernel(const float* __restrict__ v, long n, double by, double* parts, uint32_t* counter,
+__global__ __launch_bounds__(kSumThreads) void loss_sum_kernel(const double* __restrict__ v, long n, double by, double* parts, uint32_t* counter,
                                                                float* __restrict__ out) {
   __shared__ double sm[kSumThreads / 64];
   __shared__ int finishes;
@@ -394,22 +389,22 @@ __global__ __launch_bounds__(kSumThreads) void loss_sum_kernel(const float* __re
   double s = 0.0;
   long i = (long)blockIdx.x * kSumThreads + threadIdx.x;
   for (; i + 7 * step < n; i += 8 * step) {  // eight loads on their way
-    float x[8];
+    double x[8];
 #pragma unroll
     for (int u = 0; u < 8; ++u) x[u] = v[i + u * step];
 #pragma unroll
-    for (int u = 0; u < 8; ++u) s += (double)x[u];
+    for (int u = 0; u < 8; ++u) s += x[u];
   }
-  for (; i < n; i += step) s += (double)v[i];
+  for (; i < n; i += step) s += v[i];
   s = block_sum(s, sm);
   if (gridDim.x > 1) {
     if (threadIdx.x == 0) {
-      __hip_atomic_store(parts + blockIdx.x, s, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+      publish(parts + blockIdx.x, s);
       finishes = last_to_arrive(counter, gridDim.x);
     }
     __syncthreads();
     if (!finishes) return;
-    s = block_sum(threadIdx.x < gridDim.x ? __hip_atomic_load(parts + threadIdx.x, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT) : 0.0, sm);
+    s = block_sum(threadIdx.x < gridDim.x ? published(parts + threadIdx.x) : 0.0, sm);
   }
   if (threadIdx.x == 0) *out = (float)(s / by);
 }
@@ -456,7 +451,7 @@ __global__ __launch_bounds__(kSumThreads) void preference_pairs_kernel(Preferenc
       if (a.smoothing < 1.0) loss -= (1.0 - a.smoothing) * log_right;
       if (a.smoothing > 0.0) loss -= a.smoothing * log_wrong;
       const double pull = a.beta / a.pairs * (a.smoothing * right - (1.0 - a.smoothing) * wrong);
-      publish(a.pair_loss + pair, m == m ? (float)loss : __builtin_nanf(""));
+      publish(a.pair_loss + pair, m == m ? loss : __builtin_nan(""));
       a.pull[2 * pair] = (float)pull;
       a.pull[2 * pair + 1] = (float)-pull;
     }
@@ -466,7 +461,7 @@ __global__ __launch_bounds__(kSumThreads) void preference_pairs_kernel(Preferenc
 
 unsigned row_blocks(long rows) { return (unsigned)std::min<long>(rows, 1 << 20); }
 
-hipError_t sum_losses(hipStream_t s, const float* v, long n, double by, double* parts, uint32_t* counter, float* out) {
+hipError_t sum_losses(hipStream_t s, const double* v, long n, double by, double* parts, uint32_t* counter, float* out) {
   const long blocks = std::max<long>(1, std::min<long>(kSumParts, n / (8 * kSumThreads)));
   hipLaunchKernelGGL(loss_sum_kernel, dim3((unsigned)blocks), dim3(kSumThreads), 0, s, v, n, by, parts, counter, out);
   return hipGetLastError();
@@ -497,7 +492,8 @@ bool held(int rows, int classes, const F& f) {
   if (units <= 16 * 8) return TP_HELD(16, 8);
   if (units <= 64 * 4) return TP_HELD(64, 4);
   if (units <= 64 * 8) return TP_HELD(64, 8);
-  if (units <= 256 * W / 4) return TP_HELD(256, W / 4);
+  if constexpr (sizeof(T) == 4)
+    if (units <= 256 * 4) return TP_HELD(256, 4);
   if (units <= 256 * W / 2) return TP_HELD(256, W / 2);
   if (units <= 256 * W) return TP_HELD(256, W);
   if (units <= 512 * W) return TP_HELD(512, W);

@@ -32,10 +32,10 @@ struct PolicyArgs {
   const float* weights;   // or null: 1 / rows
   const float* ref_logp;  // read where kl_weight > 0
   double log_low, log_high;  // log(1 - clip_low), log(1 + clip_high)
-  float clip_low, clip_high, kl_weight;
+  double clip_low, clip_high, kl_weight;
   void* dlogits;
   float* logp;            // or null
-  float* row_loss;        // scratch, [rows]
+  double* row_loss;       // scratch, [rows]
   double* parts;          // scratch, [kSumParts]
   uint32_t* counter;      // zero before the launch and after it
   float* loss;
@@ -55,7 +55,7 @@ struct PreferenceArgs {
   RowStats* stats;        // scratch, [rows]
   uint16_t* logp_rest;    // scratch, [rows]
   float* pull;            // scratch, [2 pairs]: what a log probability of the sample weighs in the loss
-  float* pair_loss;       // scratch, [pairs]
+  double* pair_loss;      // scratch, [pairs]
   double* parts;          // scratch, [kSumParts]
   uint32_t* counter;      // zero before the launch and after it
   float* loss;

@@ -562,10 +562,9 @@ int make_plan(const tp_stage_desc* d, Plan* p) {
     if (lp.d.type == TP_LAYER_DENSE)
       wg = std::max<uint64_t>(wg, tp::wgrad_scratch_floats(d->dtype, (int)r, lp.d.out_features, lp.d.in_features));
   }
-  // the losses: a float per row, or (pairs of sequences) what a row's second pass needs, two bytes a row and three
-  // floats per sample
+  // the losses: a double per row, or (pairs of sequences) what a row's second pass needs, two bytes a row and two floats per sample
   const uint64_t loss_rows = rows * p->layers.back().tokens;
-  const uint64_t loss_floats = p->layers.back().d.type == TP_LAYER_DENSE && rows % 2 == 0 ? loss_rows * (sizeof(tp::RowStats) / 4) + (loss_rows + 1) / 2 + 2 * rows : loss_rows;
+  const uint64_t loss_floats = p->layers.back().d.type == TP_LAYER_DENSE && rows % 2 == 0 ? loss_rows * (sizeof(tp::RowStats) / 4) + (loss_rows + 1) / 2 + 2 * rows : 2 * loss_rows;
   const uint64_t loss_parts = 2 * tp::kSumParts;  // in front of them
   p->partial_floats = round_up(std::max<uint64_t>({wg, tp::update_scratch_floats(), loss_parts + loss_floats, conv_scratch, norm_scratch}), 64);
   // Every sum of partials the backward pass needs (bias and split weight gradients, scale and shift gradients of the
@@ -1421,13 +1420,13 @@ int stage_loss_policy(tp_stage* st, uint64_t mb_id, const void* logits_dev, cons
   a.ref_logp = ref_logp_dev;
   a.log_low = std::log1p(-clip_low);
   a.log_high = std::log1p(clip_high);
-  a.clip_low = (float)clip_low;
-  a.clip_high = (float)clip_high;
-  a.kl_weight = (float)kl_weight;
+  a.clip_low = clip_low;
+  a.clip_high = clip_high;
+  a.kl_weight = kl_weight;
   a.dlogits = dlogits_dev;
   a.logp = logp_dev;
   a.parts = (double*)st->partials();
-  a.row_loss = (float*)(a.parts + tp::kSumParts);
+  a.row_loss = a.parts + tp::kSumParts;
   a.counter = st->counter(tp_stage::kCountLoss);
   a.loss = loss_dev;
   ProfScope ps(st, TP_K_LOSS);
@@ -1463,7 +1462,7 @@ int stage_loss_preference(tp_stage* st, uint64_t mb_id, const void* logits_dev, 
   a.parts = (double*)st->partials();
   a.stats = (tp::RowStats*)(a.parts + tp::kSumParts);
   a.pull = (float*)(a.stats + rows);
-  a.pair_loss = a.pull + samples;
+  a.pair_loss = (double*)(a.pull + samples);
   a.logp_rest = (uint16_t*)(a.pair_loss + a.pairs);
   a.counter = st->counter(tp_stage::kCountLoss);
   a.loss = loss_dev;
