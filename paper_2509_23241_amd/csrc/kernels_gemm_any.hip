@@ -267,7 +267,7 @@ struct DenseWhole {
 };
 
 // And for contractions of any length: the k tiles that are whole are copied so, the last one with an address of each lane's own.  Which it
-// is, is known to the whole wave. 
+// is, is known to the whole wave.
 template <class T, class Sum, int R, int NW, bool COL>
 struct DenseMost : DenseWhole<T, Sum, R, NW, COL> {
   using Whole = DenseWhole<T, Sum, R, NW, COL>;
@@ -816,8 +816,8 @@ hipError_t launch_any(hipStream_t s, int M, int N, int KT, int splits, const typ
 }
 
 // ---- dense fp32 products of few tiles ------------------------------------------------------------
-// Forward products and input gradients of whole k tiles, with rows of whole 16-byte units: the same chains as above, bit for
-// bit.  Bound by the chain itself, one dependent v_mfma_f32_16x16x4_f32 per four k values, 32 cycles each.  fp32 matrix
+// Forward products and input gradients of whole k tiles, with rows of whole 16-byte units: the same chains, and the same parts of them,
+// as above, bit for bit.  Bound by the chain itself, one dependent v_mfma_f32_16x16x4_f32 per four k values, 32 cycles each.  fp32 matrix
 // instructions run on the vector ALUs: between two of them an LDS read or a scalar instruction costs 1 to 3 cycles, a
 // vector instruction 8 and more (timed in a chain of its own).  So a workgroup is ONE wave with a tile of 16 x 16, which waits
 // for its own copies and for nobody; the copies take a scalar base and a constant offset per lane, and with the loop
@@ -955,10 +955,19 @@ __global__ __launch_bounds__(64) void gemm_f32_wave_kernel(int M, int N, int KT,
       pb += step_b;
     }
   };
-  auto all_stages = [&](int t0, auto last) {  // tile t0 in stage 0; tiles below zero are left out
+  // Parts, where the epilogue wants them, are the tiles of one turn over the stages.  They begin at k = 0, as in the kernel above, so with
+  // the tile in stage `skip` of whichever turn, and the last one may be short.  Which stage that is, is a constant of the loop: a branch
+  // at every stage took 1 us more of a gated layer's pass of 35 over 1 row, 512 x 1408, and 6 more of 45 over 32 rows, 2048 x 512.
+  static_assert(Epi::kPartK == 0 || Epi::kPartK == NS * 32, "a part is one turn");
+  floatx4 parts = {0.f, 0.f, 0.f, 0.f};
+  auto all_stages = [&](int t0, auto last, auto part) {  // tile t0 in stage 0; tiles below zero are left out
     for_each_stage([&](auto stage_u) {
       constexpr int u = decltype(stage_u)::value;
       if (t0 + u < 0) return;
+      if constexpr (u == decltype(part)::value) {
+        parts += acc;
+        acc = floatx4{0.f, 0.f, 0.f, 0.f};
+      }
       if constexpr (!decltype(last)::value || u == 0) {
         wait_vmcnt<(NS - 3) * kCopies>();  // the next tile has landed
         tile(stage_u, std::true_type{}, std::true_type{});
@@ -970,18 +979,18 @@ __global__ __launch_bounds__(64) void gemm_f32_wave_kernel(int M, int N, int KT,
       }
     }, std::make_integer_sequence<int, NS>{});
   };
-  // parts, where the epilogue wants them, are the tiles of one turn over the stages
-  static_assert(Epi::kPartK == 0 || Epi::kPartK == NS * 32, "a part is one turn");
-  floatx4 parts = {0.f, 0.f, 0.f, 0.f};
-  int t0 = -skip;
-  for (; t0 + NS < KT; t0 += NS) {
-    all_stages(t0, std::false_type{});
-    if constexpr (Epi::kPartK > 0) {
-      parts += acc;
-      acc = floatx4{0.f, 0.f, 0.f, 0.f};
-    }
+  auto turns = [&](auto part) {
+    int t0 = -skip;
+    for (; t0 + NS < KT; t0 += NS) all_stages(t0, std::false_type{}, part);
+    all_stages(t0, std::true_type{}, part);
+  };
+  if constexpr (Epi::kPartK > 0) {
+    for_each_stage([&](auto stage_u) {
+      if (skip == decltype(stage_u)::value) turns(stage_u);
+    }, std::make_integer_sequence<int, NS>{});
+  } else {
+    turns(std::integral_constant<int, -1>{});
   }
-  all_stages(t0, std::true_type{});
   if constexpr (Epi::kPartK > 0) acc += parts;
   if constexpr (Epi::kSums) {
     floatx4 o = {0.f, 0.f, 0.f, 0.f};
