@@ -139,7 +139,8 @@ enum tp_layer_type {
                              out_features = F, geom = {tokens}; W[2F x in] and b[2F], whose rows are the gate (2f) and the other
                              factor (2f + 1) of each output in turn; any activation; at most 2^28 token positions in a
                              mini-batch.  Kept for the backward pass: z[2f + 1] act'(z[2f]) and act(z[2f]), in bf16 stages to 12
-                             significant bits */
+                             significant bits.  There the gradient of z, dy times what is kept, is rounded to bf16 where it enters
+                             the products for the gradients of x and W; that of b is its sum before that */
   TP_LAYER_ROTARY = 11    /* rotary positions, no parameters: in_features = out_features = (heads + 2 kv heads) * dh (queries | keys |
                              values, as the attention layers take them), geom = {tokens, heads, kv heads, rotated, layout}.  In every
                              query and key head the first `rotated` values (even, 2 .. dh <= 256) are turned in pairs: value 2i with

@@ -301,9 +301,10 @@ class Stage:
                     continue
                 x_in, z = saved[li]
                 if kind == "gated":
-                    dW, db, da = L.dense_backward(self.q(L.gated_backward(da, z, spec.act)), x_in, W_b[pi])
+                    dz = L.gated_backward(da, z, spec.act)   # stored for the two products alone
+                    dW, _, da = L.dense_backward(self.q(dz), x_in, W_b[pi])
                     g[pi] += dW
-                    g[pi + 1] += db
+                    g[pi + 1] += dz.reshape(-1, dz.shape[-1]).sum(axis=0)
                     da = self.q(da)
                     continue
                 dz = self.q(da * L.act_derivative(z, spec.act))

@@ -36,7 +36,7 @@ hipError_t launch_gated_fprop(hipStream_t s, int elt, int M, int N, int K, const
 int gated_pitch(int elt, int n);
 // M: rows of the whole mini-batch
 bool gated_padded(int elt, int M, int N, int K);
-// dz[2f] = dy[f] d[2f], dz[2f + 1] = dy[f] d[2f + 1], and gb = column sums of dz as stored; N = 2 F columns of dz, whose rows are
+// dz[2f] = dy[f] d[2f], dz[2f + 1] = dy[f] d[2f + 1], and gb = column sums of that before it is rounded; N = 2 F columns of dz, whose rows are
 // gated_pitch(elt, N) values apart with zeros behind the columns.
 // partials: scratch of colsum_scratch_floats(M, N) floats.
 hipError_t launch_gated_backward(hipStream_t s, int elt, int M, int N, const void* dy, const void* d, const uint8_t* fine, void* dz, float* gb,

@@ -143,9 +143,10 @@ __global__ __launch_bounds__(kThreads) void act_backward_colsum_kernel(int M, in
 }
 
 // The backward pass of a gated layer ahead of its products, with the structure of the kernel above over N = 2 F columns: dz of columns 2f
-// and 2f + 1 is dy[f] times what the forward pass kept there.  d and dz have rows of `pitch` values, whole 16-byte units, zeros behind the
-// columns of dz; those of dy and `fine` start anywhere.  A unit takes 16 bytes of d, 8 of dy and in bf16 4 of `fine`, the last one of a row what
-// there is of it.  8192 x 16384 in bf16 (738 MB): 152 us, the rate of a copy;
+// and 2f + 1 is dy[f] times what the forward pass kept there.  In bf16 dz is rounded for the two products that read it, which take operands
+// of no other type; its column sums are of what was there before (summed up rounded, those of few rows are 0.0017 of their norm off).  d and
+// dz have rows of `pitch` values, whole 16-byte units, zeros behind the columns of dz; those of dy and `fine` start anywhere.  A unit takes
+// 16 bytes of d, 8 of dy and in bf16 4 of `fine`, the last one of a row what there is of it.  8192 x 16384 in bf16 (738 MB): 152 us, the rate of a copy;
 // 13558 x 17898 (1.33 GB, rows of dy at odd addresses) 387.
 template <typename T>
 __global__ __launch_bounds__(kThreads) void gated_backward_kernel(int M, int N, ColsumShape cs, const T* __restrict__ dy,
@@ -187,10 +188,12 @@ __global__ __launch_bounds__(kThreads) void gated_backward_kernel(int M, int N, 
                             __uint_as_float(a.y & 0xffff0000u)};
 #pragma unroll
         for (int j = 0; j < 4; ++j) {
-          ow[j] = pack_bf16x2(g[j] * joined12(bw[j] << 16, (low >> (8 * j)) & 15u), g[j] * joined12(bw[j] & 0xffff0000u, (low >> (8 * j + 4)) & 15u));
-          if (2 * j >= left) ow[j] = 0;
-          s[(2 * j) % V] += __uint_as_float(ow[j] << 16);
-          s[(2 * j + 1) % V] += __uint_as_float(ow[j] & 0xffff0000u);
+          const bool there = 2 * j < left;
+          const float p = there ? g[j] * joined12(bw[j] << 16, (low >> (8 * j)) & 15u) : 0.f;
+          const float q = there ? g[j] * joined12(bw[j] & 0xffff0000u, (low >> (8 * j + 4)) & 15u) : 0.f;
+          ow[j] = pack_bf16x2(p, q);
+          s[(2 * j) % V] += p;
+          s[(2 * j + 1) % V] += q;
         }
       } else {
         const float g[2] = {__uint_as_float(a.x), __uint_as_float(a.y)};
