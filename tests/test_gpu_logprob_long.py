@@ -2,8 +2,8 @@
 sum of exponentials than a step of what the first ones make.
 
 Bounds, f = 2^-24: the maximum is 0, so the likely classes' exponentials are 1 exactly; the others', all alike, are off by (25 + 2) f of
-themselves and make up less than 2^-11 of the sum.  Sums: eight values at a time, then up to 2^18 classes in 256 threads, then 64 lanes and
-four waves: 8 + 16 roundings.  Together s = 26 f; log probabilities s + f |l| (stored)."""
+themselves and make up less than 2^-6 of the sum: f at most.  Sums: eight values at a time, then up to 2^18 classes in 256 threads, then 64 lanes and
+four waves: 8 + 16 roundings.  Together s = 26 f with the logarithm's; log probabilities s + f |l| (stored)."""
 import pytest
 
 from test_gpu_logprob import F, U, _row_parts, _stage
