@@ -25,9 +25,9 @@ __device__ __forceinline__ uint32_t pack_bf16x2(float lo, float hi) {
   return __builtin_bit_cast(uint32_t, __builtin_convertvector(f, bf16x2_t));
 }
 
-// Two values to 12 significant bits (halves away from zero: at most 2^-13 off): the upper halves of their fp32 words in `hi`, the second one's on
-// top, and the four bits below those in a byte, the first one's in its lower half.  Infinities and NaN stay what they are but for NaN whose
-// fraction is all ones.
+// Two values to 12 significant bits (halves away from zero: at most 2^-12 off): the upper halves of their fp32 words in `hi`, the second one's on
+// top, and the four bits below those in a byte, the first one's in its lower half.  Infinities stay what they are, and NaN but for one whose
+// fraction is all ones (or nearly), which becomes a zero: no operand may hold it.
 __device__ __forceinline__ uint32_t split12(float a, float b, uint32_t& hi) {
   const uint32_t p = __float_as_uint(a) + 0x800u, q = __float_as_uint(b) + 0x800u;
   hi = __builtin_amdgcn_perm(q, p, 0x07060302u);

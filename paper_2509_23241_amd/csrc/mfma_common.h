@@ -119,9 +119,17 @@ struct EpiGated {
   int wide = 2;  // 2: d_out is 16-byte aligned
   static constexpr bool kSwap = true, kSums = false;
   __device__ __forceinline__ bool whole_rows(int) const { return wide == 2; }
-  struct Cols { float4 b0, b1; };
+  struct Cols { float b[8]; };
+  // split12 takes any NaN but one of all bits set, which of all operands only a bias, stored in fp32, can hold
+  __device__ __forceinline__ float bias_of(int n) const {
+    const float b = bias[n];
+    return b == b ? b : __builtin_nanf("");
+  }
   __device__ __forceinline__ Cols cols(int n) const {
-    return Cols{*reinterpret_cast<const float4*>(bias + n), *reinterpret_cast<const float4*>(bias + n + 4)};
+    Cols c;
+#pragma unroll
+    for (int j = 0; j < 8; ++j) c.b[j] = bias_of(n + j);
+    return c;
   }
   __device__ __forceinline__ bool has_rows() const { return false; }
   __device__ __forceinline__ uint4 row_in(int, int) const { return make_uint4(0, 0, 0, 0); }
@@ -141,9 +149,8 @@ struct EpiGated {
     return low;
   }
   __device__ __forceinline__ uint4 row8(int m, int n, float (&v)[8], const Cols& c, const uint4&) const {
-    const float b[8] = {c.b0.x, c.b0.y, c.b0.z, c.b0.w, c.b1.x, c.b1.y, c.b1.z, c.b1.w};
 #pragma unroll
-    for (int j = 0; j < 8; ++j) v[j] += b[j];
+    for (int j = 0; j < 8; ++j) v[j] += c.b[j];
     uint32_t d[4];
     float a[4];
     const uint32_t low = pairs<4>(v, d, a);
@@ -159,7 +166,7 @@ struct EpiGated {
   __device__ __forceinline__ void quad(int m, int n, int count, float v0, float v1, float v2, float v3) const {
     const size_t i = (size_t)m * ldd + n, o = ((size_t)m * ldc + n) / 2;
     const bool both = count == 4;
-    const float z[4] = {v0 + bias[n], v1 + bias[n + 1], v2 + bias[both ? n + 2 : n], v3 + bias[both ? n + 3 : n]};
+    const float z[4] = {v0 + bias_of(n), v1 + bias_of(n + 1), v2 + bias_of(both ? n + 2 : n), v3 + bias_of(both ? n + 3 : n)};
     uint32_t d[2];
     float a[2];
     const uint32_t low = pairs<2>(z, d, a);
