@@ -149,7 +149,9 @@ enum tp_layer_type {
                              speed_i.  rel = {first, original}, rope = {base, factor, low, high, amplitude}; with s = base^(-2i /
                              rotated), speed_i = s / factor where original = 0 (low = high = 0), else s * ((1 - g) / factor + g), g =
                              (original * s / 2pi - low) / (high - low) held to 0 .. 1: pairs that turn less than `low` times over
-                             `original` positions are slowed down, those of more than `high` are not.  Angles are formed in fp64.
+                             `original` positions are slowed down, those of more than `high` are not.  Angles are formed in fp64,
+                             from base and factor as they are held here, in fp32.  Every sample of every pass starts at `first`;
+                             another start (the next token, a padded sample's own) is another stage's.
                              The backward pass turns back (times amplitude).  Between a dense layer without activation and an
                              attention layer the turn is made in place */
 };
