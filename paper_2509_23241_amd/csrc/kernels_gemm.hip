@@ -146,8 +146,8 @@ __global__ __launch_bounds__(kThreads) void act_backward_colsum_kernel(int M, in
 // and 2f + 1 is dy[f] times what the forward pass kept there.  In bf16 dz is rounded for the two products that read it, which take operands
 // of no other type; its column sums are of what was there before (summed up rounded, those of few rows are 0.0017 of their norm off).  d and
 // dz have rows of `pitch` values, whole 16-byte units, zeros behind the columns of dz; those of dy and `fine` start anywhere.  A unit takes
-// 16 bytes of d, 8 of dy and in bf16 4 of `fine`, the last one of a row what there is of it.  8192 x 16384 in bf16 (738 MB): 152 us, the rate of a copy;
-// 13558 x 17898 (1.33 GB, rows of dy at odd addresses) 387.
+// 16 bytes of d, 8 of dy and in bf16 4 of `fine`, the last one of a row what there is of it.  8192 x 16384 in bf16 (738 MB): 149 us, the rate of a
+// copy; 13558 x 17898 (1.33 GB, rows of dy at odd addresses) 388.
 template <typename T>
 __global__ __launch_bounds__(kThreads) void gated_backward_kernel(int M, int N, ColsumShape cs, const T* __restrict__ dy,
                                                                   const T* __restrict__ d, const uint8_t* __restrict__ fine,
